@@ -47,7 +47,7 @@ typedef enum {
     SISO_ERR_CUDA = 7
 } siso_status_t;
 
-typedef enum { SISO_F32 = 0, SISO_BF16 = 1 } siso_dtype_t;
+typedef enum { SISO_F32 = 0, SISO_BF16 = 1, SISO_E4M3 = 2, SISO_I8 = 3 } siso_dtype_t; /* the last two: key/value caches only */
 
 #define SISO_ACCESS_INF 0xFFFFFFFFu
 
@@ -460,6 +460,89 @@ siso_status_t siso_merge_apply_shard(siso_cache_t *c, const int32_t *d_merge_map
  *                      sweeps.  Synchronises `stream`. */
 siso_status_t siso_selftest_wait_timeout(siso_cache_t *c, uint32_t poll_limit, int32_t *d_gave_up, void *stream);
 siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *stream);
+
+/* ---- behind the cache: the language model's side of a miss, and of a near hit ------------------------------------------
+ * A query that misses goes to the language model; so does one whose best entry lies just below the threshold, but there the
+ * entry's stored answer is a good guess: its tokens can be run through the model as drafts, all at once, and the model's own
+ * probabilities say how many of them stand.  The paper leaves this side to its LLM backend (Sec. 5.1).  Three operators:
+ * a paged key/value cache that is quantised as it is written, attention of the new tokens over it, and the verification.
+ *
+ * siso_kv_create   A handle over pages that the CALLER owns and keeps alive: keys and values of n_layers layers, n_pages pages of
+ *                  page_size tokens, n_kv_heads heads, head_dim values.  Element [layer, page, token, head, d] of both lies at
+ *                  layer * stride_layer + page * stride_page + token * stride_token + head * stride_head + d (elements), so
+ *                  token-major, head-major and interleaved pools all work.  dtype SISO_BF16, or SISO_E4M3 / SISO_I8 (int8 two's
+ *                  complement) with one exponent byte per row in d_k_exp / d_v_exp [n_layers, n_pages, n_kv_heads, page_size]
+ *                  (NULL for SISO_BF16): a row of head_dim values is kept as codes c, value c * 2^(byte - 127), the byte being
+ *                  the smallest that lets the row's largest magnitude fit (448 for e4m3, 127 for i8).  Byte 255 marks a row
+ *                  that held a NaN or an infinity; it reads back as NaN.  page_size, head_dim multiples of 8 (head_dim at
+ *                  most 256), base pointers 16-byte aligned, strides multiples of 8 elements (attention over 8-bit pages: of 16), else
+ *                  SISO_ERR_UNSUPPORTED.  The handle's scratch comes from the allocator on first use.  Synchronous.
+ * siso_kv_write    Rows d_k, d_v [n_tokens, n_kv_heads, head_dim] (SISO_F32 or SISO_BF16, strides in elements, multiples of
+ *                  16 bytes) into slots d_slots [n_tokens] = page * page_size + token; a slot outside the pool (-1) is skipped.
+ *                  Slots of one call must differ.  Codes are rounded to nearest, ties to even.
+ * siso_kv_read     The reverse: rows of the slots as SISO_F32 or SISO_BF16 (8-bit values are exact in both); slots outside
+ *                  the pool read as zeros.
+ * siso_kv_attention  New tokens, already written to the cache, attend over it.  Sequence b has the queries
+ *                  d_cu_q[b] .. d_cu_q[b + 1] - 1 and d_kv_len[b] tokens in all, in the pages d_pages[b * pages_stride + i] (max_pages
+ *                  columns; kv_len is cut to what they hold); its query i stands at p = kv_len - (number of its queries) + i and sees
+ *                  tokens j < kv_len with j <= p (SISO_ATTN_CAUSAL) and j > p - window (window > 0).  Query head h reads
+ *                  key/value head h / (n_heads / n_kv_heads).
+ *                      out = sum_j softmax_j(scale q.k_j) v_j,   lse = ln sum_j exp(scale q.k_j)
+ *                  and 0 and -infinity where nothing is seen.  d_q, d_out bf16 [n_tokens, n_heads, head_dim] with strides in
+ *                  elements (multiples of 8, bases 16-byte aligned); d_lse [n_tokens, n_heads] fp32 or NULL.  head_dim 64 or 128.
+ *                  max_q: the most queries of one sequence (a hint that selects the kernel; any value gives the same result up
+ *                  to rounding).  Places beyond kv_len may hold anything, NaN included; within it values must be
+ *                  finite (a NaN there may reach rows that do not see it).  A page index outside the pool: SISO_ERR_INVALID_ARG in the
+ *                  status word, its tokens are left out.  Sums and softmax statistics are fp32; probabilities are rounded to
+ *                  bf16 before they meet the values.
+ * siso_kv_sync_status  Synchronises `stream`, returns the handle's device status word and clears it.
+ * Calls on one handle must be issued on one stream or be ordered by the caller (they share the handle's scratch).
+ *
+ * siso_verify_drafts (no handle; current device)  d_target [n_seqs, n_max + 1, vocab] probabilities of the target (SISO_F32 or
+ *                  SISO_BF16), row t the distribution of the token that draft t claims; d_draft [n_seqs, n_max, vocab] those the
+ *                  drafts were drawn from, or NULL if the drafts were certain (a stored answer); d_tokens [n_seqs, n_max] the
+ *                  drafts, d_n_drafts [n_seqs] how many of them (NULL: n_max), d_u_accept [n_seqs, n_max] and d_u_sample [n_seqs]
+ *                  uniform numbers in [0, 1).  Draft t stands if u_accept q_t(x_t) < p_t(x_t) and all before it stand; a token
+ *                  outside the vocabulary never does.  d_accepted [n_seqs] = number n that stand; d_out [n_seqs, n_max + 1] = those, then
+ *                  one token drawn from max(p_n - q_n, 0) (from p_n where all stand, or the difference is empty), then -1.
+ *                  The draw: w_v = floor(min(r_v, 1) 2^38) in 64-bit integers, the smallest v with
+ *                  2^24 (w_0 + .. + w_v) > floor(u_sample 2^24) sum(w); the same for any split of the row.  vocab at most 2^24.
+ * All asynchronous on `stream` unless stated otherwise. */
+typedef struct siso_kv siso_kv_t;
+
+typedef struct {
+    void *d_k, *d_v;
+    uint8_t *d_k_exp, *d_v_exp;
+    int64_t n_pages, stride_layer, stride_page, stride_token, stride_head;
+    int32_t n_layers, page_size, n_kv_heads, head_dim;
+    int32_t dtype, device;
+    siso_allocator_t allocator;
+} siso_kv_config_t;
+
+#define SISO_ATTN_CAUSAL 1u
+
+typedef struct {
+    const void *d_q;
+    void *d_out;
+    float *d_lse;
+    const int32_t *d_cu_q, *d_kv_len, *d_pages;
+    int64_t q_stride_token, q_stride_head, out_stride_token, out_stride_head, pages_stride, n_tokens;
+    int32_t n_seqs, max_q, max_pages, n_heads, layer, window;
+    uint32_t flags;
+    float scale;
+} siso_attention_t;
+
+siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg);
+siso_status_t siso_kv_destroy(siso_kv_t *kv);
+siso_status_t siso_kv_write(siso_kv_t *kv, int32_t layer, const void *d_k, const void *d_v, int32_t dtype, int64_t n_tokens,
+                            int64_t stride_token, int64_t stride_head, const int64_t *d_slots, void *stream);
+siso_status_t siso_kv_read(siso_kv_t *kv, int32_t layer, void *d_k, void *d_v, int32_t dtype, int64_t n_tokens, int64_t stride_token,
+                           int64_t stride_head, const int64_t *d_slots, void *stream);
+siso_status_t siso_kv_attention(siso_kv_t *kv, const siso_attention_t *args, void *stream);
+siso_status_t siso_kv_sync_status(siso_kv_t *kv, void *stream);
+siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int32_t dtype, int64_t n_seqs, int32_t n_max, int32_t vocab,
+                                 const int32_t *d_tokens, const int32_t *d_n_drafts, const float *d_u_accept, const float *d_u_sample,
+                                 int32_t *d_out, int32_t *d_accepted, void *stream);
 
 /* Number of kernels this handle has launched so far (host-side count). */
 int64_t siso_launch_count(const siso_cache_t *c);

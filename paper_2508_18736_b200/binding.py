@@ -27,7 +27,8 @@ EXPORTS = ["siso_cache_create", "siso_cache_destroy", "siso_set_option", "siso_i
            "siso_route", "siso_evict_keys", "siso_select_evict", "siso_evict_slots", "siso_selftest_wait_timeout",
            "siso_measure_fp32_fma", "siso_pair_sweep_block", "siso_merge_resolve", "siso_merge_pack",
            "siso_merge_apply_shard", "siso_tier_build", "siso_tier_work_bytes", "siso_tier_lookup", "siso_free_slots",
-           "siso_shard_plan", "siso_route_planned", "siso_select_evict_planned", "siso_norm_deviation"]
+           "siso_shard_plan", "siso_route_planned", "siso_select_evict_planned", "siso_norm_deviation", "siso_kv_create",
+           "siso_kv_destroy", "siso_kv_write", "siso_kv_read", "siso_kv_attention", "siso_kv_sync_status", "siso_verify_drafts"]
 
 
 class SisoError(RuntimeError):
@@ -116,6 +117,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.siso_tier_work_bytes.argtypes = [i64, i32, i32]
     L.siso_tier_work_bytes.restype = i64
     L.siso_tier_lookup.argtypes = [vp, vp, vp, vp, vp, i64, f32, vp, f32, vp, vp, vp, vp, ctypes.POINTER(i64), vp]
+    L.siso_kv_create.argtypes = [vp, vp]
+    L.siso_kv_destroy.argtypes = [vp]
+    L.siso_kv_write.argtypes = [vp, i32, vp, vp, i32, i64, i64, i64, vp, vp]
+    L.siso_kv_read.argtypes = [vp, i32, vp, vp, i32, i64, i64, i64, vp, vp]
+    L.siso_kv_attention.argtypes = [vp, vp, vp]
+    L.siso_kv_sync_status.argtypes = [vp, vp]
+    L.siso_verify_drafts.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     L.siso_launch_count.argtypes = [vp]
     L.siso_launch_count.restype = i64
     L.siso_status_string.argtypes = [i32]

@@ -22,6 +22,7 @@ static void *default_alloc(size_t bytes, void *, void *) {
     return p;
 }
 static void default_free(void *p, void *) { cudaFree(p); }
+siso_allocator_t default_allocator() { return siso_allocator_t{default_alloc, default_free, nullptr}; }
 
 static void *cache_alloc(Cache *c, size_t bytes, cudaStream_t s) {
     return c->alloc.alloc(bytes ? bytes : 256, s, c->alloc.ctx);

@@ -89,6 +89,7 @@ siso_status_t scratch_reserve(Cache *c, size_t bytes, cudaStream_t s, Scratch *o
 siso_status_t stage_reserve(Cache *c, size_t bytes, cudaStream_t s);   // c->stage of at least `bytes`
 // memory that lives as long as the cache, set to zero; NULL if the allocator fails
 void *cache_alloc_zeroed(Cache *c, size_t bytes);
+siso_allocator_t default_allocator();      // cudaMalloc / cudaFree
 siso_status_t check_cuda(cudaError_t e, const char *what);
 #define SISO_CUDA(expr)                                                  \
     do {                                                                 \

@@ -1,0 +1,69 @@
+// Internal declarations of the paged key/value cache: the handle, the device view that kernels get, and the code that
+// turns 8-bit codes into values.
+#pragma once
+
+#include <cuda.h>
+
+#include "common.cuh"
+
+namespace siso {
+
+constexpr int kKvMaxDim = 256;
+
+// What kernels see of the pages.  Strides in elements; the same for keys and values.
+struct KvView {
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;        // [n_layers, n_pages, n_kv_heads, page_size], 8-bit caches only
+    long long n_pages, stride_page, stride_token, stride_head;
+    int page_size, n_kv_heads, head_dim;
+};
+
+struct Kv {
+    siso_kv_config_t cfg;
+    int sm_count;
+    void *ws;                      // scratch, grown on demand
+    size_t ws_bytes;
+    int *status;                   // device status word (first error wins)
+};
+
+inline int kv_elem_bytes(int dtype) { return dtype == SISO_BF16 ? 2 : 1; }
+
+// the pages of one layer
+inline KvView kv_view(const Kv *h, int layer) {
+    const siso_kv_config_t &g = h->cfg;
+    const long long off = static_cast<long long>(layer) * g.stride_layer * kv_elem_bytes(g.dtype);
+    const long long exps = static_cast<long long>(layer) * g.n_pages * g.n_kv_heads * g.page_size;
+    KvView w;
+    w.k = static_cast<char *>(g.d_k) + off;
+    w.v = static_cast<char *>(g.d_v) + off;
+    w.k_exp = g.d_k_exp ? g.d_k_exp + exps : nullptr;
+    w.v_exp = g.d_v_exp ? g.d_v_exp + exps : nullptr;
+    w.n_pages = g.n_pages;
+    w.stride_page = g.stride_page;
+    w.stride_token = g.stride_token;
+    w.stride_head = g.stride_head;
+    w.page_size = g.page_size;
+    w.n_kv_heads = g.n_kv_heads;
+    w.head_dim = g.head_dim;
+    return w;
+}
+
+siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t s);
+
+#ifdef __CUDACC__
+// 2^(byte - 127) of a stored row; 255 marks a row that held a non-finite value
+__device__ __forceinline__ float kv_scale(uint32_t byte) {
+    return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+}
+// value of one code.  e4m3: sign, 4 exponent and 3 mantissa bits moved to their places in a float give the value times
+// 2^-120, subnormal codes too
+template <int KIND> __device__ __forceinline__ float kv_code(uint32_t b, float scale) {
+    if constexpr (KIND == SISO_E4M3)
+        return __uint_as_float(((b & 0x80u) << 24) | ((b & 0x7Fu) << 20)) * __uint_as_float(247u << 23) * scale;
+    return static_cast<float>(static_cast<int>(b << 24) >> 24) * scale;
+}
+#endif
+
+}  // namespace siso
+
+struct siso_kv : public siso::Kv {};

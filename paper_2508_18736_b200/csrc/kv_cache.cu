@@ -1,0 +1,337 @@
+// Paged key/value cache: the handle, quantisation of new rows as they are written, and reading rows back.
+//
+// A row is the head_dim values of one token in one kv head, of K or of V.  In an 8-bit cache it is kept as codes c_i and one
+// exponent byte e + 127:
+//     a = max |x_i|,   e = the smallest whole number >= -127 with a <= M 2^e   (M = 448 for e4m3, 127 for i8)
+//     c_i = x_i 2^-e rounded to the nearest code, ties to even;   read back: c_i 2^e
+// The scale is a power of two on purpose.  Both multiplications are then exact, so a code is rounded once, and c 2^e needs
+// at most 8 significant bits: it is a bf16 value, which attention multiplies as it is.  The price is a step up to twice as
+// coarse as a / M would give for i8 (e4m3 loses nothing but range at the bottom).  A row with a NaN or an infinity gets the
+// byte 255 and reads back as NaN throughout.
+//
+// Both kernels move bytes: they are bound by HBM for prompts and by latency for a step's few tokens.  G lanes own a row with 8
+// values each (one 16-byte load of bf16), so the maximum takes log2 G shuffles, and every lane has U rows in flight before
+// it uses the first.
+#include <cuda_fp8.h>
+
+#include <cstring>
+#include <new>
+
+#include "kv.cuh"
+
+namespace siso {
+namespace kvc {
+
+constexpr int THREADS = 256;
+constexpr int U = 4;
+
+struct Rows {                     // n tokens x heads rows of the caller's K and V
+    void *k, *v;
+    long long n, stride_token, stride_head;
+};
+
+template <typename T> struct Vec8;             // 8 consecutive values of the caller's type
+template <> struct Vec8<__nv_bfloat16> {
+    uint4 r;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { r = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = r; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    }
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        r = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Vec8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) { a = reinterpret_cast<const float4 *>(p)[0]; b = reinterpret_cast<const float4 *>(p)[1]; }
+    __device__ __forceinline__ void store(float *p) const { reinterpret_cast<float4 *>(p)[0] = a; reinterpret_cast<float4 *>(p)[1] = b; }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    __device__ __forceinline__ void set(const float (&x)[8]) { a = make_float4(x[0], x[1], x[2], x[3]); b = make_float4(x[4], x[5], x[6], x[7]); }
+};
+
+// exponent byte of a row whose largest magnitude is `a` (NaN where the row is not finite): M = top_mant 2^top_exp as float bits
+template <int KIND> __device__ __forceinline__ int exponent_of(float a) {
+    constexpr uint32_t top = KIND == SISO_E4M3 ? 0x43E00000u /* 448 */ : 0x42FE0000u /* 127 */;
+    const uint32_t u = __float_as_uint(a);
+    int e = static_cast<int>(u >> 23) - static_cast<int>(top >> 23) + ((u & 0x7FFFFFu) > (top & 0x7FFFFFu) ? 1 : 0);
+    return max(e, -127);          // zero and subnormal rows end here too
+}
+// 2^-e for e in [-127, 120]
+__device__ __forceinline__ float inverse_scale(int e) { return __uint_as_float(static_cast<uint32_t>(127 - e) << 23); }
+
+template <int KIND> __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv) {
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if constexpr (KIND == SISO_E4M3) {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * h] * inv, x[4 * h + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * h + 2] * inv, x[4 * h + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+            w[h] = lo | (hi << 16);
+        } else {
+            w[h] = 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[h] |= (static_cast<uint32_t>(__float2int_rn(x[4 * h + i] * inv)) & 0xFFu) << (8 * i);
+        }
+    }
+    return make_uint2(w[0], w[1]);
+}
+template <int KIND> __device__ __forceinline__ void decode8(uint2 c, float scale, float (&x)[8]) {
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kv_code<KIND>((w[i >> 2] >> (8 * (i & 3))) & 0xFFu, scale);
+}
+
+// where a slot's row of `head` starts, in elements, and its exponent
+__device__ __forceinline__ long long row_at(const KvView &kv, long long page, int tok, int head) {
+    return page * kv.stride_page + tok * kv.stride_token + head * kv.stride_head;
+}
+__device__ __forceinline__ long long exp_at(const KvView &kv, long long page, int tok, int head) {
+    return (page * kv.n_kv_heads + head) * kv.page_size + tok;
+}
+
+template <int KIND, typename T, int G, bool READ>
+__global__ void __launch_bounds__(THREADS)
+kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots) {
+    const int sub = threadIdx.x % G, d = sub * 8;
+    const bool mine = d < kv.head_dim;
+    const bool is_v = blockIdx.y != 0;
+    T *ext = static_cast<T *>(is_v ? rows.v : rows.k);
+    char *pages = static_cast<char *>(is_v ? kv.v : kv.k);
+    uint8_t *exps = is_v ? kv.v_exp : kv.k_exp;
+    constexpr int ROWS = THREADS / G;                     // rows of a block's step
+    const long long total = rows.n * kv.n_kv_heads;
+    const long long first = static_cast<long long>(blockIdx.x) * (ROWS * U) + threadIdx.x / G;
+    long long place[U], at_ext[U], at_exp[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const long long r = first + u * ROWS;
+        place[u] = -1;
+        at_ext[u] = -1;
+        if (r < total) {
+            const long long tok = total <= 0xFFFFFFFFll ? static_cast<uint32_t>(r) / static_cast<uint32_t>(kv.n_kv_heads) : r / kv.n_kv_heads;
+            const int head = static_cast<int>(r - tok * kv.n_kv_heads);
+            const long long slot = slots[tok];
+            at_ext[u] = tok * rows.stride_token + head * rows.stride_head + d;
+            const long long page = slot < 0 ? -1 : (slot <= 0xFFFFFFFFll ? static_cast<uint32_t>(slot) / static_cast<uint32_t>(kv.page_size) : slot / kv.page_size);
+            if (page >= 0 && page < kv.n_pages) {
+                const int t = static_cast<int>(slot - page * kv.page_size);
+                place[u] = row_at(kv, page, t, head) + d;
+                at_exp[u] = exp_at(kv, page, t, head);
+            }
+        }
+    }
+    if constexpr (!READ) {
+        Vec8<T> in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (mine && place[u] >= 0) in[u].load(ext + at_ext[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[8];
+            if (mine && place[u] >= 0) in[u].get(x);
+            else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            }
+            if constexpr (KIND == SISO_BF16) {
+                if (mine && place[u] >= 0) {
+                    Vec8<__nv_bfloat16> o;
+                    o.set(x);
+                    o.store(reinterpret_cast<__nv_bfloat16 *>(pages) + place[u]);
+                }
+            } else {
+                // magnitudes order like their bits, with infinities and NaN above every finite value
+                uint32_t top = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+                for (int o = 1; o < G; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                if (place[u] < 0) continue;
+                const bool finite = top < 0x7F800000u;
+                const int e = finite ? exponent_of<KIND>(__uint_as_float(top)) : 0;
+                if (!finite) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+                }
+                if (mine) *reinterpret_cast<uint2 *>(pages + place[u]) = encode8<KIND>(x, inverse_scale(e));
+                if (sub == 0) exps[at_exp[u]] = finite ? static_cast<uint8_t>(e + 127) : 255;
+            }
+        }
+    } else {
+        Vec8<__nv_bfloat16> wide[U];
+        uint2 codes[U];
+        uint32_t e[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!mine || place[u] < 0) continue;
+            if constexpr (KIND == SISO_BF16) wide[u].load(reinterpret_cast<const __nv_bfloat16 *>(pages) + place[u]);
+            else { codes[u] = *reinterpret_cast<const uint2 *>(pages + place[u]); e[u] = exps[at_exp[u]]; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!mine || at_ext[u] < 0) continue;
+            float x[8];
+            if (place[u] < 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = 0.f;
+            } else if constexpr (KIND == SISO_BF16) wide[u].get(x);
+            else decode8<KIND>(codes[u], kv_scale(e[u]), x);
+            Vec8<T> o;
+            o.set(x);
+            o.store(ext + at_ext[u]);
+        }
+    }
+}
+
+template <int KIND, typename T, bool READ>
+static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
+    const long long total = rows.n * kv.n_kv_heads;
+    const int g = kv.head_dim <= 64 ? 8 : kv.head_dim <= 128 ? 16 : 32;
+    const long long blocks = (total + THREADS / g * U - 1) / (THREADS / g * U);
+    if (blocks > 0x7FFFFFFFll) return SISO_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(blocks), 2);
+    if (g == 8) kv_rows_kernel<KIND, T, 8, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
+    else if (g == 16) kv_rows_kernel<KIND, T, 16, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
+    else kv_rows_kernel<KIND, T, 32, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
+    SISO_CUDA(cudaGetLastError());
+    return SISO_OK;
+}
+template <typename T, bool READ>
+static siso_status_t run_kind(int kind, const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
+    return kind == SISO_E4M3 ? run_rows<SISO_E4M3, T, READ>(kv, rows, slots, s)
+         : kind == SISO_I8 ? run_rows<SISO_I8, T, READ>(kv, rows, slots, s) : run_rows<SISO_BF16, T, READ>(kv, rows, slots, s);
+}
+
+static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+template <bool READ>
+static siso_status_t rows_call(Kv *h, int layer, void *k, void *v, int dtype, long long n, long long stride_token, long long stride_head,
+                               const int64_t *slots, cudaStream_t s) {
+    if (!h || layer < 0 || layer >= h->cfg.n_layers || n < 0) return SISO_ERR_INVALID_ARG;
+    if (dtype != SISO_F32 && dtype != SISO_BF16) return SISO_ERR_INVALID_ARG;
+    if (n == 0) return SISO_OK;
+    if (!k || !v || !slots || stride_token < 0 || stride_head < 0) return SISO_ERR_INVALID_ARG;
+    const int elems16 = dtype == SISO_F32 ? 4 : 8;
+    if (!aligned16(k) || !aligned16(v) || stride_token % elems16 != 0 || stride_head % elems16 != 0) return SISO_ERR_UNSUPPORTED;
+    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    const Rows rows{k, v, n, stride_token, stride_head};
+    const KvView kv = kv_view(h, layer);
+    const long long *sl = reinterpret_cast<const long long *>(slots);
+    return dtype == SISO_F32 ? run_kind<float, READ>(h->cfg.dtype, kv, rows, sl, s)
+                             : run_kind<__nv_bfloat16, READ>(h->cfg.dtype, kv, rows, sl, s);
+}
+
+}  // namespace kvc
+}  // namespace siso
+
+using namespace siso;
+
+extern "C" {
+
+siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
+    if (!out || !cfg) return SISO_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!cfg->d_k || !cfg->d_v || cfg->n_layers < 1 || cfg->n_pages < 1 || cfg->n_pages >= (1ll << 31) || cfg->page_size < 1 ||
+        cfg->n_kv_heads < 1 || cfg->head_dim < 1)
+        return SISO_ERR_INVALID_ARG;
+    if (cfg->dtype != SISO_BF16 && cfg->dtype != SISO_E4M3 && cfg->dtype != SISO_I8) return SISO_ERR_INVALID_ARG;
+    const bool eight = cfg->dtype != SISO_BF16;
+    if (eight != (cfg->d_k_exp != nullptr) || eight != (cfg->d_v_exp != nullptr)) return SISO_ERR_INVALID_ARG;
+    if ((cfg->allocator.alloc == nullptr) != (cfg->allocator.free == nullptr)) return SISO_ERR_INVALID_ARG;
+    if (cfg->page_size % 8 != 0 || cfg->page_size > 65536 || cfg->head_dim % 8 != 0 || cfg->head_dim > kKvMaxDim || cfg->n_kv_heads > 4096)
+        return SISO_ERR_UNSUPPORTED;
+    const long long strides[] = {cfg->stride_layer, cfg->stride_page, cfg->stride_token, cfg->stride_head};
+    for (long long st : strides) {
+        if (st < 0) return SISO_ERR_INVALID_ARG;
+        if (st % 8 != 0 || st >= (1ll << 38)) return SISO_ERR_UNSUPPORTED;
+    }
+    if (!kvc::aligned16(cfg->d_k) || !kvc::aligned16(cfg->d_v)) return SISO_ERR_UNSUPPORTED;
+    int n_dev = 0;
+    SISO_CUDA(cudaGetDeviceCount(&n_dev));
+    if (cfg->device < 0 || cfg->device >= n_dev) return SISO_ERR_INVALID_ARG;
+    SISO_CUDA(cudaSetDevice(cfg->device));
+    int major = 0, sms = 0;
+    SISO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, cfg->device));
+    SISO_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, cfg->device));
+    if (major != 10) return SISO_ERR_UNSUPPORTED;
+    siso_kv *h = new (std::nothrow) siso_kv();
+    if (!h) return SISO_ERR_OOM;
+    memset(static_cast<Kv *>(h), 0, sizeof(Kv));
+    h->cfg = *cfg;
+    if (!cfg->allocator.alloc) h->cfg.allocator = default_allocator();
+    h->sm_count = sms;
+    h->status = static_cast<int *>(h->cfg.allocator.alloc(256, nullptr, h->cfg.allocator.ctx));
+    if (!h->status) { delete h; return SISO_ERR_OOM; }
+    cudaError_t e = cudaMemset(h->status, 0, 256);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) { siso_kv_destroy(h); return check_cuda(e, "key/value cache initialisation"); }
+    *out = h;
+    return SISO_OK;
+}
+
+siso_status_t siso_kv_destroy(siso_kv_t *h) {
+    if (!h) return SISO_ERR_INVALID_ARG;
+    cudaSetDevice(h->cfg.device);
+    cudaDeviceSynchronize();
+    if (h->ws) h->cfg.allocator.free(h->ws, h->cfg.allocator.ctx);
+    if (h->status) h->cfg.allocator.free(h->status, h->cfg.allocator.ctx);
+    delete h;
+    return SISO_OK;
+}
+
+siso_status_t siso_kv_write(siso_kv_t *h, int32_t layer, const void *d_k, const void *d_v, int32_t dtype, int64_t n_tokens,
+                            int64_t stride_token, int64_t stride_head, const int64_t *d_slots, void *stream) {
+    return kvc::rows_call<false>(h, layer, const_cast<void *>(d_k), const_cast<void *>(d_v), dtype, n_tokens, stride_token, stride_head,
+                                 d_slots, static_cast<cudaStream_t>(stream));
+}
+
+siso_status_t siso_kv_read(siso_kv_t *h, int32_t layer, void *d_k, void *d_v, int32_t dtype, int64_t n_tokens, int64_t stride_token,
+                           int64_t stride_head, const int64_t *d_slots, void *stream) {
+    return kvc::rows_call<true>(h, layer, d_k, d_v, dtype, n_tokens, stride_token, stride_head, d_slots, static_cast<cudaStream_t>(stream));
+}
+
+siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *stream) {
+    if (!h || !a || a->n_tokens < 0 || a->n_seqs < 0 || a->layer < 0 || a->layer >= h->cfg.n_layers) return SISO_ERR_INVALID_ARG;
+    if (a->n_heads < 1 || a->n_heads % h->cfg.n_kv_heads != 0 || a->window < 0 || a->max_q < 0 || a->max_pages < 0) return SISO_ERR_INVALID_ARG;
+    if ((a->flags & ~SISO_ATTN_CAUSAL) != 0u || !(a->scale == a->scale)) return SISO_ERR_INVALID_ARG;
+    if (a->n_tokens == 0 || a->n_seqs == 0) return SISO_OK;
+    if (!a->d_q || !a->d_out || !a->d_cu_q || !a->d_kv_len || (a->max_pages > 0 && !a->d_pages) || a->pages_stride < 0) return SISO_ERR_INVALID_ARG;
+    const int64_t strides[] = {a->q_stride_token, a->q_stride_head, a->out_stride_token, a->out_stride_head};
+    for (int64_t st : strides) {
+        if (st < 0) return SISO_ERR_INVALID_ARG;
+        if (st % 8 != 0) return SISO_ERR_UNSUPPORTED;
+    }
+    if (!kvc::aligned16(a->d_q) || !kvc::aligned16(a->d_out)) return SISO_ERR_UNSUPPORTED;
+    if (h->cfg.head_dim != 64 && h->cfg.head_dim != 128) return SISO_ERR_UNSUPPORTED;
+    const int64_t elems16 = 16 / kv_elem_bytes(h->cfg.dtype);        // attention moves 16 bytes at a time
+    if (h->cfg.stride_layer % elems16 != 0 || h->cfg.stride_page % elems16 != 0 || h->cfg.stride_token % elems16 != 0 ||
+        h->cfg.stride_head % elems16 != 0)
+        return SISO_ERR_UNSUPPORTED;
+    if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31)) return SISO_ERR_UNSUPPORTED;
+    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
+}
+
+siso_status_t siso_kv_sync_status(siso_kv_t *h, void *stream) {
+    if (!h) return SISO_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    int st = 0;
+    SISO_CUDA(cudaMemcpyAsync(&st, h->status, sizeof(int), cudaMemcpyDeviceToHost, s));
+    SISO_CUDA(cudaMemsetAsync(h->status, 0, sizeof(int), s));
+    SISO_CUDA(cudaStreamSynchronize(s));
+    return static_cast<siso_status_t>(st);
+}
+
+}  // extern "C"

@@ -1,0 +1,219 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers.
+//
+// Draft t of a sequence is token x_t.  p_t is the target's row at t, q_t the row the draft was drawn from (no draft rows: x_t
+// was certain, q_t = [v = x_t]).  With u_t uniform in [0, 1):
+//     draft t stands if u_t q_t(x_t) < p_t(x_t);   n = the first that does not, or the number of drafts
+//     the next token is drawn from r = max(p_n - q_n, 0), or from p_n where every draft stands
+// which leaves the tokens distributed as the target's.  The draw inverts the distribution in whole numbers:
+//     w_v = floor(min(r_v, 1) 2^38),  W = sum of all w,  z = floor(u 2^24),  token = smallest v with 2^24 (w_0 + ... + w_v) > z W
+// Whole numbers add up to the same sum in any order, so the token does not depend on how the row is split, and a row of
+// 2^24 entries of at most 2^38 stays inside 64 bits.  Truncation moves a probability by at most 2^-38, less than an fp32 sum over
+// a vocabulary would.  Where the residual is empty (q_n >= p_n everywhere) the draw is from p_n; where that is empty too
+// the token is -1.
+//
+// Only row n of p and of q has to be read, so the call is bound by latency for one sequence and by HBM for many.  A cluster of
+// up to 8 CTAs shares a sequence: each warp sums the weights of one contiguous chunk, the chunk sums go to every CTA of the
+// cluster through distributed shared memory, and the CTA that owns the chunk with the crossing looks at it again (it comes
+// from L2) with a few consecutive entries per thread.  One launch, no scratch memory.
+#include "common.cuh"
+
+namespace siso {
+namespace ver {
+
+constexpr int THREADS = 512;
+constexpr int WARPS = THREADS / 32;
+constexpr int MAX_SPLIT = 8;
+constexpr int U = 8;                     // entries of each row that a lane has in flight
+
+struct Args {
+    const void *target, *draft;          // [n_seqs, n_max + 1, vocab], [n_seqs, n_max, vocab] or NULL
+    const int32_t *tokens, *n_drafts;    // [n_seqs, n_max], [n_seqs] or NULL
+    const float *u_accept, *u_sample;    // [n_seqs, n_max], [n_seqs]
+    int32_t *out, *accepted;             // [n_seqs, n_max + 1], [n_seqs]
+    int n_max, vocab;
+};
+
+template <typename T> __device__ __forceinline__ float value(const T *p) {
+    if constexpr (sizeof(T) == 2) return __bfloat162float(*p); else return *p;
+}
+// 38-bit weight of a probability; NaN and negative values weigh nothing
+__device__ __forceinline__ unsigned long long weight(float r) {
+    return static_cast<unsigned long long>(__float2ull_rz(fminf(fmaxf(r, 0.f), 1.f) * 274877906944.f));
+}
+__device__ __forceinline__ unsigned long long warp_sum(unsigned long long x) {
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    return x;
+}
+__device__ __forceinline__ unsigned long long warp_scan(unsigned long long x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// r_v of the row that the next token is drawn from: without = the entry to leave out (certain draft), q = NULL: nothing taken off
+template <typename T> struct Residual {
+    const T *p, *q;
+    int without;
+    __device__ __forceinline__ float at(int v) const {
+        const float a = value(p + v);
+        if (q) return a - value(q + v);
+        return v == without ? a - 1.f : a;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS)
+verify_kernel(Args g) {
+    __shared__ unsigned long long sums[2][MAX_SPLIT * WARPS];
+    __shared__ unsigned long long scan[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t rank, split;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+    const long long b = blockIdx.x / split;
+
+    // ---- which drafts stand: every warp finds it for itself
+    const int limit = g.n_drafts ? min(max(g.n_drafts[b], 0), g.n_max) : g.n_max;
+    const T *target = static_cast<const T *>(g.target) + b * (g.n_max + 1) * static_cast<long long>(g.vocab);
+    const T *draft = g.draft ? static_cast<const T *>(g.draft) + b * g.n_max * static_cast<long long>(g.vocab) : nullptr;
+    int n = limit;
+    for (int t0 = 0; t0 < limit; t0 += 32) {
+        const int t = t0 + lane;
+        bool stands = true;
+        if (t < limit) {
+            const int x = g.tokens[b * g.n_max + t];
+            stands = false;
+            if (x >= 0 && x < g.vocab) {
+                const long long at = static_cast<long long>(t) * g.vocab + x;
+                const float q = draft ? value(draft + at) : 1.f;
+                stands = g.u_accept[b * g.n_max + t] * q < value(target + at);
+            }
+        }
+        const uint32_t fails = __ballot_sync(0xFFFFFFFFu, !stands);
+        if (fails) { n = t0 + __ffs(fails) - 1; break; }
+    }
+    Residual<T> r;
+    r.p = target + static_cast<long long>(n) * g.vocab;
+    r.q = n < limit && draft ? draft + static_cast<long long>(n) * g.vocab : nullptr;
+    r.without = n < limit && !draft ? g.tokens[b * g.n_max + n] : -1;
+
+    // ---- sums of the chunks, one per warp of the cluster
+    const int chunks = static_cast<int>(split) * WARPS;
+    const int chunk = (g.vocab + chunks - 1) / chunks;
+    const int me = static_cast<int>(rank) * WARPS + warp;
+    unsigned long long total = 0ull;
+    int pass = 0;
+    for (; pass < 2; ++pass) {
+        const int lo = min(g.vocab, me * chunk), hi = min(g.vocab, lo + chunk);
+        unsigned long long sum = 0ull;
+        for (int v0 = lo + lane; v0 < hi; v0 += 32 * U) {
+            float x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) x[i] = v0 + 32 * i < hi ? r.at(v0 + 32 * i) : 0.f;
+#pragma unroll
+            for (int i = 0; i < U; ++i) sum += weight(x[i]);
+        }
+        sum = warp_sum(sum);
+        if (lane < static_cast<int>(split)) {
+            const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[pass][me]));
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(lane));
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there), "l"(sum) : "memory");
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        total = 0ull;
+        for (int c = lane; c < chunks; c += 32) total += sums[pass][c];
+        total = warp_sum(total);
+        if (total != 0ull) break;
+        r.q = nullptr;                    // nothing to draw from: from the target's row itself
+        r.without = -1;
+    }
+
+    if (rank == 0) {
+        for (int t = threadIdx.x; t <= g.n_max; t += THREADS)
+            if (t != n || total == 0ull) g.out[b * (g.n_max + 1) + t] = t < n ? g.tokens[b * g.n_max + t] : -1;
+        if (threadIdx.x == 0) g.accepted[b] = n;
+    }
+    if (total == 0ull) return;
+
+    // ---- the chunk with the crossing: first whose running sum exceeds floor(z W / 2^24)
+    const float u = g.u_sample[b];
+    const unsigned long long z = static_cast<unsigned long long>(fminf(fmaxf(u, 0.f) * 16777216.f, 16777215.f));
+    const unsigned long long cross = (__umul64hi(z, total) << 40) | ((z * total) >> 24);
+    unsigned long long before = 0ull;
+    int at = -1;
+    for (int c0 = 0; c0 < chunks && at < 0; c0 += 32) {
+        const unsigned long long mine = c0 + lane < chunks ? sums[pass][c0 + lane] : 0ull;
+        const unsigned long long upto = before + warp_scan(mine, lane);
+        const uint32_t over = __ballot_sync(0xFFFFFFFFu, upto > cross);
+        if (over) {
+            const int f = __ffs(over) - 1;
+            at = c0 + f;
+            before = __shfl_sync(0xFFFFFFFFu, upto - mine, f);
+        } else {
+            before = __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+    }
+    if (at < 0 || at / WARPS != static_cast<int>(rank)) return;
+    // ---- the entry: consecutive ones per thread, a scan over the CTA
+    const int lo = at * chunk, hi = min(g.vocab, lo + chunk);
+    const int each = (chunk + THREADS - 1) / THREADS;
+    const int v0 = lo + static_cast<int>(threadIdx.x) * each, v1 = min(hi, v0 + each);
+    unsigned long long sum = 0ull;
+    for (int v = v0; v < v1; ++v) sum += weight(r.at(v));
+    const unsigned long long upto = warp_scan(sum, lane);
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    unsigned long long start = before + upto - sum;
+    for (int w = 0; w < warp; ++w) start += scan[w];
+    if (start <= cross && start + sum > cross) {          // exactly one thread
+        int v = v0;
+        for (; v < v1 - 1; ++v) {
+            start += weight(r.at(v));
+            if (start > cross) break;
+        }
+        g.out[b * (g.n_max + 1) + n] = v;
+    }
+}
+
+template <typename T>
+static siso_status_t run(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(n_seqs * split));
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(split);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SISO_CUDA(cudaLaunchKernelEx(&cfg, verify_kernel<T>, g));
+    SISO_CUDA(cudaGetLastError());
+    return SISO_OK;
+}
+
+}  // namespace ver
+}  // namespace siso
+
+using namespace siso;
+
+extern "C" siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int32_t dtype, int64_t n_seqs, int32_t n_max,
+                                            int32_t vocab, const int32_t *d_tokens, const int32_t *d_n_drafts, const float *d_u_accept,
+                                            const float *d_u_sample, int32_t *d_out, int32_t *d_accepted, void *stream) {
+    if (dtype != SISO_F32 && dtype != SISO_BF16) return SISO_ERR_INVALID_ARG;
+    if (n_seqs < 0 || n_max < 0 || vocab < 1) return SISO_ERR_INVALID_ARG;
+    if (n_seqs == 0) return SISO_OK;
+    if (!d_target || !d_u_sample || !d_out || !d_accepted || (n_max > 0 && (!d_tokens || !d_u_accept))) return SISO_ERR_INVALID_ARG;
+    if (vocab > (1 << 24) || n_seqs > (1ll << 27)) return SISO_ERR_UNSUPPORTED;
+    // A sequence is shared by as many CTAs as fill the GPU's 148 SMs with a few CTAs each
+    const int split = n_seqs <= 64 ? 8 : n_seqs <= 128 ? 4 : n_seqs <= 256 ? 2 : 1;
+    const ver::Args g{d_target, n_max > 0 ? d_draft : nullptr, d_tokens, d_n_drafts, d_u_accept, d_u_sample, d_out, d_accepted, n_max, vocab};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return dtype == SISO_F32 ? ver::run<float>(g, n_seqs, split, s) : ver::run<__nv_bfloat16>(g, n_seqs, split, s);
+}
