@@ -1,0 +1,214 @@
+// Shared by the two attention kernels over the paged key/value cache: arguments, the cut of a call into units of work, the
+// partial results and their join.
+//
+// The queries of one sequence that share a key/value head form its rows: row r is token r / group, query head
+// kv_head * group + r % group.  An item is (sequence, key/value head, tile of MR rows); its keys are taken in tiles of 128, and
+// one tile of one item is a unit.  The units of a call, in the order (sequence, head, row tile, key tile), are dealt to the
+// CTAs in equal contiguous runs, so CTAs are equally loaded whatever the lengths are, and one long sequence spreads over
+// all of them.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
+// (unnormalised output, maximum, sum), and a second small kernel joins the parts of an item in a fixed order.
+#pragma once
+
+#include "kv.cuh"
+
+namespace siso {
+namespace kva {
+
+constexpr int TK = 128;                // keys of a unit
+
+// n / d for 0 <= n < 2^31 and 1 <= d < 2^31, by a multiplication: m = floor(2^(31 + s) / d) + 1 with s = ceil(log2 d)
+struct FastDiv {
+    uint32_t d, m, s;
+    __host__ void set(uint32_t divisor) {
+        d = divisor;
+        s = 0;
+        while ((1ull << s) < divisor) ++s;
+        m = static_cast<uint32_t>((1ull << (31 + s)) / divisor + 1);
+        if (divisor == 1) m = 0x80000001u;
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const {
+        return static_cast<uint32_t>((static_cast<unsigned long long>(n) * m) >> (31 + s));
+    }
+};
+
+struct Record {                        // an item that several CTAs share, kept at the first of them
+    int valid, b, head, row_tile, n_parts;
+};
+
+struct Args {
+    KvView kv;
+    siso_attention_t a;
+    FastDiv by_page, by_group;
+    int group;
+    float scale_log2;                  // scale * log2(e)
+    int grid;                          // CTAs that share the units
+    float *part_o, *part_ml;           // [2 grid][MR][D], [2 grid][MR][2]
+    Record *records;                   // [grid]
+    int *status;
+};
+
+#ifdef __CUDACC__
+// the row tile `rt` of a sequence: positions of its first and last row's token and the key tiles it has to see
+struct Span {
+    int first_pos, last_pos, lo, hi, tile0, tiles;
+};
+__device__ __forceinline__ int seq_len(const Args &g, int b) {
+    const long long cap = static_cast<long long>(g.a.max_pages) * g.kv.page_size;
+    return static_cast<int>(min(static_cast<long long>(max(g.a.d_kv_len[b], 0)), cap));
+}
+// queries of sequence b, cut to the tokens that the call has: q0 is its first row of d_q
+__device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
+    const int n = static_cast<int>(g.a.n_tokens);
+    q0 = min(max(g.a.d_cu_q[b], 0), n);
+    return max(0, min(g.a.d_cu_q[b + 1], n) - q0);
+}
+template <int MR> __device__ __forceinline__ Span span_of(const Args &g, int len, int n_q, int rt) {
+    Span s;
+    const int rows = n_q * g.group;
+    s.first_pos = len - n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR)));
+    s.last_pos = len - n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(min(rows, (rt + 1) * MR) - 1)));
+    s.hi = (g.a.flags & SISO_ATTN_CAUSAL) ? max(0, min(len, s.last_pos + 1)) : len;
+    s.lo = g.a.window > 0 ? max(0, s.first_pos - g.a.window + 1) : 0;
+    s.tile0 = s.lo / TK;
+    s.tiles = max(1, (s.hi + TK - 1) / TK - s.tile0);       // a row tile that sees nothing is one unit that writes zeros
+    return s;
+}
+// units of one key/value head of sequence b
+template <int MR> __device__ __forceinline__ int seq_units(const Args &g, int b) {
+    int q0;
+    const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
+    int units = 0;
+    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR>(g, len, n_q, rt).tiles;
+    return units;
+}
+
+// The item that a unit belongs to, and the unit's place in it.
+template <int MR> struct Cursor {
+    int b, head, rt, q0, n_q, len, tile;
+    Span s;
+    __device__ __forceinline__ void load_seq(const Args &g) {
+        n_q = seq_queries(g, b, q0);
+        len = seq_len(g, b);
+    }
+    __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR>(g, len, n_q, rt); }
+    // `within`: units of sequence b before this one
+    __device__ __forceinline__ void seek(const Args &g, int seq, long long within, int per_head) {
+        b = seq;
+        load_seq(g);
+        head = static_cast<int>(within / per_head);
+        int left = static_cast<int>(within - static_cast<long long>(head) * per_head);
+        for (rt = 0;; ++rt) {
+            load_span(g);
+            if (left < s.tiles) break;
+            left -= s.tiles;
+        }
+        tile = left;
+    }
+    __device__ __forceinline__ void next_item(const Args &g) {
+        tile = 0;
+        if ((rt + 1) * MR < n_q * g.group) ++rt;
+        else {
+            rt = 0;
+            if (++head == g.kv.n_kv_heads) {
+                head = 0;
+                do { ++b; load_seq(g); } while (n_q == 0);     // only called while units are left
+            }
+        }
+        load_span(g);
+    }
+};
+
+// This CTA's run [u0, u1) of the call's units and the cursor at its start; every thread of the CTA gets the same.  False: none.
+// The CTA's record is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
+template <int MR, int THREADS>
+__device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &u1, long long &total, int &ctas, Cursor<MR> &cur,
+                                       unsigned long long *buf) {
+    constexpr int WARPS = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int cta = blockIdx.x;
+    if (threadIdx.x == 0) g.records[cta].valid = 0;
+    unsigned long long first = 0ull, upto = 0ull;             // units of the first chunk of sequences: mine, and up to mine
+    int per_head = 0;
+    total = 0;
+    for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
+        const int b = c0 + static_cast<int>(threadIdx.x);
+        const int ph = b < g.a.n_seqs ? seq_units<MR>(g, b) : 0;
+        const unsigned long long mine = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads;
+        unsigned long long x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+            if (lane >= o) x += y;
+        }
+        __syncthreads();
+        if (lane == 31) buf[warp] = x;
+        __syncthreads();
+        unsigned long long before = 0ull, all = 0ull;
+        for (int w = 0; w < WARPS; ++w) {
+            if (w < warp) before += buf[w];
+            all += buf[w];
+        }
+        if (c0 == 0) { first = mine; upto = before + x; per_head = ph; }
+        total += static_cast<long long>(all);
+    }
+    ctas = static_cast<int>(min(static_cast<long long>(g.grid), total));
+    if (cta >= ctas) return false;
+    u0 = total * cta / ctas;
+    u1 = total * (cta + 1) / ctas;
+    // the sequence that unit u0 belongs to
+    long long base = 0;
+    for (int c0 = 0;; c0 += THREADS) {
+        if (c0 > 0) {
+            const int b = c0 + static_cast<int>(threadIdx.x);
+            per_head = b < g.a.n_seqs ? seq_units<MR>(g, b) : 0;
+            first = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
+            unsigned long long x = first;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
+            }
+            __syncthreads();
+            if (lane == 31) buf[warp] = x;
+            __syncthreads();
+            upto = static_cast<unsigned long long>(base) + x;
+            for (int w = 0; w < warp; ++w) upto += buf[w];
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) buf[WARPS] = ~0ull;
+        __syncthreads();
+        const unsigned long long want = static_cast<unsigned long long>(u0);
+        if (want < upto && want >= upto - first) {             // exactly one thread of one chunk
+            buf[WARPS] = (static_cast<unsigned long long>(c0 + threadIdx.x) << 32) | static_cast<uint32_t>(per_head);
+            buf[WARPS + 1] = upto - first;
+        }
+        if (threadIdx.x == THREADS - 1) buf[0] = upto;
+        __syncthreads();
+        const unsigned long long found = buf[WARPS];
+        base = static_cast<long long>(buf[0]);
+        if (found != ~0ull) {
+            cur.seek(g, static_cast<int>(found >> 32), u0 - static_cast<long long>(buf[WARPS + 1]), static_cast<int>(found & 0xFFFFFFFFull));
+            return true;
+        }
+    }
+}
+// the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u
+__device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
+    return static_cast<int>(((u + 1) * ctas - 1) / total);
+}
+// Where a part goes: a CTA's run has at most one item that began before it (place 0) and one that goes on after it (place 1).
+__device__ __forceinline__ long long part_place(int cta, bool began_before) { return 2ll * cta + (began_before ? 0 : 1); }
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+#endif  // __CUDACC__
+
+// joins the parts of every item that was cut; MR = rows of a row tile, D = head_dim
+siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s);
+siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s);
+
+}  // namespace kva
+}  // namespace siso

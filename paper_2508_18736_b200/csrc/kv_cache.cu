@@ -256,7 +256,8 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
         if (st < 0) return SISO_ERR_INVALID_ARG;
         if (st % 8 != 0 || st >= (1ll << 38)) return SISO_ERR_UNSUPPORTED;
     }
-    if (!kvc::aligned16(cfg->d_k) || !kvc::aligned16(cfg->d_v)) return SISO_ERR_UNSUPPORTED;
+    if (!kvc::aligned16(cfg->d_k) || !kvc::aligned16(cfg->d_v) || !kvc::aligned16(cfg->d_k_exp) || !kvc::aligned16(cfg->d_v_exp))
+        return SISO_ERR_UNSUPPORTED;
     int n_dev = 0;
     SISO_CUDA(cudaGetDeviceCount(&n_dev));
     if (cfg->device < 0 || cfg->device >= n_dev) return SISO_ERR_INVALID_ARG;
@@ -318,7 +319,7 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *s
     if (h->cfg.stride_layer % elems16 != 0 || h->cfg.stride_page % elems16 != 0 || h->cfg.stride_token % elems16 != 0 ||
         h->cfg.stride_head % elems16 != 0)
         return SISO_ERR_UNSUPPORTED;
-    if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31)) return SISO_ERR_UNSUPPORTED;
+    if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     SISO_CUDA(cudaSetDevice(h->cfg.device));
     return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
 }
