@@ -24,6 +24,9 @@ struct Kv {
     void *ws;                      // scratch, grown on demand
     size_t ws_bytes;
     int *status;                   // device status word (first error wins)
+    CUtensorMap map_k, map_v;      // (d, head, token, page, layer), for attention: head_dim 64 or 128
+    int box;                       // tokens of their boxes: the largest power of two that divides the page and 128
+    uint32_t attr_set;             // attention kernels that have been given their shared memory
 };
 
 inline int kv_elem_bytes(int dtype) { return dtype == SISO_BF16 ? 2 : 1; }

@@ -7,60 +7,80 @@
 // A row that sees nothing gives out = 0 and lse = -infinity.
 //
 // With few rows every byte of the cache meets few multiplications, so the call is bound by HBM: the point is to keep loads in
-// flight.  One CTA of 8 warps per SM holds a ring of units (128 keys and their values, about 190 KB in all) filled by cp.async,
-// two units or more ahead.  WK = 8 / WM groups of WM warps split the unit's keys; a warp owns 16 rows and its group's keys, so up
-// to 16 rows (WM = 1) no byte is read from shared memory twice and no warp waits for another inside a run of units.
+// flight and to spend few instructions on a byte.  One CTA per SM: four producer warps fill a ring of units (128 keys and their
+// values, about 190 KB in all) by TMA, one box per run of tokens that lie in one page, and 8 warps consume it.  A unit's keys
+// are split over WK groups of WM warps; a warp owns 8 NT rows and its group's keys, so up to 16 rows (WM = 1) no byte is
+// read from shared memory twice and no warp waits for another inside an item.
 // Matrix products are mma.sync m16n8k16 with fp32 sums: tcgen05 works on 128 rows, of which a decoding step would fill 1 to 16.
+// They are taken transposed, scores^T = K Q^T and out^T = V^T P^T, so that the rows fill the 8 columns and keys and d the 16 rows.
 // K fragments come straight from 16-byte shared loads: the sum over d may be taken in any order, so a lane takes 16 consecutive
 // bytes of its key and the queries are laid out to match.  V fragments come through ldmatrix.trans; over 8-bit codes it hands
-// a lane the pairs (key, d), (key, d + 1), (key + 1, d), (key + 1, d + 1), which are the fragments of an even and an odd column.
+// a lane the pairs (key, d), (key, d + 1), (key + 1, d), (key + 1, d + 1), the fragments of an even and an odd d.  Probabilities
+// change from the first product's layout to the second's by movmatrix.
 // 8-bit codes are turned into fp16, not bf16: one conversion per two codes, exact.  The key's scale goes to its score, the
 // value's to its probability relative to the largest one so far.  Queries are brought into fp16's range by a power of two per row
 // (exact but for elements 2^-39 below the row's largest), probabilities are scaled by 2^15.
 #include <cuda_fp16.h>
 
 #include "kv_attention.cuh"
+#include "umma_pair.cuh"
 
 namespace siso {
 namespace kva {
 
-constexpr int THREADS = 256;
-constexpr int SMEM_MOST = 232448 - 256;   // what a CTA may have, less its static part
+using umma2::mbar_arrive;
+using umma2::mbar_arrive_expect_tx;
+using umma2::mbar_init;
+using umma2::smem_u32;
 
-template <int KIND, int D, int WM> struct Shape {
-    static constexpr int WK = 8 / WM;                       // groups of warps along the keys
-    static constexpr int MR = 16 * WM;                      // rows of a row tile
-    static constexpr int NK = TK / WK;                      // keys of a group
+constexpr unsigned long long WAIT_NS = 1000000000ull;       // a wait gives up after a second
+constexpr int SMEM_MOST = 232448 - 512 - 1024;   // what a CTA may have, less its static part and the alignment of the ring
+
+constexpr int PRODUCERS = 4;             // warps that fill the ring; each has its own stages
+
+template <int KIND, int D, int WM, int NT> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
+    static constexpr int WK = 8 / WM;                       // groups of warps along a unit's keys
+    static constexpr int WARPS = 8;                         // consumers
+    static constexpr int T = EIGHT && NT == 1 ? 256 : 128;  // keys of a unit
+    static constexpr int THREADS = 32 * (WARPS + PRODUCERS);
+    static constexpr int PRODUCER_REGS = 40, CONSUMER_REGS = 232;
+    static_assert(WARPS * CONSUMER_REGS + PRODUCERS * PRODUCER_REGS == (WARPS + PRODUCERS) * 168, "168 registers a thread at launch");
+    static constexpr int MR = 8 * NT * WM;                  // rows of a row tile
+    static constexpr int NK = T / WK;                      // keys of a group
     static constexpr int RB = D * (EIGHT ? 1 : 2);          // bytes of a row
     static constexpr int CH = RB / 16;                      // 16-byte chunks of a row
-    static constexpr int STAGE = 2 * TK * RB;
-    static constexpr int META = TK * 4 + (EIGHT ? 2 * TK : 0);        // whether each key is there, exponents
-    static constexpr int MERGE = 4 * 16 * D * 4 + 8 * 16 * 2 * 4;     // outputs, maxima and sums of half the warps
+    static constexpr int STAGE = 2 * T * RB;
+    static constexpr int META = EIGHT ? 2 * T : 0;         // exponents
+    static constexpr int MERGE_O = WARPS / 2 * 8 * NT * D;  // outputs of half the warps
+    static constexpr int MERGE = (MERGE_O + WARPS / 2 * 16 * NT) * 4;
     static constexpr int FIT = (SMEM_MOST - MERGE) / (STAGE + META);
     static constexpr int STAGES = FIT > 8 ? 8 : FIT;
-    static constexpr int SMEM = STAGES * (STAGE + META) + MERGE;
+    static constexpr int SMEM = STAGES * (STAGE + META) + MERGE + 1024;
 };
 
-// byte offset of a 16-byte chunk in a tile of rows: neighbouring rows differ in the upper half of a 128-byte line (the 8 lanes of a
-// 16-byte load read 4 chunks of 2 rows), and 8 rows of one chunk differ in all of it (ldmatrix)
-template <int CH> __device__ __forceinline__ int chunk_at(int row, int chunk) {
-    if constexpr (CH == 4) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
-    else return row * (CH * 16) + ((chunk ^ (((row & 1) << 2) | ((row >> 1) & 3))) << 4);
+// byte offset of a 16-byte chunk in a tile of TK rows as TMA writes it: lines of 128 bytes with the chunk's place xor-ed with the
+// row's lowest bits (rows of 256 bytes are two such tiles), or of 64 bytes
+template <int RB, int TK> __device__ __forceinline__ int chunk_at(int row, int chunk) {
+    if constexpr (RB == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+    else return (chunk >> 3) * (TK * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool take) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy8(uint32_t dst, const void *src, bool take) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(take ? 8 : 0) : "memory");
-}
-template <bool HALF> __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+// Which of 8 keys the n-th row of a product is.  The 8 lanes of one 16-byte load read 4 chunks of rows 2i and 2i + 1: those keys have
+// to lie in different halves of their lines
+template <int RB> __device__ __forceinline__ int key_of(int n) { return RB == 64 ? n : ((n & 1) << 2) | (n >> 1); }
+
+template <bool HALF> __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
     if constexpr (HALF)
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ void load_v(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -87,383 +107,481 @@ template <int KIND, bool SPLIT> __device__ __forceinline__ void widen(uint32_t w
         hi = *reinterpret_cast<const uint32_t *>(&y);
     }
 }
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int d, int head, int token, int page, int layer, uint64_t *bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(d), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(smem_u32(bar))
+                 : "memory");
+}
+// A wait for this CTA's own copies or warps, bounded; once any has given up, none waits any more: the loops run to their ends on
+// whatever the ring holds, so every barrier of the CTA is still met.
+__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatile int *gave_up) {
+    if (umma2::mbar_try_wait_cta(bar, parity)) return;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (uint32_t it = 1; it < umma2::SPIN_LIMIT; ++it) {
+        if (umma2::mbar_try_wait_cta(bar, parity)) return;
+        if ((it & 63u) == 0u) {
+            if (*gave_up) return;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t - t0 > WAIT_NS) break;
+        }
+    }
+    *gave_up = 1;
+}
 
-template <int KIND, int D, int WM>
-__global__ void __launch_bounds__(THREADS, 1)
-attention_few_rows_kernel(const __grid_constant__ Args g) {
-    using S = Shape<KIND, D, WM>;
-    constexpr int NK = S::NK, CH = S::CH, RB = S::RB, MR = S::MR;
+template <int STAGES> struct Ring {
+    uint64_t full[STAGES], empty[STAGES];
+    uint32_t blocks[STAGES];           // bit i: the page of keys 8 i .. 8 i + 7 of the unit is in the pool
+    int gave_up;
+};
+
+template <int KIND, int D, int WM, int NT>
+__global__ void __launch_bounds__(Shape<KIND, D, WM, NT>::THREADS, 1)
+attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    using S = Shape<KIND, D, WM, NT>;
+    constexpr int NK = S::NK, CH = S::CH, RB = S::RB, MR = S::MR, STAGES = S::STAGES, WK = S::WK, WARPS = S::WARPS, TK = S::T;
     constexpr bool EIGHT = S::EIGHT;
     constexpr int SUB = NK < 32 ? NK : 32;                   // keys between two looks at the running maximum
-    constexpr int ROWS = CH / 2;                             // key rows that a thread copies per unit
-    constexpr int STEP = 32 * WM / CH;                       // rows that a group copies at once
-    constexpr int O_TILES = D / 8;
-    extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t *meta = smem + S::STAGES * S::STAGE;
-    float *merge_o = reinterpret_cast<float *>(meta + S::STAGES * S::META);
-    float *merge_ml = merge_o + 4 * 16 * D;
-    __shared__ unsigned long long buf[THREADS / 32 + 2];
+    constexpr uint32_t ALL = TK == 256 ? 0xFFFFFFFFu : 0xFFFFu;       // a bit per 8 keys
+    constexpr int LINE = RB < 128 ? RB : 128;                // bytes of a row that lie together
+    constexpr int KT = SUB / 16, DT = D / 16;                // tiles of 16 keys, of 16 d
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ unsigned long long buf[S::THREADS / 32 + 2];
+    __shared__ Ring<STAGES> ring;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // (an offset: the loads stay shared loads)
+    float *merge_o = reinterpret_cast<float *>(smem + STAGES * S::STAGE);
+    float *merge_ml = merge_o + S::MERGE_O;
+    uint8_t *meta = reinterpret_cast<uint8_t *>(merge_ml + WARPS / 2 * 16 * NT);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int kg = warp / WM, wm = warp % WM;
-    const int tg = threadIdx.x % (32 * WM);                  // thread of the group
-    const int c = lane & 3, r0 = lane >> 2;
-
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&ring.full[i], EIGHT ? 33 : 1); mbar_init(&ring.empty[i], 8); }      // 33: the bytes, and the lanes' exponents
+        ring.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
     long long u0, u1, total;
     int ctas;
-    Cursor<MR> cur;
-    if (!locate<MR, THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
-    Cursor<MR> ahead = cur;
+    Cursor<MR, TK> cur;
+    if (!locate<MR, TK, S::THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
+    volatile int *gave_up = &ring.gave_up;
 
-    // ---- loading: page indices are fetched one unit before the copies that need them
-    int pages[ROWS], exp_page = -1;
-    long long ahead_u = u0;
-    auto page_of = [&](int j) -> int {
-        if (j >= ahead.s.hi) return -1;
-        const int page = g.a.d_pages[ahead.b * g.a.pages_stride + g.by_page.div(j)];
-        if (page >= 0 && page < g.kv.n_pages) return page;
-        set_status(g.status, SISO_ERR_INVALID_ARG);
-        return -1;
-    };
-    auto fetch_pages = [&]() {
-        const int j0 = (ahead.s.tile0 + ahead.tile) * TK + kg * NK;
+    // registers move from the producers to the consumers: WARPS of CONSUMER_REGS and 4 of PRODUCER_REGS make what the CTA has
+    if (warp >= WARPS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::PRODUCER_REGS));
+        // ---- producers: lanes 0-15 own the unit's blocks of 8 keys, lanes 16-31 of 8 values, 16 blocks at a time
+        constexpr int HALVES = TK / 128;
+        const int is_v = lane >> 4;
+        const CUtensorMap *map = is_v ? &map_v : &map_k;
+        const uint8_t *exps = is_v ? g.kv.v_exp : g.kv.k_exp;
+        const int box_blocks = g.box / 8;
+        int stage = 0;
+        uint32_t phase = 0;
+        for (long long u = u0; u < u1; ++u) {
+            if (stage % PRODUCERS == warp - WARPS) {         // a stage is always filled by the same warp, so its rounds come in order
+                int page[HALVES], tok[HALVES];
+                bool first[HALVES];
+                uint32_t there = 0u, boxes = 0u;
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) pages[i] = page_of(j0 + tg / CH + i * STEP);
-        if (EIGHT && tg < NK / 4) exp_page = page_of(j0 + (tg % (NK / 8)) * 8);
-    };
-    auto issue = [&](int stage) {
-        const int j0 = (ahead.s.tile0 + ahead.tile) * TK + kg * NK;
-        const uint32_t k_dst = static_cast<uint32_t>(__cvta_generic_to_shared(smem + stage * S::STAGE));
-        const uint32_t v_dst = k_dst + TK * RB;
-        uint32_t *there = reinterpret_cast<uint32_t *>(meta + stage * S::META);
-        const int chunk = tg % CH;
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int r = kg * NK + tg / CH + i * STEP, j = j0 + tg / CH + i * STEP;
-            const int page = max(pages[i], 0);
-            const int t = j - static_cast<int>(g.by_page.div(j)) * g.kv.page_size;
-            const long long at = (page * g.kv.stride_page + t * g.kv.stride_token + ahead.head * g.kv.stride_head) * (RB / D) + chunk * 16;
-            copy16(k_dst + chunk_at<CH>(r, chunk), static_cast<const char *>(g.kv.k) + (pages[i] < 0 ? 0 : at), pages[i] >= 0);
-            copy16(v_dst + chunk_at<CH>(r, chunk), static_cast<const char *>(g.kv.v) + (pages[i] < 0 ? 0 : at), pages[i] >= 0);
-            if (chunk == 0) there[r] = pages[i] < 0 ? 0u : 0xFFFFFFFFu;
-        }
-        if (EIGHT && tg < NK / 4) {                          // 8 exponents of a page lie side by side
-            const int blk = tg % (NK / 8), j = j0 + blk * 8;
-            const bool is_v = tg >= NK / 8;
-            const int t = j - static_cast<int>(g.by_page.div(j)) * g.kv.page_size;
-            const long long at = exp_page < 0 ? 0 : (static_cast<long long>(exp_page) * g.kv.n_kv_heads + ahead.head) * g.kv.page_size + t;
-            const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(meta + stage * S::META)) + TK * 4 + (is_v ? TK : 0) + kg * NK + blk * 8;
-            copy8(dst, (is_v ? g.kv.v_exp : g.kv.k_exp) + at, exp_page >= 0);
-        }
-    };
-    auto load_unit = [&](int stage) {
-        if (ahead_u < u1) {
-            issue(stage);
-            if (++ahead_u < u1) {
-                if (++ahead.tile == ahead.s.tiles) ahead.next_item(g);
-                fetch_pages();
-            }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    fetch_pages();
-#pragma unroll 1
-    for (int s = 0; s < S::STAGES - 1; ++s) load_unit(s);
-
-    // ---- state of the row tile: this warp's 16 rows over its group's keys
-    uint32_t q[D / 16][4];
-    float o[O_TILES][4], m[2], l[2], row_scale[2];
-    int pos[2], e_top = 0;
-    long long began = u0;                                    // unit at which the current part of the item began
-    bool fresh = true;
-    int stage = 0;
-    for (long long u = u0; u < u1; ++u) {
-        if (fresh) {
-            fresh = false;
-            began = u;
-            e_top = 0;
-#pragma unroll
-            for (int t = 0; t < O_TILES; ++t) { o[t][0] = 0.f; o[t][1] = 0.f; o[t][2] = 0.f; o[t][3] = 0.f; }
-            uint4 raw[2][EIGHT ? D / 32 : D / 32];           // 16 bytes of each of D / 32 chunks, two rows
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = cur.rt * MR + wm * 16 + r0 + 8 * h;
-                const bool real = row < cur.n_q * g.group;
-                const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(real ? row : 0)));
-                const int head = cur.head * g.group + (real ? row - i * g.group : 0);
-                pos[h] = real ? cur.len - cur.n_q + i : cur.s.last_pos;
-                m[h] = -INFINITY;
-                l[h] = 0.f;
-                row_scale[h] = g.scale_log2;
-                const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    // bf16 cache: a lane's 16 bytes of a key hold 8 values; 8-bit: 16 values, two pieces of 8
-                    const int d = EIGHT ? ((x / 2) * 4 + c) * 16 + (x & 1) * 8 : (x * 4 + c) * 8;
-                    raw[h][x] = real ? *reinterpret_cast<const uint4 *>(src + d) : make_uint4(0u, 0u, 0u, 0u);
-                }
-            }
-            if constexpr (EIGHT) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t top = 0u;
-#pragma unroll
-                    for (int x = 0; x < D / 32; ++x) {
-                        const uint32_t w[4] = {raw[h][x].x, raw[h][x].y, raw[h][x].z, raw[h][x].w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7FFF0000u, w[i] & 0x7FFF0000u));
+                for (int x = 0; x < HALVES; ++x) {
+                    const int blk = x * 16 + (lane & 15), j = (cur.s.tile0 + cur.tile) * TK + blk * 8;
+                    const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
+                    tok[x] = j - at * g.kv.page_size;
+                    page[x] = -1;
+                    if (j < cur.s.hi) {
+                        page[x] = g.a.d_pages[cur.b * g.a.pages_stride + at];
+                        if (page[x] < 0 || page[x] >= g.kv.n_pages) { page[x] = -1; set_status(g.status, SISO_ERR_INVALID_ARG); }
                     }
-                    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                    const int ex = min(max(static_cast<int>(top >> 23), 16), 254);     // the row's largest value becomes 2^14 .. 2^15
-                    const float up = __uint_as_float(static_cast<uint32_t>(min(127 + 14 + 127 - ex, 254)) << 23);
-                    row_scale[h] *= 1.f / up;
+                    first[x] = j < cur.s.hi && blk % box_blocks == 0;
+                }
 #pragma unroll
-                    for (int x = 0; x < D / 32; ++x) {
-                        uint32_t w[4] = {raw[h][x].x, raw[h][x].y, raw[h][x].z, raw[h][x].w};
+                for (int x = 0; x < HALVES; ++x) {
+                    there |= (__ballot_sync(0xFFFFFFFFu, page[x] >= 0) & 0xFFFFu) << (16 * x);
+                    boxes += __popc(__ballot_sync(0xFFFFFFFFu, first[x]));
+                }
+                wait_bar(&ring.empty[stage], phase ^ 1u, gave_up);
+                if (*gave_up) break;
+                uint64_t *bar = &ring.full[stage];
+                if (lane == 0) {
+                    ring.blocks[stage] = there;
+                    mbar_arrive_expect_tx(bar, boxes * (g.box * RB));
+                }
+                __syncwarp();
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = pack(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xFFFF0000u) * up, true);
-                        raw[h][x] = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int x = 0; x < HALVES; ++x) {
+                    const int blk = x * 16 + (lane & 15);
+                    if (first[x]) {
+                        const uint32_t dst = smem_u32(smem + stage * S::STAGE) + is_v * (TK * RB) + blk * 8 * LINE;
+                        // a page outside the pool is asked for at a place beyond the tensor's end, which reads as zeros
+                        const int p = page[x] < 0 ? static_cast<int>(g.kv.n_pages) : page[x];
+#pragma unroll
+                        for (int half = 0; half < RB / LINE; ++half)
+                            load_box(dst + half * (TK * 128), map, half * 64, cur.head, tok[x], p, g.a.layer, bar);
+                    }
+                    if constexpr (EIGHT) {                   // 8 exponents of a page lie side by side
+                        const uint32_t dst = smem_u32(meta) + stage * S::META + is_v * TK + blk * 8;
+                        const long long e = page[x] < 0 ? 0 : (static_cast<long long>(page[x]) * g.kv.n_kv_heads + cur.head) * g.kv.page_size + tok[x];
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(exps + e), "r"(page[x] < 0 ? 0 : 8) : "memory");
                     }
                 }
+                if constexpr (EIGHT) asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
             }
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
+        }
+        if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
+        if (*gave_up) {
+            for (int i = 0; i < 64; ++i) __nanosleep(1000);      // copies in flight land before the shared memory is handed back
+            if (lane == 0) set_status(g.status, SISO_ERR_TIMEOUT);
+        }
+        return;
+    }
+
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::CONSUMER_REGS));
+    // ---- consumers: this warp's 8 NT rows over its group's keys.  A lane has keys (and d) r0 and r0 + 8 of a tile of 16, rows 2 c
+    // and 2 c + 1 of a tile of 8; as a query's carrier it has row r0.
+    const int kg = warp / WM, wm = warp % WM;
+    const int c = lane & 3, r0 = lane >> 2;
+    const bool causal = (g.a.flags & SISO_ATTN_CAUSAL) != 0u;
+    // the row that this lane points ldmatrix to: bf16: keys 0-7 of two chunks of 8 d, then keys 8-15; 8 bits: keys 0-7, then 8-15
+    // of a chunk of 16 d, then the next chunk
+    const uint32_t v_lane = EIGHT ? chunk_at<RB, TK>(key_of<RB>(lane & 7) + (lane & 8), lane >> 4)
+                                  : chunk_at<RB, TK>(key_of<RB>(lane & 7) + ((lane & 16) >> 1), (lane >> 3) & 1);
+    uint32_t q[NT][D / 16][2];
+    float o[NT][DT][4], m[NT][2], l[NT][2], row_scale[NT][2];
+    int pos[NT][2], e_top = 0;
+
+    // the queries of an item: 8 values of each of D / 32 pieces per lane.  bf16 cache: a lane's 16 bytes of a key hold 8 values;
+    // 8-bit: 16 values, two pieces of 8
+    auto fetch_q = [&]() {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = cur.rt * MR + (wm * NT + t) * 8 + r0;
+            const bool real = row < cur.n_q * g.group;
+            const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(real ? row : 0)));
+            const int head = cur.head * g.group + (real ? row - i * g.group : 0);
+            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
-                q[2 * x][0] = raw[0][x].x; q[2 * x][2] = raw[0][x].y; q[2 * x + 1][0] = raw[0][x].z; q[2 * x + 1][2] = raw[0][x].w;
-                q[2 * x][1] = raw[1][x].x; q[2 * x][3] = raw[1][x].y; q[2 * x + 1][1] = raw[1][x].z; q[2 * x + 1][3] = raw[1][x].w;
+                const int d = EIGHT ? ((x / 2) * 4 + c) * 16 + (x & 1) * 8 : (x * 4 + c) * 8;
+                const uint4 w = real ? *reinterpret_cast<const uint4 *>(src + d) : make_uint4(0u, 0u, 0u, 0u);
+                q[t][2 * x][0] = w.x; q[t][2 * x][1] = w.y; q[t][2 * x + 1][0] = w.z; q[t][2 * x + 1][1] = w.w;
             }
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::STAGES - 2) : "memory");
-        if constexpr (WM == 1) __syncwarp();
-        else asm volatile("bar.sync %0, %1;" ::"r"(kg + 1), "n"(32 * WM) : "memory");
-        load_unit(stage == 0 ? S::STAGES - 1 : stage - 1);
-
-        const uint8_t *k_tile = smem + stage * S::STAGE;
-        const uint32_t v_tile = static_cast<uint32_t>(__cvta_generic_to_shared(k_tile)) + TK * RB;
+    };
+    auto begin_item = [&]() {
+        e_top = 0;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) { o[t][d][0] = 0.f; o[t][d][1] = 0.f; o[t][d][2] = 0.f; o[t][d][3] = 0.f; }
+            float back = 1.f;
+            if constexpr (EIGHT) {
+                uint32_t top = 0u;
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) top = max(top, max((q[t][x][i] << 16) & 0x7FFF0000u, q[t][x][i] & 0x7FFF0000u));
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                const int ex = min(max(static_cast<int>(top >> 23), 16), 254);     // the row's largest value becomes 2^14 .. 2^15
+                const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
+                back = __uint_as_float(static_cast<uint32_t>(max(ex - 14, 1)) << 23);
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        q[t][x][i] = pack(__uint_as_float(q[t][x][i] << 16) * up, __uint_as_float(q[t][x][i] & 0xFFFF0000u) * up, true);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = cur.rt * MR + (wm * NT + t) * 8 + 2 * c + h;
+                pos[t][h] = row < cur.n_q * g.group ? cur.len - cur.n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))) : cur.s.last_pos;
+                m[t][h] = -INFINITY;
+                l[t][h] = 0.f;
+                row_scale[t][h] = g.scale_log2 * __shfl_sync(0xFFFFFFFFu, back, (2 * c + h) * 4);
+            }
+        }
+    };
+    fetch_q();
+    begin_item();
+    long long began = u0;                                    // unit at which the current part of the item began
+    int stage = 0;
+    uint32_t phase = 0;
+    for (long long u = u0; u < u1; ++u) {
+        wait_bar(&ring.full[stage], phase, gave_up);
+        uint8_t *tile = smem + stage * S::STAGE;
+        const int k_first = stage * S::STAGE + chunk_at<RB, TK>(key_of<RB>(r0), c);
+        const uint32_t v_first = smem_u32(tile) + TK * RB + v_lane;
         const uint8_t *mt = meta + stage * S::META;
         const int j0 = (cur.s.tile0 + cur.tile) * TK;
-        const bool cut = ((g.a.flags & SISO_ATTN_CAUSAL) && j0 + TK - 1 > cur.s.first_pos) ||
+        const uint32_t blocks = ring.blocks[stage];
+        const bool cut = j0 + TK > cur.s.hi || blocks != ALL || (causal && j0 + TK - 1 > cur.s.first_pos) ||
                          (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
+        if (j0 + TK > cur.s.hi) {    // values beyond the end may be anything: zeros, or 0 times NaN would reach the sums
+            for (int x = wm * 32 + lane; x < NK * CH; x += 32 * WM) {
+                const int row = kg * NK + x / CH;
+                if (j0 + row >= cur.s.hi) *reinterpret_cast<uint4 *>(tile + TK * RB + chunk_at<RB, TK>(row, x % CH)) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            if constexpr (WM == 1) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" ::"r"(kg + 2), "n"(32 * WM) : "memory");
+        }
 #pragma unroll 1
         for (int n0 = kg * NK; n0 < (kg + 1) * NK; n0 += SUB) {
-            float s[SUB / 8][4];
+            float s[KT][NT][4];
 #pragma unroll
-            for (int i = 0; i < SUB / 8; ++i) { s[i][0] = 0.f; s[i][1] = 0.f; s[i][2] = 0.f; s[i][3] = 0.f; }
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) { s[i][t][0] = 0.f; s[i][t][1] = 0.f; s[i][t][2] = 0.f; s[i][t][3] = 0.f; }
 #pragma unroll
             for (int a = 0; a < RB / 64; ++a) {
 #pragma unroll
-                for (int i = 0; i < SUB / 8; ++i) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(k_tile + chunk_at<CH>(n0 + 8 * i + r0, 4 * a + c));
+                for (int i = 0; i < KT; ++i) {
+                    // chunk 4 a + c of keys row and row + 8: tiles start at multiples of 1024, so a only flips bits
+                    const int at = ((k_first + (n0 + 16 * i) * LINE) ^ ((a & 1) << 6)) + (a >> 1) * (TK * 128);
+                    const uint4 w0 = *reinterpret_cast<const uint4 *>(smem + at);
+                    const uint4 w1 = *reinterpret_cast<const uint4 *>(smem + at + 8 * LINE);
+                    const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
                     if constexpr (!EIGHT) {
-                        mma<false>(s[i], q[2 * a], w.x, w.y);
-                        mma<false>(s[i], q[2 * a + 1], w.z, w.w);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const uint32_t f[4] = {x0[2 * x], x1[2 * x], x0[2 * x + 1], x1[2 * x + 1]};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma<false>(s[i][t], f, q[t][2 * a + x]);
+                        }
                     } else {
-                        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            uint32_t b0, b1;
-                            widen<KIND, false>(ws[x], b0, b1);
-                            mma<true>(s[i], q[4 * a + x], b0, b1);
+                            uint32_t f[4];
+                            widen<KIND, false>(x0[x], f[0], f[2]);
+                            widen<KIND, false>(x1[x], f[1], f[3]);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma<true>(s[i][t], f, q[t][4 * a + x]);
                         }
                     }
                 }
             }
-            // scores in powers of two, masks, running maximum.  A key that is not there is left out by selection, not by adding
-            // -infinity: its exponents may be anything
-            float top[2] = {-INFINITY, -INFINITY};
-            uint32_t ev[SUB / 8];
-            uint32_t e_max = 0u;
+            // scores in powers of two; element 2 e + h of a tile: key 8 e + key_of(r0) of the 16, row 2 c + h
+            uint32_t ev[KT][2];
 #pragma unroll
-            for (int i = 0; i < SUB / 8; ++i) {
-                const int n = n0 + 8 * i + 2 * c;
-                const uint2 there = *reinterpret_cast<const uint2 *>(mt + n * 4);
-                float ks0 = 1.f, ks1 = 1.f;
-                if constexpr (EIGHT) {
-                    const uint32_t e = *reinterpret_cast<const uint16_t *>(mt + TK * 4 + n);
-                    ks0 = kv_scale(e & 0xFFu);
-                    ks1 = kv_scale(e >> 8);
-                    ev[i] = *reinterpret_cast<const uint16_t *>(mt + TK * 5 + n) & (there.x & 0xFFu | there.y & 0xFF00u);
-                    e_max = max(e_max, max(ev[i] & 0xFFu, ev[i] >> 8));
-                }
+            for (int i = 0; i < KT; ++i)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float x0 = EIGHT ? s[i][2 * h] * ks0 * row_scale[h] : s[i][2 * h] * row_scale[h];
-                    const float x1 = EIGHT ? s[i][2 * h + 1] * ks1 * row_scale[h] : s[i][2 * h + 1] * row_scale[h];
-                    s[i][2 * h] = there.x ? x0 : -INFINITY;
-                    s[i][2 * h + 1] = there.y ? x1 : -INFINITY;
-                    if (cut) {
-                        const int j = j0 + n;
-                        const int last = (g.a.flags & SISO_ATTN_CAUSAL) ? pos[h] : 0x7FFFFFFF;
-                        const int first = g.a.window > 0 ? pos[h] - g.a.window : -0x7FFFFFFF;
-                        if (j > last || j <= first) s[i][2 * h] = -INFINITY;
-                        if (j + 1 > last || j + 1 <= first) s[i][2 * h + 1] = -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    float f = 1.f;
+                    if constexpr (EIGHT) {       // (byte 0: nothing above 2^-118, counts as zero; byte 255: infinity, then NaN)
+                        const int n = n0 + 16 * i + 8 * e + key_of<RB>(r0);
+                        f = __uint_as_float(static_cast<uint32_t>(mt[n]) << 23);
+                        ev[i][e] = mt[TK + n];
                     }
-                    top[h] = fmaxf(top[h], fmaxf(s[i][2 * h], s[i][2 * h + 1]));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) s[i][t][2 * e + h] *= EIGHT ? f * row_scale[t][h] : row_scale[t][h];
                 }
+            if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
+#pragma unroll
+                for (int i = 0; i < KT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int n = n0 + 16 * i + 8 * e, j = j0 + n + key_of<RB>(r0);
+                        const bool in = ((blocks >> (n / 8)) & 1u) && j < cur.s.hi;
+                        if (EIGHT && !in) ev[i][e] = 0u;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                if (!in || (causal && j > pos[t][h]) || (g.a.window > 0 && j <= pos[t][h] - g.a.window)) s[i][t][2 * e + h] = -INFINITY;
+                    }
             }
-            float shift[2], corr[2];
+            float shift[NT][2], corr[NT][2];
             bool moved = false;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                top[h] = fmaxf(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], 1));
-                top[h] = fmaxf(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], 2));
-                const float m2 = fmaxf(m[h], top[h]);
-                corr[h] = m[h] == m2 ? 1.f : ex2(m[h] - m2);
-                moved = moved || m[h] != m2;
-                m[h] = m2;
-                shift[h] = m2 == -INFINITY ? 0.f : m2 - (EIGHT ? 15.f : 0.f);
-                l[h] *= corr[h];
-            }
-            float rel[SUB / 8][2];                            // 2^(value exponent - largest so far)
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float top = fmaxf(s[0][t][h], s[0][t][2 + h]);
+#pragma unroll
+                    for (int i = 1; i < KT; ++i) top = fmaxf(top, fmaxf(s[i][t][h], s[i][t][2 + h]));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+                    const float m2 = fmaxf(m[t][h], top);
+                    corr[t][h] = m[t][h] == m2 ? 1.f : ex2(m[t][h] - m2);
+                    moved = moved || m[t][h] != m2;
+                    m[t][h] = m2;
+                    shift[t][h] = m2 == -INFINITY ? 0.f : m2 - (EIGHT ? 15.f : 0.f);
+                    l[t][h] *= corr[t][h];
+                }
             if constexpr (EIGHT) {
+                uint32_t e_max = max(ev[0][0], ev[0][1]);
+#pragma unroll
+                for (int i = 1; i < KT; ++i) e_max = max(e_max, max(ev[i][0], ev[i][1]));
                 e_max = __reduce_max_sync(0xFFFFFFFFu, e_max);
                 if (static_cast<int>(e_max) > e_top) {
                     const float down = ex2(static_cast<float>(e_top - static_cast<int>(e_max)));
-                    corr[0] *= down;
-                    corr[1] *= down;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) { corr[t][0] *= down; corr[t][1] *= down; }
                     moved = true;
                     e_top = static_cast<int>(e_max);
-                }
-#pragma unroll
-                for (int i = 0; i < SUB / 8; ++i) {
-                    rel[i][0] = __uint_as_float(static_cast<uint32_t>(max(127 + static_cast<int>(ev[i] & 0xFFu) - e_top, 0)) << 23);
-                    rel[i][1] = __uint_as_float(static_cast<uint32_t>(max(127 + static_cast<int>(ev[i] >> 8) - e_top, 0)) << 23);
                 }
             }
             if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
-                for (int t = 0; t < O_TILES; ++t) { o[t][0] *= corr[0]; o[t][1] *= corr[0]; o[t][2] *= corr[1]; o[t][3] *= corr[1]; }
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) { o[t][d][0] *= corr[t][0]; o[t][d][1] *= corr[t][1]; o[t][d][2] *= corr[t][0]; o[t][d][3] *= corr[t][1]; }
             }
-            uint32_t p[SUB / 8][2];
 #pragma unroll
-            for (int i = 0; i < SUB / 8; ++i) {
+            for (int i = 0; i < KT; ++i) {
+                uint32_t p[NT][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(s[i][2 * h] - shift[h]), p1 = ex2(s[i][2 * h + 1] - shift[h]);
-                    l[h] += p0 + p1;
-                    p[i][h] = EIGHT ? pack(p0 * rel[i][0], p1 * rel[i][1], true) : pack(p0, p1, false);
+                for (int e = 0; e < 2; ++e) {
+                    float rel = 1.f;                      // 2^(value exponent - largest so far)
+                    if constexpr (EIGHT) rel = __uint_as_float(static_cast<uint32_t>(max(127 - e_top + static_cast<int>(ev[i][e]), 0)) << 23);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const float p0 = ex2(s[i][t][2 * e] - shift[t][0]), p1 = ex2(s[i][t][2 * e + 1] - shift[t][1]);
+                        l[t][0] += p0;
+                        l[t][1] += p1;
+                        p[t][e] = transposed(EIGHT ? pack(p0 * rel, p1 * rel, true) : pack(p0, p1, false));
+                    }
                 }
-            }
+                const uint32_t v_at = v_first + (n0 + 16 * i) * LINE;
+                if constexpr (!EIGHT) {
 #pragma unroll
-            for (int k16 = 0; k16 < SUB / 16; ++k16) {
-                const uint32_t a[4] = {p[2 * k16][0], p[2 * k16][1], p[2 * k16 + 1][0], p[2 * k16 + 1][1]};
-                const int row = n0 + 16 * k16 + (lane & 15);
+                    for (int d = 0; d < DT; ++d) {        // keys 0-7 and 8-15 of two chunks of 8 d
+                        uint32_t f[4];
+                        load_v((v_at ^ (((2 * d) & 7) << 4)) + (d >> 2) * (TK * 128), f);
 #pragma unroll
-                for (int x = 0; x < CH; x += 2) {             // two chunks at once: keys 0-7 and 8-15 of each
-                    uint32_t v[4];
-                    load_v(v_tile + chunk_at<CH>(row, x + (lane >> 4)), v);
-                    if constexpr (!EIGHT) {
-                        mma<false>(o[x], a, v[0], v[1]);
-                        mma<false>(o[x + 1], a, v[2], v[3]);
-                    } else {
-                        uint32_t e0, d0, e1, d1;
-                        widen<KIND, true>(v[0], e0, d0);
-                        widen<KIND, true>(v[1], e1, d1);
-                        mma<true>(o[2 * x], a, e0, e1);
-                        mma<true>(o[2 * x + 1], a, d0, d1);
-                        widen<KIND, true>(v[2], e0, d0);
-                        widen<KIND, true>(v[3], e1, d1);
-                        mma<true>(o[2 * x + 2], a, e0, e1);
-                        mma<true>(o[2 * x + 3], a, d0, d1);
+                        for (int t = 0; t < NT; ++t) mma<false>(o[t][d], f, p[t]);
+                    }
+                } else {
+#pragma unroll
+                    for (int d = 0; d < DT; d += 2) {     // keys 0-7 and 8-15 of two chunks of 16 d
+                        uint32_t v[4], f[4];
+                        load_v(v_at ^ (d << 4), v);
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {     // rows 0-7 of the product: even d, rows 8-15: odd d
+                            widen<KIND, true>(v[2 * x], f[0], f[1]);
+                            widen<KIND, true>(v[2 * x + 1], f[2], f[3]);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma<true>(o[t][d + x], f, p[t]);
+                        }
                     }
                 }
             }
         }
-        if (++stage == S::STAGES) stage = 0;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ring.empty[stage]);
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         if (++cur.tile < cur.s.tiles && u + 1 < u1) continue;
 
-        // ---- end of the item, or of this CTA's part of it: join the groups' results, halving their number each time
-        fresh = true;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 1);
-            l[h] += __shfl_xor_sync(0xFFFFFFFFu, l[h], 2);
-            if (EIGHT) m[h] -= 15.f;
+        // ---- end of the item, or of this CTA's part of it.  The next one's queries are on their way meanwhile
+        const int t_end = cur.tile;                           // tiles [t_begin, t_end) of the item were done here
+        const int t_begin = t_end - static_cast<int>(u + 1 - began);
+        const bool whole = t_begin == 0 && t_end == cur.s.tiles;
+        const int done_b = cur.b, done_head = cur.head, done_rt = cur.rt, done_q0 = cur.q0, done_rows = cur.n_q * g.group, done_tiles = cur.s.tiles;
+        began = u + 1;
+        if (u + 1 < u1) {
+            cur.next_item(g);
+            fetch_q();
         }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 4);
+                l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 8);
+                l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 16);
+                if (EIGHT) m[t][h] -= 15.f;
+            }
         if constexpr (EIGHT) {
             const float back = kv_scale(static_cast<uint32_t>(e_top));
 #pragma unroll
-            for (int t = 0; t < O_TILES; ++t) { o[t][0] *= back; o[t][1] *= back; o[t][2] *= back; o[t][3] *= back; }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) { o[t][d][0] *= back; o[t][d][1] *= back; o[t][d][2] *= back; o[t][d][3] *= back; }
         }
 #pragma unroll 1
-        for (int half = S::WK / 2; half >= 1; half >>= 1) {
-            float4 *mo = reinterpret_cast<float4 *>(merge_o) + ((kg % half) * WM + wm) * (O_TILES * 32) + lane;
-            float *ml = merge_ml + ((kg % half) * WM + wm) * 32 + 4 * r0;
+        for (int half = WK / 2; half >= 1; half >>= 1) { // join the groups' results, halving their number each time
+            float4 *mo = reinterpret_cast<float4 *>(merge_o) + ((kg % half) * WM + wm) * (NT * DT * 32) + lane;
+            float *ml = merge_ml + ((kg % half) * WM + wm) * (16 * NT) + 4 * c;
             if (kg >= half && kg < 2 * half) {
 #pragma unroll
-                for (int t = 0; t < O_TILES; ++t) mo[t * 32] = make_float4(o[t][0], o[t][1], o[t][2], o[t][3]);
-                if (c == 0) { ml[0] = m[0]; ml[1] = l[0]; ml[2] = m[1]; ml[3] = l[1]; }
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) mo[(t * DT + d) * 32] = make_float4(o[t][d][0], o[t][d][1], o[t][d][2], o[t][d][3]);
+                    if (r0 == 0) { ml[16 * t] = m[t][0]; ml[16 * t + 1] = l[t][0]; ml[16 * t + 2] = m[t][1]; ml[16 * t + 3] = l[t][1]; }
+                }
             }
-            __syncthreads();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
             if (kg < half) {
-                float mine[2], theirs[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float m1 = ml[2 * h], l1 = ml[2 * h + 1], m2 = fmaxf(m[h], m1);
-                    mine[h] = m[h] == -INFINITY ? 0.f : ex2(m[h] - m2);
-                    theirs[h] = m1 == -INFINITY ? 0.f : ex2(m1 - m2);
-                    l[h] = l[h] * mine[h] + l1 * theirs[h];
-                    m[h] = m2;
-                }
+                for (int t = 0; t < NT; ++t) {
+                    float mine[2], theirs[2];
 #pragma unroll
-                for (int t = 0; t < O_TILES; ++t) {
-                    const float4 y = mo[t * 32];
-                    o[t][0] = o[t][0] * mine[0] + y.x * theirs[0];
-                    o[t][1] = o[t][1] * mine[0] + y.y * theirs[0];
-                    o[t][2] = o[t][2] * mine[1] + y.z * theirs[1];
-                    o[t][3] = o[t][3] * mine[1] + y.w * theirs[1];
+                    for (int h = 0; h < 2; ++h) {
+                        const float m1 = ml[16 * t + 2 * h], l1 = ml[16 * t + 2 * h + 1], m2 = fmaxf(m[t][h], m1);
+                        mine[h] = m[t][h] == -INFINITY ? 0.f : ex2(m[t][h] - m2);
+                        theirs[h] = m1 == -INFINITY ? 0.f : ex2(m1 - m2);
+                        l[t][h] = l[t][h] * mine[h] + l1 * theirs[h];
+                        m[t][h] = m2;
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const float4 y = mo[(t * DT + d) * 32];
+                        o[t][d][0] = o[t][d][0] * mine[0] + y.x * theirs[0];
+                        o[t][d][1] = o[t][d][1] * mine[1] + y.y * theirs[1];
+                        o[t][d][2] = o[t][d][2] * mine[0] + y.z * theirs[0];
+                        o[t][d][3] = o[t][d][3] * mine[1] + y.w * theirs[1];
+                    }
                 }
             }
-            __syncthreads();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
         }
-        const int t_end = cur.tile;                           // tiles [t_end - (u + 1 - began), t_end) of the item are done here
-        const int t_begin = t_end - static_cast<int>(u + 1 - began);
-        const bool whole = t_begin == 0 && t_end == cur.s.tiles;
         if (kg == 0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int in_tile = wm * 16 + r0 + 8 * h, row = cur.rt * MR + in_tile;
-                if (row < cur.n_q * g.group) {
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int in_tile = (wm * NT + t) * 8 + 2 * c + h, row = done_rt * MR + in_tile;
+                    if (row >= done_rows) continue;
                     if (whole) {
                         const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row)));
-                        const int head = cur.head * g.group + row - i * g.group;
-                        const float inv = l[h] > 0.f ? 1.f / l[h] : 0.f;
-                        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(cur.q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
-                        if constexpr (!EIGHT) {
+                        const int head = done_head * g.group + row - i * g.group;
+                        const float inv = l[t][h] > 0.f ? 1.f / l[t][h] : 0.f;
+                        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(done_q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
 #pragma unroll
-                            for (int t = 0; t < O_TILES; ++t)
-                                *reinterpret_cast<uint32_t *>(dst + 8 * t + 2 * c) = pack(o[t][2 * h] * inv, o[t][2 * h + 1] * inv, false);
-                        } else {
-#pragma unroll
-                            for (int t = 0; t < O_TILES; t += 2)
-                                *reinterpret_cast<uint2 *>(dst + 8 * t + 4 * c) = make_uint2(pack(o[t][2 * h] * inv, o[t + 1][2 * h] * inv, false),
-                                                                                            pack(o[t][2 * h + 1] * inv, o[t + 1][2 * h + 1] * inv, false));
+                        for (int d = 0; d < DT; ++d) {
+                            if constexpr (!EIGHT) {
+                                dst[16 * d + r0] = __float2bfloat16_rn(o[t][d][h] * inv);
+                                dst[16 * d + 8 + r0] = __float2bfloat16_rn(o[t][d][2 + h] * inv);
+                            } else {
+                                *reinterpret_cast<uint32_t *>(dst + 16 * d + 2 * r0) = pack(o[t][d][h] * inv, o[t][d][2 + h] * inv, false);
+                            }
                         }
-                        if (g.a.d_lse && c == 0)
-                            g.a.d_lse[static_cast<long long>(cur.q0 + i) * g.a.n_heads + head] = l[h] > 0.f ? (m[h] + log2f(l[h])) * 0.6931471805599453f : -INFINITY;
+                        if (g.a.d_lse && r0 == 0)
+                            g.a.d_lse[static_cast<long long>(done_q0 + i) * g.a.n_heads + head] = l[t][h] > 0.f ? (m[t][h] + log2f(l[t][h])) * 0.6931471805599453f : -INFINITY;
                     } else {
                         const long long place = part_place(blockIdx.x, t_begin > 0) * MR + in_tile;
                         float *dst = g.part_o + place * D;
 #pragma unroll
-                        for (int t = 0; t < O_TILES; t += 2) {
-                            if constexpr (!EIGHT) {
-                                *reinterpret_cast<float2 *>(dst + 8 * t + 2 * c) = make_float2(o[t][2 * h], o[t][2 * h + 1]);
-                                *reinterpret_cast<float2 *>(dst + 8 * t + 8 + 2 * c) = make_float2(o[t + 1][2 * h], o[t + 1][2 * h + 1]);
-                            } else {
-                                *reinterpret_cast<float4 *>(dst + 8 * t + 4 * c) = make_float4(o[t][2 * h], o[t + 1][2 * h], o[t][2 * h + 1], o[t + 1][2 * h + 1]);
-                            }
+                        for (int d = 0; d < DT; ++d) {
+                            if constexpr (!EIGHT) { dst[16 * d + r0] = o[t][d][h]; dst[16 * d + 8 + r0] = o[t][d][2 + h]; }
+                            else *reinterpret_cast<float2 *>(dst + 16 * d + 2 * r0) = make_float2(o[t][d][h], o[t][d][2 + h]);
                         }
-                        if (c == 0) *reinterpret_cast<float2 *>(g.part_ml + place * 2) = make_float2(m[h], l[h]);
+                        if (r0 == 0) *reinterpret_cast<float2 *>(g.part_ml + place * 2) = make_float2(m[t][h], l[t][h]);
                     }
                 }
-            }
         }
         if (!whole && t_begin == 0 && threadIdx.x == 0) {
-            const long long end = u + 1 + (cur.s.tiles - t_end);
-            g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.rt, cta_of(end - 1, total, ctas) - static_cast<int>(blockIdx.x) + 1};
+            const long long end = u + 1 + (done_tiles - t_end);
+            g.records[blockIdx.x] = Record{1, done_b, done_head, done_rt, cta_of(end - 1, total, ctas) - static_cast<int>(blockIdx.x) + 1};
         }
-        if (u + 1 < u1) cur.next_item(g);
+        if (u + 1 < u1) begin_item();
     }
 }
 
@@ -560,8 +678,8 @@ template <int MR, int D> static siso_status_t run_join(const Args &g, cudaStream
     return SISO_OK;
 }
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
-    if (dim == 128) return mr == 16 ? run_join<16, 128>(g, s) : mr == 32 ? run_join<32, 128>(g, s) : run_join<64, 128>(g, s);
-    return mr == 16 ? run_join<16, 64>(g, s) : mr == 32 ? run_join<32, 64>(g, s) : run_join<64, 64>(g, s);
+    if (dim == 128) return mr == 8 ? run_join<8, 128>(g, s) : mr == 16 ? run_join<16, 128>(g, s) : mr == 32 ? run_join<32, 128>(g, s) : run_join<64, 128>(g, s);
+    return mr == 8 ? run_join<8, 64>(g, s) : mr == 16 ? run_join<16, 64>(g, s) : mr == 32 ? run_join<32, 64>(g, s) : run_join<64, 64>(g, s);
 }
 
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s) {
@@ -578,19 +696,23 @@ siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s) {
     return SISO_OK;
 }
 
-template <int KIND, int D, int WM> static siso_status_t run_few(Args &g, cudaStream_t s) {
-    using S = Shape<KIND, D, WM>;
-    // the opt-in to large shared memory is an attribute of the function on the current device; setting it again is cheap
-    SISO_CUDA(cudaFuncSetAttribute(attention_few_rows_kernel<KIND, D, WM>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
-    attention_few_rows_kernel<KIND, D, WM><<<g.grid, THREADS, S::SMEM, s>>>(g);
+template <int KIND, int D, int WM, int NT> static siso_status_t run_few(Kv *h, Args &g, cudaStream_t s) {
+    using S = Shape<KIND, D, WM, NT>;
+    constexpr uint32_t bit = 1u << (NT == 1 ? 0 : WM);        // a handle has one type and head_dim
+    if (!(h->attr_set & bit)) {
+        SISO_CUDA(cudaFuncSetAttribute(attention_few_rows_kernel<KIND, D, WM, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        h->attr_set |= bit;
+    }
+    attention_few_rows_kernel<KIND, D, WM, NT><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
     SISO_CUDA(cudaGetLastError());
     return launch_join(g, S::MR, D, s);
 }
-template <int KIND, int D> static siso_status_t run_few_wm(Args &g, int wm, cudaStream_t s) {
-    return wm == 1 ? run_few<KIND, D, 1>(g, s) : wm == 2 ? run_few<KIND, D, 2>(g, s) : run_few<KIND, D, 4>(g, s);
+template <int KIND, int D> static siso_status_t run_few_rows(Kv *h, Args &g, int mr, cudaStream_t s) {
+    return mr == 8 ? run_few<KIND, D, 1, 1>(h, g, s) : mr == 16 ? run_few<KIND, D, 1, 2>(h, g, s) : mr == 32 ? run_few<KIND, D, 2, 2>(h, g, s)
+                                                                                                : run_few<KIND, D, 4, 2>(h, g, s);
 }
-template <int KIND> static siso_status_t run_few_dim(Args &g, int dim, int wm, cudaStream_t s) {
-    return dim == 128 ? run_few_wm<KIND, 128>(g, wm, s) : run_few_wm<KIND, 64>(g, wm, s);
+template <int KIND> static siso_status_t run_few_dim(Kv *h, Args &g, int dim, int mr, cudaStream_t s) {
+    return dim == 128 ? run_few_rows<KIND, 128>(h, g, mr, s) : run_few_rows<KIND, 64>(h, g, mr, s);
 }
 
 }  // namespace kva
@@ -605,11 +727,11 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t
     g.by_group.set(static_cast<uint32_t>(g.group));
     g.scale_log2 = a->scale * 1.4426950408889634f;
     g.status = h->status;
+    g.box = h->box;
     g.grid = h->sm_count;
     const int dim = h->cfg.head_dim;
     const long long rows = static_cast<long long>(a->max_q) * g.group;      // rows per key/value head of the longest chunk
-    const int wm = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int mr = 16 * wm;
+    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     const size_t records = pad256(sizeof(Record) * g.grid), ml = pad256(sizeof(float) * 2 * g.grid * mr * 2);
     // sized for the widest kernel, so that a handle that has served one call serves every other without a new block
     const size_t most = records + pad256(sizeof(float) * 2 * g.grid * 64 * 2) + sizeof(float) * 2 * g.grid * 64 * static_cast<size_t>(dim);
@@ -619,9 +741,9 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t
     g.part_ml = reinterpret_cast<float *>(ws + records);
     g.part_o = reinterpret_cast<float *>(ws + records + ml);
     switch (h->cfg.dtype) {
-        case SISO_BF16: return run_few_dim<SISO_BF16>(g, dim, wm, s);
-        case SISO_E4M3: return run_few_dim<SISO_E4M3>(g, dim, wm, s);
-        default: return run_few_dim<SISO_I8>(g, dim, wm, s);
+        case SISO_BF16: return run_few_dim<SISO_BF16>(h, g, dim, mr, s);
+        case SISO_E4M3: return run_few_dim<SISO_E4M3>(h, g, dim, mr, s);
+        default: return run_few_dim<SISO_I8>(h, g, dim, mr, s);
     }
 }
 

@@ -2,7 +2,7 @@
 // partial results and their join.
 //
 // The queries of one sequence that share a key/value head form its rows: row r is token r / group, query head
-// kv_head * group + r % group.  An item is (sequence, key/value head, tile of MR rows); its keys are taken in tiles of 128, and
+// kv_head * group + r % group.  An item is (sequence, key/value head, tile of MR rows); its keys are taken in tiles of TK, and
 // one tile of one item is a unit.  The units of a call, in the order (sequence, head, row tile, key tile), are dealt to the
 // CTAs in equal contiguous runs, so CTAs are equally loaded whatever the lengths are, and one long sequence spreads over
 // all of them.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
@@ -13,8 +13,6 @@
 
 namespace siso {
 namespace kva {
-
-constexpr int TK = 128;                // keys of a unit
 
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31, by a multiplication: m = floor(2^(31 + s) / d) + 1 with s = ceil(log2 d)
 struct FastDiv {
@@ -41,6 +39,7 @@ struct Args {
     FastDiv by_page, by_group;
     int group;
     float scale_log2;                  // scale * log2(e)
+    int box;                           // tokens of one TMA box: they lie in one page
     int grid;                          // CTAs that share the units
     float *part_o, *part_ml;           // [2 grid][MR][D], [2 grid][MR][2]
     Record *records;                   // [grid]
@@ -62,7 +61,7 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
     q0 = min(max(g.a.d_cu_q[b], 0), n);
     return max(0, min(g.a.d_cu_q[b + 1], n) - q0);
 }
-template <int MR> __device__ __forceinline__ Span span_of(const Args &g, int len, int n_q, int rt) {
+template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g, int len, int n_q, int rt) {
     Span s;
     const int rows = n_q * g.group;
     s.first_pos = len - n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR)));
@@ -74,23 +73,23 @@ template <int MR> __device__ __forceinline__ Span span_of(const Args &g, int len
     return s;
 }
 // units of one key/value head of sequence b
-template <int MR> __device__ __forceinline__ int seq_units(const Args &g, int b) {
+template <int MR, int TK> __device__ __forceinline__ int seq_units(const Args &g, int b) {
     int q0;
     const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
     int units = 0;
-    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR>(g, len, n_q, rt).tiles;
+    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR, TK>(g, len, n_q, rt).tiles;
     return units;
 }
 
 // The item that a unit belongs to, and the unit's place in it.
-template <int MR> struct Cursor {
+template <int MR, int TK> struct Cursor {
     int b, head, rt, q0, n_q, len, tile;
     Span s;
     __device__ __forceinline__ void load_seq(const Args &g) {
         n_q = seq_queries(g, b, q0);
         len = seq_len(g, b);
     }
-    __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR>(g, len, n_q, rt); }
+    __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR, TK>(g, len, n_q, rt); }
     // `within`: units of sequence b before this one
     __device__ __forceinline__ void seek(const Args &g, int seq, long long within, int per_head) {
         b = seq;
@@ -120,8 +119,8 @@ template <int MR> struct Cursor {
 
 // This CTA's run [u0, u1) of the call's units and the cursor at its start; every thread of the CTA gets the same.  False: none.
 // The CTA's record is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
-template <int MR, int THREADS>
-__device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &u1, long long &total, int &ctas, Cursor<MR> &cur,
+template <int MR, int TK, int THREADS>
+__device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &u1, long long &total, int &ctas, Cursor<MR, TK> &cur,
                                        unsigned long long *buf) {
     constexpr int WARPS = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -132,7 +131,7 @@ __device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &
     total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
         const int b = c0 + static_cast<int>(threadIdx.x);
-        const int ph = b < g.a.n_seqs ? seq_units<MR>(g, b) : 0;
+        const int ph = b < g.a.n_seqs ? seq_units<MR, TK>(g, b) : 0;
         const unsigned long long mine = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads;
         unsigned long long x = mine;
 #pragma unroll
@@ -160,7 +159,7 @@ __device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
             const int b = c0 + static_cast<int>(threadIdx.x);
-            per_head = b < g.a.n_seqs ? seq_units<MR>(g, b) : 0;
+            per_head = b < g.a.n_seqs ? seq_units<MR, TK>(g, b) : 0;
             first = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
             unsigned long long x = first;
 #pragma unroll

@@ -232,6 +232,42 @@ static siso_status_t rows_call(Kv *h, int layer, void *k, void *v, int dtype, lo
                              : run_kind<__nv_bfloat16, READ>(h->cfg.dtype, kv, rows, sl, s);
 }
 
+// Tensor maps of the pages for attention: boxes of `box` tokens of one page and head, 128 bytes wide (64 where a row has no more),
+// swizzled so that consecutive tokens start in different banks.
+static siso_status_t encode_maps(Kv *h) {
+    const siso_kv_config_t &g = h->cfg;
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult res;
+    SISO_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &res));
+    if (!fn || res != cudaDriverEntryPointSuccess) return check_cuda(cudaErrorNotSupported, "cuTensorMapEncodeTiled lookup");
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint64_t eb = kv_elem_bytes(g.dtype), row = g.head_dim * eb;
+    for (h->box = 128; g.page_size % h->box != 0;) h->box /= 2;
+    const cuuint64_t dims[5] = {static_cast<cuuint64_t>(g.head_dim), static_cast<cuuint64_t>(g.n_kv_heads), static_cast<cuuint64_t>(g.page_size),
+                                static_cast<cuuint64_t>(g.n_pages), static_cast<cuuint64_t>(g.n_layers)};
+    // a dimension of one entry has no stride of its own
+    const cuuint64_t strides[4] = {std::max<cuuint64_t>(g.stride_head * eb, 16), std::max<cuuint64_t>(g.stride_token * eb, 16),
+                                   std::max<cuuint64_t>(g.stride_page * eb, 16), std::max<cuuint64_t>(g.stride_layer * eb, 16)};
+    const cuuint32_t box[5] = {static_cast<cuuint32_t>(std::min<cuuint64_t>(row, 128) / eb), 1u, static_cast<cuuint32_t>(h->box), 1u, 1u};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i) {
+        const CUresult r = reinterpret_cast<Encode>(fn)(
+            i ? &h->map_v : &h->map_k, eb == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, i ? g.d_v : g.d_k, dims, strides,
+            box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, row >= 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            row >= 256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : row >= 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) return check_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+    }
+    return SISO_OK;
+}
+
+// whether attention can read these pages: its head sizes, and 16 bytes at a time
+static bool attends(const siso_kv_config_t &g) {
+    const int64_t elems16 = 16 / kv_elem_bytes(g.dtype);
+    return (g.head_dim == 64 || g.head_dim == 128) && g.stride_layer % elems16 == 0 && g.stride_page % elems16 == 0 &&
+           g.stride_token % elems16 == 0 && g.stride_head % elems16 == 0;
+}
+
 }  // namespace kvc
 }  // namespace siso
 
@@ -272,6 +308,10 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
     h->cfg = *cfg;
     if (!cfg->allocator.alloc) h->cfg.allocator = default_allocator();
     h->sm_count = sms;
+    if (kvc::attends(h->cfg)) {
+        const siso_status_t st = kvc::encode_maps(h);
+        if (st != SISO_OK) { delete h; return st; }
+    }
     h->status = static_cast<int *>(h->cfg.allocator.alloc(256, nullptr, h->cfg.allocator.ctx));
     if (!h->status) { delete h; return SISO_ERR_OOM; }
     cudaError_t e = cudaMemset(h->status, 0, 256);
@@ -314,11 +354,7 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *s
         if (st % 8 != 0) return SISO_ERR_UNSUPPORTED;
     }
     if (!kvc::aligned16(a->d_q) || !kvc::aligned16(a->d_out)) return SISO_ERR_UNSUPPORTED;
-    if (h->cfg.head_dim != 64 && h->cfg.head_dim != 128) return SISO_ERR_UNSUPPORTED;
-    const int64_t elems16 = 16 / kv_elem_bytes(h->cfg.dtype);        // attention moves 16 bytes at a time
-    if (h->cfg.stride_layer % elems16 != 0 || h->cfg.stride_page % elems16 != 0 || h->cfg.stride_token % elems16 != 0 ||
-        h->cfg.stride_head % elems16 != 0)
-        return SISO_ERR_UNSUPPORTED;
+    if (!kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
     if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     SISO_CUDA(cudaSetDevice(h->cfg.device));
     return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
