@@ -23,7 +23,6 @@
 #include <cuda_fp16.h>
 
 #include "kv_attention.cuh"
-#include "umma_pair.cuh"
 
 namespace siso {
 namespace kva {
@@ -33,7 +32,6 @@ using umma2::mbar_arrive_expect_tx;
 using umma2::mbar_init;
 using umma2::smem_u32;
 
-constexpr unsigned long long WAIT_NS = 1000000000ull;       // a wait gives up after a second
 constexpr int SMEM_MOST = 232448 - 512 - 1024;   // what a CTA may have, less its static part and the alignment of the ring
 
 constexpr int PRODUCERS = 4;             // warps that fill the ring; each has its own stages
@@ -59,12 +57,6 @@ template <int KIND, int D, int WM, int NT> struct Shape {
     static constexpr int SMEM = STAGES * (STAGE + META) + MERGE + 1024;
 };
 
-// byte offset of a 16-byte chunk in a tile of TK rows as TMA writes it: lines of 128 bytes with the chunk's place xor-ed with the
-// row's lowest bits (rows of 256 bytes are two such tiles), or of 64 bytes
-template <int RB, int TK> __device__ __forceinline__ int chunk_at(int row, int chunk) {
-    if constexpr (RB == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
-    else return (chunk >> 3) * (TK * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-}
 // Which of 8 keys the n-th row of a product is.  The 8 lanes of one 16-byte load read 4 chunks of rows 2i and 2i + 1: those keys have
 // to lie in different halves of their lines
 template <int RB> __device__ __forceinline__ int key_of(int n) { return RB == 64 ? n : ((n & 1) << 2) | (n >> 1); }
@@ -86,12 +78,6 @@ __device__ __forceinline__ void load_v(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi, bool half) {
-    uint32_t r;
-    if (half) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // Two codes as fp16: bytes 0, 1 and 2, 3 of a word (SPLIT false), or bytes 0, 2 and 1, 3 (SPLIT true)
 template <int KIND, bool SPLIT> __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
     if constexpr (KIND == SISO_E4M3) {
@@ -107,28 +93,6 @@ template <int KIND, bool SPLIT> __device__ __forceinline__ void widen(uint32_t w
         hi = *reinterpret_cast<const uint32_t *>(&y);
     }
 }
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int d, int head, int token, int page, int layer, uint64_t *bar) {
-    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(d), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(smem_u32(bar))
-                 : "memory");
-}
-// A wait for this CTA's own copies or warps, bounded; once any has given up, none waits any more: the loops run to their ends on
-// whatever the ring holds, so every barrier of the CTA is still met.
-__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatile int *gave_up) {
-    if (umma2::mbar_try_wait_cta(bar, parity)) return;
-    unsigned long long t0, t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
-    for (uint32_t it = 1; it < umma2::SPIN_LIMIT; ++it) {
-        if (umma2::mbar_try_wait_cta(bar, parity)) return;
-        if ((it & 63u) == 0u) {
-            if (*gave_up) return;
-            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-            if (t - t0 > WAIT_NS) break;
-        }
-    }
-    *gave_up = 1;
-}
-
 template <int STAGES> struct Ring {
     uint64_t full[STAGES], empty[STAGES];
     uint32_t blocks[STAGES];           // bit i: the page of keys 8 i .. 8 i + 7 of the unit is in the pool
@@ -678,8 +642,13 @@ template <int MR, int D> static siso_status_t run_join(const Args &g, cudaStream
     return SISO_OK;
 }
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
-    if (dim == 128) return mr == 8 ? run_join<8, 128>(g, s) : mr == 16 ? run_join<16, 128>(g, s) : mr == 32 ? run_join<32, 128>(g, s) : run_join<64, 128>(g, s);
-    return mr == 8 ? run_join<8, 64>(g, s) : mr == 16 ? run_join<16, 64>(g, s) : mr == 32 ? run_join<32, 64>(g, s) : run_join<64, 64>(g, s);
+    switch (mr) {
+        case 8: return dim == 128 ? run_join<8, 128>(g, s) : run_join<8, 64>(g, s);
+        case 16: return dim == 128 ? run_join<16, 128>(g, s) : run_join<16, 64>(g, s);
+        case 32: return dim == 128 ? run_join<32, 128>(g, s) : run_join<32, 64>(g, s);
+        case 64: return dim == 128 ? run_join<64, 128>(g, s) : run_join<64, 64>(g, s);
+        default: return dim == 128 ? run_join<TC_ROWS, 128>(g, s) : run_join<TC_ROWS, 64>(g, s);
+    }
 }
 
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s) {
@@ -731,15 +700,16 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t
     g.grid = h->sm_count;
     const int dim = h->cfg.head_dim;
     const long long rows = static_cast<long long>(a->max_q) * g.group;      // rows per key/value head of the longest chunk
-    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : TC_ROWS;
     const size_t records = pad256(sizeof(Record) * g.grid), ml = pad256(sizeof(float) * 2 * g.grid * mr * 2);
     // sized for the widest kernel, so that a handle that has served one call serves every other without a new block
-    const size_t most = records + pad256(sizeof(float) * 2 * g.grid * 64 * 2) + sizeof(float) * 2 * g.grid * 64 * static_cast<size_t>(dim);
+    const size_t most = records + pad256(sizeof(float) * 2 * g.grid * TC_ROWS * 2) + sizeof(float) * 2 * g.grid * TC_ROWS * static_cast<size_t>(dim);
     SISO_TRY(kv_scratch(h, most, s));
     char *ws = static_cast<char *>(h->ws);
     g.records = reinterpret_cast<Record *>(ws);
     g.part_ml = reinterpret_cast<float *>(ws + records);
     g.part_o = reinterpret_cast<float *>(ws + records + ml);
+    if (mr == TC_ROWS) return launch_many_rows(h, g, s);
     switch (h->cfg.dtype) {
         case SISO_BF16: return run_few_dim<SISO_BF16>(h, g, dim, mr, s);
         case SISO_E4M3: return run_few_dim<SISO_E4M3>(h, g, dim, mr, s);

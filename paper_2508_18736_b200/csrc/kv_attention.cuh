@@ -10,6 +10,7 @@
 #pragma once
 
 #include "kv.cuh"
+#include "umma_pair.cuh"
 
 namespace siso {
 namespace kva {
@@ -203,10 +204,50 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+constexpr unsigned long long WAIT_NS = 1000000000ull;       // a wait gives up after a second
+
+// byte offset of a 16-byte chunk in a tile of TK rows as TMA writes it: lines of 128 bytes with the chunk's place xor-ed with the
+// row's lowest bits (rows of 256 bytes are two such tiles), or of 64 bytes
+template <int RB, int TK> __device__ __forceinline__ int chunk_at(int row, int chunk) {
+    if constexpr (RB == 64) return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);
+    else return (chunk >> 3) * (TK * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi, bool half) {
+    uint32_t r;
+    if (half) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int d, int head, int token, int page, int layer, uint64_t *bar) {
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(d), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(umma2::smem_u32(bar))
+                 : "memory");
+}
+// A wait for this CTA's own copies or warps, bounded; once any has given up, none waits any more: the loops run to their ends on
+// whatever the ring holds, so every barrier of the CTA is still met.
+__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatile int *gave_up) {
+    if (umma2::mbar_try_wait_cta(bar, parity)) return;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (uint32_t it = 1; it < umma2::SPIN_LIMIT; ++it) {
+        if (umma2::mbar_try_wait_cta(bar, parity)) return;
+        if ((it & 63u) == 0u) {
+            if (*gave_up) return;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t - t0 > WAIT_NS) break;
+        }
+    }
+    *gave_up = 1;
+}
+
 #endif  // __CUDACC__
 
 // joins the parts of every item that was cut; MR = rows of a row tile, D = head_dim
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s);
+// many rows per key/value head (tcgen05): row tiles of TC_ROWS
+constexpr int TC_ROWS = 256;
+siso_status_t launch_many_rows(Kv *h, Args &g, cudaStream_t s);
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s);
 
 }  // namespace kva

@@ -1,0 +1,574 @@
+// Attention of new tokens over the paged key/value cache, many rows per key/value head: prompts and their chunks.
+// The formulas are in kv_attention.cu, the dealing of units to CTAs in kv_attention.cuh.
+//
+// With many rows the call is bound by the tensor cores and, nearly as much, by the exponentials: a tile of 128 x 128 scores takes
+// 2 x 512 cycles of tcgen05.mma (d = 128) and 1024 cycles of the SM's 16 exponentials a cycle.  So a CTA works on two
+// tiles of 128 rows at once: while the softmax of one runs on the CUDA cores the products of the other run on the tensor cores.
+//   warps 0-3, 4-7   softmax of row tile 0, 1: thread = row = TMEM lane.  Load the row's 128 scores from TMEM, running maximum, exponentials,
+//                    probabilities as bf16 back into TMEM over the scores.  The output in TMEM is rescaled only where a maximum has
+//                    grown by more than 8 (a factor 2^8, which fp32 sums and bf16 probabilities bear); then by these warps.
+//   warp 8           issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
+//                    an MN-major operand)
+//   warps 9-11       fill the ring of K and V tiles by TMA, one box per run of tokens in one page
+//   warps 12-15      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
+// TMEM: S_0, S_1 (128 columns each), O_0, O_1.
+#include "kv_attention.cuh"
+
+namespace siso {
+namespace kva {
+namespace tc {
+
+using namespace umma2;
+
+constexpr int TK = 128;
+constexpr int PRODUCERS = 3;
+
+template <int KIND, int D> struct Shape {
+    static constexpr bool EIGHT = KIND != SISO_BF16;
+    static constexpr int THREADS = EIGHT ? 512 : 384;
+    static constexpr int Q_BYTES = 2 * 128 * D * 2;
+    static constexpr int TILE = TK * D * 2;                              // a tile of K or V in bf16
+    static constexpr int RAW = EIGHT ? TK * D : 0;                       // and as codes
+    static constexpr int RAW_META = EIGHT ? TK : 0;                      // exponents
+    static constexpr int ROOM = 232448 - 1024 - 1024 - Q_BYTES;          // alignment; barriers
+    static constexpr int RAWS = EIGHT ? 4 : 0;
+    static constexpr int FIT = (ROOM - RAWS * (RAW + RAW_META)) / TILE;
+    static constexpr int STAGES = FIT > 6 ? 6 : FIT;
+    static constexpr int SMEM = 1024 + Q_BYTES + STAGES * TILE + RAWS * (RAW + RAW_META);
+    // registers: what the CTA has at launch (168 x 384 or 128 x 512), moved to the softmax
+    static constexpr int SOFTMAX_REGS = EIGHT ? 152 : 192, OTHER_REGS = EIGHT ? 88 : 120, CONVERT_REGS = 120;
+    static_assert(2 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? CONVERT_REGS : 0) == (EIGHT ? 4 * 128 : 3 * 168), "register split");
+};
+
+struct Bars {
+    uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
+    uint64_t kv_full[6], kv_empty[6], raw_full[4], raw_empty[4], tail[PRODUCERS];
+    uint32_t blocks[8];        // of unit i at i % 8: which runs of 8 keys have a page in the pool
+    uint32_t tmem;
+    int gave_up;
+};
+
+// D fp32, A and B bf16; A from shared memory or TMEM, K-major; B K-major, or MN-major (bit 16)
+template <int N, bool MN>
+constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | (MN ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
+// B operand that lies key by key: rows of 128 bytes (64 d) 128-byte swizzled, 8 keys 1024 bytes apart, the next 64 d after TK rows
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>((TK * 128) >> 4) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+          "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+          "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+          "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long &>(d))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<unsigned long long &>(d)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return d;
+}
+__device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t sub2_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// 4 codes as bf16 values: (0, 2) and (1, 3).  e4m3: sign, exponent and mantissa moved to their places give the value times 2^-120, subnormal
+// codes too; `factor` makes up for it.  i8: the low 7 bits as the mantissa of 128 + u less 128 or, for negative codes, 256.
+template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t factor, uint32_t &lo, uint32_t &hi) {
+    if constexpr (KIND == SISO_E4M3) {
+        lo = mul2_bf16(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u), factor);
+        hi = mul2_bf16(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u), factor);
+    } else {
+        const uint32_t x = w >> 8;
+        lo = mul2_bf16(sub2_bf16((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u), factor);
+        hi = mul2_bf16(sub2_bf16((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u), factor);
+    }
+}
+
+template <int KIND, int D>
+__global__ void __launch_bounds__(Shape<KIND, D>::THREADS, 1)
+attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    using S = Shape<KIND, D>;
+    constexpr bool EIGHT = S::EIGHT;
+    constexpr int STAGES = S::STAGES, RAWS = S::RAWS;
+    constexpr int RB = D * (EIGHT ? 1 : 2), LINE = RB < 128 ? RB : 128;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ unsigned long long buf[S::THREADS / 32 + 2];
+    __shared__ Bars bars;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint8_t *q_smem = smem, *tiles = smem + S::Q_BYTES, *raws = tiles + STAGES * S::TILE, *metas = raws + RAWS * S::RAW;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 4); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t], 4); mbar_init(&bars.o_done[t], 1); }
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 4 : 1); mbar_init(&bars.kv_empty[i], 1); }
+        for (int i = 0; i < RAWS; ++i) { mbar_init(&bars.raw_full[i], 33); mbar_init(&bars.raw_empty[i], 4); }
+        for (int i = 0; i < PRODUCERS; ++i) mbar_init(&bars.tail[i], 1);
+        bars.gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    long long u0, u1, total;
+    int ctas;
+    Cursor<TC_ROWS, TK> cur;
+    if (!locate<TC_ROWS, TK, S::THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = bars.tmem;
+    volatile int *gave_up = &bars.gave_up;
+
+    if (warp >= 12) {
+        if constexpr (EIGHT) {
+            // ---- codes -> bf16 tiles.  8 (4) lanes share a row of 128 (64) bytes: conflict-free loads; each writes two chunks of 8 values,
+            // lanes of the upper half of a row the second one first
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::CONVERT_REGS));
+            constexpr int CH = RB / 16, PER = 32 / CH;                    // chunks of a row, rows of a warp's step
+            const int w4 = warp - 12, chunk = lane % CH;
+            int stage = 0, raw = 0;
+            uint32_t phase = 0, raw_phase = 0;
+            for (long long u = u0; u < u1; ++u) {
+                const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;          // rows of the tile that are there
+                for (int is_v = 0; is_v < 2; ++is_v) {
+                    wait_bar(&bars.raw_full[raw], raw_phase, gave_up);
+                    wait_bar(&bars.kv_empty[stage], phase ^ 1u, gave_up);
+                    const uint8_t *src = raws + raw * S::RAW, *exps = metas + raw * S::RAW_META;
+                    uint8_t *dst = tiles + stage * S::TILE;
+#pragma unroll 2
+                    for (int r = w4 * 32 + lane / CH; r < (w4 + 1) * 32; r += PER) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(src + chunk_at<RB, TK>(r, chunk));
+                        const int e = exps[r];
+                        const int field = KIND == SISO_E4M3 ? min(e + 120, 254) : e;
+                        const uint32_t f16 = e == 255 ? 0x7FC0u : static_cast<uint32_t>(field) << 7;
+                        const uint32_t factor = f16 | (f16 << 16);
+                        const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t out[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) widen<KIND>(in[i], factor, out[2 * i], out[2 * i + 1]);
+                        if (KIND == SISO_E4M3 && e > 134 && e < 255) {              // 2^(e - 7) itself is beyond bf16
+                            const uint32_t more = static_cast<uint32_t>(e - 134 + 127) << 7;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) out[i] = mul2_bf16(out[i], more | (more << 16));
+                        }
+                        if (r >= left) {                                            // anything may stand there
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) out[i] = 0u;
+                        }
+                        const int flip = CH == 8 ? chunk >> 2 : 0;
+                        const uint4 a = make_uint4(out[0], out[1], out[2], out[3]), b = make_uint4(out[4], out[5], out[6], out[7]);
+                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(r, 2 * chunk + flip)) = flip ? b : a;
+                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(r, 2 * chunk + 1 - flip)) = flip ? a : b;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(&bars.kv_full[stage]); mbar_arrive(&bars.raw_empty[raw]); }
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    if (++raw == RAWS) { raw = 0; raw_phase ^= 1u; }
+                }
+                if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
+            }
+        }
+    } else if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
+        if (warp > 8) {
+            // ---- producers: K and V tiles alternate in the ring; lanes 0-15 own the tile's runs of 8 tokens
+            constexpr int RING = EIGHT ? RAWS : STAGES;
+            const int box_blocks = g.box / 8;
+            int stage = 0;
+            uint32_t phase = 0, tail_phase = 0;
+            for (long long u = u0; u < u1; ++u) {
+                const int j0 = (cur.s.tile0 + cur.tile) * TK, j = j0 + (lane & 15) * 8;
+                for (int is_v = 0; is_v < 2; ++is_v) {
+                    if (stage % PRODUCERS == warp - 9) {          // a stage is always filled by the same warp, so its rounds come in order
+                        const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), tok = j - at * g.kv.page_size;
+                        int page = -1;
+                        if (lane < 16 && j < cur.s.hi) {
+                            page = g.a.d_pages[cur.b * g.a.pages_stride + at];
+                            if (page < 0 || page >= g.kv.n_pages) { page = -1; set_status(g.status, SISO_ERR_INVALID_ARG); }
+                        }
+                        const bool first = lane < 16 && j < cur.s.hi && lane % box_blocks == 0;
+                        const uint32_t there = __ballot_sync(0xFFFFFFFFu, page >= 0);
+                        const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, first));
+                        uint64_t *full = EIGHT ? &bars.raw_full[stage] : &bars.kv_full[stage];
+                        wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up);
+                        uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
+                        // the last values of a bf16 cache: what lies beyond the end may be anything and is zeroed before it is used
+                        const bool tail = !EIGHT && is_v && j0 + TK > cur.s.hi;
+                        uint64_t *bar = tail ? &bars.tail[warp - 9] : full;
+                        if (*gave_up == 0) {
+                            if (lane == 0) {
+                                if (!is_v) bars.blocks[static_cast<int>(u - u0) & 7] = there;
+                                mbar_arrive_expect_tx(bar, boxes * (g.box * RB));
+                            }
+                            __syncwarp();
+                            if (first) {
+                                // a page outside the pool is asked for at a place beyond the tensor's end, which reads as zeros
+                                const int p = page < 0 ? static_cast<int>(g.kv.n_pages) : page;
+#pragma unroll
+                                for (int half = 0; half < RB / LINE; ++half)
+                                    load_box(smem_u32(dst) + half * (TK * 128) + lane * 8 * LINE, is_v ? &map_v : &map_k, half * 64, cur.head, tok, p, g.a.layer, bar);
+                            }
+                            if constexpr (EIGHT) {
+                                const long long e = page < 0 ? 0 : (static_cast<long long>(page) * g.kv.n_kv_heads + cur.head) * g.kv.page_size + tok;
+                                if (lane < 16)
+                                    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(metas + stage * S::RAW_META + lane * 8)),
+                                                 "l"((is_v ? g.kv.v_exp : g.kv.k_exp) + e), "r"(page < 0 ? 0 : 8) : "memory");
+                                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+                            }
+                            if (tail) {
+                                wait_bar(&bars.tail[warp - 9], tail_phase, gave_up);
+                                tail_phase ^= 1u;
+                                for (int x = lane; x < TK * (RB / 16); x += 32) {
+                                    const int row = x / (RB / 16);
+                                    if (j0 + row >= cur.s.hi) *reinterpret_cast<uint4 *>(dst + chunk_at<RB, TK>(row, x % (RB / 16))) = make_uint4(0u, 0u, 0u, 0u);
+                                }
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(full);
+                            }
+                        }
+                    }
+                    if (++stage == RING) { stage = 0; phase ^= 1u; }
+                }
+                if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
+            }
+            if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
+        } else if (lane == 0) {
+            // ---- products
+            const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + D};
+            int stage = 0;
+            uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+            auto step = [&]() { if (++stage == STAGES) { stage = 0; phase ^= 1u; } };
+            auto scores = [&](int t, int at) {
+                const uint64_t a = smem_desc_sw128(smem_u32(q_smem) + t * (S::Q_BYTES / 2)), b = smem_desc_sw128(smem_u32(tiles) + at * S::TILE);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {          // 32 bytes further along a line, or the next 64 d
+                    const uint64_t off = static_cast<uint64_t>(2 * (k % 4) + (k / 4) * ((TK * 128) >> 4));
+                    umma_bf16(s_col[t], a + off, b + off, IDESC<128, false>, k ? 1u : 0u);
+                }
+                umma_commit(&bars.s_full[t]);
+            };
+            for (long long u = u0; u < u1;) {
+                const int n = static_cast<int>(min(static_cast<long long>(cur.s.tiles - cur.tile), u1 - u));
+                const int two = cur.n_q * g.group - cur.rt * TC_ROWS > 128 ? 2 : 1;
+                wait_bar(&bars.kv_full[stage], phase, gave_up);
+                for (int t = 0; t < two; ++t) {
+                    wait_bar(&bars.q_full[t], q_phase[t], gave_up);
+                    q_phase[t] ^= 1u;
+                    tcgen05_fence_after();
+                    scores(t, stage);
+                }
+                umma_commit(&bars.kv_empty[stage]);
+                step();
+                for (int j = 0; j < n; ++j) {
+                    const int v_stage = stage;
+                    wait_bar(&bars.kv_full[v_stage], phase, gave_up);
+                    step();
+                    const bool more = j + 1 < n;
+                    if (more) wait_bar(&bars.kv_full[stage], phase, gave_up);
+                    const uint64_t b = desc_mn(smem_u32(tiles) + v_stage * S::TILE);
+                    for (int t = 0; t < two; ++t) {
+                        wait_bar(&bars.p_full[t], p_phase[t], gave_up);
+                        p_phase[t] ^= 1u;
+                        tcgen05_fence_after();
+#pragma unroll
+                        for (int k = 0; k < TK / 16; ++k)
+                            mma_ts(o_col[t], s_col[t] + 64 + 8 * k, b + static_cast<uint64_t>(k * (2048 >> 4)), IDESC<D, true>, (j | k) ? 1u : 0u);
+                        umma_commit(&bars.o_done[t]);
+                        if (t + 1 == two) umma_commit(&bars.kv_empty[v_stage]);
+                        if (more) scores(t, stage);
+                    }
+                    if (more) { umma_commit(&bars.kv_empty[stage]); step(); }
+                }
+                u += n;
+                cur.tile += n - 1;
+                if (u < u1) cur.next_item(g);
+            }
+        }
+    } else {
+        // ---- softmax: this thread's row of its tile
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SOFTMAX_REGS));
+        const int t = warp >> 2, in_tile = threadIdx.x;                   // row of the 256
+        const uint32_t lane_at = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lane_at + t * 128, o_at = tmem + lane_at + 256 + t * D;
+        const bool causal = (g.a.flags & SISO_ATTN_CAUSAL) != 0u;
+        // the sign of the scale goes to the queries, so that the largest product is the largest score; scale 0: queries of zeros
+        const float scale = g.scale_log2 == 0.f ? 1.f : fabsf(g.scale_log2);
+        const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
+        uint32_t tile_phase = 0;
+        int unit = 0;                                                     // units of this CTA so far
+        long long u = u0;
+        bool pending = false;                                             // an item whose output is still in TMEM
+        float m = -INFINITY, l = 0.f;
+        int out_row = -1, out_head = 0, out_q0 = 0;                       // of that item: output row, or row of the parts
+        long long out_place = -1;
+        auto store_item = [&]() {
+            wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
+            tcgen05_fence_after();
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(out_q0) * g.a.out_stride_token + out_head * g.a.out_stride_head;
+            float *part = g.part_o + out_place * D;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t r[32];
+                tmem_ld_32x32(o_at + c * 32, r);
+                tmem_ld_fence(r);
+                if constexpr (EIGHT) {                                    // d 0 2 1 3 of every four
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) { const uint32_t x = r[i + 1]; r[i + 1] = r[i + 2]; r[i + 2] = x; }
+                }
+                if (out_row >= 0) {
+                    if (out_place < 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) w[k] = pack(__uint_as_float(r[i + 2 * k]) * inv, __uint_as_float(r[i + 2 * k + 1]) * inv, false);
+                            *reinterpret_cast<uint4 *>(dst + c * 32 + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(part + c * 32 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+                    }
+                }
+            }
+            if (out_row >= 0) {
+                if (out_place >= 0) *reinterpret_cast<float2 *>(g.part_ml + out_place * 2) = make_float2(m, l);
+                else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_q0) * g.a.n_heads + out_head] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            }
+            tcgen05_fence_before();
+        };
+        while (u < u1) {
+            const int n = static_cast<int>(min(static_cast<long long>(cur.s.tiles - cur.tile), u1 - u));
+            const int rows = cur.n_q * g.group - cur.rt * TC_ROWS;        // rows of the item from this row tile on
+            const bool mine = t == 0 || rows > 128;
+            if (mine) {
+                const bool real = in_tile < rows;
+                const int row = cur.rt * TC_ROWS + (real ? in_tile : 0);
+                const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = cur.head * g.group + row - i * g.group;
+                // the last scores of the item before have come, so its queries are no longer read
+                const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
+                uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
+#pragma unroll
+                for (int c0 = 0; c0 < D / 8; c0 += 8) {
+                    uint4 x[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) x[c] = real ? *reinterpret_cast<const uint4 *>(src + (c0 + c) * 8) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t w[4] = {(x[c].x ^ flip) & keep, (x[c].y ^ flip) & keep, (x[c].z ^ flip) & keep, (x[c].w ^ flip) & keep};
+                        if constexpr (EIGHT) {                            // the order in which the codes come
+#pragma unroll
+                            for (int k = 0; k < 4; k += 2) {
+                                const uint32_t a = w[k], b = w[k + 1];
+                                w[k] = __byte_perm(a, b, 0x5410);
+                                w[k + 1] = __byte_perm(a, b, 0x7632);
+                            }
+                        }
+                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(in_tile & 127, c0 + c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.q_full[t]);
+                if (pending) store_item();
+                pending = true;
+                const bool whole = cur.tile == 0 && n == cur.s.tiles;
+                out_row = real ? in_tile : -1;
+                out_head = head;
+                out_q0 = cur.q0 + i;
+                out_place = whole ? -1 : part_place(blockIdx.x, cur.tile > 0) * TC_ROWS + in_tile;
+                const int pos = real ? cur.len - cur.n_q + i : cur.s.last_pos;
+                m = -INFINITY;
+                l = 0.f;
+                for (int k = 0; k < n; ++k) {
+                    const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
+                    wait_bar(&bars.s_full[t], tile_phase, gave_up);
+                    tcgen05_fence_after();
+                    const uint32_t blocks = bars.blocks[(unit + k) & 7];
+                    const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) ||
+                                     (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
+                    const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0;
+                    const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 : 0;
+                    // keys that are not seen, or not there, are left out by selection: they may hold anything
+                    auto mask = [&](uint32_t (&r)[32], int c) {
+                        if (cut) {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (c * 32 + x > last || c * 32 + x < first || !((blocks >> ((c * 32 + x) / 8)) & 1u)) r[x] = 0xFF800000u;
+                        }
+                    };
+                    auto largest = [&](const uint32_t (&r)[32], float top) {
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(r[x]));
+                        return top;
+                    };
+                    // 128 scores and the probabilities do not fit the registers at once: the first half is read again from TMEM, where
+                    // the probabilities take the columns of the second half
+                    uint32_t ra[32], rb[32], rc[32];
+                    tmem_ld_32x32(s_at, ra);
+                    tmem_ld_32x32(s_at + 32, rb);
+                    tmem_ld_fence(ra);
+                    tmem_ld_fence(rb);
+                    mask(ra, 0);
+                    mask(rb, 1);
+                    float top0 = largest(ra, -INFINITY), top1 = largest(rb, -INFINITY);
+                    tmem_ld_32x32(s_at + 64, ra);
+                    tmem_ld_32x32(s_at + 96, rb);
+                    tmem_ld_fence(ra);
+                    tmem_ld_fence(rb);
+                    mask(ra, 2);
+                    mask(rb, 3);
+                    top0 = largest(ra, top0);
+                    top1 = largest(rb, top1);
+                    const float m2 = fmaxf(m, fmaxf(top0, top1) * scale);
+                    if (__any_sync(0xFFFFFFFFu, m2 > m + 8.f || (m == -INFINITY && m2 != m))) {
+                        const float corr = m == m2 ? 1.f : ex2(m - m2);
+                        m = m2;
+                        l *= corr;
+                        if (k > 0) {
+                            wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
+                            tcgen05_fence_after();
+#pragma unroll
+                            for (int c = 0; c < D / 16; ++c) {            // 16 columns at a time: the scores stay in registers
+                                uint32_t y[16];
+                                asm volatile(
+                                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                                    "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+                                    "tcgen05.wait::ld.sync.aligned;"
+                                    : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]),
+                                      "=r"(y[9]), "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
+                                    : "r"(o_at + c * 16) : "memory");
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(y[x]) * corr);
+                                tmem_st_32x16(o_at + c * 16, y);
+                            }
+                        }
+                    }
+                    const float shift = m == -INFINITY ? 0.f : -m;
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    auto weigh = [&](const uint32_t (&r)[32], int c) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
+                            y.x = ex2(y.x);
+                            y.y = ex2(y.y);
+                            sum[x & 1] = add2(sum[x & 1], y);
+                            p[x] = pack(y.x, y.y, false);
+                        }
+                        tmem_st_32x16(s_at + 64 + c * 16, p);
+                    };
+                    tmem_ld_32x32(s_at, rc);
+                    weigh(ra, 2);
+                    tmem_ld_fence(rc);
+                    mask(rc, 0);
+                    tmem_ld_32x32(s_at + 32, ra);
+                    weigh(rb, 3);
+                    weigh(rc, 0);
+                    tmem_ld_fence(ra);
+                    mask(ra, 1);
+                    weigh(ra, 1);
+                    sum[0] = add2(sum[0], sum[1]);
+                    l += sum[0].x + sum[0].y;
+                    tmem_st_wait();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.p_full[t]);
+                    tile_phase ^= 1u;
+                }
+            }
+            if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) {
+                const long long end = u + cur.s.tiles;
+                g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.rt, cta_of(end - 1, total, ctas) - static_cast<int>(blockIdx.x) + 1};
+            }
+            u += n;
+            unit += n;
+            cur.tile += n - 1;
+            if (u < u1) cur.next_item(g);
+        }
+        if (pending) store_item();
+    }
+
+    // ---- teardown
+    __syncwarp();
+    if (*gave_up) {
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);      // copies in flight land before the shared memory is handed back
+        if (threadIdx.x == 0) set_status(g.status, SISO_ERR_TIMEOUT);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <int KIND, int D> static siso_status_t run(Kv *h, Args &g, cudaStream_t s) {
+    using S = Shape<KIND, D>;
+    constexpr uint32_t bit = 1u << 8;
+    if (!(h->attr_set & bit)) {
+        SISO_CUDA(cudaFuncSetAttribute(attention_many_rows_kernel<KIND, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        h->attr_set |= bit;
+    }
+    attention_many_rows_kernel<KIND, D><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
+    SISO_CUDA(cudaGetLastError());
+    return launch_join(g, TC_ROWS, D, s);
+}
+
+}  // namespace tc
+
+siso_status_t launch_many_rows(Kv *h, Args &g, cudaStream_t s) {
+    const bool wide = h->cfg.head_dim == 128;
+    switch (h->cfg.dtype) {
+        case SISO_BF16: return wide ? tc::run<SISO_BF16, 128>(h, g, s) : tc::run<SISO_BF16, 64>(h, g, s);
+        case SISO_E4M3: return wide ? tc::run<SISO_E4M3, 128>(h, g, s) : tc::run<SISO_E4M3, 64>(h, g, s);
+        default: return wide ? tc::run<SISO_I8, 128>(h, g, s) : tc::run<SISO_I8, 64>(h, g, s);
+    }
+}
+
+}  // namespace kva
+}  // namespace siso
