@@ -4,13 +4,14 @@
 // With many rows the call is bound by the tensor cores and, nearly as much, by the exponentials: a tile of 128 x 128 scores takes
 // 2 x 512 cycles of tcgen05.mma (d = 128) and 1024 cycles of the SM's 16 exponentials a cycle.  So a CTA works on two
 // tiles of 128 rows at once: while the softmax of one runs on the CUDA cores the products of the other run on the tensor cores.
-//   warps 0-3, 4-7   softmax of row tile 0, 1: thread = row = TMEM lane.  Load the row's 128 scores from TMEM, running maximum, exponentials,
-//                    probabilities as bf16 back into TMEM over the scores.  The output in TMEM is rescaled only where a maximum has
-//                    grown by more than 8 (a factor 2^8, which fp32 sums and bf16 probabilities bear); then by these warps.
-//   warp 8           issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
+//   warps 0-7, 8-15  softmax of row tile 0, 1: a row (= TMEM lane) belongs to two threads, each with 64 of its 128 scores.  Scores from
+//                    TMEM, running maximum, exponentials, probabilities as bf16 back into TMEM over the scores.  The output in
+//                    TMEM is rescaled only where a maximum has grown by more than 8 (a factor 2^8, which fp32 sums and bf16
+//                    probabilities bear); then by these warps.
+//   warp 16          issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
 //                    an MN-major operand)
-//   warps 9-11       fill the ring of K and V tiles by TMA, one box per run of tokens in one page
-//   warps 12-15      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
+//   warps 17-19      fill the ring of K and V tiles by TMA, one box per run of tokens in one page
+//   warps 20-23      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
 // TMEM: S_0, S_1 (128 columns each), O_0, O_1.
 #include "kv_attention.cuh"
 
@@ -22,30 +23,35 @@ using namespace umma2;
 
 constexpr int TK = 128;
 constexpr int PRODUCERS = 3;
+constexpr int POLY = 8;               // of 16 pairs of exponentials are taken on the FMA pipe
+
+struct Bars {
+    uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
+    uint64_t kv_full[6], kv_empty[6], raw_full[4], raw_empty[4], tail[PRODUCERS];
+    uint32_t blocks[8];        // of unit i at i % 8: which runs of 8 keys have a page in the pool
+    long long total;           // units of the call, and the CTAs that share them
+    int ctas;
+    uint32_t tmem;
+    int gave_up;
+    unsigned long long buf[26];
+    float peer[2][2][128];     // a row's maximum, or sum, on its way to the other thread of the row
+};
 
 template <int KIND, int D> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
-    static constexpr int THREADS = EIGHT ? 512 : 384;
+    static constexpr int THREADS = EIGHT ? 768 : 640;
     static constexpr int Q_BYTES = 2 * 128 * D * 2;
     static constexpr int TILE = TK * D * 2;                              // a tile of K or V in bf16
     static constexpr int RAW = EIGHT ? TK * D : 0;                       // and as codes
     static constexpr int RAW_META = EIGHT ? TK : 0;                      // exponents
-    static constexpr int ROOM = 232448 - 1024 - 1024 - Q_BYTES;          // alignment; barriers
+    static constexpr int ROOM = 232448 - static_cast<int>(sizeof(Bars)) - Q_BYTES;
     static constexpr int RAWS = EIGHT ? 4 : 0;
     static constexpr int FIT = (ROOM - RAWS * (RAW + RAW_META)) / TILE;
     static constexpr int STAGES = FIT > 6 ? 6 : FIT;
-    static constexpr int SMEM = 1024 + Q_BYTES + STAGES * TILE + RAWS * (RAW + RAW_META);
-    // registers: what the CTA has at launch (168 x 384 or 128 x 512), moved to the softmax
-    static constexpr int SOFTMAX_REGS = EIGHT ? 152 : 192, OTHER_REGS = EIGHT ? 88 : 120, CONVERT_REGS = 120;
-    static_assert(2 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? CONVERT_REGS : 0) == (EIGHT ? 4 * 128 : 3 * 168), "register split");
-};
-
-struct Bars {
-    uint64_t q_full[2], s_full[2], p_full[2], o_done[2];
-    uint64_t kv_full[6], kv_empty[6], raw_full[4], raw_empty[4], tail[PRODUCERS];
-    uint32_t blocks[8];        // of unit i at i % 8: which runs of 8 keys have a page in the pool
-    uint32_t tmem;
-    int gave_up;
+    static constexpr int SMEM = Q_BYTES + STAGES * TILE + RAWS * (RAW + RAW_META) + static_cast<int>(sizeof(Bars));
+    // registers: what the CTA has at launch (96 x 640 or 80 x 768), moved to the softmax
+    static constexpr int SOFTMAX_REGS = EIGHT ? 96 : 104, OTHER_REGS = EIGHT ? 40 : 64, CONVERT_REGS = 56;
+    static_assert(4 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? CONVERT_REGS : 0) == (EIGHT ? 6 * 80 : 5 * 96), "register split");
 };
 
 // D fp32, A and B bf16; A from shared memory or TMEM, K-major; B K-major, or MN-major (bit 16)
@@ -60,6 +66,11 @@ __device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
     d |= static_cast<uint64_t>(1) << 46;
     d |= static_cast<uint64_t>(2) << 61;
     return d;
+}
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0u;
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t accumulate) {
     asm volatile(
@@ -98,6 +109,28 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         : "=l"(reinterpret_cast<unsigned long long &>(d)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
     return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 2^x for x in [-126, 127] (below: as -126) on the FMA pipe: x = n + f with n whole and f in [-1/2, 1/2], a polynomial of degree 4 for 2^f
+// (largest relative error on the interval minimised numerically: 2.7e-6, a thousandth of what rounding to bf16 adds), n added to the exponent
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float big = 12582912.f;                     // 1.5 2^23: adding it rounds to a whole number, which then stands in the low bits
+    const float2 t = add2(x, make_float2(big, big));
+    const float2 f = add2(x, fma2(t, make_float2(-1.f, -1.f), make_float2(big, big)));
+    float2 y = make_float2(0.009570102207362652f, 0.009570102207362652f);
+    y = fma2(y, f, make_float2(0.05591786280274391f, 0.05591786280274391f));
+    y = fma2(y, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    y = fma2(y, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    y = fma2(y, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    y.x = __uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23));
+    y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
+    return y;
+}
 __device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -129,16 +162,15 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     constexpr bool EIGHT = S::EIGHT;
     constexpr int STAGES = S::STAGES, RAWS = S::RAWS;
     constexpr int RB = D * (EIGHT ? 1 : 2), LINE = RB < 128 ? RB : 128;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ unsigned long long buf[S::THREADS / 32 + 2];
-    __shared__ Bars bars;
-    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) uint8_t smem[];           // all of it: nothing static, so that it begins on a boundary of the swizzle
     uint8_t *q_smem = smem, *tiles = smem + S::Q_BYTES, *raws = tiles + STAGES * S::TILE, *metas = raws + RAWS * S::RAW;
+    Bars &bars = *reinterpret_cast<Bars *>(metas + RAWS * S::RAW_META);
+    unsigned long long *buf = bars.buf;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
-        for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 4); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t], 4); mbar_init(&bars.o_done[t], 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 8); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t][0], 4); mbar_init(&bars.p_full[t][1], 4); mbar_init(&bars.o_done[t], 1); }
         for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 4 : 1); mbar_init(&bars.kv_empty[i], 1); }
         for (int i = 0; i < RAWS; ++i) { mbar_init(&bars.raw_full[i], 33); mbar_init(&bars.raw_empty[i], 4); }
         for (int i = 0; i < PRODUCERS; ++i) mbar_init(&bars.tail[i], 1);
@@ -151,7 +183,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     int ctas;
     Cursor<TC_ROWS, TK> cur;
     if (!locate<TC_ROWS, TK, S::THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
-    if (warp == 8) {
+    if (threadIdx.x == 0) { bars.total = total; bars.ctas = ctas; }
+    if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -161,13 +194,13 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     const uint32_t tmem = bars.tmem;
     volatile int *gave_up = &bars.gave_up;
 
-    if (warp >= 12) {
+    if (warp >= 20) {
         if constexpr (EIGHT) {
             // ---- codes -> bf16 tiles.  8 (4) lanes share a row of 128 (64) bytes: conflict-free loads; each writes two chunks of 8 values,
             // lanes of the upper half of a row the second one first
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::CONVERT_REGS));
             constexpr int CH = RB / 16, PER = 32 / CH;                    // chunks of a row, rows of a warp's step
-            const int w4 = warp - 12, chunk = lane % CH;
+            const int w4 = warp - 20, chunk = lane % CH;
             int stage = 0, raw = 0;
             uint32_t phase = 0, raw_phase = 0;
             for (long long u = u0; u < u1; ++u) {
@@ -211,9 +244,9 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
             }
         }
-    } else if (warp >= 8) {
+    } else if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
-        if (warp > 8) {
+        if (warp > 16) {
             // ---- producers: K and V tiles alternate in the ring; lanes 0-15 own the tile's runs of 8 tokens
             constexpr int RING = EIGHT ? RAWS : STAGES;
             const int box_blocks = g.box / 8;
@@ -222,7 +255,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             for (long long u = u0; u < u1; ++u) {
                 const int j0 = (cur.s.tile0 + cur.tile) * TK, j = j0 + (lane & 15) * 8;
                 for (int is_v = 0; is_v < 2; ++is_v) {
-                    if (stage % PRODUCERS == warp - 9) {          // a stage is always filled by the same warp, so its rounds come in order
+                    if (stage % PRODUCERS == warp - 17) {          // a stage is always filled by the same warp, so its rounds come in order
                         const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), tok = j - at * g.kv.page_size;
                         int page = -1;
                         if (lane < 16 && j < cur.s.hi) {
@@ -237,7 +270,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
                         // the last values of a bf16 cache: what lies beyond the end may be anything and is zeroed before it is used
                         const bool tail = !EIGHT && is_v && j0 + TK > cur.s.hi;
-                        uint64_t *bar = tail ? &bars.tail[warp - 9] : full;
+                        uint64_t *bar = tail ? &bars.tail[warp - 17] : full;
                         if (*gave_up == 0) {
                             if (lane == 0) {
                                 if (!is_v) bars.blocks[static_cast<int>(u - u0) & 7] = there;
@@ -259,7 +292,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                 asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
                             }
                             if (tail) {
-                                wait_bar(&bars.tail[warp - 9], tail_phase, gave_up);
+                                wait_bar(&bars.tail[warp - 17], tail_phase, gave_up);
                                 tail_phase ^= 1u;
                                 for (int x = lane; x < TK * (RB / 16); x += 32) {
                                     const int row = x / (RB / 16);
@@ -276,32 +309,43 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
             }
             if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
-        } else if (lane == 0) {
-            // ---- products
-            const uint32_t s_col[2] = {tmem, tmem + 128}, o_col[2] = {tmem + 256, tmem + 256 + D};
+        } else {
+            // ---- products.  The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one
+            // lane issues
+            const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+            const uint32_t s_col[2] = {base, base + 128}, o_col[2] = {base + 256, base + 256 + D};
+            const uint64_t q_desc = smem_desc_sw128(smem_u32(q_smem)), k_desc = smem_desc_sw128(smem_u32(tiles)), v_desc = desc_mn(smem_u32(tiles));
             int stage = 0;
             uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
             auto step = [&]() { if (++stage == STAGES) { stage = 0; phase ^= 1u; } };
             auto scores = [&](int t, int at) {
-                const uint64_t a = smem_desc_sw128(smem_u32(q_smem) + t * (S::Q_BYTES / 2)), b = smem_desc_sw128(smem_u32(tiles) + at * S::TILE);
+                const uint64_t a = q_desc + static_cast<uint64_t>(t * (S::Q_BYTES / 2 >> 4)), b = k_desc + static_cast<uint64_t>(at * (S::TILE >> 4));
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {          // 32 bytes further along a line, or the next 64 d
-                    const uint64_t off = static_cast<uint64_t>(2 * (k % 4) + (k / 4) * ((TK * 128) >> 4));
-                    umma_bf16(s_col[t], a + off, b + off, IDESC<128, false>, k ? 1u : 0u);
+                    for (int k = 0; k < D / 16; ++k) {      // 32 bytes further along a line, or the next 64 d
+                        const uint64_t off = static_cast<uint64_t>(2 * (k % 4) + (k / 4) * ((TK * 128) >> 4));
+                        umma_bf16(s_col[t], a + off, b + off, IDESC<128, false>, k ? 1u : 0u);
+                    }
+                    umma_commit(&bars.s_full[t]);
                 }
-                umma_commit(&bars.s_full[t]);
+                __syncwarp();
             };
-            for (long long u = u0; u < u1;) {
-                const int n = static_cast<int>(min(static_cast<long long>(cur.s.tiles - cur.tile), u1 - u));
+            const int units = static_cast<int>(u1 - u0);
+            for (int u = 0; u < units;) {
+                const int n = min(cur.s.tiles - cur.tile, units - u);
                 const int two = cur.n_q * g.group - cur.rt * TC_ROWS > 128 ? 2 : 1;
                 wait_bar(&bars.kv_full[stage], phase, gave_up);
-                for (int t = 0; t < two; ++t) {
-                    wait_bar(&bars.q_full[t], q_phase[t], gave_up);
-                    q_phase[t] ^= 1u;
-                    tcgen05_fence_after();
-                    scores(t, stage);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (t < two) {
+                        wait_bar(&bars.q_full[t], q_phase[t], gave_up);
+                        q_phase[t] ^= 1u;
+                        tcgen05_fence_after();
+                        scores(t, stage);
+                    }
                 }
-                umma_commit(&bars.kv_empty[stage]);
+                if (elect_one()) umma_commit(&bars.kv_empty[stage]);
+                __syncwarp();
                 step();
                 for (int j = 0; j < n; ++j) {
                     const int v_stage = stage;
@@ -309,50 +353,68 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     step();
                     const bool more = j + 1 < n;
                     if (more) wait_bar(&bars.kv_full[stage], phase, gave_up);
-                    const uint64_t b = desc_mn(smem_u32(tiles) + v_stage * S::TILE);
-                    for (int t = 0; t < two; ++t) {
-                        wait_bar(&bars.p_full[t], p_phase[t], gave_up);
-                        p_phase[t] ^= 1u;
-                        tcgen05_fence_after();
+                    const uint64_t b = v_desc + static_cast<uint64_t>(v_stage * (S::TILE >> 4));
 #pragma unroll
-                        for (int k = 0; k < TK / 16; ++k)
-                            mma_ts(o_col[t], s_col[t] + 64 + 8 * k, b + static_cast<uint64_t>(k * (2048 >> 4)), IDESC<D, true>, (j | k) ? 1u : 0u);
-                        umma_commit(&bars.o_done[t]);
-                        if (t + 1 == two) umma_commit(&bars.kv_empty[v_stage]);
-                        if (more) scores(t, stage);
+                    for (int t = 0; t < 2; ++t) {
+                        if (t < two) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {   // keys 0-63, 64-127: each as soon as its probabilities are there
+                                wait_bar(&bars.p_full[t][h], p_phase[t], gave_up);
+                                tcgen05_fence_after();
+                                if (elect_one()) {
+#pragma unroll
+                                    for (int k = 4 * h; k < 4 * h + 4; ++k)
+                                        mma_ts(o_col[t], s_col[t] + 64 * h + 8 * (k & 3), b + static_cast<uint64_t>(k * (2048 >> 4)), IDESC<D, true>,
+                                               (j > 0 || k > 0) ? 1u : 0u);
+                                    if (h == 1) {
+                                        umma_commit(&bars.o_done[t]);
+                                        if (t + 1 == two) umma_commit(&bars.kv_empty[v_stage]);
+                                    }
+                                }
+                                __syncwarp();
+                            }
+                            p_phase[t] ^= 1u;
+                            if (more) scores(t, stage);
+                        }
                     }
-                    if (more) { umma_commit(&bars.kv_empty[stage]); step(); }
+                    if (more) {
+                        if (elect_one()) umma_commit(&bars.kv_empty[stage]);
+                        __syncwarp();
+                        step();
+                    }
                 }
                 u += n;
                 cur.tile += n - 1;
-                if (u < u1) cur.next_item(g);
+                if (u < units) cur.next_item(g);
             }
         }
     } else {
-        // ---- softmax: this thread's row of its tile
+        // ---- softmax: half of a row of one tile
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SOFTMAX_REGS));
-        const int t = warp >> 2, in_tile = threadIdx.x;                   // row of the 256
+        const int t = warp >> 3, half = (warp >> 2) & 1, in_tile = t * 128 + (threadIdx.x & 127);      // row of the 256
         const uint32_t lane_at = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + lane_at + t * 128, o_at = tmem + lane_at + 256 + t * D;
+        const uint32_t s_at = tmem + lane_at + t * 128 + half * 64, o_at = tmem + lane_at + 256 + t * D + half * (D / 2);
         const bool causal = (g.a.flags & SISO_ATTN_CAUSAL) != 0u;
         // the sign of the scale goes to the queries, so that the largest product is the largest score; scale 0: queries of zeros
         const float scale = g.scale_log2 == 0.f ? 1.f : fabsf(g.scale_log2);
-        const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
+        float &mine_out = bars.peer[t][half][threadIdx.x & 127], &theirs_in = bars.peer[t][half ^ 1][threadIdx.x & 127];
         uint32_t tile_phase = 0;
         int unit = 0;                                                     // units of this CTA so far
-        long long u = u0;
+        const int units = static_cast<int>(u1 - u0);
         bool pending = false;                                             // an item whose output is still in TMEM
         float m = -INFINITY, l = 0.f;
-        int out_row = -1, out_head = 0, out_q0 = 0;                       // of that item: output row, or row of the parts
-        long long out_place = -1;
+        int out_token = -1, out_head = 0, out_place = -1;                 // of that item: where the row goes, or its place among the parts
+        auto together = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1 + t) : "memory"); };
         auto store_item = [&]() {
             wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
             tcgen05_fence_after();
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(out_q0) * g.a.out_stride_token + out_head * g.a.out_stride_head;
-            float *part = g.part_o + out_place * D;
+            mine_out = l;
+            together();
+            const float sum = half ? theirs_in + l : l + theirs_in;       // the same sum in both threads
+            const bool none = m == -INFINITY;                             // (the sum may hold remainders of 2^-126)
+            const float inv = none ? 0.f : 1.f / sum;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < D / 64; ++c) {
                 uint32_t r[32];
                 tmem_ld_32x32(o_at + c * 32, r);
                 tmem_ld_fence(r);
@@ -360,45 +422,46 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) { const uint32_t x = r[i + 1]; r[i + 1] = r[i + 2]; r[i + 2] = x; }
                 }
-                if (out_row >= 0) {
-                    if (out_place < 0) {
+                if (out_token >= 0 && out_place < 0) {
+                    __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(out_token) * g.a.out_stride_token + out_head * g.a.out_stride_head +
+                                         half * (D / 2) + c * 32;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint32_t w[4];
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t w[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) w[k] = pack(__uint_as_float(r[i + 2 * k]) * inv, __uint_as_float(r[i + 2 * k + 1]) * inv, false);
-                            *reinterpret_cast<uint4 *>(dst + c * 32 + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(part + c * 32 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+                        for (int k = 0; k < 4; ++k) w[k] = pack(__uint_as_float(r[i + 2 * k]) * inv, __uint_as_float(r[i + 2 * k + 1]) * inv, false);
+                        *reinterpret_cast<uint4 *>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
+                } else if (out_token >= 0) {
+                    float *part = g.part_o + static_cast<long long>(out_place) * D + half * (D / 2) + c * 32;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(part + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
                 }
             }
-            if (out_row >= 0) {
-                if (out_place >= 0) *reinterpret_cast<float2 *>(g.part_ml + out_place * 2) = make_float2(m, l);
-                else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_q0) * g.a.n_heads + out_head] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            if (out_token >= 0 && half == 0) {
+                if (out_place >= 0) *reinterpret_cast<float2 *>(g.part_ml + 2ll * out_place) = make_float2(m, sum);
+                else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_token) * g.a.n_heads + out_head] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
             }
             tcgen05_fence_before();
+            together();                                                   // the exchange place is free again
         };
-        while (u < u1) {
-            const int n = static_cast<int>(min(static_cast<long long>(cur.s.tiles - cur.tile), u1 - u));
+        while (unit < units) {
+            const int n = min(cur.s.tiles - cur.tile, units - unit);
             const int rows = cur.n_q * g.group - cur.rt * TC_ROWS;        // rows of the item from this row tile on
             const bool mine = t == 0 || rows > 128;
             if (mine) {
                 const bool real = in_tile < rows;
                 const int row = cur.rt * TC_ROWS + (real ? in_tile : 0);
                 const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = cur.head * g.group + row - i * g.group;
-                // the last scores of the item before have come, so its queries are no longer read
-                const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
-                uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
+                {   // the last scores of the item before have come, so its queries are no longer read
+                    const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
+                    const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
+                    uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
+                    uint4 x[D / 16];
 #pragma unroll
-                for (int c0 = 0; c0 < D / 8; c0 += 8) {
-                    uint4 x[8];
+                    for (int c = 0; c < D / 16; ++c) x[c] = real ? *reinterpret_cast<const uint4 *>(src + (half * (D / 16) + c) * 8) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) x[c] = real ? *reinterpret_cast<const uint4 *>(src + (c0 + c) * 8) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < D / 16; ++c) {
                         uint32_t w[4] = {(x[c].x ^ flip) & keep, (x[c].y ^ flip) & keep, (x[c].z ^ flip) & keep, (x[c].w ^ flip) & keep};
                         if constexpr (EIGHT) {                            // the order in which the codes come
 #pragma unroll
@@ -408,19 +471,17 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                 w[k + 1] = __byte_perm(a, b, 0x7632);
                             }
                         }
-                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(in_tile & 127, c0 + c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(in_tile & 127, half * (D / 16) + c)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.q_full[t]);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.q_full[t]);
                 if (pending) store_item();
                 pending = true;
-                const bool whole = cur.tile == 0 && n == cur.s.tiles;
-                out_row = real ? in_tile : -1;
+                out_token = real ? cur.q0 + i : -1;
                 out_head = head;
-                out_q0 = cur.q0 + i;
-                out_place = whole ? -1 : part_place(blockIdx.x, cur.tile > 0) * TC_ROWS + in_tile;
+                out_place = cur.tile == 0 && n == cur.s.tiles ? -1 : static_cast<int>(part_place(blockIdx.x, cur.tile > 0)) * TC_ROWS + in_tile;
                 const int pos = real ? cur.len - cur.n_q + i : cur.s.last_pos;
                 m = -INFINITY;
                 l = 0.f;
@@ -428,52 +489,52 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
                     wait_bar(&bars.s_full[t], tile_phase, gave_up);
                     tcgen05_fence_after();
+                    uint32_t ra[32], rb[32];
+                    tmem_ld_32x32(s_at, ra);
+                    tmem_ld_32x32(s_at + 32, rb);
                     const uint32_t blocks = bars.blocks[(unit + k) & 7];
                     const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) ||
                                      (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
-                    const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0;
-                    const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 : 0;
-                    // keys that are not seen, or not there, are left out by selection: they may hold anything
-                    auto mask = [&](uint32_t (&r)[32], int c) {
-                        if (cut) {
+                    tmem_ld_fence(ra);
+                    tmem_ld_fence(rb);
+                    if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
+                        const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0 - half * 64;
+                        const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 - half * 64 : 0;
+                        const uint32_t my_blocks = blocks >> (half * 8);
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (c * 32 + x > last || c * 32 + x < first || !((blocks >> ((c * 32 + x) / 8)) & 1u)) r[x] = 0xFF800000u;
+                        for (int x = 0; x < 32; ++x) {
+                            if (x > last || x < first || !((my_blocks >> (x / 8)) & 1u)) ra[x] = 0xFF800000u;
+                            if (32 + x > last || 32 + x < first || !((my_blocks >> (4 + x / 8)) & 1u)) rb[x] = 0xFF800000u;
                         }
-                    };
-                    auto largest = [&](const uint32_t (&r)[32], float top) {
+                    }
+                    float top[4] = {__uint_as_float(ra[0]), __uint_as_float(ra[1]), __uint_as_float(rb[0]), __uint_as_float(rb[1])};
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(r[x]));
-                        return top;
-                    };
-                    // 128 scores and the probabilities do not fit the registers at once: the first half is read again from TMEM, where
-                    // the probabilities take the columns of the second half
-                    uint32_t ra[32], rb[32], rc[32];
-                    tmem_ld_32x32(s_at, ra);
-                    tmem_ld_32x32(s_at + 32, rb);
-                    tmem_ld_fence(ra);
-                    tmem_ld_fence(rb);
-                    mask(ra, 0);
-                    mask(rb, 1);
-                    float top0 = largest(ra, -INFINITY), top1 = largest(rb, -INFINITY);
-                    tmem_ld_32x32(s_at + 64, ra);
-                    tmem_ld_32x32(s_at + 96, rb);
-                    tmem_ld_fence(ra);
-                    tmem_ld_fence(rb);
-                    mask(ra, 2);
-                    mask(rb, 3);
-                    top0 = largest(ra, top0);
-                    top1 = largest(rb, top1);
-                    const float m2 = fmaxf(m, fmaxf(top0, top1) * scale);
-                    if (__any_sync(0xFFFFFFFFu, m2 > m + 8.f || (m == -INFINITY && m2 != m))) {
+                    for (int x = 2; x < 32; x += 4) {
+                        top[0] = max3(top[0], __uint_as_float(ra[x]), __uint_as_float(ra[x + 1]));
+                        top[2] = max3(top[2], __uint_as_float(rb[x]), __uint_as_float(rb[x + 1]));
+                        if (x + 2 < 32) {
+                            top[1] = max3(top[1], __uint_as_float(ra[x + 2]), __uint_as_float(ra[x + 3]));
+                            top[3] = max3(top[3], __uint_as_float(rb[x + 2]), __uint_as_float(rb[x + 3]));
+                        }
+                    }
+                    float m2 = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]) * scale);
+                    uint32_t grown;
+                    asm volatile(
+                        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
+                        "barrier.cta.red.or.aligned.pred q, %1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                        : "=r"(grown) : "r"(1 + t), "r"((m2 > m + 8.f || (m == -INFINITY && m2 != m)) ? 1u : 0u) : "memory");
+                    if (grown) {
+                        mine_out = m2;
+                        together();
+                        m2 = fmaxf(m2, theirs_in);
                         const float corr = m == m2 ? 1.f : ex2(m - m2);
                         m = m2;
                         l *= corr;
                         if (k > 0) {
                             wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
                             tcgen05_fence_after();
-#pragma unroll
-                            for (int c = 0; c < D / 16; ++c) {            // 16 columns at a time: the scores stay in registers
+#pragma unroll 1
+                            for (int c = 0; c < D / 2; c += 16) {         // 16 columns at a time: the scores stay in registers
                                 uint32_t y[16];
                                 asm volatile(
                                     "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -481,12 +542,16 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                     "tcgen05.wait::ld.sync.aligned;"
                                     : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]),
                                       "=r"(y[9]), "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
-                                    : "r"(o_at + c * 16) : "memory");
+                                    : "r"(o_at + c) : "memory");
 #pragma unroll
                                 for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(y[x]) * corr);
-                                tmem_st_32x16(o_at + c * 16, y);
+                                tmem_st_32x16(o_at + c, y);
                             }
+                            tmem_st_wait();
+                            tcgen05_fence_before();
                         }
+                        together();        // no product of this unit begins before both halves of the output are rescaled
+                        tcgen05_fence_after();
                     }
                     const float shift = m == -INFINITY ? 0.f : -m;
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -495,40 +560,31 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
                             float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
-                            y.x = ex2(y.x);
-                            y.y = ex2(y.y);
+                            if ((x * POLY) % 16 < POLY) y = ex2_poly(y);
+                            else { y.x = ex2(y.x); y.y = ex2(y.y); }
                             sum[x & 1] = add2(sum[x & 1], y);
                             p[x] = pack(y.x, y.y, false);
                         }
-                        tmem_st_32x16(s_at + 64 + c * 16, p);
+                        tmem_st_32x16(s_at + c * 16, p);
                     };
-                    tmem_ld_32x32(s_at, rc);
-                    weigh(ra, 2);
-                    tmem_ld_fence(rc);
-                    mask(rc, 0);
-                    tmem_ld_32x32(s_at + 32, ra);
-                    weigh(rb, 3);
-                    weigh(rc, 0);
-                    tmem_ld_fence(ra);
-                    mask(ra, 1);
-                    weigh(ra, 1);
-                    sum[0] = add2(sum[0], sum[1]);
-                    l += sum[0].x + sum[0].y;
+                    weigh(ra, 0);
+                    weigh(rb, 1);
                     tmem_st_wait();
                     tcgen05_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&bars.p_full[t]);
+                    if (lane == 0) mbar_arrive(&bars.p_full[t][half]);
+                    sum[0] = add2(sum[0], sum[1]);
+                    l += sum[0].x + sum[0].y;
                     tile_phase ^= 1u;
                 }
             }
             if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) {
-                const long long end = u + cur.s.tiles;
-                g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.rt, cta_of(end - 1, total, ctas) - static_cast<int>(blockIdx.x) + 1};
+                const long long end = u0 + unit + cur.s.tiles;
+                g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.rt, cta_of(end - 1, bars.total, bars.ctas) - static_cast<int>(blockIdx.x) + 1};
             }
-            u += n;
             unit += n;
             cur.tile += n - 1;
-            if (u < u1) cur.next_item(g);
+            if (unit < units) cur.next_item(g);
         }
         if (pending) store_item();
     }
@@ -541,7 +597,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     }
     tcgen05_fence_before();
     __syncthreads();
-    if (warp == 8) {
+    if (warp == 16) {
         tcgen05_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
