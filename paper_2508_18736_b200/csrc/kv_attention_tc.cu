@@ -11,7 +11,7 @@
 //   warp 16          issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
 //                    an MN-major operand)
 //   warps 17-19      fill the ring of K and V tiles by TMA, one box per run of tokens in one page
-//   warps 20-23      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
+//   warps 20-27      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
 // TMEM: S_0, S_1 (128 columns each), O_0, O_1.
 #include "kv_attention.cuh"
 
@@ -23,7 +23,6 @@ using namespace umma2;
 
 constexpr int TK = 128;
 constexpr int PRODUCERS = 3;
-constexpr int POLY = 8;               // of 16 pairs of exponentials are taken on the FMA pipe
 
 struct Bars {
     uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
@@ -33,25 +32,27 @@ struct Bars {
     int ctas;
     uint32_t tmem;
     int gave_up;
-    unsigned long long buf[26];
+    unsigned long long buf[30];
     float peer[2][2][128];     // a row's maximum, or sum, on its way to the other thread of the row
 };
 
 template <int KIND, int D> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
-    static constexpr int THREADS = EIGHT ? 768 : 640;
+    static constexpr int THREADS = EIGHT ? 896 : 640;
     static constexpr int Q_BYTES = 2 * 128 * D * 2;
     static constexpr int TILE = TK * D * 2;                              // a tile of K or V in bf16
     static constexpr int RAW = EIGHT ? TK * D : 0;                       // and as codes
     static constexpr int RAW_META = EIGHT ? TK : 0;                      // exponents
     static constexpr int ROOM = 232448 - static_cast<int>(sizeof(Bars)) - Q_BYTES;
-    static constexpr int RAWS = EIGHT ? 4 : 0;
+    static constexpr int RAWS = EIGHT ? (D == 128 ? 2 : 4) : 0;
     static constexpr int FIT = (ROOM - RAWS * (RAW + RAW_META)) / TILE;
     static constexpr int STAGES = FIT > 6 ? 6 : FIT;
     static constexpr int SMEM = Q_BYTES + STAGES * TILE + RAWS * (RAW + RAW_META) + static_cast<int>(sizeof(Bars));
-    // registers: what the CTA has at launch (96 x 640 or 80 x 768), moved to the softmax
-    static constexpr int SOFTMAX_REGS = EIGHT ? 96 : 104, OTHER_REGS = EIGHT ? 40 : 64, CONVERT_REGS = 56;
-    static_assert(4 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? CONVERT_REGS : 0) == (EIGHT ? 6 * 80 : 5 * 96), "register split");
+    // registers: what the CTA has at launch (96 x 640 or 72 x 896), moved to the softmax
+    static constexpr int SOFTMAX_REGS = EIGHT ? 96 : 104, OTHER_REGS = EIGHT ? 40 : 64, CONVERT_REGS = 40;
+    // pairs of 16 whose exponentials are taken on the FMA pipe: the exponentials' own pipe limits bf16 (d = 64 by 15 %), instruction issue 8 bits
+    static constexpr int POLY = EIGHT ? 0 : 2;
+    static_assert(4 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? 2 * CONVERT_REGS : 0) == (EIGHT ? 7 * 72 : 5 * 96), "register split");
 };
 
 // D fp32, A and B bf16; A from shared memory or TMEM, K-major; B K-major, or MN-major (bit 16)
@@ -170,9 +171,9 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
-        for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 8); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t][0], 4); mbar_init(&bars.p_full[t][1], 4); mbar_init(&bars.o_done[t], 1); }
-        for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 4 : 1); mbar_init(&bars.kv_empty[i], 1); }
-        for (int i = 0; i < RAWS; ++i) { mbar_init(&bars.raw_full[i], 33); mbar_init(&bars.raw_empty[i], 4); }
+        for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 8); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t][0], 8); mbar_init(&bars.p_full[t][1], 8); mbar_init(&bars.o_done[t], 1); }
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 8 : 1); mbar_init(&bars.kv_empty[i], 1); }
+        for (int i = 0; i < RAWS; ++i) { mbar_init(&bars.raw_full[i], 33); mbar_init(&bars.raw_empty[i], 8); }
         for (int i = 0; i < PRODUCERS; ++i) mbar_init(&bars.tail[i], 1);
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -199,41 +200,43 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             // ---- codes -> bf16 tiles.  8 (4) lanes share a row of 128 (64) bytes: conflict-free loads; each writes two chunks of 8 values,
             // lanes of the upper half of a row the second one first
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::CONVERT_REGS));
-            constexpr int CH = RB / 16, PER = 32 / CH;                    // chunks of a row, rows of a warp's step
-            const int w4 = warp - 20, chunk = lane % CH;
+            constexpr int CH = RB / 16, PER = 32 / CH, MINE = TK / 8;     // chunks of a row, rows of a warp's step, rows of a warp
+            const int chunk = lane % CH, r0 = (warp - 20) * MINE + lane / CH, flip = CH == 8 ? chunk >> 2 : 0;
+            // rows PER further on: the same place in the swizzle, or (PER = 4) bit 6 flipped
+            const int src0 = chunk_at<RB, TK>(r0, chunk), dst0 = chunk_at<2 * D, TK>(r0, 2 * chunk + flip), dst1 = chunk_at<2 * D, TK>(r0, 2 * chunk + 1 - flip);
             int stage = 0, raw = 0;
             uint32_t phase = 0, raw_phase = 0;
-            for (long long u = u0; u < u1; ++u) {
+            const int units = static_cast<int>(u1 - u0);
+            for (int u = 0; u < units; ++u) {
                 const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;          // rows of the tile that are there
                 for (int is_v = 0; is_v < 2; ++is_v) {
                     wait_bar(&bars.raw_full[raw], raw_phase, gave_up);
                     wait_bar(&bars.kv_empty[stage], phase ^ 1u, gave_up);
-                    const uint8_t *src = raws + raw * S::RAW, *exps = metas + raw * S::RAW_META;
+                    const uint8_t *src = raws + raw * S::RAW, *exps = metas + raw * S::RAW_META + r0;
                     uint8_t *dst = tiles + stage * S::TILE;
-#pragma unroll 2
-                    for (int r = w4 * 32 + lane / CH; r < (w4 + 1) * 32; r += PER) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(src + chunk_at<RB, TK>(r, chunk));
-                        const int e = exps[r];
-                        const int field = KIND == SISO_E4M3 ? min(e + 120, 254) : e;
-                        const uint32_t f16 = e == 255 ? 0x7FC0u : static_cast<uint32_t>(field) << 7;
-                        const uint32_t factor = f16 | (f16 << 16);
-                        const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < MINE / PER; ++i) {
+                        const int x = PER == 4 ? (i & 1) << 6 : 0;
+                        const uint4 w = *reinterpret_cast<const uint4 *>(src + (src0 ^ x) + i * PER * RB);
+                        const int e = exps[i * PER];
+                        const uint32_t f16 = e == 255 ? 0x7FC0u : static_cast<uint32_t>(KIND == SISO_E4M3 ? min(e + 120, 254) : e) << 7;
+                        const uint32_t factor = f16 * 0x10001u;
+                        const uint32_t in[4] = {w.x, w.y, w.z, w.w};
                         uint32_t out[8];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) widen<KIND>(in[i], factor, out[2 * i], out[2 * i + 1]);
+                        for (int k = 0; k < 4; ++k) widen<KIND>(in[k], factor, out[2 * k], out[2 * k + 1]);
                         if (KIND == SISO_E4M3 && e > 134 && e < 255) {              // 2^(e - 7) itself is beyond bf16
                             const uint32_t more = static_cast<uint32_t>(e - 134 + 127) << 7;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) out[i] = mul2_bf16(out[i], more | (more << 16));
+                            for (int k = 0; k < 8; ++k) out[k] = mul2_bf16(out[k], more * 0x10001u);
                         }
-                        if (r >= left) {                                            // anything may stand there
+                        if (left < TK && r0 + i * PER >= left) {                    // anything may stand there
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) out[i] = 0u;
+                            for (int k = 0; k < 8; ++k) out[k] = 0u;
                         }
-                        const int flip = CH == 8 ? chunk >> 2 : 0;
                         const uint4 a = make_uint4(out[0], out[1], out[2], out[3]), b = make_uint4(out[4], out[5], out[6], out[7]);
-                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(r, 2 * chunk + flip)) = flip ? b : a;
-                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(r, 2 * chunk + 1 - flip)) = flip ? a : b;
+                        *reinterpret_cast<uint4 *>(dst + (dst0 ^ x) + i * PER * 128) = flip ? b : a;
+                        *reinterpret_cast<uint4 *>(dst + (dst1 ^ x) + i * PER * 128) = flip ? a : b;
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -241,7 +244,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                     if (++raw == RAWS) { raw = 0; raw_phase ^= 1u; }
                 }
-                if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
+                if (++cur.tile == cur.s.tiles && u + 1 < units) cur.next_item(g);
             }
         }
     } else if (warp >= 16) {
@@ -358,15 +361,17 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     for (int t = 0; t < 2; ++t) {
                         if (t < two) {
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {   // keys 0-63, 64-127: each as soon as its probabilities are there
-                                wait_bar(&bars.p_full[t][h], p_phase[t], gave_up);
+                            for (int c = 0; c < 2; ++c) {   // the first 32 keys of both halves, the others: each as soon as its probabilities are there
+                                wait_bar(&bars.p_full[t][c], p_phase[t], gave_up);
                                 tcgen05_fence_after();
                                 if (elect_one()) {
 #pragma unroll
-                                    for (int k = 4 * h; k < 4 * h + 4; ++k)
-                                        mma_ts(o_col[t], s_col[t] + 64 * h + 8 * (k & 3), b + static_cast<uint64_t>(k * (2048 >> 4)), IDESC<D, true>,
-                                               (j > 0 || k > 0) ? 1u : 0u);
-                                    if (h == 1) {
+                                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                        for (int k = 2 * c; k < 2 * c + 2; ++k)
+                                            mma_ts(o_col[t], s_col[t] + 64 * h + 8 * k, b + static_cast<uint64_t>((4 * h + k) * (2048 >> 4)), IDESC<D, true>,
+                                                   (j > 0 || c > 0 || h > 0 || k > 0) ? 1u : 0u);
+                                    if (c == 1) {
                                         umma_commit(&bars.o_done[t]);
                                         if (t + 1 == two) umma_commit(&bars.kv_empty[v_stage]);
                                     }
@@ -560,19 +565,19 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
                             float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
-                            if ((x * POLY) % 16 < POLY) y = ex2_poly(y);
+                            if ((x * S::POLY) % 16 < S::POLY) y = ex2_poly(y);
                             else { y.x = ex2(y.x); y.y = ex2(y.y); }
                             sum[x & 1] = add2(sum[x & 1], y);
                             p[x] = pack(y.x, y.y, false);
                         }
                         tmem_st_32x16(s_at + c * 16, p);
+                        tmem_st_wait();
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars.p_full[t][c]);
                     };
                     weigh(ra, 0);
                     weigh(rb, 1);
-                    tmem_st_wait();
-                    tcgen05_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bars.p_full[t][half]);
                     sum[0] = add2(sum[0], sum[1]);
                     l += sum[0].x + sum[0].y;
                     tile_phase ^= 1u;
