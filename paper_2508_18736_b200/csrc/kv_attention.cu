@@ -550,8 +550,8 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 }
 
 // ---- joining the parts ------------------------------------------------------------------------------------------------
-// CTA (x, y): the item that is recorded at CTA x, MR / 8 of its rows.  The parts lie at place 1 of CTA x and place 0 of the next
-// ones.  256 / (MR / 8) threads share a row: 32 lanes over d, the warps over the parts; sums are taken in the same order every time.
+// CTA (x, y): the item that is recorded at CTA x, ROWS of its rows.  The parts lie at place 1 of CTA x and place 0 of the next
+// ones.  8 / ROWS warps share a row: 32 lanes over d, the warps over the parts; sums are taken in the same order every time.
 template <int MR, int D>
 __global__ void __launch_bounds__(256)
 join_kernel(const __grid_constant__ Args g) {
@@ -564,7 +564,8 @@ join_kernel(const __grid_constant__ Args g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int q0;
     const int n_q = seq_queries(g, rec.b, q0);
-    for (int base = blockIdx.y * (MR / 8); base < (blockIdx.y + 1) * (MR / 8); base += ROWS) {
+    {
+        const int base = blockIdx.y * ROWS;
         const int in_tile = base + warp / WPR, part0 = warp % WPR;
         const int row = rec.row_tile * MR + in_tile;
         const bool real = row < n_q * g.group;
@@ -604,7 +605,7 @@ join_kernel(const __grid_constant__ Args g) {
             for (int x = 0; x < N; ++x) so[warp][x * 32 + lane] = o[x];
             if (lane == 0) { sml[warp][0] = m; sml[warp][1] = l; }
             __syncthreads();
-            if (part0 != 0) continue;
+            if (part0 != 0) return;
 #pragma unroll
             for (int w = 1; w < WPR; ++w) {
                 const float m1 = sml[warp + w][0], l1 = sml[warp + w][1];
@@ -616,7 +617,7 @@ join_kernel(const __grid_constant__ Args g) {
                 for (int x = 0; x < N; ++x) o[x] = o[x] * a + so[warp + w][x * 32 + lane] * b;
             }
         }
-        if (!real) continue;
+        if (!real) return;
         const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
@@ -629,7 +630,7 @@ join_kernel(const __grid_constant__ Args g) {
 
 template <int MR, int D> static siso_status_t run_join(const Args &g, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(g.grid), 8);
+    cfg.gridDim = dim3(static_cast<unsigned>(g.grid), MR >= 64 ? MR / 8 : 8);
     cfg.blockDim = dim3(256);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];

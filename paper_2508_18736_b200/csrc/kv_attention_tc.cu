@@ -10,7 +10,8 @@
 //                    probabilities bear); then by these warps.
 //   warp 16          issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
 //                    an MN-major operand)
-//   warps 17-19      fill the ring of K and V tiles by TMA, one box per run of tokens in one page
+//   warps 17, 18     fill the ring of K and V tiles by TMA, one box per run of tokens in one page
+//   warp 19          zeroes what lies beyond the end in the last values of an item (bf16 caches; the widening does it for the others)
 //   warps 20-27      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
 // TMEM: S_0, S_1 (128 columns each), O_0, O_1.
 #include "kv_attention.cuh"
@@ -22,11 +23,11 @@ namespace tc {
 using namespace umma2;
 
 constexpr int TK = 128;
-constexpr int PRODUCERS = 3;
+constexpr int PRODUCERS = 2;
 
 struct Bars {
     uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
-    uint64_t kv_full[6], kv_empty[6], raw_full[4], raw_empty[4], tail[PRODUCERS];
+    uint64_t kv_full[6], kv_empty[6], landed[6], raw_full[4], raw_empty[4];
     uint32_t blocks[8];        // of unit i at i % 8: which runs of 8 keys have a page in the pool
     long long total;           // units of the call, and the CTAs that share them
     int ctas;
@@ -143,6 +144,20 @@ __device__ __forceinline__ uint32_t sub2_bf16(uint32_t a, uint32_t b) {
     return d;
 }
 
+// Lane i of every four has pieces 0 to 3 of row i: afterwards it has piece i of rows 0 to 3
+__device__ __forceinline__ void swap_piece(uint4 &keep, uint4 &give, int mask, bool upper) {      // lanes with `upper` give `keep`'s place away
+    const uint4 x = upper ? keep : give;
+    const uint4 y = make_uint4(__shfl_xor_sync(0xFFFFFFFFu, x.x, mask), __shfl_xor_sync(0xFFFFFFFFu, x.y, mask), __shfl_xor_sync(0xFFFFFFFFu, x.z, mask),
+                               __shfl_xor_sync(0xFFFFFFFFu, x.w, mask));
+    if (upper) keep = y; else give = y;
+}
+__device__ __forceinline__ void turn4(uint4 (&w)[4], int lane) {
+    swap_piece(w[0], w[1], 1, lane & 1);
+    swap_piece(w[2], w[3], 1, lane & 1);
+    swap_piece(w[0], w[2], 2, lane & 2);
+    swap_piece(w[1], w[3], 2, lane & 2);
+}
+
 // 4 codes as bf16 values: (0, 2) and (1, 3).  e4m3: sign, exponent and mantissa moved to their places give the value times 2^-120, subnormal
 // codes too; `factor` makes up for it.  i8: the low 7 bits as the mantissa of 128 + u less 128 or, for negative codes, 256.
 template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t factor, uint32_t &lo, uint32_t &hi) {
@@ -172,9 +187,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
         for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 8); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t][0], 8); mbar_init(&bars.p_full[t][1], 8); mbar_init(&bars.o_done[t], 1); }
-        for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 8 : 1); mbar_init(&bars.kv_empty[i], 1); }
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&bars.kv_full[i], EIGHT ? 8 : 1); mbar_init(&bars.kv_empty[i], 1); mbar_init(&bars.landed[i], 1); }
         for (int i = 0; i < RAWS; ++i) { mbar_init(&bars.raw_full[i], 33); mbar_init(&bars.raw_empty[i], 8); }
-        for (int i = 0; i < PRODUCERS; ++i) mbar_init(&bars.tail[i], 1);
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -249,12 +263,35 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         }
     } else if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
-        if (warp > 16) {
+        if (warp == 19) {
+            if constexpr (!EIGHT) {
+                // ---- what lies beyond the end in the last values of an item may be anything: zeros, or 0 times NaN would reach the sums
+                int stage = 0;
+                uint32_t phases = 0;                          // bit i: the round that stage i's barrier is in
+                const int units = static_cast<int>(u1 - u0);
+                for (int u = 0; u < units; ++u) {
+                    if (++stage == STAGES) stage = 0;
+                    const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;
+                    if (left < TK) {
+                        wait_bar(&bars.landed[stage], (phases >> stage) & 1u, gave_up);
+                        phases ^= 1u << stage;
+                        uint8_t *dst = tiles + stage * S::TILE;
+                        for (int x = max(left, 0) * (RB / 16) + lane; x < TK * (RB / 16); x += 32)
+                            *reinterpret_cast<uint4 *>(dst + chunk_at<RB, TK>(x / (RB / 16), x % (RB / 16))) = make_uint4(0u, 0u, 0u, 0u);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars.kv_full[stage]);
+                    }
+                    if (++stage == STAGES) stage = 0;
+                    if (++cur.tile == cur.s.tiles && u + 1 < units) cur.next_item(g);
+                }
+            }
+        } else if (warp > 16) {
             // ---- producers: K and V tiles alternate in the ring; lanes 0-15 own the tile's runs of 8 tokens
             constexpr int RING = EIGHT ? RAWS : STAGES;
             const int box_blocks = g.box / 8;
             int stage = 0;
-            uint32_t phase = 0, tail_phase = 0;
+            uint32_t phase = 0;
             for (long long u = u0; u < u1; ++u) {
                 const int j0 = (cur.s.tile0 + cur.tile) * TK, j = j0 + (lane & 15) * 8;
                 for (int is_v = 0; is_v < 2; ++is_v) {
@@ -271,9 +308,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         uint64_t *full = EIGHT ? &bars.raw_full[stage] : &bars.kv_full[stage];
                         wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up);
                         uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
-                        // the last values of a bf16 cache: what lies beyond the end may be anything and is zeroed before it is used
-                        const bool tail = !EIGHT && is_v && j0 + TK > cur.s.hi;
-                        uint64_t *bar = tail ? &bars.tail[warp - 17] : full;
+                        // the last values of an item in a bf16 cache go through warp 19
+                        uint64_t *bar = !EIGHT && is_v && j0 + TK > cur.s.hi ? &bars.landed[stage] : full;
                         if (*gave_up == 0) {
                             if (lane == 0) {
                                 if (!is_v) bars.blocks[static_cast<int>(u - u0) & 7] = there;
@@ -293,17 +329,6 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(metas + stage * S::RAW_META + lane * 8)),
                                                  "l"((is_v ? g.kv.v_exp : g.kv.k_exp) + e), "r"(page < 0 ? 0 : 8) : "memory");
                                 asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-                            }
-                            if (tail) {
-                                wait_bar(&bars.tail[warp - 17], tail_phase, gave_up);
-                                tail_phase ^= 1u;
-                                for (int x = lane; x < TK * (RB / 16); x += 32) {
-                                    const int row = x / (RB / 16);
-                                    if (j0 + row >= cur.s.hi) *reinterpret_cast<uint4 *>(dst + chunk_at<RB, TK>(row, x % (RB / 16))) = make_uint4(0u, 0u, 0u, 0u);
-                                }
-                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(full);
                             }
                         }
                     }
@@ -427,20 +452,34 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) { const uint32_t x = r[i + 1]; r[i + 1] = r[i + 2]; r[i + 2] = x; }
                 }
-                if (out_token >= 0 && out_place < 0) {
-                    __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(out_token) * g.a.out_stride_token + out_head * g.a.out_stride_head +
-                                         half * (D / 2) + c * 32;
+                // four lanes turn their four pieces of 16 bytes round, so that they write 64 bytes of a row together
+                if (out_place < 0) {
+                    uint4 w[4];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t w[4];
+                    for (int i = 0; i < 4; ++i)
+                        w[i] = make_uint4(pack(__uint_as_float(r[8 * i]) * inv, __uint_as_float(r[8 * i + 1]) * inv, false),
+                                          pack(__uint_as_float(r[8 * i + 2]) * inv, __uint_as_float(r[8 * i + 3]) * inv, false),
+                                          pack(__uint_as_float(r[8 * i + 4]) * inv, __uint_as_float(r[8 * i + 5]) * inv, false),
+                                          pack(__uint_as_float(r[8 * i + 6]) * inv, __uint_as_float(r[8 * i + 7]) * inv, false));
+                    turn4(w, lane);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) w[k] = pack(__uint_as_float(r[i + 2 * k]) * inv, __uint_as_float(r[i + 2 * k + 1]) * inv, false);
-                        *reinterpret_cast<uint4 *>(dst + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int i = 0; i < 4; ++i) {
+                        const int token = __shfl_sync(0xFFFFFFFFu, out_token, (lane & ~3) + i), head = __shfl_sync(0xFFFFFFFFu, out_head, (lane & ~3) + i);
+                        if (token >= 0)
+                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(token) * g.a.out_stride_token +
+                                                       static_cast<long long>(head) * g.a.out_stride_head + half * (D / 2) + c * 32 + (lane & 3) * 8) = w[i];
                     }
-                } else if (out_token >= 0) {
-                    float *part = g.part_o + static_cast<long long>(out_place) * D + half * (D / 2) + c * 32;
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(part + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+                    for (int p = 0; p < 2; ++p) {
+                        uint4 w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = make_uint4(r[16 * p + 4 * i], r[16 * p + 4 * i + 1], r[16 * p + 4 * i + 2], r[16 * p + 4 * i + 3]);
+                        turn4(w, lane);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)                       // places of neighbouring rows are neighbours; unused rows are never read
+                            *reinterpret_cast<uint4 *>(g.part_o + static_cast<long long>(out_place - (lane & 3) + i) * D + half * (D / 2) + c * 32 + p * 16 + (lane & 3) * 4) = w[i];
+                    }
                 }
             }
             if (out_token >= 0 && half == 0) {
@@ -458,16 +497,25 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 const bool real = in_tile < rows;
                 const int row = cur.rt * TC_ROWS + (real ? in_tile : 0);
                 const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = cur.head * g.group + row - i * g.group;
-                {   // the last scores of the item before have come, so its queries are no longer read
+                {   // the last scores of the item before have come, so its queries are no longer read.  8 (4) lanes share half a row
                     const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
-                    const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + i) * g.a.q_stride_token + head * g.a.q_stride_head;
+                    constexpr int LANES = D / 16, PER = 32 / LANES;
                     uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
-                    uint4 x[D / 16];
+                    const int c = half * LANES + lane % LANES, first = (warp & 3) * 32 + lane / LANES;
+                    uint4 x[32 / PER];
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) x[c] = real ? *reinterpret_cast<const uint4 *>(src + (half * (D / 16) + c) * 8) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int y = 0; y < 32 / PER; ++y) {
+                        const int at = t * 128 + first + y * PER, r = cur.rt * TC_ROWS + at;
+                        x[y] = make_uint4(0u, 0u, 0u, 0u);
+                        if (at < rows) {
+                            const int tok = static_cast<int>(g.by_group.div(static_cast<uint32_t>(r)));
+                            x[y] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + tok) * g.a.q_stride_token +
+                                                                    static_cast<long long>(cur.head * g.group + r - tok * g.group) * g.a.q_stride_head + c * 8);
+                        }
+                    }
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t w[4] = {(x[c].x ^ flip) & keep, (x[c].y ^ flip) & keep, (x[c].z ^ flip) & keep, (x[c].w ^ flip) & keep};
+                    for (int y = 0; y < 32 / PER; ++y) {
+                        uint32_t w[4] = {(x[y].x ^ flip) & keep, (x[y].y ^ flip) & keep, (x[y].z ^ flip) & keep, (x[y].w ^ flip) & keep};
                         if constexpr (EIGHT) {                            // the order in which the codes come
 #pragma unroll
                             for (int k = 0; k < 4; k += 2) {
@@ -476,7 +524,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                 w[k + 1] = __byte_perm(a, b, 0x7632);
                             }
                         }
-                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(in_tile & 127, half * (D / 16) + c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(first + y * PER, c)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
