@@ -126,10 +126,9 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    long long u0, u1, total;
-    int ctas;
-    Cursor<MR, TK> cur;
-    if (!locate<MR, TK, S::THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
+    Run run;
+    Cursor<MR, TK, 0> cur;
+    if (!locate<MR, TK, 0, S::THREADS>(g, run, cur, buf)) return;
     volatile int *gave_up = &ring.gave_up;
 
     // registers move from the producers to the consumers: WARPS of CONSUMER_REGS and 4 of PRODUCER_REGS make what the CTA has
@@ -143,7 +142,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         const int box_blocks = g.box / 8;
         int stage = 0;
         uint32_t phase = 0;
-        for (long long u = u0; u < u1; ++u) {
+        do {
             if (stage % PRODUCERS == warp - WARPS) {         // a stage is always filled by the same warp, so its rounds come in order
                 int page[HALVES], tok[HALVES];
                 bool first[HALVES];
@@ -193,8 +192,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                 if constexpr (EIGHT) asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
             }
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-            if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
-        }
+        } while (cur.step(g));
         if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
         if (*gave_up) {
             for (int i = 0; i < 64; ++i) __nanosleep(1000);      // copies in flight land before the shared memory is handed back
@@ -271,10 +269,10 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     };
     fetch_q();
     begin_item();
-    long long began = u0;                                    // unit at which the current part of the item began
+    int t_begin = cur.tile;                                  // tile at which the current part of the item began
     int stage = 0;
     uint32_t phase = 0;
-    for (long long u = u0; u < u1; ++u) {
+    for (bool more = true; more;) {
         wait_bar(&ring.full[stage], phase, gave_up);
         uint8_t *tile = smem + stage * S::STAGE;
         const int k_first = stage * S::STAGE + chunk_at<RB, TK>(key_of<RB>(r0), c);
@@ -441,18 +439,18 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&ring.empty[stage]);
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if (++cur.tile < cur.s.tiles && u + 1 < u1) continue;
+        if (cur.tiles_here() > 1) {
+            cur.step(g);
+            continue;
+        }
 
         // ---- end of the item, or of this CTA's part of it.  The next one's queries are on their way meanwhile
-        const int t_end = cur.tile;                           // tiles [t_begin, t_end) of the item were done here
-        const int t_begin = t_end - static_cast<int>(u + 1 - began);
-        const bool whole = t_begin == 0 && t_end == cur.s.tiles;
+        const int t_end = cur.tile + 1;                       // tiles [t_begin, t_end) of the item were done here
         const int done_b = cur.b, done_head = cur.head, done_rt = cur.rt, done_q0 = cur.q0, done_rows = cur.n_q * g.group, done_tiles = cur.s.tiles;
-        began = u + 1;
-        if (u + 1 < u1) {
-            cur.next_item(g);
-            fetch_q();
-        }
+        const bool whole = t_begin == 0 && t_end == done_tiles, began_before = t_begin > 0;
+        more = cur.step(g);
+        t_begin = 0;
+        if (more) fetch_q();
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -530,7 +528,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                         if (g.a.d_lse && r0 == 0)
                             g.a.d_lse[static_cast<long long>(done_q0 + i) * g.a.n_heads + head] = l[t][h] > 0.f ? (m[t][h] + log2f(l[t][h])) * 0.6931471805599453f : -INFINITY;
                     } else {
-                        const long long place = part_place(blockIdx.x, t_begin > 0) * MR + in_tile;
+                        const long long place = part_place(blockIdx.x, began_before) * MR + in_tile;
                         float *dst = g.part_o + place * D;
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
@@ -541,11 +539,8 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     }
                 }
         }
-        if (!whole && t_begin == 0 && threadIdx.x == 0) {
-            const long long end = u + 1 + (done_tiles - t_end);
-            g.records[blockIdx.x] = Record{1, done_b, done_head, done_rt, cta_of(end - 1, total, ctas) - static_cast<int>(blockIdx.x) + 1};
-        }
-        if (u + 1 < u1) begin_item();
+        if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of(run, done_b, done_head, done_rt, done_tiles, t_end);
+        if (more) begin_item();
     }
 }
 

@@ -5,7 +5,7 @@
 // kv_head * group + r % group.  An item is (sequence, key/value head, tile of MR rows); its keys are taken in tiles of TK, and
 // one tile of one item is a unit.  The units of a call, in the order (sequence, head, row tile, key tile), are dealt to the
 // CTAs in equal contiguous runs, so CTAs are equally loaded whatever the lengths are, and one long sequence spreads over
-// all of them.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
+// all of them.  An item counts a few units more for its beginning and end.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
 // (unnormalised output, maximum, sum), and a second small kernel joins the parts of an item in a fixed order.
 #pragma once
 
@@ -73,36 +73,38 @@ template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g,
     s.tiles = max(1, (s.hi + TK - 1) / TK - s.tile0);       // a row tile that sees nothing is one unit that writes zeros
     return s;
 }
-// units of one key/value head of sequence b
-template <int MR, int TK> __device__ __forceinline__ int seq_units(const Args &g, int b) {
+// units of one key/value head of sequence b; an item counts EXTRA more than its key tiles, for its beginning and end
+template <int MR, int TK, int EXTRA> __device__ __forceinline__ int seq_units(const Args &g, int b) {
     int q0;
     const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
     int units = 0;
-    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR, TK>(g, len, n_q, rt).tiles;
+    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
     return units;
 }
 
-// The item that a unit belongs to, and the unit's place in it.
-template <int MR, int TK> struct Cursor {
+// A place in this CTA's run of units: an item and a key tile of it.
+template <int MR, int TK, int EXTRA> struct Cursor {
     int b, head, rt, q0, n_q, len, tile;
+    int left;                                                  // units of the run that are left, this tile's included
     Span s;
     __device__ __forceinline__ void load_seq(const Args &g) {
         n_q = seq_queries(g, b, q0);
         len = seq_len(g, b);
     }
     __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR, TK>(g, len, n_q, rt); }
-    // `within`: units of sequence b before this one
+    // `within`: units of sequence `seq` before this one
     __device__ __forceinline__ void seek(const Args &g, int seq, long long within, int per_head) {
         b = seq;
         load_seq(g);
         head = static_cast<int>(within / per_head);
-        int left = static_cast<int>(within - static_cast<long long>(head) * per_head);
+        int x = static_cast<int>(within - static_cast<long long>(head) * per_head);
         for (rt = 0;; ++rt) {
             load_span(g);
-            if (left < s.tiles) break;
-            left -= s.tiles;
+            if (x < s.tiles + EXTRA) break;
+            x -= s.tiles + EXTRA;
         }
-        tile = left;
+        tile = max(x - EXTRA, 0);                              // the extra units come first
+        left -= max(EXTRA - x, 0);
     }
     __device__ __forceinline__ void next_item(const Args &g) {
         tile = 0;
@@ -116,85 +118,101 @@ template <int MR, int TK> struct Cursor {
         }
         load_span(g);
     }
+    // key tiles of this item that belong to the run
+    __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, left); }
+    // n <= tiles_here() tiles further; false: the run is over
+    __device__ __forceinline__ bool step(const Args &g, int n = 1) {
+        tile += n;
+        left -= n;
+        if (left > 0 && tile == s.tiles) {
+            left -= EXTRA;
+            if (left > 0) next_item(g);
+        }
+        return left > 0;
+    }
 };
 
-// This CTA's run [u0, u1) of the call's units and the cursor at its start; every thread of the CTA gets the same.  False: none.
-// The CTA's record is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
-template <int MR, int TK, int THREADS>
-__device__ __forceinline__ bool locate(const Args &g, long long &u0, long long &u1, long long &total, int &ctas, Cursor<MR, TK> &cur,
-                                       unsigned long long *buf) {
-    constexpr int WARPS = THREADS / 32;
+// inclusive sum over the CTA's threads; `all`: the total.  Two barriers
+template <int THREADS>
+__device__ __forceinline__ unsigned long long cta_scan(unsigned long long x, unsigned long long &all, unsigned long long *buf) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) buf[warp] = x;
+    __syncthreads();
+    unsigned long long before = 0ull;
+    all = 0ull;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) before += buf[w];
+        all += buf[w];
+    }
+    return before + x;
+}
+
+// The run of this CTA among the call's units: it ends before unit `end` of `total`, which `ctas` CTAs share.
+struct Run {
+    long long end, total;
+    int ctas;
+};
+// This CTA's run and the cursor at its start; every thread of the CTA gets the same.  False: nothing to do.  The CTA's record
+// is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
+template <int MR, int TK, int EXTRA, int THREADS>
+__device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA> &cur, unsigned long long *buf) {
+    constexpr int WARPS = THREADS / 32;
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) g.records[cta].valid = 0;
-    unsigned long long first = 0ull, upto = 0ull;             // units of the first chunk of sequences: mine, and up to mine
+    unsigned long long mine = 0ull, upto = 0ull, all;          // units of this thread's sequence of the first chunk, and up to them
     int per_head = 0;
-    total = 0;
+    run.total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
         const int b = c0 + static_cast<int>(threadIdx.x);
-        const int ph = b < g.a.n_seqs ? seq_units<MR, TK>(g, b) : 0;
-        const unsigned long long mine = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads;
-        unsigned long long x = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-            if (lane >= o) x += y;
-        }
-        __syncthreads();
-        if (lane == 31) buf[warp] = x;
-        __syncthreads();
-        unsigned long long before = 0ull, all = 0ull;
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) before += buf[w];
-            all += buf[w];
-        }
-        if (c0 == 0) { first = mine; upto = before + x; per_head = ph; }
-        total += static_cast<long long>(all);
+        const int ph = b < g.a.n_seqs ? seq_units<MR, TK, EXTRA>(g, b) : 0;
+        const unsigned long long x = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads, s = cta_scan<THREADS>(x, all, buf);
+        if (c0 == 0) { mine = x; upto = s; per_head = ph; }
+        run.total += static_cast<long long>(all);
     }
-    ctas = static_cast<int>(min(static_cast<long long>(g.grid), total));
-    if (cta >= ctas) return false;
-    u0 = total * cta / ctas;
-    u1 = total * (cta + 1) / ctas;
-    // the sequence that unit u0 belongs to
-    long long base = 0;
+    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), run.total));
+    if (cta >= run.ctas) return false;
+    const unsigned long long want = static_cast<unsigned long long>(run.total * cta / run.ctas);
+    run.end = run.total * (cta + 1) / run.ctas;
+    cur.left = static_cast<int>(run.end - static_cast<long long>(want));
+    // the sequence that the first unit belongs to
+    unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
             const int b = c0 + static_cast<int>(threadIdx.x);
-            per_head = b < g.a.n_seqs ? seq_units<MR, TK>(g, b) : 0;
-            first = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
-            unsigned long long x = first;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-                if (lane >= o) x += y;
-            }
-            __syncthreads();
-            if (lane == 31) buf[warp] = x;
-            __syncthreads();
-            upto = static_cast<unsigned long long>(base) + x;
-            for (int w = 0; w < warp; ++w) upto += buf[w];
+            per_head = b < g.a.n_seqs ? seq_units<MR, TK, EXTRA>(g, b) : 0;
+            mine = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
+            upto = base + cta_scan<THREADS>(mine, all, buf);
         }
         __syncthreads();
         if (threadIdx.x == 0) buf[WARPS] = ~0ull;
         __syncthreads();
-        const unsigned long long want = static_cast<unsigned long long>(u0);
-        if (want < upto && want >= upto - first) {             // exactly one thread of one chunk
+        if (want < upto && want >= upto - mine) {              // exactly one thread of one chunk
             buf[WARPS] = (static_cast<unsigned long long>(c0 + threadIdx.x) << 32) | static_cast<uint32_t>(per_head);
-            buf[WARPS + 1] = upto - first;
+            buf[WARPS + 1] = upto - mine;
         }
         if (threadIdx.x == THREADS - 1) buf[0] = upto;
         __syncthreads();
         const unsigned long long found = buf[WARPS];
-        base = static_cast<long long>(buf[0]);
+        base = buf[0];
         if (found != ~0ull) {
-            cur.seek(g, static_cast<int>(found >> 32), u0 - static_cast<long long>(buf[WARPS + 1]), static_cast<int>(found & 0xFFFFFFFFull));
-            return true;
+            cur.seek(g, static_cast<int>(found >> 32), static_cast<long long>(want - buf[WARPS + 1]), static_cast<int>(found & 0xFFFFFFFFull));
+            return cur.left > 0;
         }
     }
 }
 // the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
     return static_cast<int>(((u + 1) * ctas - 1) / total);
+}
+// what is noted of an item whose first part ends this CTA's run at key tile `tile_end`
+__device__ __forceinline__ Record record_of(const Run &run, int b, int head, int row_tile, int tiles, int tile_end) {
+    return Record{1, b, head, row_tile, cta_of(run.end + (tiles - tile_end) - 1, run.total, run.ctas) - static_cast<int>(blockIdx.x) + 1};
 }
 // Where a part goes: a CTA's run has at most one item that began before it (place 0) and one that goes on after it (place 1).
 __device__ __forceinline__ long long part_place(int cta, bool began_before) { return 2ll * cta + (began_before ? 0 : 1); }

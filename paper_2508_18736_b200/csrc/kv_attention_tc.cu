@@ -24,13 +24,13 @@ using namespace umma2;
 
 constexpr int TK = 128;
 constexpr int PRODUCERS = 2;
+constexpr int EXTRA = 2;               // units that an item's beginning and end cost: 4.6 us were measured, a unit takes 1.6 to 2
 
 struct Bars {
     uint64_t q_full[2], s_full[2], p_full[2][2], o_done[2];
     uint64_t kv_full[6], kv_empty[6], landed[6], raw_full[4], raw_empty[4];
     uint32_t blocks[8];        // of unit i at i % 8: which runs of 8 keys have a page in the pool
-    long long total;           // units of the call, and the CTAs that share them
-    int ctas;
+    Run run;
     uint32_t tmem;
     int gave_up;
     unsigned long long buf[30];
@@ -194,11 +194,12 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    long long u0, u1, total;
-    int ctas;
-    Cursor<TC_ROWS, TK> cur;
-    if (!locate<TC_ROWS, TK, S::THREADS>(g, u0, u1, total, ctas, cur, buf)) return;
-    if (threadIdx.x == 0) { bars.total = total; bars.ctas = ctas; }
+    Cursor<TC_ROWS, TK, EXTRA> cur;
+    {
+        Run run;
+        if (!locate<TC_ROWS, TK, EXTRA, S::THREADS>(g, run, cur, buf)) return;
+        if (threadIdx.x == 0) bars.run = run;
+    }
     if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -220,8 +221,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             const int src0 = chunk_at<RB, TK>(r0, chunk), dst0 = chunk_at<2 * D, TK>(r0, 2 * chunk + flip), dst1 = chunk_at<2 * D, TK>(r0, 2 * chunk + 1 - flip);
             int stage = 0, raw = 0;
             uint32_t phase = 0, raw_phase = 0;
-            const int units = static_cast<int>(u1 - u0);
-            for (int u = 0; u < units; ++u) {
+            do {
                 const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;          // rows of the tile that are there
                 for (int is_v = 0; is_v < 2; ++is_v) {
                     wait_bar(&bars.raw_full[raw], raw_phase, gave_up);
@@ -258,8 +258,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                     if (++raw == RAWS) { raw = 0; raw_phase ^= 1u; }
                 }
-                if (++cur.tile == cur.s.tiles && u + 1 < units) cur.next_item(g);
-            }
+            } while (cur.step(g));
         }
     } else if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
@@ -268,8 +267,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 // ---- what lies beyond the end in the last values of an item may be anything: zeros, or 0 times NaN would reach the sums
                 int stage = 0;
                 uint32_t phases = 0;                          // bit i: the round that stage i's barrier is in
-                const int units = static_cast<int>(u1 - u0);
-                for (int u = 0; u < units; ++u) {
+                do {
                     if (++stage == STAGES) stage = 0;
                     const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;
                     if (left < TK) {
@@ -283,16 +281,15 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         if (lane == 0) mbar_arrive(&bars.kv_full[stage]);
                     }
                     if (++stage == STAGES) stage = 0;
-                    if (++cur.tile == cur.s.tiles && u + 1 < units) cur.next_item(g);
-                }
+                } while (cur.step(g));
             }
         } else if (warp > 16) {
             // ---- producers: K and V tiles alternate in the ring; lanes 0-15 own the tile's runs of 8 tokens
             constexpr int RING = EIGHT ? RAWS : STAGES;
             const int box_blocks = g.box / 8;
-            int stage = 0;
+            int stage = 0, unit = 0;
             uint32_t phase = 0;
-            for (long long u = u0; u < u1; ++u) {
+            do {
                 const int j0 = (cur.s.tile0 + cur.tile) * TK, j = j0 + (lane & 15) * 8;
                 for (int is_v = 0; is_v < 2; ++is_v) {
                     if (stage % PRODUCERS == warp - 17) {          // a stage is always filled by the same warp, so its rounds come in order
@@ -312,7 +309,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         uint64_t *bar = !EIGHT && is_v && j0 + TK > cur.s.hi ? &bars.landed[stage] : full;
                         if (*gave_up == 0) {
                             if (lane == 0) {
-                                if (!is_v) bars.blocks[static_cast<int>(u - u0) & 7] = there;
+                                if (!is_v) bars.blocks[unit & 7] = there;
                                 mbar_arrive_expect_tx(bar, boxes * (g.box * RB));
                             }
                             __syncwarp();
@@ -334,8 +331,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     }
                     if (++stage == RING) { stage = 0; phase ^= 1u; }
                 }
-                if (++cur.tile == cur.s.tiles && u + 1 < u1) cur.next_item(g);
-            }
+                ++unit;
+            } while (cur.step(g));
             if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
         } else {
             // ---- products.  The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one
@@ -358,9 +355,9 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 }
                 __syncwarp();
             };
-            const int units = static_cast<int>(u1 - u0);
-            for (int u = 0; u < units;) {
-                const int n = min(cur.s.tiles - cur.tile, units - u);
+            int n;
+            do {
+                n = cur.tiles_here();
                 const int two = cur.n_q * g.group - cur.rt * TC_ROWS > 128 ? 2 : 1;
                 wait_bar(&bars.kv_full[stage], phase, gave_up);
 #pragma unroll
@@ -413,10 +410,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         step();
                     }
                 }
-                u += n;
-                cur.tile += n - 1;
-                if (u < units) cur.next_item(g);
-            }
+            } while (cur.step(g, n));
         }
     } else {
         // ---- softmax: half of a row of one tile
@@ -430,7 +424,6 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         float &mine_out = bars.peer[t][half][threadIdx.x & 127], &theirs_in = bars.peer[t][half ^ 1][threadIdx.x & 127];
         uint32_t tile_phase = 0;
         int unit = 0;                                                     // units of this CTA so far
-        const int units = static_cast<int>(u1 - u0);
         bool pending = false;                                             // an item whose output is still in TMEM
         float m = -INFINITY, l = 0.f;
         int out_token = -1, out_head = 0, out_place = -1;                 // of that item: where the row goes, or its place among the parts
@@ -489,8 +482,9 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             tcgen05_fence_before();
             together();                                                   // the exchange place is free again
         };
-        while (unit < units) {
-            const int n = min(cur.s.tiles - cur.tile, units - unit);
+        int n;
+        do {
+            n = cur.tiles_here();
             const int rows = cur.n_q * g.group - cur.rt * TC_ROWS;        // rows of the item from this row tile on
             const bool mine = t == 0 || rows > 128;
             if (mine) {
@@ -631,14 +625,9 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     tile_phase ^= 1u;
                 }
             }
-            if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) {
-                const long long end = u0 + unit + cur.s.tiles;
-                g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.rt, cta_of(end - 1, bars.total, bars.ctas) - static_cast<int>(blockIdx.x) + 1};
-            }
+            if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) g.records[blockIdx.x] = record_of(bars.run, cur.b, cur.head, cur.rt, cur.s.tiles, n);
             unit += n;
-            cur.tile += n - 1;
-            if (unit < units) cur.next_item(g);
-        }
+        } while (cur.step(g, n));
         if (pending) store_item();
     }
 
