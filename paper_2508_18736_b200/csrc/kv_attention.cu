@@ -642,7 +642,6 @@ siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
         case 8: return dim == 128 ? run_join<8, 128>(g, s) : run_join<8, 64>(g, s);
         case 16: return dim == 128 ? run_join<16, 128>(g, s) : run_join<16, 64>(g, s);
         case 32: return dim == 128 ? run_join<32, 128>(g, s) : run_join<32, 64>(g, s);
-        case 64: return dim == 128 ? run_join<64, 128>(g, s) : run_join<64, 64>(g, s);
         default: return dim == 128 ? run_join<TC_ROWS, 128>(g, s) : run_join<TC_ROWS, 64>(g, s);
     }
 }
@@ -673,8 +672,7 @@ template <int KIND, int D, int WM, int NT> static siso_status_t run_few(Kv *h, A
     return launch_join(g, S::MR, D, s);
 }
 template <int KIND, int D> static siso_status_t run_few_rows(Kv *h, Args &g, int mr, cudaStream_t s) {
-    return mr == 8 ? run_few<KIND, D, 1, 1>(h, g, s) : mr == 16 ? run_few<KIND, D, 1, 2>(h, g, s) : mr == 32 ? run_few<KIND, D, 2, 2>(h, g, s)
-                                                                                                : run_few<KIND, D, 4, 2>(h, g, s);
+    return mr == 8 ? run_few<KIND, D, 1, 1>(h, g, s) : mr == 16 ? run_few<KIND, D, 1, 2>(h, g, s) : run_few<KIND, D, 2, 2>(h, g, s);
 }
 template <int KIND> static siso_status_t run_few_dim(Kv *h, Args &g, int dim, int mr, cudaStream_t s) {
     return dim == 128 ? run_few_rows<KIND, 128>(h, g, mr, s) : run_few_rows<KIND, 64>(h, g, mr, s);
@@ -696,7 +694,7 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t
     g.grid = h->sm_count;
     const int dim = h->cfg.head_dim;
     const long long rows = static_cast<long long>(a->max_q) * g.group;      // rows per key/value head of the longest chunk
-    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : TC_ROWS;
+    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : TC_ROWS;
     const size_t records = pad256(sizeof(Record) * g.grid), ml = pad256(sizeof(float) * 2 * g.grid * mr * 2);
     // sized for the widest kernel, so that a handle that has served one call serves every other without a new block
     const size_t most = records + pad256(sizeof(float) * 2 * g.grid * TC_ROWS * 2) + sizeof(float) * 2 * g.grid * TC_ROWS * static_cast<size_t>(dim);

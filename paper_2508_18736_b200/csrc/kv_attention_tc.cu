@@ -7,7 +7,8 @@
 //   warps 0-7, 8-15  softmax of row tile 0, 1: a row (= TMEM lane) belongs to two threads, each with 64 of its 128 scores.  Scores from
 //                    TMEM, running maximum, exponentials, probabilities as bf16 back into TMEM over the scores.  The output in
 //                    TMEM is rescaled only where a maximum has grown by more than 8 (a factor 2^8, which fp32 sums and bf16
-//                    probabilities bear); then by these warps.
+//                    probabilities bear); then by these warps.  Up to 128 rows both tiles hold the same rows, each with every
+//                    other tile of keys, and are joined at the end: the alternation stays.
 //   warp 16          issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
 //                    an MN-major operand)
 //   warps 17, 18     fill the ring of K and V tiles by TMA, one box per run of tokens in one page
@@ -80,6 +81,16 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "setp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d), "r"(a), "l"(b), "r"(id), "r"(accumulate) : "memory");
+}
+// 16 columns, complete on return
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
@@ -289,24 +300,34 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             const int box_blocks = g.box / 8;
             int stage = 0, unit = 0;
             uint32_t phase = 0;
-            do {
-                const int j0 = (cur.s.tile0 + cur.tile) * TK, j = j0 + (lane & 15) * 8;
+            // this lane's run of 8 tokens of a unit; the page index is asked for one unit before it is needed
+            struct Place { int j0, hi, head, tok, page; } at;
+            auto look_up = [&](Place &p) {
+                p.j0 = (cur.s.tile0 + cur.tile) * TK;
+                p.hi = cur.s.hi;
+                p.head = cur.head;
+                const int j = p.j0 + (lane & 15) * 8, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
+                p.tok = j - i * g.kv.page_size;
+                p.page = lane < 16 && j < p.hi ? g.a.d_pages[cur.b * g.a.pages_stride + i] : -1;
+            };
+            look_up(at);
+            for (bool more = true; more; ++unit) {
+                Place ahead = at;
+                more = cur.step(g);
+                if (more) look_up(ahead);
+                const int j = at.j0 + (lane & 15) * 8;
+                const bool wanted = lane < 16 && j < at.hi, in_pool = wanted && at.page >= 0 && at.page < g.kv.n_pages;
+                if (wanted && !in_pool) set_status(g.status, SISO_ERR_INVALID_ARG);
+                const bool first = wanted && lane % box_blocks == 0;
+                const uint32_t there = __ballot_sync(0xFFFFFFFFu, in_pool);
+                const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, first));
                 for (int is_v = 0; is_v < 2; ++is_v) {
-                    if (stage % PRODUCERS == warp - 17) {          // a stage is always filled by the same warp, so its rounds come in order
-                        const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), tok = j - at * g.kv.page_size;
-                        int page = -1;
-                        if (lane < 16 && j < cur.s.hi) {
-                            page = g.a.d_pages[cur.b * g.a.pages_stride + at];
-                            if (page < 0 || page >= g.kv.n_pages) { page = -1; set_status(g.status, SISO_ERR_INVALID_ARG); }
-                        }
-                        const bool first = lane < 16 && j < cur.s.hi && lane % box_blocks == 0;
-                        const uint32_t there = __ballot_sync(0xFFFFFFFFu, page >= 0);
-                        const uint32_t boxes = __popc(__ballot_sync(0xFFFFFFFFu, first));
+                    if (stage % PRODUCERS == warp - 17) {         // a stage is always filled by the same warp, so its rounds come in order
                         uint64_t *full = EIGHT ? &bars.raw_full[stage] : &bars.kv_full[stage];
                         wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up);
                         uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
                         // the last values of an item in a bf16 cache go through warp 19
-                        uint64_t *bar = !EIGHT && is_v && j0 + TK > cur.s.hi ? &bars.landed[stage] : full;
+                        uint64_t *bar = !EIGHT && is_v && at.j0 + TK > at.hi ? &bars.landed[stage] : full;
                         if (*gave_up == 0) {
                             if (lane == 0) {
                                 if (!is_v) bars.blocks[unit & 7] = there;
@@ -315,99 +336,98 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                             __syncwarp();
                             if (first) {
                                 // a page outside the pool is asked for at a place beyond the tensor's end, which reads as zeros
-                                const int p = page < 0 ? static_cast<int>(g.kv.n_pages) : page;
+                                const int p = in_pool ? at.page : static_cast<int>(g.kv.n_pages);
 #pragma unroll
                                 for (int half = 0; half < RB / LINE; ++half)
-                                    load_box(smem_u32(dst) + half * (TK * 128) + lane * 8 * LINE, is_v ? &map_v : &map_k, half * 64, cur.head, tok, p, g.a.layer, bar);
+                                    load_box(smem_u32(dst) + half * (TK * 128) + lane * 8 * LINE, is_v ? &map_v : &map_k, half * 64, at.head, at.tok, p, g.a.layer, bar);
                             }
                             if constexpr (EIGHT) {
-                                const long long e = page < 0 ? 0 : (static_cast<long long>(page) * g.kv.n_kv_heads + cur.head) * g.kv.page_size + tok;
+                                const long long e = in_pool ? (static_cast<long long>(at.page) * g.kv.n_kv_heads + at.head) * g.kv.page_size + at.tok : 0;
                                 if (lane < 16)
                                     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(metas + stage * S::RAW_META + lane * 8)),
-                                                 "l"((is_v ? g.kv.v_exp : g.kv.k_exp) + e), "r"(page < 0 ? 0 : 8) : "memory");
+                                                 "l"((is_v ? g.kv.v_exp : g.kv.k_exp) + e), "r"(in_pool ? 8 : 0) : "memory");
                                 asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
                             }
                         }
                     }
                     if (++stage == RING) { stage = 0; phase ^= 1u; }
                 }
-                ++unit;
-            } while (cur.step(g));
+                at = ahead;
+            }
             if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
         } else {
             // ---- products.  The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers; one
             // lane issues
             const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-            const uint32_t s_col[2] = {base, base + 128}, o_col[2] = {base + 256, base + 256 + D};
             const uint64_t q_desc = smem_desc_sw128(smem_u32(q_smem)), k_desc = smem_desc_sw128(smem_u32(tiles)), v_desc = desc_mn(smem_u32(tiles));
-            int stage = 0;
-            uint32_t phase = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-            auto step = [&]() { if (++stage == STAGES) { stage = 0; phase ^= 1u; } };
-            auto scores = [&](int t, int at) {
-                const uint64_t a = q_desc + static_cast<uint64_t>(t * (S::Q_BYTES / 2 >> 4)), b = k_desc + static_cast<uint64_t>(at * (S::TILE >> 4));
+            int k_stage = 0, v_stage = 1;                   // K and V tiles alternate in the ring
+            uint32_t k_phase = 0, v_phase = 0, q_phase = 0, p_phases = 0;
+            auto next = [&](int &stage, uint32_t &phase) __attribute__((always_inline)) {
+                stage += 2;
+                if (stage >= STAGES) { stage -= STAGES; phase ^= 1u; }
+            };
+            auto release = [&](int stage) __attribute__((always_inline)) {
+                if (elect_one()) umma_commit(&bars.kv_empty[stage]);
+                __syncwarp();
+            };
+            auto scores = [&](int t) __attribute__((always_inline)) {                      // S_t = Q_t K^T
+                const uint64_t a = q_desc + static_cast<uint64_t>(t * (S::Q_BYTES / 2 >> 4)), b = k_desc + static_cast<uint64_t>(k_stage * (S::TILE >> 4));
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {      // 32 bytes further along a line, or the next 64 d
                         const uint64_t off = static_cast<uint64_t>(2 * (k % 4) + (k / 4) * ((TK * 128) >> 4));
-                        umma_bf16(s_col[t], a + off, b + off, IDESC<128, false>, k ? 1u : 0u);
+                        umma_bf16(base + t * 128, a + off, b + off, IDESC<128, false>, k ? 1u : 0u);
                     }
                     umma_commit(&bars.s_full[t]);
                 }
                 __syncwarp();
             };
+            auto values = [&](int t, bool fresh) __attribute__((always_inline)) {          // O_t += P_t V, or O_t = P_t V
+                const uint64_t b = v_desc + static_cast<uint64_t>(v_stage * (S::TILE >> 4));
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {               // the first 32 keys of both halves, the others: each as soon as its probabilities are there
+                    wait_bar(&bars.p_full[t][c], (p_phases >> t) & 1u, gave_up);
+                    tcgen05_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int k = 2 * c; k < 2 * c + 2; ++k)
+                                mma_ts(base + 256 + t * D, base + t * 128 + 64 * h + 8 * k, b + static_cast<uint64_t>((4 * h + k) * (2048 >> 4)), IDESC<D, true>,
+                                       (!fresh || c > 0 || h > 0 || k > 0) ? 1u : 0u);
+                        if (c == 1) umma_commit(&bars.o_done[t]);
+                    }
+                    __syncwarp();
+                }
+                p_phases ^= 1u << t;
+            };
             int n;
             do {
                 n = cur.tiles_here();
-                const int two = cur.n_q * g.group - cur.rt * TC_ROWS > 128 ? 2 : 1;
-                wait_bar(&bars.kv_full[stage], phase, gave_up);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (t < two) {
-                        wait_bar(&bars.q_full[t], q_phase[t], gave_up);
-                        q_phase[t] ^= 1u;
-                        tcgen05_fence_after();
-                        scores(t, stage);
-                    }
-                }
-                if (elect_one()) umma_commit(&bars.kv_empty[stage]);
-                __syncwarp();
-                step();
-                for (int j = 0; j < n; ++j) {
-                    const int v_stage = stage;
-                    wait_bar(&bars.kv_full[v_stage], phase, gave_up);
-                    step();
-                    const bool more = j + 1 < n;
-                    if (more) wait_bar(&bars.kv_full[stage], phase, gave_up);
-                    const uint64_t b = v_desc + static_cast<uint64_t>(v_stage * (S::TILE >> 4));
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (t < two) {
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {   // the first 32 keys of both halves, the others: each as soon as its probabilities are there
-                                wait_bar(&bars.p_full[t][c], p_phase[t], gave_up);
-                                tcgen05_fence_after();
-                                if (elect_one()) {
-#pragma unroll
-                                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                                        for (int k = 2 * c; k < 2 * c + 2; ++k)
-                                            mma_ts(o_col[t], s_col[t] + 64 * h + 8 * k, b + static_cast<uint64_t>((4 * h + k) * (2048 >> 4)), IDESC<D, true>,
-                                                   (j > 0 || c > 0 || h > 0 || k > 0) ? 1u : 0u);
-                                    if (c == 1) {
-                                        umma_commit(&bars.o_done[t]);
-                                        if (t + 1 == two) umma_commit(&bars.kv_empty[v_stage]);
-                                    }
-                                }
-                                __syncwarp();
-                            }
-                            p_phase[t] ^= 1u;
-                            if (more) scores(t, stage);
+                wait_bar(&bars.q_full[0], q_phase, gave_up);
+                wait_bar(&bars.q_full[1], q_phase, gave_up);
+                q_phase ^= 1u;
+                // two tiles of rows, each with every tile of keys; or one twice, each with every other tile of keys
+                const bool split = cur.n_q * g.group - cur.rt * TC_ROWS <= 128;
+                const int ahead = split ? 2 : 1, per_tile = split ? 1 : 2;
+                for (int j = -ahead; j < n; ++j) {
+                    if (j >= 0) wait_bar(&bars.kv_full[v_stage], v_phase, gave_up);
+                    for (int i = 0; i < per_tile; ++i) {
+                        const int t = split ? j & 1 : i;
+                        if (j >= 0) values(t, j < ahead);
+                        if (j >= 0 && i + 1 == per_tile) {
+                            release(v_stage);
+                            next(v_stage, v_phase);
                         }
-                    }
-                    if (more) {
-                        if (elect_one()) umma_commit(&bars.kv_empty[stage]);
-                        __syncwarp();
-                        step();
+                        if (j + ahead < n) {
+                            if (i == 0) wait_bar(&bars.kv_full[k_stage], k_phase, gave_up);
+                            tcgen05_fence_after();
+                            scores(t);
+                            if (i + 1 == per_tile) {
+                                release(k_stage);
+                                next(k_stage, k_phase);
+                            }
+                        }
                     }
                 }
             } while (cur.step(g, n));
@@ -415,38 +435,69 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     } else {
         // ---- softmax: half of a row of one tile
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SOFTMAX_REGS));
-        const int t = warp >> 3, half = (warp >> 2) & 1, in_tile = t * 128 + (threadIdx.x & 127);      // row of the 256
+        const int t = warp >> 3, half = (warp >> 2) & 1, lane_row = threadIdx.x & 127;
         const uint32_t lane_at = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lane_at + t * 128 + half * 64, o_at = tmem + lane_at + 256 + t * D + half * (D / 2);
         const bool causal = (g.a.flags & SISO_ATTN_CAUSAL) != 0u;
         // the sign of the scale goes to the queries, so that the largest product is the largest score; scale 0: queries of zeros
         const float scale = g.scale_log2 == 0.f ? 1.f : fabsf(g.scale_log2);
-        float &mine_out = bars.peer[t][half][threadIdx.x & 127], &theirs_in = bars.peer[t][half ^ 1][threadIdx.x & 127];
+        float &mine_out = bars.peer[t][half][lane_row], &theirs_in = bars.peer[t][half ^ 1][lane_row];
         uint32_t tile_phase = 0;
         int unit = 0;                                                     // units of this CTA so far
-        bool pending = false;                                             // an item whose output is still in TMEM
+        bool pending = false, split = false;                              // an item whose output is still in TMEM, in two parts
         float m = -INFINITY, l = 0.f;
         int out_token = -1, out_head = 0, out_place = -1;                 // of that item: where the row goes, or its place among the parts
         auto together = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1 + t) : "memory"); };
-        auto store_item = [&]() {
+        auto everyone = [&]() { asm volatile("bar.sync 3, 512;" ::: "memory"); };
+        auto store_item = [&](bool split_item) {
+            const bool to_part = __any_sync(0xFFFFFFFFu, out_place >= 0), split = __any_sync(0xFFFFFFFFu, split_item);      // (uniform, visibly)
             wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
             tcgen05_fence_after();
             mine_out = l;
             together();
-            const float sum = half ? theirs_in + l : l + theirs_in;       // the same sum in both threads
+            float sum = half ? theirs_in + l : l + theirs_in;             // the same sum in both threads
+            float f0 = 1.f, f1 = 0.f;
+            if (split) {                                                  // the rows' other tiles of keys are with the other tile
+                if (t == 1) {
+                    together();
+                    if (half == 0) { bars.peer[1][0][lane_row] = m; bars.peer[1][1][lane_row] = sum; }
+                    tcgen05_fence_before();
+                    everyone();
+                    everyone();                                           // until that output has been read
+                    tcgen05_fence_after();
+                    return;
+                }
+                everyone();
+                tcgen05_fence_after();
+                const float m1 = bars.peer[1][0][lane_row], l1 = bars.peer[1][1][lane_row], m2 = fmaxf(m, m1);
+                f0 = m == -INFINITY ? 0.f : ex2(m - m2);
+                f1 = m1 == -INFINITY ? 0.f : ex2(m1 - m2);
+                sum = sum * f0 + l1 * f1;
+                m = m2;
+            }
             const bool none = m == -INFINITY;                             // (the sum may hold remainders of 2^-126)
             const float inv = none ? 0.f : 1.f / sum;
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D / 64; ++c) {
                 uint32_t r[32];
                 tmem_ld_32x32(o_at + c * 32, r);
                 tmem_ld_fence(r);
+                if (split) {
+#pragma unroll
+                    for (int p = 0; p < 32; p += 16) {
+                        uint32_t y[16];
+                        tmem_ld_32x16(o_at + D + c * 32 + p, y);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)                      // (an output without tiles holds anything)
+                            r[p + i] = __float_as_uint((f0 == 0.f ? 0.f : f0 * __uint_as_float(r[p + i])) + (f1 == 0.f ? 0.f : f1 * __uint_as_float(y[i])));
+                    }
+                }
                 if constexpr (EIGHT) {                                    // d 0 2 1 3 of every four
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) { const uint32_t x = r[i + 1]; r[i + 1] = r[i + 2]; r[i + 2] = x; }
                 }
                 // four lanes turn their four pieces of 16 bytes round, so that they write 64 bytes of a row together
-                if (out_place < 0) {
+                if (!to_part) {
                     uint4 w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -463,6 +514,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                                                        static_cast<long long>(head) * g.a.out_stride_head + half * (D / 2) + c * 32 + (lane & 3) * 8) = w[i];
                     }
                 } else {
+                    // (places of neighbouring rows are neighbours; unused rows are never read)
+                    float *dst = g.part_o + static_cast<long long>(out_place - (lane & 3)) * D + half * (D / 2) + c * 32 + (lane & 3) * 4;
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         uint4 w[4];
@@ -470,8 +523,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         for (int i = 0; i < 4; ++i) w[i] = make_uint4(r[16 * p + 4 * i], r[16 * p + 4 * i + 1], r[16 * p + 4 * i + 2], r[16 * p + 4 * i + 3]);
                         turn4(w, lane);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)                       // places of neighbouring rows are neighbours; unused rows are never read
-                            *reinterpret_cast<uint4 *>(g.part_o + static_cast<long long>(out_place - (lane & 3) + i) * D + half * (D / 2) + c * 32 + p * 16 + (lane & 3) * 4) = w[i];
+                        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(dst + i * D + p * 16) = w[i];
                     }
                 }
             }
@@ -480,155 +532,151 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_token) * g.a.n_heads + out_head] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
             }
             tcgen05_fence_before();
-            together();                                                   // the exchange place is free again
+            if (split) everyone();
+            else together();                                              // the exchange place is free again
         };
-        int n;
-        do {
-            n = cur.tiles_here();
+        for (bool more = true;;) {
             const int rows = cur.n_q * g.group - cur.rt * TC_ROWS;        // rows of the item from this row tile on
-            const bool mine = t == 0 || rows > 128;
-            if (mine) {
-                const bool real = in_tile < rows;
-                const int row = cur.rt * TC_ROWS + (real ? in_tile : 0);
-                const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = cur.head * g.group + row - i * g.group;
-                {   // the last scores of the item before have come, so its queries are no longer read.  8 (4) lanes share half a row
-                    const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
-                    constexpr int LANES = D / 16, PER = 32 / LANES;
-                    uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
-                    const int c = half * LANES + lane % LANES, first = (warp & 3) * 32 + lane / LANES;
-                    uint4 x[32 / PER];
+            const bool split_next = rows <= 128;                      // one tile of rows twice, with every other tile of keys
+            const int tile_row = split_next ? 0 : t * 128, in_tile = tile_row + lane_row;
+            if (more) {   // the last scores of the item before have come, so its queries are no longer read.  8 (4) lanes share half a row
+                const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
+                constexpr int LANES = D / 16, PER = 32 / LANES;
+                uint8_t *dst = q_smem + t * (S::Q_BYTES / 2);
+                const int c = half * LANES + lane % LANES, first = (warp & 3) * 32 + lane / LANES;
+                uint4 x[32 / PER];
 #pragma unroll
-                    for (int y = 0; y < 32 / PER; ++y) {
-                        const int at = t * 128 + first + y * PER, r = cur.rt * TC_ROWS + at;
-                        x[y] = make_uint4(0u, 0u, 0u, 0u);
-                        if (at < rows) {
-                            const int tok = static_cast<int>(g.by_group.div(static_cast<uint32_t>(r)));
-                            x[y] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + tok) * g.a.q_stride_token +
-                                                                    static_cast<long long>(cur.head * g.group + r - tok * g.group) * g.a.q_stride_head + c * 8);
-                        }
+                for (int y = 0; y < 32 / PER; ++y) {
+                    const int at = tile_row + first + y * PER, r = cur.rt * TC_ROWS + at;
+                    x[y] = make_uint4(0u, 0u, 0u, 0u);
+                    if (at < rows) {
+                        const int tok = static_cast<int>(g.by_group.div(static_cast<uint32_t>(r)));
+                        x[y] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(g.a.d_q) + static_cast<long long>(cur.q0 + tok) * g.a.q_stride_token +
+                                                                static_cast<long long>(cur.head * g.group + r - tok * g.group) * g.a.q_stride_head + c * 8);
                     }
-#pragma unroll
-                    for (int y = 0; y < 32 / PER; ++y) {
-                        uint32_t w[4] = {(x[y].x ^ flip) & keep, (x[y].y ^ flip) & keep, (x[y].z ^ flip) & keep, (x[y].w ^ flip) & keep};
-                        if constexpr (EIGHT) {                            // the order in which the codes come
-#pragma unroll
-                            for (int k = 0; k < 4; k += 2) {
-                                const uint32_t a = w[k], b = w[k + 1];
-                                w[k] = __byte_perm(a, b, 0x5410);
-                                w[k + 1] = __byte_perm(a, b, 0x7632);
-                            }
-                        }
-                        *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(first + y * PER, c)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bars.q_full[t]);
                 }
-                if (pending) store_item();
-                pending = true;
-                out_token = real ? cur.q0 + i : -1;
-                out_head = head;
-                out_place = cur.tile == 0 && n == cur.s.tiles ? -1 : static_cast<int>(part_place(blockIdx.x, cur.tile > 0)) * TC_ROWS + in_tile;
-                const int pos = real ? cur.len - cur.n_q + i : cur.s.last_pos;
-                m = -INFINITY;
-                l = 0.f;
-                for (int k = 0; k < n; ++k) {
-                    const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
-                    wait_bar(&bars.s_full[t], tile_phase, gave_up);
-                    tcgen05_fence_after();
-                    uint32_t ra[32], rb[32];
-                    tmem_ld_32x32(s_at, ra);
-                    tmem_ld_32x32(s_at + 32, rb);
-                    const uint32_t blocks = bars.blocks[(unit + k) & 7];
-                    const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) ||
-                                     (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
-                    tmem_ld_fence(ra);
-                    tmem_ld_fence(rb);
-                    if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
-                        const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0 - half * 64;
-                        const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 - half * 64 : 0;
-                        const uint32_t my_blocks = blocks >> (half * 8);
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) {
-                            if (x > last || x < first || !((my_blocks >> (x / 8)) & 1u)) ra[x] = 0xFF800000u;
-                            if (32 + x > last || 32 + x < first || !((my_blocks >> (4 + x / 8)) & 1u)) rb[x] = 0xFF800000u;
+                for (int y = 0; y < 32 / PER; ++y) {
+                    uint32_t w[4] = {(x[y].x ^ flip) & keep, (x[y].y ^ flip) & keep, (x[y].z ^ flip) & keep, (x[y].w ^ flip) & keep};
+                    if constexpr (EIGHT) {                            // the order in which the codes come
+#pragma unroll
+                        for (int k = 0; k < 4; k += 2) {
+                            const uint32_t a = w[k], b = w[k + 1];
+                            w[k] = __byte_perm(a, b, 0x5410);
+                            w[k + 1] = __byte_perm(a, b, 0x7632);
                         }
                     }
-                    float top[4] = {__uint_as_float(ra[0]), __uint_as_float(ra[1]), __uint_as_float(rb[0]), __uint_as_float(rb[1])};
+                    *reinterpret_cast<uint4 *>(dst + chunk_at<2 * D, TK>(first + y * PER, c)) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.q_full[t]);
+            }
+            if (pending) store_item(split);
+            if (!more) break;
+            pending = true;
+            const int n = cur.tiles_here();
+            const bool real = in_tile < rows;
+            const int row = cur.rt * TC_ROWS + (real ? in_tile : 0);
+            const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = cur.head * g.group + row - i * g.group;
+            split = split_next;
+            out_token = real ? cur.q0 + i : -1;
+            out_head = head;
+            out_place = cur.tile == 0 && n == cur.s.tiles ? -1 : static_cast<int>(part_place(blockIdx.x, cur.tile > 0)) * TC_ROWS + in_tile;
+            const int pos = real ? cur.len - cur.n_q + i : cur.s.last_pos;
+            m = -INFINITY;
+            l = 0.f;
+            const int k0 = split ? t : 0, k_step = split ? 2 : 1;
+            for (int k = k0; k < n; k += k_step) {
+                const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
+                wait_bar(&bars.s_full[t], tile_phase, gave_up);
+                tcgen05_fence_after();
+                uint32_t ra[32], rb[32];
+                tmem_ld_32x32(s_at, ra);
+                tmem_ld_32x32(s_at + 32, rb);
+                const uint32_t blocks = bars.blocks[(unit + k) & 7];
+                const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) ||
+                                 (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
+                tmem_ld_fence(ra);
+                tmem_ld_fence(rb);
+                if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
+                    const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0 - half * 64;
+                    const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 - half * 64 : 0;
+                    const uint32_t my_blocks = blocks >> (half * 8);
 #pragma unroll
-                    for (int x = 2; x < 32; x += 4) {
-                        top[0] = max3(top[0], __uint_as_float(ra[x]), __uint_as_float(ra[x + 1]));
-                        top[2] = max3(top[2], __uint_as_float(rb[x]), __uint_as_float(rb[x + 1]));
-                        if (x + 2 < 32) {
-                            top[1] = max3(top[1], __uint_as_float(ra[x + 2]), __uint_as_float(ra[x + 3]));
-                            top[3] = max3(top[3], __uint_as_float(rb[x + 2]), __uint_as_float(rb[x + 3]));
-                        }
+                    for (int x = 0; x < 32; ++x) {
+                        if (x > last || x < first || !((my_blocks >> (x / 8)) & 1u)) ra[x] = 0xFF800000u;
+                        if (32 + x > last || 32 + x < first || !((my_blocks >> (4 + x / 8)) & 1u)) rb[x] = 0xFF800000u;
                     }
-                    float m2 = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]) * scale);
-                    uint32_t grown;
-                    asm volatile(
-                        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
-                        "barrier.cta.red.or.aligned.pred q, %1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                        : "=r"(grown) : "r"(1 + t), "r"((m2 > m + 8.f || (m == -INFINITY && m2 != m)) ? 1u : 0u) : "memory");
-                    if (grown) {
-                        mine_out = m2;
-                        together();
-                        m2 = fmaxf(m2, theirs_in);
-                        const float corr = m == m2 ? 1.f : ex2(m - m2);
-                        m = m2;
-                        l *= corr;
-                        if (k > 0) {
-                            wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
-                            tcgen05_fence_after();
-#pragma unroll 1
-                            for (int c = 0; c < D / 2; c += 16) {         // 16 columns at a time: the scores stay in registers
-                                uint32_t y[16];
-                                asm volatile(
-                                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-                                    "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-                                    "tcgen05.wait::ld.sync.aligned;"
-                                    : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]), "=r"(y[4]), "=r"(y[5]), "=r"(y[6]), "=r"(y[7]), "=r"(y[8]),
-                                      "=r"(y[9]), "=r"(y[10]), "=r"(y[11]), "=r"(y[12]), "=r"(y[13]), "=r"(y[14]), "=r"(y[15])
-                                    : "r"(o_at + c) : "memory");
+                }
+                float top[4] = {__uint_as_float(ra[0]), __uint_as_float(ra[1]), __uint_as_float(rb[0]), __uint_as_float(rb[1])};
 #pragma unroll
-                                for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(y[x]) * corr);
-                                tmem_st_32x16(o_at + c, y);
-                            }
-                            tmem_st_wait();
-                            tcgen05_fence_before();
-                        }
-                        together();        // no product of this unit begins before both halves of the output are rescaled
+                for (int x = 2; x < 32; x += 4) {
+                    top[0] = max3(top[0], __uint_as_float(ra[x]), __uint_as_float(ra[x + 1]));
+                    top[2] = max3(top[2], __uint_as_float(rb[x]), __uint_as_float(rb[x + 1]));
+                    if (x + 2 < 32) {
+                        top[1] = max3(top[1], __uint_as_float(ra[x + 2]), __uint_as_float(ra[x + 3]));
+                        top[3] = max3(top[3], __uint_as_float(rb[x + 2]), __uint_as_float(rb[x + 3]));
+                    }
+                }
+                float m2 = fmaxf(m, max3(fmaxf(top[0], top[1]), top[2], top[3]) * scale);
+                uint32_t grown;
+                asm volatile(
+                    "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
+                    "barrier.cta.red.or.aligned.pred q, %1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                    : "=r"(grown) : "r"(1 + t), "r"((m2 > m + 8.f || (m == -INFINITY && m2 != m)) ? 1u : 0u) : "memory");
+                if (grown) {
+                    mine_out = m2;
+                    together();
+                    m2 = fmaxf(m2, theirs_in);
+                    const float corr = m == m2 ? 1.f : ex2(m - m2);
+                    m = m2;
+                    l *= corr;
+                    if (k > k0) {
+                        wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
                         tcgen05_fence_after();
-                    }
-                    const float shift = m == -INFINITY ? 0.f : -m;
-                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    auto weigh = [&](const uint32_t (&r)[32], int c) {
-                        uint32_t p[16];
+#pragma unroll 1
+                        for (int c = 0; c < D / 2; c += 16) {         // 16 columns at a time: the scores stay in registers
+                            uint32_t y[16];
+                            tmem_ld_32x16(o_at + c, y);
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
-                            if ((x * S::POLY) % 16 < S::POLY) y = ex2_poly(y);
-                            else { y.x = ex2(y.x); y.y = ex2(y.y); }
-                            sum[x & 1] = add2(sum[x & 1], y);
-                            p[x] = pack(y.x, y.y, false);
+                            for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(y[x]) * corr);
+                            tmem_st_32x16(o_at + c, y);
                         }
-                        tmem_st_32x16(s_at + c * 16, p);
                         tmem_st_wait();
                         tcgen05_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&bars.p_full[t][c]);
-                    };
-                    weigh(ra, 0);
-                    weigh(rb, 1);
-                    sum[0] = add2(sum[0], sum[1]);
-                    l += sum[0].x + sum[0].y;
-                    tile_phase ^= 1u;
+                    }
+                    together();        // no product of this unit begins before both halves of the output are rescaled
+                    tcgen05_fence_after();
                 }
+                const float shift = m == -INFINITY ? 0.f : -m;
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                auto weigh = [&](const uint32_t (&r)[32], int c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
+                        if ((x * S::POLY) % 16 < S::POLY) y = ex2_poly(y);
+                        else { y.x = ex2(y.x); y.y = ex2(y.y); }
+                        sum[x & 1] = add2(sum[x & 1], y);
+                        p[x] = pack(y.x, y.y, false);
+                    }
+                    tmem_st_32x16(s_at + c * 16, p);
+                    tmem_st_wait();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.p_full[t][c]);
+                };
+                weigh(ra, 0);
+                weigh(rb, 1);
+                sum[0] = add2(sum[0], sum[1]);
+                l += sum[0].x + sum[0].y;
+                tile_phase ^= 1u;
             }
             if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) g.records[blockIdx.x] = record_of(bars.run, cur.b, cur.head, cur.rt, cur.s.tiles, n);
             unit += n;
-        } while (cur.step(g, n));
-        if (pending) store_item();
+            more = cur.step(g, n);
+        }
     }
 
     // ---- teardown

@@ -4,19 +4,19 @@ marshalling only; names and rules follow include/siso.h."""
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
 import torch
 
-from .binding import SisoError, _ALLOC_FN, _FREE_FN, _Allocator, _ptr, load_library
+from .binding import SisoError, _ALLOC_FN, _FREE_FN, _Allocator, load_library
 
 ATTN_CAUSAL = 1
 _CACHE_TYPES = {torch.bfloat16: 1, torch.float8_e4m3fn: 2, torch.int8: 3}
 _ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _stream(stream: Optional[torch.cuda.Stream], dev: torch.device) -> int:
-    return (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+_raw_stream = torch._C._cuda_getCurrentRawStream        # the current stream's handle, without building a Stream object
 
 
 class _KvConfig(ctypes.Structure):
@@ -27,13 +27,8 @@ class _KvConfig(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("device", ctypes.c_int32), ("allocator", _Allocator)]
 
 
-class _Attention(ctypes.Structure):
-    _fields_ = [("d_q", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("d_lse", ctypes.c_void_p), ("d_cu_q", ctypes.c_void_p),
-                ("d_kv_len", ctypes.c_void_p), ("d_pages", ctypes.c_void_p), ("q_stride_token", ctypes.c_int64),
-                ("q_stride_head", ctypes.c_int64), ("out_stride_token", ctypes.c_int64), ("out_stride_head", ctypes.c_int64),
-                ("pages_stride", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_q", ctypes.c_int32),
-                ("max_pages", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("layer", ctypes.c_int32), ("window", ctypes.c_int32),
-                ("flags", ctypes.c_uint32), ("scale", ctypes.c_float)]
+# siso_attention_t: 6 pointers, 6 int64, 6 int32, uint32, float.  Packed by hand: a call costs the host a few microseconds in all
+_ATTENTION = struct.Struct("@6P6q6iIf")
 
 
 class PagedKV:
@@ -61,7 +56,7 @@ class PagedKV:
         self._lib = load_library()
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = layers, pages, tokens, heads, dim
-        self._dev = k.device
+        self._dev, self._index = k.device, k.get_device()
         self._blocks = {}
 
         def _alloc(nbytes, stream, ctx):          # scratch from the pool of the stream it is first used on
@@ -88,8 +83,8 @@ class PagedKV:
         st = self._lib.siso_kv_create(ctypes.byref(h), ctypes.byref(cfg))
         self._h = h if st == 0 else None
         self._check(st, "siso_kv_create")
-        self._args = _Attention()
-        self._args_ref = ctypes.byref(self._args)
+        self._args = ctypes.create_string_buffer(_ATTENTION.size)
+        self._default_scale = dim ** -0.5
 
     @classmethod
     def allocate(cls, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
@@ -120,26 +115,30 @@ class PagedKV:
             pass
 
     def _rows(self, t: torch.Tensor, n: int, name: str) -> torch.Tensor:
-        if t.dtype not in _ROW_TYPES or t.device != self._dev or tuple(t.shape) != (n, self.n_kv_heads, self.head_dim):
+        if t.dtype not in _ROW_TYPES or t.get_device() != self._index or t.shape != (n, self.n_kv_heads, self.head_dim):
             raise ValueError(f"{name} must be a [{n}, {self.n_kv_heads}, {self.head_dim}] float32 or bfloat16 tensor on {self._dev}")
         return t if t.stride(2) == 1 else t.contiguous()
 
     def _slots(self, slots: torch.Tensor) -> torch.Tensor:
-        if slots.dtype != torch.int64 or slots.dim() != 1 or slots.device != self._dev:
+        if slots.dtype is not torch.int64 or slots.dim() != 1 or slots.get_device() != self._index:
             raise ValueError(f"slots must be a one-dimensional int64 tensor on {self._dev}")
-        return slots.contiguous()
+        return slots if slots.is_contiguous() else slots.contiguous()
 
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, layer: int = 0, stream=None) -> None:
         """Rows k, v [n, kv heads, head dim] (fp32 or bf16) into `slots` [n] = page * page size + token (-1: skipped)."""
         slots = self._slots(slots)
         n = slots.shape[0]
         k, v = self._rows(k, n, "k"), self._rows(v, n, "v")
-        if k.dtype != v.dtype:
+        if k.dtype is not v.dtype:
             raise ValueError("k and v must have the same type")
-        if k.stride() != v.stride():
+        strides = k.stride()
+        if strides != v.stride():
             k, v = k.contiguous(), v.contiguous()
-        self._check(self._lib.siso_kv_write(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, k.stride(0), k.stride(1),
-                                            slots.data_ptr(), _stream(stream, self._dev)), "siso_kv_write")
+            strides = k.stride()
+        st = self._lib.siso_kv_write(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, strides[0], strides[1],
+                                     slots.data_ptr(), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if st:
+            self._check(st, "siso_kv_write")
 
     def read(self, slots: torch.Tensor, layer: int = 0, dtype: torch.dtype = torch.bfloat16, stream=None, out=None
              ) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -149,13 +148,16 @@ class PagedKV:
         if out is None:
             if dtype not in _ROW_TYPES:
                 raise ValueError("dtype must be float32 or bfloat16")
-            k, v = (torch.empty((n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self._dev) for _ in range(2))
+            k, v = torch.empty((2, n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self._dev).unbind()
         else:
             k, v = out
-            if self._rows(k, n, "out k") is not k or self._rows(v, n, "out v") is not v or k.stride() != v.stride() or k.dtype != v.dtype:
+            if self._rows(k, n, "out k") is not k or self._rows(v, n, "out v") is not v or k.stride() != v.stride() or k.dtype is not v.dtype:
                 raise ValueError("outputs must have contiguous rows, the same strides and the same type")
-        self._check(self._lib.siso_kv_read(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, k.stride(0), k.stride(1),
-                                           slots.data_ptr(), _stream(stream, self._dev)), "siso_kv_read")
+        strides = k.stride()
+        st = self._lib.siso_kv_read(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, strides[0], strides[1],
+                                    slots.data_ptr(), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+        if st:
+            self._check(st, "siso_kv_read")
         return k, v
 
     def attention(self, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, max_q: int, layer: int = 0,
@@ -164,38 +166,45 @@ class PagedKV:
         """q [n, heads, head dim] bf16: the queries of all sequences one after the other, sequence b's from cu_q[b] on (int32
         [seqs + 1]); kv_len int32 [seqs]: tokens in all, the new ones included (already written); pages int32 [seqs, max pages].
         Returns out [n, heads, head dim], or (out, lse [n, heads] fp32) with want_lse."""
-        if q.dtype != torch.bfloat16 or q.dim() != 3 or q.shape[2] != self.head_dim or q.device != self._dev:
+        index, i32 = self._index, torch.int32
+        shape = q.shape
+        if q.dtype is not torch.bfloat16 or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
             raise ValueError(f"q must be a [n, heads, {self.head_dim}] bfloat16 tensor on {self._dev}")
-        if not cu_q.dtype == kv_len.dtype == pages.dtype == torch.int32 or not cu_q.device == kv_len.device == pages.device == self._dev:
+        if cu_q.dtype is not i32 or kv_len.dtype is not i32 or pages.dtype is not i32 or cu_q.get_device() != index or kv_len.get_device() != index \
+                or pages.get_device() != index:
             raise ValueError(f"cu_q, kv_len and pages must be int32 tensors on {self._dev}")
-        n, heads, _ = q.shape
-        seqs = kv_len.shape[0]
-        if cu_q.dim() != 1 or kv_len.dim() != 1 or cu_q.shape[0] != seqs + 1 or pages.dim() != 2 or pages.shape[0] != seqs:
+        n, heads, dim = shape
+        table = pages.shape
+        seqs = kv_len.numel()
+        if cu_q.dim() != 1 or kv_len.dim() != 1 or cu_q.numel() != seqs + 1 or len(table) != 2 or table[0] != seqs:
             raise ValueError("cu_q must be [seqs + 1], kv_len [seqs], pages [seqs, max pages]")
-        if q.stride(2) != 1:
+        sq = q.stride()
+        if sq[2] != 1:
             q = q.contiguous()
+            sq = q.stride()
         if pages.stride(1) != 1:
             pages = pages.contiguous()
-        cu_q, kv_len = cu_q.contiguous(), kv_len.contiguous()
+        if not cu_q.is_contiguous():
+            cu_q = cu_q.contiguous()
+        if not kv_len.is_contiguous():
+            kv_len = kv_len.contiguous()
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=torch.bfloat16, device=self._dev)
-        elif out.dtype != torch.bfloat16 or out.shape != q.shape or out.device != self._dev or out.stride(2) != 1:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+        elif out.dtype is not torch.bfloat16 or out.shape != shape or out.get_device() != index or out.stride(2) != 1:
             raise ValueError("out must be a bfloat16 tensor like q with contiguous rows")
+        so = out.stride()
         lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev) if want_lse else None
-        a = self._args
-        a.d_q, a.d_out, a.d_lse = q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else None
-        a.d_cu_q, a.d_kv_len, a.d_pages = cu_q.data_ptr(), kv_len.data_ptr(), pages.data_ptr()
-        a.q_stride_token, a.q_stride_head, _ = q.stride()
-        a.out_stride_token, a.out_stride_head, _ = out.stride()
-        a.pages_stride, a.n_tokens, a.n_seqs, a.max_q, a.max_pages = pages.stride(0), n, seqs, max_q, pages.shape[1]
-        a.n_heads, a.layer, a.window, a.flags = heads, layer, window, ATTN_CAUSAL if causal else 0
-        a.scale = self.head_dim ** -0.5 if scale is None else scale
-        self._check(self._lib.siso_kv_attention(self._h, self._args_ref, _stream(stream, self._dev)), "siso_kv_attention")
+        _ATTENTION.pack_into(self._args, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, cu_q.data_ptr(), kv_len.data_ptr(),
+                             pages.data_ptr(), sq[0], sq[1], so[0], so[1], pages.stride(0), n, seqs, max_q, table[1], heads, layer, window,
+                             ATTN_CAUSAL if causal else 0, self._default_scale if scale is None else scale)
+        st = self._lib.siso_kv_attention(self._h, self._args, _raw_stream(index) if stream is None else stream.cuda_stream)
+        if st:
+            self._check(st, "siso_kv_attention")
         return (out, lse) if want_lse else out
 
     def sync_status(self, stream=None) -> int:
         """Synchronise and return the handle's device status word (0 = clear); it is cleared by the call."""
-        return int(self._lib.siso_kv_sync_status(self._h, _stream(stream, self._dev)))
+        return int(self._lib.siso_kv_sync_status(self._h, _raw_stream(self._index) if stream is None else stream.cuda_stream))
 
     def check_status(self, stream=None) -> None:
         st = self.sync_status(stream)
@@ -208,27 +217,48 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: t
     """target [seqs, drafts + 1, vocab] and draft [seqs, drafts, vocab] (or None: certain drafts) probabilities, fp32 or bf16;
     tokens int32 [seqs, drafts]; n_drafts int32 [seqs] or None (all); u_accept [seqs, drafts], u_sample [seqs] fp32 in [0, 1).
     Returns (tokens out int32 [seqs, drafts + 1]: those that stand, one drawn, then -1; accepted int32 [seqs])."""
-    if target.dtype not in _ROW_TYPES or target.dim() != 3 or not target.is_cuda:
+    shape, i32, f32 = target.shape, torch.int32, torch.float32
+    if target.dtype not in _ROW_TYPES or len(shape) != 3 or not target.is_cuda:
         raise ValueError("target must be a [seqs, drafts + 1, vocab] float32 or bfloat16 tensor on a GPU")
-    seqs, n_max, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
-    dev = target.device
+    seqs, rows, vocab = shape
+    n_max, index = rows - 1, target.get_device()
     if n_max < 0:
         raise ValueError("target needs at least one row per sequence")
-    if draft is not None and (draft.dtype != target.dtype or tuple(draft.shape) != (seqs, n_max, vocab) or draft.device != dev):
-        raise ValueError("draft must be [seqs, drafts, vocab] of target's type and device")
-    for t, dtype, shape, name in ((tokens, torch.int32, (seqs, n_max), "tokens"), (n_drafts, torch.int32, (seqs,), "n_drafts"),
-                                  (u_accept, torch.float32, (seqs, n_max), "u_accept"), (u_sample, torch.float32, (seqs,), "u_sample")):
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or t.device != dev):
-            raise ValueError(f"{name} must be a {list(shape)} {dtype} tensor on {dev}")
-    target, tokens, u_accept, u_sample = target.contiguous(), tokens.contiguous(), u_accept.contiguous(), u_sample.contiguous()
-    draft = None if draft is None else draft.contiguous()
-    n_drafts = None if n_drafts is None else n_drafts.contiguous()
-    new, accepted = out if out is not None else (torch.empty((seqs, n_max + 1), dtype=torch.int32, device=dev),
-                                                 torch.empty((seqs,), dtype=torch.int32, device=dev))
-    L = load_library()
-    with torch.cuda.device(dev):
-        st = L.siso_verify_drafts(_ptr(target), _ptr(draft), _ROW_TYPES[target.dtype], seqs, n_max, vocab, _ptr(tokens), _ptr(n_drafts),
-                                  _ptr(u_accept), _ptr(u_sample), _ptr(new), _ptr(accepted), _stream(stream, dev))
-    if st != 0:
-        raise SisoError(st, "siso_verify_drafts", L.siso_last_cuda_error().decode() if st == 7 else "")
+    if draft is not None:
+        if draft.dtype is not target.dtype or draft.shape != (seqs, n_max, vocab) or draft.get_device() != index:
+            raise ValueError("draft must be [seqs, drafts, vocab] of target's type and device")
+        if not draft.is_contiguous():
+            draft = draft.contiguous()
+    if tokens.dtype is not i32 or tokens.shape != (seqs, n_max) or tokens.get_device() != index:
+        raise ValueError(f"tokens must be an int32 [{seqs}, {n_max}] tensor on {target.device}")
+    if n_drafts is not None and (n_drafts.dtype is not i32 or n_drafts.shape != (seqs,) or n_drafts.get_device() != index):
+        raise ValueError(f"n_drafts must be an int32 [{seqs}] tensor on {target.device}")
+    if u_accept.dtype is not f32 or u_accept.shape != (seqs, n_max) or u_accept.get_device() != index:
+        raise ValueError(f"u_accept must be a float32 [{seqs}, {n_max}] tensor on {target.device}")
+    if u_sample.dtype is not f32 or u_sample.shape != (seqs,) or u_sample.get_device() != index:
+        raise ValueError(f"u_sample must be a float32 [{seqs}] tensor on {target.device}")
+    target, tokens, u_accept, u_sample = (t if t.is_contiguous() else t.contiguous() for t in (target, tokens, u_accept, u_sample))
+    if n_drafts is not None and not n_drafts.is_contiguous():
+        n_drafts = n_drafts.contiguous()
+    if out is None:
+        both = torch.empty((seqs * (rows + 1),), dtype=i32, device=target.device)
+        new, accepted = both[:seqs * rows].view(seqs, rows), both[seqs * rows:]
+    else:
+        new, accepted = out
+        if new.dtype is not i32 or new.shape != (seqs, rows) or not new.is_contiguous() or accepted.dtype is not i32 or accepted.shape != (seqs,) \
+                or not accepted.is_contiguous() or new.get_device() != index or accepted.get_device() != index:
+            raise ValueError("out must be contiguous int32 tensors [seqs, drafts + 1] and [seqs] beside target")
+    here = torch._C._cuda_getDevice()
+    if here != index:
+        torch.cuda.set_device(index)
+    try:
+        st = load_library().siso_verify_drafts(target.data_ptr(), 0 if draft is None else draft.data_ptr(), _ROW_TYPES[target.dtype], seqs, n_max, vocab,
+                                               tokens.data_ptr(), 0 if n_drafts is None else n_drafts.data_ptr(), u_accept.data_ptr(),
+                                               u_sample.data_ptr(), new.data_ptr(), accepted.data_ptr(),
+                                               _raw_stream(index) if stream is None else stream.cuda_stream)
+    finally:
+        if here != index:
+            torch.cuda.set_device(here)
+    if st:
+        raise SisoError(st, "siso_verify_drafts", load_library().siso_last_cuda_error().decode() if st == 7 else "")
     return new, accepted
