@@ -9,9 +9,9 @@
 // coarse as a / M would give for i8 (e4m3 loses nothing but range at the bottom).  A row with a NaN or an infinity gets the
 // byte 255 and reads back as NaN throughout.
 //
-// Both kernels move bytes: they are bound by HBM for prompts and by latency for a step's few tokens.  G lanes own a row with 8
-// values each (one 16-byte load of bf16), so the maximum takes log2 G shuffles, and every lane has U rows in flight before
-// it uses the first.
+// Both kernels move bytes: they are bound by HBM for prompts and by latency for a step's few tokens.  G lanes own the rows of one
+// token with 8 values each (one 16-byte load of bf16), so the maximum takes log2 G shuffles; they look the slot up once and go
+// through heads, U rows in flight.
 #include <cuda_fp8.h>
 
 #include <cstring>
@@ -49,6 +49,13 @@ template <> struct Vec8<__nv_bfloat16> {
         }
         r = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ __forceinline__ void clear() { r = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void as_bf16(__nv_bfloat16 *p) const { store(p); }
+    // bits of the largest magnitude, two values at a time: 16-bit patterns order like the values too
+    __device__ __forceinline__ uint32_t largest() const {
+        const uint32_t m = 0x7FFF7FFFu, x = __vmaxu2(__vmaxu2(r.x & m, r.y & m), __vmaxu2(r.z & m, r.w & m));
+        return max(x << 16, x & 0xFFFF0000u);
+    }
 };
 template <> struct Vec8<float> {
     float4 a, b;
@@ -58,6 +65,22 @@ template <> struct Vec8<float> {
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     }
     __device__ __forceinline__ void set(const float (&x)[8]) { a = make_float4(x[0], x[1], x[2], x[3]); b = make_float4(x[4], x[5], x[6], x[7]); }
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void as_bf16(__nv_bfloat16 *p) const {
+        float x[8];
+        get(x);
+        Vec8<__nv_bfloat16> o;
+        o.set(x);
+        o.store(p);
+    }
+    __device__ __forceinline__ uint32_t largest() const {
+        float x[8];
+        get(x);
+        uint32_t top = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+        return top;
+    }
 };
 
 // exponent byte of a row whose largest magnitude is `a` (NaN where the row is not finite): M = top_mant 2^top_exp as float bits
@@ -92,118 +115,101 @@ template <int KIND> __device__ __forceinline__ void decode8(uint2 c, float scale
     for (int i = 0; i < 8; ++i) x[i] = kv_code<KIND>((w[i >> 2] >> (8 * (i & 3))) & 0xFFu, scale);
 }
 
-// where a slot's row of `head` starts, in elements, and its exponent
-__device__ __forceinline__ long long row_at(const KvView &kv, long long page, int tok, int head) {
-    return page * kv.stride_page + tok * kv.stride_token + head * kv.stride_head;
-}
-__device__ __forceinline__ long long exp_at(const KvView &kv, long long page, int tok, int head) {
-    return (page * kv.n_kv_heads + head) * kv.page_size + tok;
-}
-
 template <int KIND, typename T, int G, bool READ>
 __global__ void __launch_bounds__(THREADS)
-kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots) {
+kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots, int heads_each) {
     const int sub = threadIdx.x % G, d = sub * 8;
     const bool mine = d < kv.head_dim;
     const bool is_v = blockIdx.y != 0;
-    T *ext = static_cast<T *>(is_v ? rows.v : rows.k);
     char *pages = static_cast<char *>(is_v ? kv.v : kv.k);
     uint8_t *exps = is_v ? kv.v_exp : kv.k_exp;
-    constexpr int ROWS = THREADS / G;                     // rows of a block's step
-    const long long total = rows.n * kv.n_kv_heads;
-    const long long first = static_cast<long long>(blockIdx.x) * (ROWS * U) + threadIdx.x / G;
-    long long place[U], at_ext[U], at_exp[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long r = first + u * ROWS;
-        place[u] = -1;
-        at_ext[u] = -1;
-        if (r < total) {
-            const long long tok = total <= 0xFFFFFFFFll ? static_cast<uint32_t>(r) / static_cast<uint32_t>(kv.n_kv_heads) : r / kv.n_kv_heads;
-            const int head = static_cast<int>(r - tok * kv.n_kv_heads);
-            const long long slot = slots[tok];
-            at_ext[u] = tok * rows.stride_token + head * rows.stride_head + d;
-            const long long page = slot < 0 ? -1 : (slot <= 0xFFFFFFFFll ? static_cast<uint32_t>(slot) / static_cast<uint32_t>(kv.page_size) : slot / kv.page_size);
-            if (page >= 0 && page < kv.n_pages) {
-                const int t = static_cast<int>(slot - page * kv.page_size);
-                place[u] = row_at(kv, page, t, head) + d;
-                at_exp[u] = exp_at(kv, page, t, head);
-            }
+    const long long tok = static_cast<long long>(blockIdx.x) * (THREADS / G) + threadIdx.x / G;
+    const int h0 = blockIdx.z * heads_each, h1 = min(kv.n_kv_heads, h0 + heads_each);
+    // where the token's row of head 0 lies: in the caller's rows, in the pages, its exponent
+    T *ext = static_cast<T *>(is_v ? rows.v : rows.k) + tok * rows.stride_token + d;
+    long long place = -1, at_exp = 0;
+    const bool there = tok < rows.n;
+    if (there) {
+        const long long slot = slots[tok];
+        const long long page = slot < 0 ? -1 : (slot <= 0xFFFFFFFFll ? static_cast<uint32_t>(slot) / static_cast<uint32_t>(kv.page_size) : slot / kv.page_size);
+        if (page >= 0 && page < kv.n_pages) {
+            const int t = static_cast<int>(slot - page * kv.page_size);
+            place = page * kv.stride_page + t * kv.stride_token + d;
+            at_exp = page * kv.n_kv_heads * kv.page_size + t;
         }
     }
-    if constexpr (!READ) {
-        Vec8<T> in[U];
+    const bool in_pool = place >= 0;
+    for (int h = h0; h < h1; h += U) {
+        if constexpr (!READ) {
+            Vec8<T> in[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (mine && place[u] >= 0) in[u].load(ext + at_ext[u]);
+            for (int u = 0; u < U; ++u)
+                if (mine && in_pool && h + u < h1) in[u].load(ext + (h + u) * rows.stride_head);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[8];
-            if (mine && place[u] >= 0) in[u].get(x);
-            else {
+            for (int u = 0; u < U; ++u) {
+                const bool store = mine && in_pool && h + u < h1;
+                if (!store) in[u].clear();
+                if constexpr (KIND == SISO_BF16) {
+                    if (store) in[u].as_bf16(reinterpret_cast<__nv_bfloat16 *>(pages) + place + (h + u) * kv.stride_head);
+                } else {
+                    // magnitudes order like their bits, with infinities and NaN above every finite value
+                    uint32_t top = in[u].largest();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.f;
+                    for (int o = 1; o < G; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                    const bool finite = top < 0x7F800000u;
+                    const int e = finite ? exponent_of<KIND>(__uint_as_float(top)) : 0;
+                    if (!finite) in[u].clear();
+                    float x[8];
+                    in[u].get(x);
+                    if (store) *reinterpret_cast<uint2 *>(pages + place + (h + u) * kv.stride_head) = encode8<KIND>(x, inverse_scale(e));
+                    if (store && sub == 0) exps[at_exp + static_cast<long long>(h + u) * kv.page_size] = finite ? static_cast<uint8_t>(e + 127) : 255;
+                }
             }
-            if constexpr (KIND == SISO_BF16) {
-                if (mine && place[u] >= 0) {
-                    Vec8<__nv_bfloat16> o;
+        } else {
+            Vec8<__nv_bfloat16> wide[U];
+            uint2 codes[U];
+            uint32_t e[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                wide[u].clear();
+                codes[u] = make_uint2(0u, 0u);
+                e[u] = 127u;
+                if (!mine || !in_pool || h + u >= h1) continue;
+                if constexpr (KIND == SISO_BF16) wide[u].load(reinterpret_cast<const __nv_bfloat16 *>(pages) + place + (h + u) * kv.stride_head);
+                else {
+                    codes[u] = *reinterpret_cast<const uint2 *>(pages + place + (h + u) * kv.stride_head);
+                    e[u] = exps[at_exp + static_cast<long long>(h + u) * kv.page_size];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!mine || !there || h + u >= h1) continue;
+                T *dst = ext + (h + u) * rows.stride_head;
+                if constexpr (KIND == SISO_BF16 && sizeof(T) == 2) wide[u].store(dst);
+                else {
+                    float x[8];
+                    if constexpr (KIND == SISO_BF16) wide[u].get(x);
+                    else decode8<KIND>(codes[u], kv_scale(e[u]), x);
+                    Vec8<T> o;
                     o.set(x);
-                    o.store(reinterpret_cast<__nv_bfloat16 *>(pages) + place[u]);
+                    o.store(dst);
                 }
-            } else {
-                // magnitudes order like their bits, with infinities and NaN above every finite value
-                uint32_t top = 0u;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-#pragma unroll
-                for (int o = 1; o < G; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                if (place[u] < 0) continue;
-                const bool finite = top < 0x7F800000u;
-                const int e = finite ? exponent_of<KIND>(__uint_as_float(top)) : 0;
-                if (!finite) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-                }
-                if (mine) *reinterpret_cast<uint2 *>(pages + place[u]) = encode8<KIND>(x, inverse_scale(e));
-                if (sub == 0) exps[at_exp[u]] = finite ? static_cast<uint8_t>(e + 127) : 255;
             }
-        }
-    } else {
-        Vec8<__nv_bfloat16> wide[U];
-        uint2 codes[U];
-        uint32_t e[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!mine || place[u] < 0) continue;
-            if constexpr (KIND == SISO_BF16) wide[u].load(reinterpret_cast<const __nv_bfloat16 *>(pages) + place[u]);
-            else { codes[u] = *reinterpret_cast<const uint2 *>(pages + place[u]); e[u] = exps[at_exp[u]]; }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!mine || at_ext[u] < 0) continue;
-            float x[8];
-            if (place[u] < 0) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.f;
-            } else if constexpr (KIND == SISO_BF16) wide[u].get(x);
-            else decode8<KIND>(codes[u], kv_scale(e[u]), x);
-            Vec8<T> o;
-            o.set(x);
-            o.store(ext + at_ext[u]);
         }
     }
 }
 
 template <int KIND, typename T, bool READ>
 static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
-    const long long total = rows.n * kv.n_kv_heads;
     const int g = kv.head_dim <= 64 ? 8 : kv.head_dim <= 128 ? 16 : 32;
-    const long long blocks = (total + THREADS / g * U - 1) / (THREADS / g * U);
+    const long long blocks = (rows.n + THREADS / g - 1) / (THREADS / g);
     if (blocks > 0x7FFFFFFFll) return SISO_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(blocks), 2);
-    if (g == 8) kv_rows_kernel<KIND, T, 8, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
-    else if (g == 16) kv_rows_kernel<KIND, T, 16, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
-    else kv_rows_kernel<KIND, T, 32, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots);
+    // a prompt's lanes go through all heads of their token; the few tokens of a step are spread over more CTAs, a head each
+    const int heads_each = blocks >= 148 ? kv.n_kv_heads : 1;
+    const dim3 grid(static_cast<unsigned>(blocks), 2, static_cast<unsigned>((kv.n_kv_heads + heads_each - 1) / heads_each));
+    if (g == 8) kv_rows_kernel<KIND, T, 8, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
+    else if (g == 16) kv_rows_kernel<KIND, T, 16, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
+    else kv_rows_kernel<KIND, T, 32, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
     SISO_CUDA(cudaGetLastError());
     return SISO_OK;
 }

@@ -85,6 +85,7 @@ class PagedKV:
         self._check(st, "siso_kv_create")
         self._args = ctypes.create_string_buffer(_ATTENTION.size)
         self._default_scale = dim ** -0.5
+        self._none = {t: torch.empty(0, dtype=t, device=self._dev) for t in _ROW_TYPES}
 
     @classmethod
     def allocate(cls, n_layers: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
@@ -148,7 +149,7 @@ class PagedKV:
         if out is None:
             if dtype not in _ROW_TYPES:
                 raise ValueError("dtype must be float32 or bfloat16")
-            k, v = torch.empty((2, n, self.n_kv_heads, self.head_dim), dtype=dtype, device=self._dev).unbind()
+            k, v = self._none[dtype].new_empty((2, n, self.n_kv_heads, self.head_dim)).unbind()
         else:
             k, v = out
             if self._rows(k, n, "out k") is not k or self._rows(v, n, "out v") is not v or k.stride() != v.stride() or k.dtype is not v.dtype:
@@ -189,7 +190,7 @@ class PagedKV:
         if not kv_len.is_contiguous():
             kv_len = kv_len.contiguous()
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=self._dev)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.dtype is not torch.bfloat16 or out.shape != shape or out.get_device() != index or out.stride(2) != 1:
             raise ValueError("out must be a bfloat16 tensor like q with contiguous rows")
         so = out.stride()
@@ -237,12 +238,19 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: t
         raise ValueError(f"u_accept must be a float32 [{seqs}, {n_max}] tensor on {target.device}")
     if u_sample.dtype is not f32 or u_sample.shape != (seqs,) or u_sample.get_device() != index:
         raise ValueError(f"u_sample must be a float32 [{seqs}] tensor on {target.device}")
-    target, tokens, u_accept, u_sample = (t if t.is_contiguous() else t.contiguous() for t in (target, tokens, u_accept, u_sample))
+    if not target.is_contiguous():
+        target = target.contiguous()
+    if not tokens.is_contiguous():
+        tokens = tokens.contiguous()
+    if not u_accept.is_contiguous():
+        u_accept = u_accept.contiguous()
+    if not u_sample.is_contiguous():
+        u_sample = u_sample.contiguous()
     if n_drafts is not None and not n_drafts.is_contiguous():
         n_drafts = n_drafts.contiguous()
     if out is None:
-        both = torch.empty((seqs * (rows + 1),), dtype=i32, device=target.device)
-        new, accepted = both[:seqs * rows].view(seqs, rows), both[seqs * rows:]
+        new = tokens.new_empty((seqs, rows))
+        accepted = tokens.new_empty((seqs,)) if n_drafts is None else torch.empty_like(n_drafts)
     else:
         new, accepted = out
         if new.dtype is not i32 or new.shape != (seqs, rows) or not new.is_contiguous() or accepted.dtype is not i32 or accepted.shape != (seqs,) \
