@@ -439,7 +439,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&ring.empty[stage]);
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if (cur.tiles_here() > 1) {
+        if (__any_sync(0xFFFFFFFFu, cur.tiles_here() > 1)) {   // (uniform, visibly: the barriers further down cost no registers then)
             cur.step(g);
             continue;
         }

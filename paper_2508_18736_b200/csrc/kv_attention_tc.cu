@@ -403,12 +403,13 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             };
             int n;
             do {
-                n = cur.tiles_here();
+                n = __shfl_sync(0xFFFFFFFFu, cur.tiles_here(), 0);
                 wait_bar(&bars.q_full[0], q_phase, gave_up);
                 wait_bar(&bars.q_full[1], q_phase, gave_up);
                 q_phase ^= 1u;
-                // two tiles of rows, each with every tile of keys; or one twice, each with every other tile of keys
-                const bool split = cur.n_q * g.group - cur.rt * TC_ROWS <= 128;
+                // two tiles of rows, each with every tile of keys; or one twice, each with every other tile of keys.  (One loop for both:
+                // unrolled for each it spilled, six prompts 116 us and not 108)
+                const bool split = __any_sync(0xFFFFFFFFu, cur.n_q * g.group - cur.rt * TC_ROWS <= 128);
                 const int ahead = split ? 2 : 1, per_tile = split ? 1 : 2;
                 for (int j = -ahead; j < n; ++j) {
                     if (j >= 0) wait_bar(&bars.kv_full[v_stage], v_phase, gave_up);
@@ -537,7 +538,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         };
         for (bool more = true;;) {
             const int rows = cur.n_q * g.group - cur.rt * TC_ROWS;        // rows of the item from this row tile on
-            const bool split_next = rows <= 128;                      // one tile of rows twice, with every other tile of keys
+            const bool split_next = __any_sync(0xFFFFFFFFu, rows <= 128);      // (uniform, visibly)  one tile of rows twice, with every other tile of keys
             const int tile_row = split_next ? 0 : t * 128, in_tile = tile_row + lane_row;
             if (more) {   // the last scores of the item before have come, so its queries are no longer read.  8 (4) lanes share half a row
                 const uint32_t flip = g.scale_log2 < 0.f ? 0x80008000u : 0u, keep = g.scale_log2 == 0.f ? 0u : 0xFFFFFFFFu;
@@ -625,7 +626,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\t"
                     "barrier.cta.red.or.aligned.pred q, %1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
                     : "=r"(grown) : "r"(1 + t), "r"((m2 > m + 8.f || (m == -INFINITY && m2 != m)) ? 1u : 0u) : "memory");
-                if (grown) {
+                if (__any_sync(0xFFFFFFFFu, grown)) {                     // (uniform, visibly: the barriers in it cost no registers then)
                     mine_out = m2;
                     together();
                     m2 = fmaxf(m2, theirs_in);

@@ -57,23 +57,26 @@ class PagedKV:
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_layers, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = layers, pages, tokens, heads, dim
         self._dev, self._index = k.device, k.get_device()
-        self._blocks = {}
+        blocks, dev = {}, k.device
+        self._blocks = blocks
 
-        def _alloc(nbytes, stream, ctx):          # scratch from the pool of the stream it is first used on
+        # scratch from the pool of the stream it is first used on.  (The callbacks hold no reference to the handle: it has to go, and
+        # give its pages back, with the last reference to it)
+        def _alloc(nbytes, stream, ctx):
             try:
-                with torch.cuda.device(self._dev):
+                with torch.cuda.device(dev):
                     if stream:
-                        with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=self._dev)):
-                            t = torch.empty(int(nbytes), dtype=torch.uint8, device=self._dev)
+                        with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=dev)):
+                            t = torch.empty(int(nbytes), dtype=torch.uint8, device=dev)
                     else:
-                        t = torch.empty(int(nbytes), dtype=torch.uint8, device=self._dev)
+                        t = torch.empty(int(nbytes), dtype=torch.uint8, device=dev)
             except Exception:                     # out of memory -> NULL -> SISO_ERR_OOM
                 return None
-            self._blocks[t.data_ptr()] = t
+            blocks[t.data_ptr()] = t
             return t.data_ptr()
 
         def _free(ptr, ctx):
-            self._blocks.pop(ptr, None)
+            blocks.pop(ptr, None)
 
         self._alloc_cb, self._free_cb = _ALLOC_FN(_alloc), _FREE_FN(_free)
         cfg = _KvConfig(k.data_ptr(), v.data_ptr(), None if k_exp is None else k_exp.data_ptr(), None if v_exp is None else v_exp.data_ptr(),
