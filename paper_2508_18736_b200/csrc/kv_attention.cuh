@@ -15,6 +15,8 @@
 namespace siso {
 namespace kva {
 
+constexpr int TC_ROWS = 256;           // rows of a row tile of the tcgen05 kernel
+
 // n / d for 0 <= n < 2^31 and 1 <= d < 2^31, by a multiplication: m = floor(2^(31 + s) / d) + 1 with s = ceil(log2 d)
 struct FastDiv {
     uint32_t d, m, s;
@@ -92,18 +94,9 @@ template <int MR, int TK, int EXTRA> struct Cursor {
         len = seq_len(g, b);
     }
     __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR, TK>(g, len, n_q, rt); }
-    // `within`: units of sequence `seq` before this one
-    __device__ __forceinline__ void seek(const Args &g, int seq, long long within, int per_head) {
-        b = seq;
-        load_seq(g);
-        head = static_cast<int>(within / per_head);
-        int x = static_cast<int>(within - static_cast<long long>(head) * per_head);
-        for (rt = 0;; ++rt) {
-            load_span(g);
-            if (x < s.tiles + EXTRA) break;
-            x -= s.tiles + EXTRA;
-        }
-        tile = max(x - EXTRA, 0);                              // the extra units come first
+    // to the item `rt` of its head, `x` units into it; the extra units come first
+    __device__ __forceinline__ void enter(int x) {
+        tile = max(x - EXTRA, 0);
         left -= max(EXTRA - x, 0);
     }
     __device__ __forceinline__ void next_item(const Args &g) {
@@ -158,6 +151,25 @@ struct Run {
     long long end, total;
     int ctas;
 };
+constexpr int FEW_TILES = 16;          // row tiles that one thread goes through alone; the CTA takes more of them together
+
+// units of one head of the sequences b0 .. b0 + THREADS - 1 that the call has, one per thread
+template <int MR, int TK, int EXTRA, int THREADS>
+__device__ __forceinline__ int chunk_units(const Args &g, int b0, unsigned long long *buf) {
+    const int n = min(g.a.n_seqs - b0, THREADS);
+    // a thread per sequence, unless there are a few long ones: then a thread per row tile (six prompts of 4 to 15 row tiles: 108 us and 111 us)
+    if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA>(g, b0 + threadIdx.x) : 0;
+    int mine = 0;
+    for (int i = 0; i < n; ++i) {
+        int q0;
+        const int n_q = seq_queries(g, b0 + i, q0), len = seq_len(g, b0 + i), tiles = (n_q * g.group + MR - 1) / MR;
+        unsigned long long x = 0ull, all;
+        for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
+        cta_scan<THREADS>(x, all, buf);
+        if (static_cast<int>(threadIdx.x) == i) mine = static_cast<int>(all);
+    }
+    return mine;
+}
 // This CTA's run and the cursor at its start; every thread of the CTA gets the same.  False: nothing to do.  The CTA's record
 // is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
 template <int MR, int TK, int EXTRA, int THREADS>
@@ -169,8 +181,7 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     int per_head = 0;
     run.total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
-        const int b = c0 + static_cast<int>(threadIdx.x);
-        const int ph = b < g.a.n_seqs ? seq_units<MR, TK, EXTRA>(g, b) : 0;
+        const int ph = chunk_units<MR, TK, EXTRA, THREADS>(g, c0, buf);
         const unsigned long long x = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads, s = cta_scan<THREADS>(x, all, buf);
         if (c0 == 0) { mine = x; upto = s; per_head = ph; }
         run.total += static_cast<long long>(all);
@@ -180,31 +191,56 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     const unsigned long long want = static_cast<unsigned long long>(run.total * cta / run.ctas);
     run.end = run.total * (cta + 1) / run.ctas;
     cur.left = static_cast<int>(run.end - static_cast<long long>(want));
+    // buf[WARPS], buf[WARPS + 1]: what the one thread that finds it says
+    auto found = [&](bool here, unsigned long long a, unsigned long long b) {
+        __syncthreads();
+        if (threadIdx.x == 0) buf[WARPS] = ~0ull;
+        __syncthreads();
+        if (here) { buf[WARPS] = a; buf[WARPS + 1] = b; }
+        __syncthreads();
+        return buf[WARPS] != ~0ull;
+    };
     // the sequence that the first unit belongs to
     unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
-            const int b = c0 + static_cast<int>(threadIdx.x);
-            per_head = b < g.a.n_seqs ? seq_units<MR, TK, EXTRA>(g, b) : 0;
+            per_head = chunk_units<MR, TK, EXTRA, THREADS>(g, c0, buf);
             mine = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
             upto = base + cta_scan<THREADS>(mine, all, buf);
         }
+        if (found(want < upto && want >= upto - mine, (static_cast<unsigned long long>(c0 + threadIdx.x) << 32) | static_cast<uint32_t>(per_head), upto - mine)) break;
         __syncthreads();
-        if (threadIdx.x == 0) buf[WARPS] = ~0ull;
-        __syncthreads();
-        if (want < upto && want >= upto - mine) {              // exactly one thread of one chunk
-            buf[WARPS] = (static_cast<unsigned long long>(c0 + threadIdx.x) << 32) | static_cast<uint32_t>(per_head);
-            buf[WARPS + 1] = upto - mine;
-        }
         if (threadIdx.x == THREADS - 1) buf[0] = upto;
         __syncthreads();
-        const unsigned long long found = buf[WARPS];
         base = buf[0];
-        if (found != ~0ull) {
-            cur.seek(g, static_cast<int>(found >> 32), static_cast<long long>(want - buf[WARPS + 1]), static_cast<int>(found & 0xFFFFFFFFull));
-            return cur.left > 0;
-        }
     }
+    cur.b = static_cast<int>(buf[WARPS] >> 32);
+    cur.load_seq(g);
+    const unsigned long long within = want - buf[WARPS + 1];
+    const int head_units = static_cast<int>(buf[WARPS] & 0xFFFFFFFFull), tiles = (cur.n_q * g.group + MR - 1) / MR;
+    cur.head = static_cast<int>(within / head_units);
+    int x = static_cast<int>(within - static_cast<unsigned long long>(cur.head) * head_units);
+    cur.rt = 0;
+    if (tiles <= FEW_TILES) {
+        for (cur.load_span(g); x >= cur.s.tiles + EXTRA; cur.load_span(g)) {
+            x -= cur.s.tiles + EXTRA;
+            ++cur.rt;
+        }
+    } else {
+        unsigned long long before = 0ull;
+        for (int c0 = 0;; c0 += THREADS) {
+            const int rt = c0 + static_cast<int>(threadIdx.x);
+            const unsigned long long n = rt < tiles ? span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
+            const unsigned long long s = before + cta_scan<THREADS>(n, all, buf);
+            if (found(static_cast<unsigned long long>(x) < s && static_cast<unsigned long long>(x) >= s - n, static_cast<unsigned long long>(rt), s - n)) break;
+            before += all;
+        }
+        cur.rt = static_cast<int>(buf[WARPS]);
+        x -= static_cast<int>(buf[WARPS + 1]);
+        cur.load_span(g);
+    }
+    cur.enter(x);
+    return cur.left > 0;
 }
 // the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
@@ -263,8 +299,7 @@ __device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatil
 
 // joins the parts of every item that was cut; MR = rows of a row tile, D = head_dim
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s);
-// many rows per key/value head (tcgen05): row tiles of TC_ROWS
-constexpr int TC_ROWS = 256;
+// many rows per key/value head (tcgen05)
 siso_status_t launch_many_rows(Kv *h, Args &g, cudaStream_t s);
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s);
 

@@ -20,7 +20,6 @@
 namespace siso {
 namespace ver {
 
-constexpr int MAX_WARPS = 16;
 constexpr int MAX_SPLIT = 8;
 constexpr int BYTES = 64;                // of each row that a lane has in flight
 
@@ -108,12 +107,13 @@ __device__ __forceinline__ unsigned long long chunk_sum(const Residual<T> &r, in
     return sum;
 }
 
-template <typename T, int W>
-__global__ void __launch_bounds__(32 * MAX_WARPS)
+template <typename T, int W, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 verify_kernel(Args g) {
-    __shared__ unsigned long long sums[2][MAX_SPLIT * MAX_WARPS];
-    __shared__ unsigned long long scan[MAX_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = blockDim.x, warps = threads / 32;
+    constexpr int WARPS = THREADS / 32;
+    __shared__ unsigned long long sums[2][MAX_SPLIT * WARPS];
+    __shared__ unsigned long long scan[WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t rank, split;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
@@ -145,9 +145,9 @@ verify_kernel(Args g) {
     r.without = n < limit && !draft ? g.tokens[b * g.n_max + n] : -1;
 
     // ---- sums of the chunks, one per warp of the cluster
-    const int chunks = static_cast<int>(split) * warps;
+    const int chunks = static_cast<int>(split) * WARPS;
     const int chunk = ((g.vocab + chunks - 1) / chunks + 7) & ~7;      // whole pieces of 16 bytes
-    const int me = static_cast<int>(rank) * warps + warp;
+    const int me = static_cast<int>(rank) * WARPS + warp;
     unsigned long long total = 0ull;
     int pass = 0;
     for (; pass < 2; ++pass) {
@@ -170,7 +170,7 @@ verify_kernel(Args g) {
     }
 
     if (rank == 0) {
-        for (int t = threadIdx.x; t <= g.n_max; t += threads)
+        for (int t = threadIdx.x; t <= g.n_max; t += THREADS)
             if (t != n || total == 0ull) g.out[b * (g.n_max + 1) + t] = t < n ? g.tokens[b * g.n_max + t] : -1;
         if (threadIdx.x == 0) g.accepted[b] = n;
     }
@@ -194,10 +194,10 @@ verify_kernel(Args g) {
             before = __shfl_sync(0xFFFFFFFFu, upto, 31);
         }
     }
-    if (at < 0 || at / warps != static_cast<int>(rank)) return;
+    if (at < 0 || at / WARPS != static_cast<int>(rank)) return;
     // ---- the entry: consecutive ones per thread, a scan over the CTA
     const int lo = at * chunk, hi = min(g.vocab, lo + chunk);
-    const int each = (chunk + threads - 1) / threads;
+    const int each = (chunk + THREADS - 1) / THREADS;
     const int v0 = lo + static_cast<int>(threadIdx.x) * each, v1 = min(hi, v0 + each);
     unsigned long long sum = 0ull;
     for (int v = v0; v < v1; ++v) sum += weight(r.at(v));
@@ -216,14 +216,11 @@ verify_kernel(Args g) {
     }
 }
 
-template <typename T, int W>
-static siso_status_t run(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
-    // few sequences: many loads in flight on the few SMs that work; many: CTAs small enough that all of them run at once (64 x 128256
-    // fp32: 512 threads 20.5 us, 256 threads 16.8 us; one row of 32000: 6.5 us and 7.7 us)
-    const int threads = n_seqs <= 16 ? 512 : 256;
+template <typename T, int W, int THREADS>
+static siso_status_t launch(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(n_seqs * split));
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.blockDim = dim3(THREADS);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -232,9 +229,16 @@ static siso_status_t run(const Args &g, int64_t n_seqs, int split, cudaStream_t 
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    SISO_CUDA(cudaLaunchKernelEx(&cfg, verify_kernel<T, W>, g));
+    SISO_CUDA(cudaLaunchKernelEx(&cfg, verify_kernel<T, W, THREADS>, g));
     SISO_CUDA(cudaGetLastError());
     return SISO_OK;
+}
+
+template <typename T, int W>
+static siso_status_t run(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
+    // few sequences: many loads in flight on the few SMs that work; many: CTAs small enough that all of them run at once (64 x 128256
+    // fp32: 512 threads 20.5 us, 256 threads 16.8 us; one row of 32000: 6.5 us and 7.7 us)
+    return n_seqs <= 16 ? launch<T, W, 512>(g, n_seqs, split, s) : launch<T, W, 256>(g, n_seqs, split, s);
 }
 
 }  // namespace ver

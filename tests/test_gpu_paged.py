@@ -223,6 +223,27 @@ def test_long_sequences_are_split_and_joined(q_len):
     run_case("e4m3", 64, 4, 1, 64, [30001, 3], [q_len, min(q_len, 3)])
 
 
+@pytest.mark.parametrize("kind,heads,window", [("bf16", 8, 0), ("e4m3", 8, 700)])
+def test_a_prompt_of_many_row_tiles(kind, heads, window):
+    # 21,000 tokens x 8 heads: more row tiles than the kernel has threads.  Rows at the start, in the middle and at the end are compared
+    n, page, dim = 21_000, 64, 64
+    held = -(-n // page)
+    k, v, ke, ve = ref.make_pages(kind, 1, held, page, 1, dim, seed=9)
+    kv = siso.PagedKV(k, v, ke, ve)
+    table = torch.randperm(held, device="cuda").to(torch.int32)[None]
+    slots = (table[0].long()[:, None] * page + torch.arange(page, device="cuda")).reshape(-1)[:n]
+    rows = [r.double() for r in kv.read(slots, dtype=torch.float32)]
+    q = torch.randn((n, heads, dim), device="cuda").to(torch.bfloat16)
+    cu, lens = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, n], [n]))
+    out, lse = kv.attention(q, cu, lens, table, n, window=window, want_lse=True)
+    for lo in (0, 63, 10_441, n - 40):
+        hi = lo + 40
+        want = ref.attention(q[lo:hi], rows[0][:hi], rows[1][:hi], 40, window=window)
+        check_attention(out[lo:hi], lse[lo:hi], want, dim)
+    assert kv.sync_status() == 0
+    kv.close()
+
+
 @pytest.mark.parametrize("n_q", [1, 100])
 def test_page_outside_the_pool_is_reported_and_left_out(n_q):
     page = 16
