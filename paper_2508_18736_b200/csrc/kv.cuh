@@ -54,6 +54,28 @@ inline KvView kv_view(const Kv *h, int layer) {
 siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t s);
 
 #ifdef __CUDACC__
+// Launches a kernel that may be set up while the one before it in the stream still runs (programmatic dependent launch).  It calls
+// wait_for_earlier() before it touches memory.
+template <typename... Params, typename... Given>
+inline siso_status_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s, const Given &...given) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SISO_CUDA(cudaLaunchKernelEx(&cfg, kernel, given...));
+    return SISO_OK;
+}
+// Waits until the kernels before this one in the stream are complete and their writes visible.
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets a kernel that was launched early be set up.  That happens once every CTA of this one has come here, so all have their places
+// and none waits for room that the next kernel has taken.
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // 2^(byte - 127) of a stored row; 255 marks a row that held a non-finite value
 __device__ __forceinline__ float kv_scale(uint32_t byte) {
     return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);

@@ -117,7 +117,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     float *merge_ml = merge_o + S::MERGE_O;
     uint8_t *meta = reinterpret_cast<uint8_t *>(merge_ml + WARPS / 2 * 16 * NT);
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    dependents_may_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) { mbar_init(&ring.full[i], EIGHT ? 33 : 1); mbar_init(&ring.empty[i], 8); }      // 33: the bytes, and the lanes' exponents
@@ -553,7 +553,7 @@ join_kernel(const __grid_constant__ Args g) {
     constexpr int ROWS = MR / 8 < 8 ? MR / 8 : 8, WPR = 8 / ROWS;          // rows of a CTA at a time, warps of a row
     constexpr int N = D / 32;
     __shared__ float so[8][D], sml[8][2];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_earlier();
     const Record rec = g.records[blockIdx.x];
     if (!rec.valid) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -624,18 +624,7 @@ join_kernel(const __grid_constant__ Args g) {
 }
 
 template <int MR, int D> static siso_status_t run_join(const Args &g, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(g.grid), MR >= 64 ? MR / 8 : 8);
-    cfg.blockDim = dim3(256);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // its CTAs may be set up while the parts are still made
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    SISO_CUDA(cudaLaunchKernelEx(&cfg, join_kernel<MR, D>, g));
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    return launch_early(join_kernel<MR, D>, dim3(static_cast<unsigned>(g.grid), MR >= 64 ? MR / 8 : 8), 256, 0, s, g);
 }
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
     switch (mr) {

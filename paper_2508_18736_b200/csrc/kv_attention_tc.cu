@@ -52,8 +52,9 @@ template <int KIND, int D> struct Shape {
     static constexpr int SMEM = Q_BYTES + STAGES * TILE + RAWS * (RAW + RAW_META) + static_cast<int>(sizeof(Bars));
     // registers: what the CTA has at launch (96 x 640 or 72 x 896), moved to the softmax
     static constexpr int SOFTMAX_REGS = EIGHT ? 96 : 104, OTHER_REGS = EIGHT ? 40 : 64, CONVERT_REGS = 40;
-    // pairs of 16 whose exponentials are taken on the FMA pipe: the exponentials' own pipe limits bf16 (d = 64 by 15 %), instruction issue 8 bits
-    static constexpr int POLY = EIGHT ? 0 : 2;
+    // pairs of 8 whose exponentials are taken on the FMA pipe: of d = 64 their own pipe is the limit (chunk over 33333: none 735 us,
+    // two 657 us), of d = 128 (863 us; two 880 us) and of 8 bits the issue of instructions
+    static constexpr int POLY = EIGHT ? 0 : (D == 64 ? 2 : 0);
     static_assert(4 * SOFTMAX_REGS + OTHER_REGS + (EIGHT ? 2 * CONVERT_REGS : 0) == (EIGHT ? 7 * 72 : 5 * 96), "register split");
 };
 
@@ -99,14 +100,9 @@ __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r
         ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
           "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-          "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-          "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -194,7 +190,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     Bars &bars = *reinterpret_cast<Bars *>(metas + RAWS * S::RAW_META);
     unsigned long long *buf = bars.buf;
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    dependents_may_start();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
         for (int t = 0; t < 2; ++t) { mbar_init(&bars.q_full[t], 8); mbar_init(&bars.s_full[t], 1); mbar_init(&bars.p_full[t][0], 8); mbar_init(&bars.p_full[t][1], 8); mbar_init(&bars.o_done[t], 1); }
@@ -652,24 +648,31 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 }
                 const float shift = m == -INFINITY ? 0.f : -m;
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                auto weigh = [&](const uint32_t (&r)[32], int c) {
-                    uint32_t p[16];
+                // 16 columns of probabilities at a time; what waits for their way into TMEM waits behind the next 16
+                auto weigh = [&](const uint32_t (&r)[32], int from, int at) {
+                    uint32_t p[8];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float2 y = fma2(make_float2(__uint_as_float(r[2 * x]), __uint_as_float(r[2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
-                        if ((x * S::POLY) % 16 < S::POLY) y = ex2_poly(y);
+                    for (int x = 0; x < 8; ++x) {
+                        float2 y = fma2(make_float2(__uint_as_float(r[from + 2 * x]), __uint_as_float(r[from + 2 * x + 1])), make_float2(scale, scale), make_float2(shift, shift));
+                        if ((x * S::POLY) % 8 < S::POLY) y = ex2_poly(y);
                         else { y.x = ex2(y.x); y.y = ex2(y.y); }
                         sum[x & 1] = add2(sum[x & 1], y);
                         p[x] = pack(y.x, y.y, false);
                     }
-                    tmem_st_32x16(s_at + c * 16, p);
+                    tmem_st_32x8(s_at + at, p);
+                };
+                auto bring = [&](int c) {
                     tmem_st_wait();
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars.p_full[t][c]);
                 };
-                weigh(ra, 0);
-                weigh(rb, 1);
+                weigh(ra, 0, 0);
+                weigh(ra, 16, 8);
+                weigh(rb, 0, 16);
+                bring(0);
+                weigh(rb, 16, 24);
+                bring(1);
                 sum[0] = add2(sum[0], sum[1]);
                 l += sum[0].x + sum[0].y;
                 tile_phase ^= 1u;

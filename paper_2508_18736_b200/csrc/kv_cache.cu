@@ -118,6 +118,8 @@ template <int KIND> __device__ __forceinline__ void decode8(uint2 c, float scale
 template <int KIND, typename T, int G, bool READ>
 __global__ void __launch_bounds__(THREADS)
 kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots, int heads_each) {
+    wait_for_earlier();
+    dependents_may_start();
     const int sub = threadIdx.x % G, d = sub * 8;
     const bool mine = d < kv.head_dim;
     const bool is_v = blockIdx.y != 0;
@@ -207,11 +209,9 @@ static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long lon
     // a prompt's lanes go through all heads of their token; the few tokens of a step are spread over more CTAs, a head each
     const int heads_each = blocks >= 148 ? kv.n_kv_heads : 1;
     const dim3 grid(static_cast<unsigned>(blocks), 2, static_cast<unsigned>((kv.n_kv_heads + heads_each - 1) / heads_each));
-    if (g == 8) kv_rows_kernel<KIND, T, 8, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
-    else if (g == 16) kv_rows_kernel<KIND, T, 16, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
-    else kv_rows_kernel<KIND, T, 32, READ><<<grid, THREADS, 0, s>>>(kv, rows, slots, heads_each);
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    if (g == 8) return launch_early(kv_rows_kernel<KIND, T, 8, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
+    if (g == 16) return launch_early(kv_rows_kernel<KIND, T, 16, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
+    return launch_early(kv_rows_kernel<KIND, T, 32, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
 }
 template <typename T, bool READ>
 static siso_status_t run_kind(int kind, const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
