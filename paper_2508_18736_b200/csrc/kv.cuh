@@ -80,6 +80,43 @@ __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepco
 __device__ __forceinline__ float kv_scale(uint32_t byte) {
     return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
 }
+__device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t sub2_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// Codes of one row as bf16, exactly: c 2^(byte - 127) has at most 8 significant bits.  e4m3: sign, exponent and mantissa moved to their places
+// give the value times 2^-120, subnormal codes too, and the factor makes up for it.  i8: the low 7 bits as the mantissa of 128 + u,
+// less 128 or, for negative codes, 256.
+template <int KIND> struct CodeScale {
+    uint32_t factor, more;                 // a second factor where 2^(byte - 7) itself is beyond bf16
+    __device__ __forceinline__ explicit CodeScale(int byte) {
+        const int field = KIND == SISO_E4M3 ? byte + 120 : byte;
+        factor = (byte == 255 ? 0x7FC0u : field == 0 ? 0x0040u : static_cast<uint32_t>(min(field, 254)) << 7) * 0x10001u;
+        more = KIND == SISO_E4M3 && byte > 134 && byte < 255 ? (static_cast<uint32_t>(field - 254 + 127) << 7) * 0x10001u : 0u;
+    }
+    // codes 0, 2 and 1, 3 of a word
+    __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) const {
+        if constexpr (KIND == SISO_E4M3) {
+            lo = mul2_bf16(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u), factor);
+            hi = mul2_bf16(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u), factor);
+            if (more) {
+                lo = mul2_bf16(lo, more);
+                hi = mul2_bf16(hi, more);
+            }
+        } else {
+            const uint32_t x = w >> 8;
+            lo = mul2_bf16(sub2_bf16((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u), factor);
+            hi = mul2_bf16(sub2_bf16((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u), factor);
+        }
+    }
+};
 // value of one code.  e4m3: sign, 4 exponent and 3 mantissa bits moved to their places in a float give the value times
 // 2^-120, subnormal codes too
 template <int KIND> __device__ __forceinline__ float kv_code(uint32_t b, float scale) {

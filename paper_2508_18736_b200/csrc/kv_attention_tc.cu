@@ -140,17 +140,6 @@ __device__ __forceinline__ float2 ex2_poly(float2 x) {
     y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
     return y;
 }
-__device__ __forceinline__ uint32_t mul2_bf16(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t sub2_bf16(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
 // Lane i of every four has pieces 0 to 3 of row i: afterwards it has piece i of rows 0 to 3
 __device__ __forceinline__ void swap_piece(uint4 &keep, uint4 &give, int mask, bool upper) {      // lanes with `upper` give `keep`'s place away
     const uint4 x = upper ? keep : give;
@@ -163,19 +152,6 @@ __device__ __forceinline__ void turn4(uint4 (&w)[4], int lane) {
     swap_piece(w[2], w[3], 1, lane & 1);
     swap_piece(w[0], w[2], 2, lane & 2);
     swap_piece(w[1], w[3], 2, lane & 2);
-}
-
-// 4 codes as bf16 values: (0, 2) and (1, 3).  e4m3: sign, exponent and mantissa moved to their places give the value times 2^-120, subnormal
-// codes too; `factor` makes up for it.  i8: the low 7 bits as the mantissa of 128 + u less 128 or, for negative codes, 256.
-template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t factor, uint32_t &lo, uint32_t &hi) {
-    if constexpr (KIND == SISO_E4M3) {
-        lo = mul2_bf16(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u), factor);
-        hi = mul2_bf16(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u), factor);
-    } else {
-        const uint32_t x = w >> 8;
-        lo = mul2_bf16(sub2_bf16((w & 0x007F007Fu) | 0x43004300u, (w & 0x00800080u) | 0x43004300u), factor);
-        hi = mul2_bf16(sub2_bf16((x & 0x007F007Fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u), factor);
-    }
 }
 
 template <int KIND, int D>
@@ -239,18 +215,11 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     for (int i = 0; i < MINE / PER; ++i) {
                         const int x = PER == 4 ? (i & 1) << 6 : 0;
                         const uint4 w = *reinterpret_cast<const uint4 *>(src + (src0 ^ x) + i * PER * RB);
-                        const int e = exps[i * PER];
-                        const uint32_t f16 = e == 255 ? 0x7FC0u : static_cast<uint32_t>(KIND == SISO_E4M3 ? min(e + 120, 254) : e) << 7;
-                        const uint32_t factor = f16 * 0x10001u;
+                        const CodeScale<KIND> scale(exps[i * PER]);
                         const uint32_t in[4] = {w.x, w.y, w.z, w.w};
                         uint32_t out[8];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) widen<KIND>(in[k], factor, out[2 * k], out[2 * k + 1]);
-                        if (KIND == SISO_E4M3 && e > 134 && e < 255) {              // 2^(e - 7) itself is beyond bf16
-                            const uint32_t more = static_cast<uint32_t>(e - 134 + 127) << 7;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) out[k] = mul2_bf16(out[k], more * 0x10001u);
-                        }
+                        for (int k = 0; k < 4; ++k) scale.widen(in[k], out[2 * k], out[2 * k + 1]);
                         if (left < TK && r0 + i * PER >= left) {                    // anything may stand there
 #pragma unroll
                             for (int k = 0; k < 8; ++k) out[k] = 0u;

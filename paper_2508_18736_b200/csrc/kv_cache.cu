@@ -10,8 +10,8 @@
 // byte 255 and reads back as NaN throughout.
 //
 // Both kernels move bytes: they are bound by HBM for prompts and by latency for a step's few tokens.  G lanes own the rows of one
-// token with 8 values each (one 16-byte load of bf16), so the maximum takes log2 G shuffles; they look the slot up once and go
-// through heads, U rows in flight.
+// token with 16 values each, so the maximum takes log2 G shuffles; they look the slot up once and go through heads, U rows in
+// flight.  (With 8 values a lane what a row costs beside its values made issue the limit: 23 us and 19 us for 16385 tokens x 8 x 128.)
 #include <cuda_fp8.h>
 
 #include <cstring>
@@ -23,7 +23,7 @@ namespace siso {
 namespace kvc {
 
 constexpr int THREADS = 256;
-constexpr int U = 4;
+constexpr int U = 2;                     // (16385 x 8 x 128: 39.1 us, four 37.6; but 1000 tokens 6.3 and 8.0, fp32 rows 30.5 and 46.6)
 
 struct Rows {                     // n tokens x heads rows of the caller's K and V
     void *k, *v;
@@ -102,9 +102,11 @@ template <int KIND> __device__ __forceinline__ uint2 encode8(const float (&x)[8]
             const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * h + 2] * inv, x[4 * h + 3] * inv), __NV_SATFINITE, __NV_E4M3);
             w[h] = lo | (hi << 16);
         } else {
-            w[h] = 0u;
+            // 1.5 2^23 added: rounded to a whole number (nearest, ties to even) that stands in the low bits, negative ones in two's complement
+            uint32_t c[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[h] |= (static_cast<uint32_t>(__float2int_rn(x[4 * h + i] * inv)) & 0xFFu) << (8 * i);
+            for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(fmaf(x[4 * h + i], inv, 12582912.f));
+            w[h] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
         }
     }
     return make_uint2(w[0], w[1]);
@@ -120,98 +122,125 @@ __global__ void __launch_bounds__(THREADS)
 kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots, int heads_each) {
     wait_for_earlier();
     dependents_may_start();
-    const int sub = threadIdx.x % G, d = sub * 8;
-    const bool mine = d < kv.head_dim;
+    const int sub = threadIdx.x % G, d = sub * 8;          // a lane has the values d .. d + 7 and d + 8 G .. d + 8 G + 7: neighbours load neighbours
+    const bool mine[2] = {d < kv.head_dim, d + 8 * G < kv.head_dim};
     const bool is_v = blockIdx.y != 0;
     char *pages = static_cast<char *>(is_v ? kv.v : kv.k);
     uint8_t *exps = is_v ? kv.v_exp : kv.k_exp;
+    constexpr int EB = KIND == SISO_BF16 ? 2 : 1;
     const long long tok = static_cast<long long>(blockIdx.x) * (THREADS / G) + threadIdx.x / G;
     const int h0 = blockIdx.z * heads_each, h1 = min(kv.n_kv_heads, h0 + heads_each);
-    // where the token's row of head 0 lies: in the caller's rows, in the pages, its exponent
-    T *ext = static_cast<T *>(is_v ? rows.v : rows.k) + tok * rows.stride_token + d;
-    long long place = -1, at_exp = 0;
+    // the token's row of head h0: in the caller's rows, in the pages, its exponent
+    T *ext = static_cast<T *>(is_v ? rows.v : rows.k) + tok * rows.stride_token + h0 * rows.stride_head + d;
     const bool there = tok < rows.n;
+    bool in_pool = false;
     if (there) {
         const long long slot = slots[tok];
         const long long page = slot < 0 ? -1 : (slot <= 0xFFFFFFFFll ? static_cast<uint32_t>(slot) / static_cast<uint32_t>(kv.page_size) : slot / kv.page_size);
         if (page >= 0 && page < kv.n_pages) {
             const int t = static_cast<int>(slot - page * kv.page_size);
-            place = page * kv.stride_page + t * kv.stride_token + d;
-            at_exp = page * kv.n_kv_heads * kv.page_size + t;
+            in_pool = true;
+            pages += (page * kv.stride_page + t * kv.stride_token + h0 * kv.stride_head + d) * EB;
+            exps += (page * kv.n_kv_heads + h0) * kv.page_size + t;
         }
     }
-    const bool in_pool = place >= 0;
     for (int h = h0; h < h1; h += U) {
         if constexpr (!READ) {
-            Vec8<T> in[U];
+            Vec8<T> in[U][2];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (mine && in_pool && h + u < h1) in[u].load(ext + (h + u) * rows.stride_head);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (mine[x] && there && h + u < h1) in[u][x].load(ext + u * rows.stride_head + 8 * G * x);
+                    else in[u][x].clear();
+                }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const bool store = mine && in_pool && h + u < h1;
-                if (!store) in[u].clear();
+                const bool store = in_pool && h + u < h1;
+                char *dst = pages + u * kv.stride_head * EB;
                 if constexpr (KIND == SISO_BF16) {
-                    if (store) in[u].as_bf16(reinterpret_cast<__nv_bfloat16 *>(pages) + place + (h + u) * kv.stride_head);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (store && mine[x]) in[u][x].as_bf16(reinterpret_cast<__nv_bfloat16 *>(dst) + 8 * G * x);
                 } else {
                     // magnitudes order like their bits, with infinities and NaN above every finite value
-                    uint32_t top = in[u].largest();
+                    uint32_t top = max(in[u][0].largest(), in[u][1].largest());
 #pragma unroll
                     for (int o = 1; o < G; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
                     const bool finite = top < 0x7F800000u;
                     const int e = finite ? exponent_of<KIND>(__uint_as_float(top)) : 0;
-                    if (!finite) in[u].clear();
-                    float x[8];
-                    in[u].get(x);
-                    if (store) *reinterpret_cast<uint2 *>(pages + place + (h + u) * kv.stride_head) = encode8<KIND>(x, inverse_scale(e));
-                    if (store && sub == 0) exps[at_exp + static_cast<long long>(h + u) * kv.page_size] = finite ? static_cast<uint8_t>(e + 127) : 255;
+                    const float inv = inverse_scale(e);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (!finite) in[u][x].clear();
+                        float y[8];
+                        in[u][x].get(y);
+                        if (store && mine[x]) *reinterpret_cast<uint2 *>(dst + 8 * G * x) = encode8<KIND>(y, inv);
+                    }
+                    if (store && sub == 0) exps[u * kv.page_size] = finite ? static_cast<uint8_t>(e + 127) : 255;
                 }
             }
         } else {
-            Vec8<__nv_bfloat16> wide[U];
-            uint2 codes[U];
+            Vec8<__nv_bfloat16> wide[U][2];
+            uint2 codes[U][2];
             uint32_t e[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                wide[u].clear();
-                codes[u] = make_uint2(0u, 0u);
                 e[u] = 127u;
-                if (!mine || !in_pool || h + u >= h1) continue;
-                if constexpr (KIND == SISO_BF16) wide[u].load(reinterpret_cast<const __nv_bfloat16 *>(pages) + place + (h + u) * kv.stride_head);
-                else {
-                    codes[u] = *reinterpret_cast<const uint2 *>(pages + place + (h + u) * kv.stride_head);
-                    e[u] = exps[at_exp + static_cast<long long>(h + u) * kv.page_size];
+                if (KIND != SISO_BF16 && in_pool && h + u < h1) e[u] = exps[u * kv.page_size];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const char *src = pages + (u * kv.stride_head + 8 * G * x) * EB;
+                    wide[u][x].clear();
+                    codes[u][x] = make_uint2(0u, 0u);
+                    if (!mine[x] || !in_pool || h + u >= h1) continue;
+                    if constexpr (KIND == SISO_BF16) wide[u][x].load(reinterpret_cast<const __nv_bfloat16 *>(src));
+                    else codes[u][x] = *reinterpret_cast<const uint2 *>(src);
                 }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (!mine || !there || h + u >= h1) continue;
-                T *dst = ext + (h + u) * rows.stride_head;
-                if constexpr (KIND == SISO_BF16 && sizeof(T) == 2) wide[u].store(dst);
-                else {
-                    float x[8];
-                    if constexpr (KIND == SISO_BF16) wide[u].get(x);
-                    else decode8<KIND>(codes[u], kv_scale(e[u]), x);
-                    Vec8<T> o;
-                    o.set(x);
-                    o.store(dst);
+                if (!there || h + u >= h1) continue;
+                const CodeScale<KIND> scale(static_cast<int>(e[u]));
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!mine[x]) continue;
+                    T *dst = ext + u * rows.stride_head + 8 * G * x;
+                    if constexpr (KIND == SISO_BF16 && sizeof(T) == 2) wide[u][x].store(dst);
+                    else if constexpr (KIND != SISO_BF16 && sizeof(T) == 2) {
+                        uint32_t w[4];
+                        scale.widen(codes[u][x].x, w[0], w[1]);
+                        scale.widen(codes[u][x].y, w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(dst) = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[0], w[1], 0x7632),
+                                                                    __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[2], w[3], 0x7632));
+                    } else {
+                        float y[8];
+                        if constexpr (KIND == SISO_BF16) wide[u][x].get(y);
+                        else decode8<KIND>(codes[u][x], kv_scale(e[u]), y);
+                        Vec8<T> o;
+                        o.set(y);
+                        o.store(dst);
+                    }
                 }
             }
         }
+        ext += U * rows.stride_head;
+        pages += U * kv.stride_head * EB;
+        exps += U * kv.page_size;
     }
 }
 
 template <int KIND, typename T, bool READ>
 static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
-    const int g = kv.head_dim <= 64 ? 8 : kv.head_dim <= 128 ? 16 : 32;
+    const int g = kv.head_dim <= 64 ? 4 : kv.head_dim <= 128 ? 8 : 16;
     const long long blocks = (rows.n + THREADS / g - 1) / (THREADS / g);
     if (blocks > 0x7FFFFFFFll) return SISO_ERR_UNSUPPORTED;
     // a prompt's lanes go through all heads of their token; the few tokens of a step are spread over more CTAs, a head each
     const int heads_each = blocks >= 148 ? kv.n_kv_heads : 1;
     const dim3 grid(static_cast<unsigned>(blocks), 2, static_cast<unsigned>((kv.n_kv_heads + heads_each - 1) / heads_each));
+    if (g == 4) return launch_early(kv_rows_kernel<KIND, T, 4, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
     if (g == 8) return launch_early(kv_rows_kernel<KIND, T, 8, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
-    if (g == 16) return launch_early(kv_rows_kernel<KIND, T, 16, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
-    return launch_early(kv_rows_kernel<KIND, T, 32, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
+    return launch_early(kv_rows_kernel<KIND, T, 16, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
 }
 template <typename T, bool READ>
 static siso_status_t run_kind(int kind, const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
