@@ -127,8 +127,8 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     }
     __syncthreads();
     Run run;
-    Cursor<MR, TK, 0> cur;
-    if (!locate<MR, TK, 0, S::THREADS>(g, run, cur, buf)) return;
+    Cursor<MR, TK, 1, 2> cur;            // an item's beginning and end: half a tile
+    if (!locate<MR, TK, 1, 2, S::THREADS>(g, run, cur, buf)) return;
     volatile int *gave_up = &ring.gave_up;
 
     // registers move from the producers to the consumers: WARPS of CONSUMER_REGS and 4 of PRODUCER_REGS make what the CTA has
@@ -448,6 +448,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         const int t_end = cur.tile + 1;                       // tiles [t_begin, t_end) of the item were done here
         const int done_b = cur.b, done_head = cur.head, done_rt = cur.rt, done_q0 = cur.q0, done_rows = cur.n_q * g.group, done_tiles = cur.s.tiles;
         const bool whole = t_begin == 0 && t_end == done_tiles, began_before = t_begin > 0;
+        const int done_left = cur.left;
         more = cur.step(g);
         t_begin = 0;
         if (more) fetch_q();
@@ -539,7 +540,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     }
                 }
         }
-        if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of(run, done_b, done_head, done_rt, done_tiles, t_end);
+        if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of<2>(run, done_left, done_b, done_head, done_rt, done_tiles, t_end - 1);
         if (more) begin_item();
     }
 }

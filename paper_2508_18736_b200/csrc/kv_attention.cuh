@@ -3,9 +3,9 @@
 //
 // The queries of one sequence that share a key/value head form its rows: row r is token r / group, query head
 // kv_head * group + r % group.  An item is (sequence, key/value head, tile of MR rows); its keys are taken in tiles of TK, and
-// one tile of one item is a unit.  The units of a call, in the order (sequence, head, row tile, key tile), are dealt to the
+// one tile of one item is a unit of work.  The units of a call, in the order (sequence, head, row tile, key tile), are dealt to the
 // CTAs in equal contiguous runs, so CTAs are equally loaded whatever the lengths are, and one long sequence spreads over
-// all of them.  An item counts a few units more for its beginning and end.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
+// all of them.  A tile may count more than one unit, and an item counts some more for its beginning and end.  A CTA that holds all units of an item writes its output; otherwise it writes a partial result
 // (unnormalised output, maximum, sum), and a second small kernel joins the parts of an item in a fixed order.
 #pragma once
 
@@ -75,30 +75,25 @@ template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g,
     s.tiles = max(1, (s.hi + TK - 1) / TK - s.tile0);       // a row tile that sees nothing is one unit that writes zeros
     return s;
 }
-// units of one key/value head of sequence b; an item counts EXTRA more than its key tiles, for its beginning and end
-template <int MR, int TK, int EXTRA> __device__ __forceinline__ int seq_units(const Args &g, int b) {
+// units of one key/value head of sequence b: a key tile counts W, and an item EXTRA more, for its beginning and end
+template <int MR, int TK, int EXTRA, int W> __device__ __forceinline__ int seq_units(const Args &g, int b) {
     int q0;
     const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
     int units = 0;
-    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
+    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
     return units;
 }
 
 // A place in this CTA's run of units: an item and a key tile of it.
-template <int MR, int TK, int EXTRA> struct Cursor {
+template <int MR, int TK, int EXTRA, int W> struct Cursor {
     int b, head, rt, q0, n_q, len, tile;
-    int left;                                                  // units of the run that are left, this tile's included
+    int left;                                                  // units from this tile's first to the run's end
     Span s;
     __device__ __forceinline__ void load_seq(const Args &g) {
         n_q = seq_queries(g, b, q0);
         len = seq_len(g, b);
     }
     __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR, TK>(g, len, n_q, rt); }
-    // to the item `rt` of its head, `x` units into it; the extra units come first
-    __device__ __forceinline__ void enter(int x) {
-        tile = max(x - EXTRA, 0);
-        left -= max(EXTRA - x, 0);
-    }
     __device__ __forceinline__ void next_item(const Args &g) {
         tile = 0;
         if ((rt + 1) * MR < n_q * g.group) ++rt;
@@ -111,12 +106,22 @@ template <int MR, int TK, int EXTRA> struct Cursor {
         }
         load_span(g);
     }
+    // from the item `rt` of its head, `x` units into it, to the first tile that begins there or later: a tile belongs to the run that
+    // its first unit lies in
+    __device__ __forceinline__ void enter(const Args &g, int x) {
+        tile = max(x - EXTRA + W - 1, 0) / W;
+        left -= EXTRA + W * tile - x;
+        if (left > 0 && tile == s.tiles) {
+            left -= EXTRA;
+            if (left > 0) next_item(g);
+        }
+    }
     // key tiles of this item that belong to the run
-    __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, left); }
+    __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, (left + W - 1) / W); }
     // n <= tiles_here() tiles further; false: the run is over
     __device__ __forceinline__ bool step(const Args &g, int n = 1) {
         tile += n;
-        left -= n;
+        left -= W * n;
         if (left > 0 && tile == s.tiles) {
             left -= EXTRA;
             if (left > 0) next_item(g);
@@ -154,17 +159,17 @@ struct Run {
 constexpr int FEW_TILES = 16;          // row tiles that one thread goes through alone; the CTA takes more of them together
 
 // units of one head of the sequences b0 .. b0 + THREADS - 1 that the call has, one per thread
-template <int MR, int TK, int EXTRA, int THREADS>
+template <int MR, int TK, int EXTRA, int W, int THREADS>
 __device__ __forceinline__ int chunk_units(const Args &g, int b0, unsigned long long *buf) {
     const int n = min(g.a.n_seqs - b0, THREADS);
     // a thread per sequence, unless there are a few long ones: then a thread per row tile (six prompts of 4 to 15 row tiles: 108 us and 111 us)
-    if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA>(g, b0 + threadIdx.x) : 0;
+    if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA, W>(g, b0 + threadIdx.x) : 0;
     int mine = 0;
     for (int i = 0; i < n; ++i) {
         int q0;
         const int n_q = seq_queries(g, b0 + i, q0), len = seq_len(g, b0 + i), tiles = (n_q * g.group + MR - 1) / MR;
         unsigned long long x = 0ull, all;
-        for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
+        for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
         cta_scan<THREADS>(x, all, buf);
         if (static_cast<int>(threadIdx.x) == i) mine = static_cast<int>(all);
     }
@@ -172,8 +177,8 @@ __device__ __forceinline__ int chunk_units(const Args &g, int b0, unsigned long 
 }
 // This CTA's run and the cursor at its start; every thread of the CTA gets the same.  False: nothing to do.  The CTA's record
 // is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
-template <int MR, int TK, int EXTRA, int THREADS>
-__device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA> &cur, unsigned long long *buf) {
+template <int MR, int TK, int EXTRA, int W, int THREADS>
+__device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA, W> &cur, unsigned long long *buf) {
     constexpr int WARPS = THREADS / 32;
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) g.records[cta].valid = 0;
@@ -181,12 +186,12 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     int per_head = 0;
     run.total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
-        const int ph = chunk_units<MR, TK, EXTRA, THREADS>(g, c0, buf);
+        const int ph = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
         const unsigned long long x = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads, s = cta_scan<THREADS>(x, all, buf);
         if (c0 == 0) { mine = x; upto = s; per_head = ph; }
         run.total += static_cast<long long>(all);
     }
-    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), run.total));
+    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + W - 1) / W));      // (so that every run within an item has a tile)
     if (cta >= run.ctas) return false;
     const unsigned long long want = static_cast<unsigned long long>(run.total * cta / run.ctas);
     run.end = run.total * (cta + 1) / run.ctas;
@@ -204,7 +209,7 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
-            per_head = chunk_units<MR, TK, EXTRA, THREADS>(g, c0, buf);
+            per_head = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
             mine = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
             upto = base + cta_scan<THREADS>(mine, all, buf);
         }
@@ -222,15 +227,15 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     int x = static_cast<int>(within - static_cast<unsigned long long>(cur.head) * head_units);
     cur.rt = 0;
     if (tiles <= FEW_TILES) {
-        for (cur.load_span(g); x >= cur.s.tiles + EXTRA; cur.load_span(g)) {
-            x -= cur.s.tiles + EXTRA;
+        for (cur.load_span(g); x >= W * cur.s.tiles + EXTRA; cur.load_span(g)) {
+            x -= W * cur.s.tiles + EXTRA;
             ++cur.rt;
         }
     } else {
         unsigned long long before = 0ull;
         for (int c0 = 0;; c0 += THREADS) {
             const int rt = c0 + static_cast<int>(threadIdx.x);
-            const unsigned long long n = rt < tiles ? span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
+            const unsigned long long n = rt < tiles ? W * span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
             const unsigned long long s = before + cta_scan<THREADS>(n, all, buf);
             if (found(static_cast<unsigned long long>(x) < s && static_cast<unsigned long long>(x) >= s - n, static_cast<unsigned long long>(rt), s - n)) break;
             before += all;
@@ -239,16 +244,17 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
         x -= static_cast<int>(buf[WARPS + 1]);
         cur.load_span(g);
     }
-    cur.enter(x);
+    cur.enter(g, x);
     return cur.left > 0;
 }
 // the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
     return static_cast<int>(((u + 1) * ctas - 1) / total);
 }
-// what is noted of an item whose first part ends this CTA's run at key tile `tile_end`
-__device__ __forceinline__ Record record_of(const Run &run, int b, int head, int row_tile, int tiles, int tile_end) {
-    return Record{1, b, head, row_tile, cta_of(run.end + (tiles - tile_end) - 1, run.total, run.ctas) - static_cast<int>(blockIdx.x) + 1};
+// what is noted of an item whose first part ends this CTA's run; tile `tile` of it begins `left` units before the run's end
+template <int W>
+__device__ __forceinline__ Record record_of(const Run &run, int left, int b, int head, int row_tile, int tiles, int tile) {
+    return Record{1, b, head, row_tile, cta_of(run.end - left + W * (tiles - 1 - tile), run.total, run.ctas) - static_cast<int>(blockIdx.x) + 1};
 }
 // Where a part goes: a CTA's run has at most one item that began before it (place 0) and one that goes on after it (place 1).
 __device__ __forceinline__ long long part_place(int cta, bool began_before) { return 2ll * cta + (began_before ? 0 : 1); }

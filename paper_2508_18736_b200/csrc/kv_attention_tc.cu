@@ -177,10 +177,10 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    Cursor<TC_ROWS, TK, EXTRA> cur;
+    Cursor<TC_ROWS, TK, EXTRA, 1> cur;
     {
         Run run;
-        if (!locate<TC_ROWS, TK, EXTRA, S::THREADS>(g, run, cur, buf)) return;
+        if (!locate<TC_ROWS, TK, EXTRA, 1, S::THREADS>(g, run, cur, buf)) return;
         if (threadIdx.x == 0) bars.run = run;
     }
     if (warp == 16) {
@@ -646,7 +646,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 l += sum[0].x + sum[0].y;
                 tile_phase ^= 1u;
             }
-            if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) g.records[blockIdx.x] = record_of(bars.run, cur.b, cur.head, cur.rt, cur.s.tiles, n);
+            if (threadIdx.x == 0 && cur.tile == 0 && n < cur.s.tiles) g.records[blockIdx.x] = record_of<1>(bars.run, cur.left, cur.b, cur.head, cur.rt, cur.s.tiles, 0);
             unit += n;
             more = cur.step(g, n);
         }
