@@ -1,7 +1,8 @@
 """B200 (sm_100a) kernels for the hot path of a centroid-based semantic cache: exact batched
 cosine lookup with top-k and a per-query hit threshold, running-mean hit updates,
-MergeCentroids / FilteringCentroids and spare-space insertion, behind the C ABI of
-``include/siso.h``.  This package is the thin Python binding: it marshals torch tensors to
+MergeCentroids / FilteringCentroids and spare-space insertion, and the language model's side of a miss or a near
+hit: a paged key/value cache quantised as it is written, attention of new tokens over it and the verification of
+drafted tokens; behind the C ABI of ``include/siso.h``.  This package is the thin Python binding: it marshals torch tensors to
 pointers and calls ``libsiso.so``; every step runs in the library's own CUDA kernels."""
 from .binding import (ACCESS_INF, EVICT_DECAY, MERGE_SIZES_ONLY, MERGE_WEIGHTED_MEAN, OPT_LOOKUP_PATH,
                       OPT_MERGE_MAX_CANDIDATES, OPT_MERGE_PATH, OPT_STREAM_FUSED, OPT_TENSOR_CTA_PAIR, OPT_SWEEP_FINALIZE,

@@ -20,7 +20,6 @@
 namespace siso {
 namespace ver {
 
-constexpr int MAX_SPLIT = 8;
 constexpr int BYTES = 64;                // of each row that a lane has in flight
 
 struct Args {
@@ -107,16 +106,16 @@ __device__ __forceinline__ unsigned long long chunk_sum(const Residual<T> &r, in
     return sum;
 }
 
-template <typename T, int W, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+template <typename T, int W, int THREADS, int SPLIT>
+__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(THREADS)
 verify_kernel(Args g) {
     constexpr int WARPS = THREADS / 32;
-    __shared__ unsigned long long sums[2][MAX_SPLIT * WARPS];
+    __shared__ unsigned long long sums[2][SPLIT * WARPS];
     __shared__ unsigned long long scan[WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t rank, split;
+    uint32_t rank;
+    constexpr int split = SPLIT;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
     const long long b = blockIdx.x / split;
 
     // ---- which drafts stand: every warp finds it for itself
@@ -145,7 +144,7 @@ verify_kernel(Args g) {
     r.without = n < limit && !draft ? g.tokens[b * g.n_max + n] : -1;
 
     // ---- sums of the chunks, one per warp of the cluster
-    const int chunks = static_cast<int>(split) * WARPS;
+    const int chunks = split * WARPS;
     const int chunk = ((g.vocab + chunks - 1) / chunks + 7) & ~7;      // whole pieces of 16 bytes
     const int me = static_cast<int>(rank) * WARPS + warp;
     unsigned long long total = 0ull;
@@ -154,7 +153,7 @@ verify_kernel(Args g) {
         const int lo = min(g.vocab, me * chunk), hi = min(g.vocab, lo + chunk);
         unsigned long long sum = chunk_sum<T, W>(r, lo, hi, lane);
         sum = warp_sum(sum);
-        if (lane < static_cast<int>(split)) {
+        if (lane < split) {
             const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[pass][me]));
             uint32_t there;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(lane));
@@ -216,29 +215,21 @@ verify_kernel(Args g) {
     }
 }
 
-template <typename T, int W, int THREADS>
-static siso_status_t launch(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(n_seqs * split));
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(split);
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    SISO_CUDA(cudaLaunchKernelEx(&cfg, verify_kernel<T, W, THREADS>, g));
+// (the cluster's size is the kernel's own: 192 x 50257 bf16 13.8 us with a size given at launch, 12.8 us so)
+template <typename T, int W, int THREADS, int SPLIT> static siso_status_t launch(const Args &g, int64_t n_seqs, cudaStream_t s) {
+    verify_kernel<T, W, THREADS, SPLIT><<<static_cast<unsigned>(n_seqs * SPLIT), THREADS, 0, s>>>(g);
     SISO_CUDA(cudaGetLastError());
     return SISO_OK;
 }
-
-template <typename T, int W>
-static siso_status_t run(const Args &g, int64_t n_seqs, int split, cudaStream_t s) {
-    // few sequences: many loads in flight on the few SMs that work; many: CTAs small enough that all of them run at once (64 x 128256
-    // fp32: 512 threads 20.5 us, 256 threads 16.8 us; one row of 32000: 6.5 us and 7.7 us)
-    return n_seqs <= 16 ? launch<T, W, 512>(g, n_seqs, split, s) : launch<T, W, 256>(g, n_seqs, split, s);
+template <typename T, int W> static siso_status_t run(const Args &g, int64_t n_seqs, cudaStream_t s) {
+    // A sequence is shared by as many CTAs as give each of the 148 SMs a few.  Few sequences: many loads in flight on the few SMs that work;
+    // many: CTAs small enough that all of them run at once (64 x 128256 fp32: 512 threads 20.5 us, 256 threads 16.8 us; one row of
+    // 32000: 6.5 us and 7.7 us)
+    if (n_seqs <= 16) return launch<T, W, 512, 8>(g, n_seqs, s);
+    if (n_seqs <= 64) return launch<T, W, 256, 8>(g, n_seqs, s);
+    if (n_seqs <= 128) return launch<T, W, 256, 4>(g, n_seqs, s);
+    if (n_seqs <= 256) return launch<T, W, 256, 2>(g, n_seqs, s);
+    return launch<T, W, 256, 1>(g, n_seqs, s);
 }
 
 }  // namespace ver
@@ -254,12 +245,10 @@ extern "C" siso_status_t siso_verify_drafts(const void *d_target, const void *d_
     if (n_seqs == 0) return SISO_OK;
     if (!d_target || !d_u_sample || !d_out || !d_accepted || (n_max > 0 && (!d_tokens || !d_u_accept))) return SISO_ERR_INVALID_ARG;
     if (vocab > (1 << 24) || n_seqs > (1ll << 27)) return SISO_ERR_UNSUPPORTED;
-    // A sequence is shared by as many CTAs as fill the GPU's 148 SMs with a few CTAs each
-    const int split = n_seqs <= 64 ? 8 : n_seqs <= 128 ? 4 : n_seqs <= 256 ? 2 : 1;
     const ver::Args g{d_target, n_max > 0 ? d_draft : nullptr, d_tokens, d_n_drafts, d_u_accept, d_u_sample, d_out, d_accepted, n_max, vocab};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     // 16 bytes at a time where every row starts on a boundary of 16 bytes
     const bool wide = vocab % (dtype == SISO_F32 ? 4 : 8) == 0 && ((reinterpret_cast<uintptr_t>(d_target) | reinterpret_cast<uintptr_t>(g.draft)) & 15u) == 0;
-    if (dtype == SISO_F32) return wide ? ver::run<float, 4>(g, n_seqs, split, s) : ver::run<float, 1>(g, n_seqs, split, s);
-    return wide ? ver::run<__nv_bfloat16, 8>(g, n_seqs, split, s) : ver::run<__nv_bfloat16, 1>(g, n_seqs, split, s);
+    if (dtype == SISO_F32) return wide ? ver::run<float, 4>(g, n_seqs, s) : ver::run<float, 1>(g, n_seqs, s);
+    return wide ? ver::run<__nv_bfloat16, 8>(g, n_seqs, s) : ver::run<__nv_bfloat16, 1>(g, n_seqs, s);
 }

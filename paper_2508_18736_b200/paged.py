@@ -152,7 +152,8 @@ class PagedKV:
         if out is None:
             if dtype not in _ROW_TYPES:
                 raise ValueError("dtype must be float32 or bfloat16")
-            k, v = self._none[dtype].new_empty((2, n, self.n_kv_heads, self.head_dim)).unbind()
+            k = self._none[dtype].new_empty((n, self.n_kv_heads, self.head_dim))
+            v = torch.empty_like(k)
         else:
             k, v = out
             if self._rows(k, n, "out k") is not k or self._rows(v, n, "out v") is not v or k.stride() != v.stride() or k.dtype is not v.dtype:
