@@ -15,12 +15,12 @@
 // up to 8 CTAs shares a sequence: each warp sums the weights of one contiguous chunk, the chunk sums go to every CTA of the
 // cluster through distributed shared memory, and the CTA that owns the chunk with the crossing looks at it again (it comes
 // from L2) with a few consecutive entries per thread.  One launch, no scratch memory.
+// Measured with rows in HBM: 64 x 128256 fp32 (66 MB) 13.4 us, 4.9 TB/s; 192 x 50257 bf16 (39 MB, rows not aligned) 13.6 us, 2.8 TB/s; one
+// sequence of 32000 fp32 3.8 us, most of it the launch and three round trips to memory (which drafts stand, the row, the crossing).
 #include "common.cuh"
 
 namespace siso {
 namespace ver {
-
-constexpr int BYTES = 64;                // of each row that a lane has in flight
 
 struct Args {
     const void *target, *draft;          // [n_seqs, n_max + 1, vocab], [n_seqs, n_max, vocab] or NULL
@@ -32,6 +32,17 @@ struct Args {
 
 template <typename T> __device__ __forceinline__ float value(const T *p) {
     if constexpr (sizeof(T) == 2) return __bfloat162float(*p); else return *p;
+}
+// Loads that stay where they are written: left to itself the compiler takes them one by one to save registers
+__device__ __forceinline__ float load_now(const float *p) {
+    float x;
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(x) : "l"(p));
+    return x;
+}
+__device__ __forceinline__ float load_now(const __nv_bfloat16 *p) {
+    uint16_t x;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(x) : "l"(p));
+    return __uint_as_float(static_cast<uint32_t>(x) << 16);
 }
 // 38-bit weight of a probability or a difference of two; NaN and negative values weigh nothing
 __device__ __forceinline__ unsigned long long weight(float r) { return __float2ull_rz(__saturatef(r) * 274877906944.f); }
@@ -60,48 +71,62 @@ template <typename T> struct Residual {
     }
 };
 
-// W entries at once, 16 bytes or one entry
+// 16 bytes of entries at once
 template <typename T, int W> struct Some {
-    T x[W];
+    uint4 r;
     __device__ __forceinline__ void load(const T *p) {
-        if constexpr (W == 1) x[0] = *p;
-        else *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(p);
+        asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
     }
-    __device__ __forceinline__ float get(int i) const { return value(x + i); }
+    __device__ __forceinline__ void clear() { r = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        if constexpr (W == 4) return __uint_as_float(w[i]);
+        return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
 };
-// This lane's weights of the entries [lo, hi): the warp takes 32 W entries together, whole rounds of them without a test of the end
-template <typename T, int W>
+// This lane's weights of the entries [lo, hi), whose ends are whole pieces of W.  U pieces of each row are in flight: with the rows in DRAM a
+// round of loads takes over a microsecond, so rounds are what a call's time is made of
+template <typename T, int W, int U, bool Q>
 __device__ __forceinline__ unsigned long long chunk_sum(const Residual<T> &r, int lo, int hi, int lane) {
-    constexpr int U = BYTES / (W == 1 ? 8 : 16), ROUND = 32 * W * U;
     unsigned long long sum = 0ull;
-    int v0 = lo;
-    if (r.q) {
-        for (; v0 + ROUND <= hi; v0 += ROUND) {
-            Some<T, W> a[U], b[U];
+    if constexpr (W == 1) {
+        int v0 = lo;                   // (entry by entry, tests of the end cost more than they are worth: 192 x 50257 bf16 31 us and 15.6 us)
+        for (; v0 + 32 * U <= hi; v0 += 32 * U) {
+            float a[U], b[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i) { a[i].load(r.p + v0 + (32 * i + lane) * W); b[i].load(r.q + v0 + (32 * i + lane) * W); }
+            for (int i = 0; i < U; ++i) {
+                a[i] = load_now(r.p + v0 + 32 * i + lane);
+                b[i] = Q ? load_now(r.q + v0 + 32 * i + lane) : 0.f;
+            }
 #pragma unroll
-            for (int i = 0; i < U; ++i)
+            for (int i = 0; i < U; ++i) sum += !Q && v0 + 32 * i + lane == r.without ? 0ull : weight(a[i] - b[i]);
+        }
+        for (v0 += lane; v0 < hi; v0 += 32 * U) {
+            float x[U];
 #pragma unroll
-                for (int w = 0; w < W; ++w) sum += weight(a[i].get(w) - b[i].get(w));
+            for (int i = 0; i < U; ++i) x[i] = v0 + 32 * i < hi ? r.at(v0 + 32 * i) : 0.f;
+#pragma unroll
+            for (int i = 0; i < U; ++i) sum += weight(x[i]);
         }
     } else {
-        for (; v0 + ROUND <= hi; v0 += ROUND) {
-            Some<T, W> a[U];
+        for (int v0 = lo + lane * W; v0 < hi; v0 += 32 * W * U) {
+            Some<T, W> a[U], b[U];
 #pragma unroll
-            for (int i = 0; i < U; ++i) a[i].load(r.p + v0 + (32 * i + lane) * W);
+            for (int i = 0; i < U; ++i) {
+                const int v = v0 + 32 * W * i;
+                a[i].clear();
+                b[i].clear();
+                if (v < hi) {
+                    a[i].load(r.p + v);
+                    if (Q) b[i].load(r.q + v);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < U; ++i)
 #pragma unroll
-                for (int w = 0; w < W; ++w) sum += v0 + (32 * i + lane) * W + w == r.without ? 0ull : weight(a[i].get(w));
+                for (int w = 0; w < W; ++w)
+                    sum += Q ? weight(a[i].get(w) - b[i].get(w)) : v0 + 32 * W * i + w == r.without ? 0ull : weight(a[i].get(w));
         }
-    }
-    for (; v0 < hi; v0 += 32 * 8) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = v0 + 32 * i + lane < hi ? r.at(v0 + 32 * i + lane) : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += weight(x[i]);
     }
     return sum;
 }
@@ -151,7 +176,8 @@ verify_kernel(Args g) {
     int pass = 0;
     for (; pass < 2; ++pass) {
         const int lo = min(g.vocab, me * chunk), hi = min(g.vocab, lo + chunk);
-        unsigned long long sum = chunk_sum<T, W>(r, lo, hi, lane);
+        constexpr int U = W == 1 ? 16 : 4;       // (192 x 50257 bf16, entry by entry: 8 20.3 us, 16 15.1 us; 64 x 128256 fp32: 2 14.5 us, 4 13.5 us)
+        unsigned long long sum = r.q ? chunk_sum<T, W, U, true>(r, lo, hi, lane) : chunk_sum<T, W, U, false>(r, lo, hi, lane);
         sum = warp_sum(sum);
         if (lane < split) {
             const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[pass][me]));
@@ -222,13 +248,14 @@ template <typename T, int W, int THREADS, int SPLIT> static siso_status_t launch
     return SISO_OK;
 }
 template <typename T, int W> static siso_status_t run(const Args &g, int64_t n_seqs, cudaStream_t s) {
-    // A sequence is shared by as many CTAs as give each of the 148 SMs a few.  Few sequences: many loads in flight on the few SMs that work;
-    // many: CTAs small enough that all of them run at once (64 x 128256 fp32: 512 threads 20.5 us, 256 threads 16.8 us; one row of
-    // 32000: 6.5 us and 7.7 us)
-    if (n_seqs <= 16) return launch<T, W, 512, 8>(g, n_seqs, s);
+    // A sequence is shared by as many CTAs as give each of the 148 SMs a few, small enough that all of them run at once (64 x 128256
+    // fp32: 256 threads 13.4 us, 512 threads 17.3 us; 192 x 50257 bf16: four CTAs 13.6 us, two 15.1 us; 512 x 32000 fp32: two 32.8 us,
+    // one 34.8 us).  Few sequences with long rows get larger CTAs, fewer rounds of loads (4 x 128256 fp32: 512 threads 6.5 us, 256
+    // threads 7.7 us; 1 x 32000: 4.2 us and 3.8 us)
+    if (n_seqs <= 16 && g.vocab >= 65536) return launch<T, W, 512, 8>(g, n_seqs, s);
     if (n_seqs <= 64) return launch<T, W, 256, 8>(g, n_seqs, s);
-    if (n_seqs <= 128) return launch<T, W, 256, 4>(g, n_seqs, s);
-    if (n_seqs <= 256) return launch<T, W, 256, 2>(g, n_seqs, s);
+    if (n_seqs <= 256) return launch<T, W, 256, 4>(g, n_seqs, s);
+    if (n_seqs <= 512) return launch<T, W, 256, 2>(g, n_seqs, s);
     return launch<T, W, 256, 1>(g, n_seqs, s);
 }
 
