@@ -493,8 +493,9 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  max_q: the most queries of one sequence (a hint that selects the kernel; any value gives the same result up
  *                  to rounding).  Places beyond kv_len may hold anything, NaN included; within it values must be
  *                  finite (a NaN there may reach rows that do not see it).  A page index outside the pool: SISO_ERR_INVALID_ARG in the
- *                  status word, its tokens are left out.  Sums and softmax statistics are fp32; probabilities are rounded to
- *                  bf16 before they meet the values.
+ *                  status word, its tokens are left out.  Sums and softmax statistics are fp32; probabilities (over 8-bit pages with few
+ *                  rows times a power of two that stands for the value's scale) are rounded to bf16 before they meet the values.
+ *                  There a query's elements below 2^-31 of its row's largest lose bits, and below 2^-40 count as zero.
  * siso_kv_sync_status  Synchronises `stream`, returns the handle's device status word and clears it.
  * Calls on one handle must be issued on one stream or be ordered by the caller (they share the handle's scratch).
  *

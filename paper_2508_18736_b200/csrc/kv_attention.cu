@@ -17,9 +17,11 @@
 // bytes of its key and the queries are laid out to match.  V fragments come through ldmatrix.trans; over 8-bit codes it hands
 // a lane the pairs (key, d), (key, d + 1), (key + 1, d), (key + 1, d + 1), the fragments of an even and an odd d.  Probabilities
 // change from the first product's layout to the second's by movmatrix.
-// 8-bit codes are turned into fp16, not bf16: one conversion per two codes, exact.  The key's scale goes to its score, the
-// value's to its probability relative to the largest one so far.  Queries are brought into fp16's range by a power of two per row
-// (exact but for elements 2^-39 below the row's largest), probabilities are scaled by 2^15.
+// 8-bit codes of keys are turned into fp16: one conversion per two codes, exact.  The key's scale goes to its score.  Queries are brought
+// into fp16's range by a power of two per row (exact but for elements below 2^-31 of the row's largest).  Codes of values are turned into
+// bf16, exactly, and the value's scale goes to its probability, relative to the largest one so far: probabilities and scales of
+// neighbouring tokens may lie many powers of two apart, for which fp16 has no room (a probability of 2^-40 would be zero).  bf16 costs
+// nothing over i8; over e4m3 (no conversion to it) 0 to 6 %: 64 sequences of 201 to 8190 tokens 107 us either way, head size 64 72 and 76 us.
 // Measured, 8 kv heads x 128, 4 query heads each, caches in HBM: 64 sequences of 4096 tokens bf16 164 us, 6.5 TB/s (8192 tokens: 6.8 TB/s);
 // e4m3 107 us, 5.1 TB/s, where the dependent steps of a consumer warp on a unit are the limit; one sequence of 1025 tokens 9.4 us, latency.
 #include <cuda_fp16.h>
@@ -80,19 +82,34 @@ __device__ __forceinline__ void load_v(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-// Two codes as fp16: bytes 0, 1 and 2, 3 of a word (SPLIT false), or bytes 0, 2 and 1, 3 (SPLIT true)
-template <int KIND, bool SPLIT> __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
+// Codes of keys as fp16: bytes 0, 1 and 2, 3 of a word
+template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
     if constexpr (KIND == SISO_E4M3) {
-        if constexpr (SPLIT) w = __byte_perm(w, 0u, 0x3120);
         asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
             : "=r"(lo), "=r"(hi) : "r"(w));
     } else {
         w ^= 0x80808080u;                                   // c + 128; beside the byte 0x64 it is the fp16 number 1024 + c + 128
         const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));
-        const uint32_t a = __byte_perm(w, 0x64646464u, SPLIT ? 0x4240 : 0x4140), b = __byte_perm(w, 0x64646464u, SPLIT ? 0x4341 : 0x4342);
+        const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
         const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
         lo = *reinterpret_cast<const uint32_t *>(&x);
         hi = *reinterpret_cast<const uint32_t *>(&y);
+    }
+}
+// Codes of values as bf16, exactly: bytes 0, 2 and 1, 3 of a word.  e4m3: 2^-120 of the code, subnormal ones too (see CodeScale).  i8: the
+// byte u = c + 128 as the bits of a bf16 number is u 2^-133, in the subnormal range and in the first binade above it alike; times 2^127, less 2,
+// it is c 2^-6.  UP powers of two more on the probabilities make up for these factors, or most of them, so that the sums of e4m3 stay in
+// the middle of fp32's range; BACK for the rest
+template <int KIND> constexpr int UP = KIND == SISO_E4M3 ? 100 : 6;
+template <int KIND> constexpr float BACK = KIND == SISO_E4M3 ? 1048576.f : 1.f;
+template <int KIND> __device__ __forceinline__ void widen_values(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    if constexpr (KIND == SISO_E4M3) {
+        lo = ((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u);
+        hi = ((w >> 4) & 0x07F007F0u) | (w & 0x80008000u);
+    } else {
+        w ^= 0x80808080u;
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(lo) : "r"(__byte_perm(w, 0u, 0x4240)), "r"(0x7F007F00u), "r"(0xC000C000u));
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(hi) : "r"(__byte_perm(w, 0u, 0x4341)), "r"(0x7F007F00u), "r"(0xC000C000u));
     }
 }
 template <int STAGES> struct Ring {
@@ -320,8 +337,8 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             uint32_t f[4];
-                            widen<KIND, false>(x0[x], f[0], f[2]);
-                            widen<KIND, false>(x1[x], f[1], f[3]);
+                            widen<KIND>(x0[x], f[0], f[2]);
+                            widen<KIND>(x1[x], f[1], f[3]);
 #pragma unroll
                             for (int t = 0; t < NT; ++t) mma<true>(s[i][t], f, q[t][4 * a + x]);
                         }
@@ -376,7 +393,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     corr[t][h] = m[t][h] == m2 ? 1.f : ex2(m[t][h] - m2);
                     moved = moved || m[t][h] != m2;
                     m[t][h] = m2;
-                    shift[t][h] = m2 == -INFINITY ? 0.f : m2 - (EIGHT ? 15.f : 0.f);
+                    shift[t][h] = m2 == -INFINITY ? 0.f : m2;
                     l[t][h] *= corr[t][h];
                 }
             if constexpr (EIGHT) {
@@ -404,13 +421,13 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float rel = 1.f;                      // 2^(value exponent - largest so far)
-                    if constexpr (EIGHT) rel = __uint_as_float(static_cast<uint32_t>(max(127 - e_top + static_cast<int>(ev[i][e]), 0)) << 23);
+                    if constexpr (EIGHT) rel = __uint_as_float(static_cast<uint32_t>(max(127 + UP<KIND> - e_top + static_cast<int>(ev[i][e]), 0)) << 23);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         const float p0 = ex2(s[i][t][2 * e] - shift[t][0]), p1 = ex2(s[i][t][2 * e + 1] - shift[t][1]);
                         l[t][0] += p0;
                         l[t][1] += p1;
-                        p[t][e] = transposed(EIGHT ? pack(p0 * rel, p1 * rel, true) : pack(p0, p1, false));
+                        p[t][e] = transposed(EIGHT ? pack(p0 * rel, p1 * rel, false) : pack(p0, p1, false));
                     }
                 }
                 const uint32_t v_at = v_first + (n0 + 16 * i) * LINE;
@@ -429,10 +446,10 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                         load_v(v_at ^ (d << 4), v);
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {     // rows 0-7 of the product: even d, rows 8-15: odd d
-                            widen<KIND, true>(v[2 * x], f[0], f[1]);
-                            widen<KIND, true>(v[2 * x + 1], f[2], f[3]);
+                            widen_values<KIND>(v[2 * x], f[0], f[1]);
+                            widen_values<KIND>(v[2 * x + 1], f[2], f[3]);
 #pragma unroll
-                            for (int t = 0; t < NT; ++t) mma<true>(o[t][d + x], f, p[t]);
+                            for (int t = 0; t < NT; ++t) mma<false>(o[t][d + x], f, p[t]);
                         }
                     }
                 }
@@ -461,14 +478,15 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                 l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 4);
                 l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 8);
                 l[t][h] += __shfl_xor_sync(0xFFFFFFFFu, l[t][h], 16);
-                if (EIGHT) m[t][h] -= 15.f;
             }
         if constexpr (EIGHT) {
             const float back = kv_scale(static_cast<uint32_t>(e_top));
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) { o[t][d][0] *= back; o[t][d][1] *= back; o[t][d][2] *= back; o[t][d][3] *= back; }
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[t][d][x] = o[t][d][x] * BACK<KIND> * back;
         }
 #pragma unroll 1
         for (int half = WK / 2; half >= 1; half >>= 1) { // join the groups' results, halving their number each time

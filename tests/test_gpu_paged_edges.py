@@ -1,0 +1,107 @@
+"""The paged key/value cache and what reads it at the edges of their arguments, against the 64-bit statements of paged_ref.  Tolerances are
+those of test_gpu_paged, derived there."""
+import pytest
+import torch
+
+import paged_ref as ref
+from test_gpu_paged import check_attention
+
+pytestmark = pytest.mark.gpu
+
+siso = pytest.importorskip("paper_2508_18736_b200")
+I32 = dict(dtype=torch.int32, device="cuda")
+
+
+def filled(kind, n, page, kv_heads, dim, scale=None, holes=False, seed=3, spare=1):
+    """A cache that holds n tokens in shuffled pages, whose value rows are `scale` [n] times as large, every second value of large rows zero if
+    `holes`: (kv, table [1, pages], keys, values as the cache holds them, in 64 bits)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    held = -(-n // page)
+    kv = siso.PagedKV(*ref.make_pages(kind, 1, held + spare, page, kv_heads, dim, fill="nan"))
+    table = torch.randperm(held + spare, device="cuda", generator=g)[:held].to(torch.int32)[None]
+    i = torch.arange(n, device="cuda")
+    slots = table[0].long()[i // page] * page + i % page
+    k, v = (torch.randn((n, kv_heads, dim), device="cuda", generator=g) for _ in range(2))
+    if scale is not None:
+        v *= scale[:, None, None]
+        if holes:
+            v[scale > 1, :, ::2] = 0.0
+    kv.write(k, v, slots)
+    if kind == "bf16":
+        return kv, table, k.to(torch.bfloat16).double(), v.to(torch.bfloat16).double()
+    return kv, table, ref.values(*ref.quantised(k, kind)), ref.values(*ref.quantised(v, kind))
+
+
+def attend(kv, table, n, n_q, heads, dim, k, v, gain=1.0, causal=True, window=0, hint=None, seed=4):
+    """Attention of the last n_q of n tokens (more than n: the first ones stand before the start) is compared with its statement."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    q = (gain * torch.randn((n_q, heads, dim), device="cuda", generator=g)).to(torch.bfloat16)
+    cu, lens = (torch.tensor(x, **I32) for x in ([0, n_q], [n]))
+    out, lse = kv.attention(q, cu, lens, table, n_q if hint is None else hint, causal=causal, window=window, want_lse=True)
+    assert kv.sync_status() == 0
+    check_attention(out, lse, ref.attention(q, k, v, n_q, causal, window), dim)
+
+
+# ---- value rows of unlike size ------------------------------------------------------------------------------------------------
+ROWS = [1, 2, 4, 6, 9]              # queries of 4 heads per kv head: 4, 8, 16, 24 and 36 rows, every kernel and shape
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n_q", ROWS)
+@pytest.mark.parametrize("holes", [False, True])
+def test_value_rows_of_unlike_size(kind, dim, n_q, holes):
+    n = 700
+    steps = torch.randint(-40, 41, (n,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n_q)).float()
+    for scale in (torch.exp2(steps), torch.exp2(steps.abs().neg()), torch.exp2(torch.linspace(-60, 60, n, device="cuda").round())):
+        kv, table, k, v = filled(kind, n, 16, 2, dim, scale, holes)
+        attend(kv, table, n, n_q, 8, dim, k, v)
+        kv.close()
+
+
+@pytest.mark.parametrize("n_q", ROWS)
+def test_e4m3_codes_below_the_normal_range(n_q):
+    # one large value a row, in the first place; the others are codes of 2^-9 to 7 x 2^-9
+    n, dim = 150, 128
+    g = torch.Generator(device="cuda").manual_seed(n_q)
+    kv = siso.PagedKV.allocate(1, 10, 16, 1, dim, torch.float8_e4m3fn)
+    k = torch.randn((n, 1, dim), device="cuda", generator=g)
+    v = torch.randint(1, 8, (n, 1, dim), device="cuda", generator=g) * 2.0 ** -9 * torch.where(torch.rand((n, 1, dim), device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    v[:, :, 0] = 448.0
+    kv.write(k, v, torch.arange(n, device="cuda"))
+    assert torch.equal(kv.read(torch.arange(n, device="cuda"), dtype=torch.float32)[1], v)
+    attend(kv, torch.arange(10, **I32)[None], n, n_q, 4, dim, ref.values(*ref.quantised(k, "e4m3")), v.double())
+    kv.close()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("n_q,window", [(2, 1), (8, 3), (9, 0), (9, 5), (60, 40)])
+def test_large_value_rows_that_a_query_does_not_see(kind, n_q, window):
+    # the first token of all, the one before the window of the last query, and the last token, which only the last query sees
+    n, dim = 300, 128
+    scale = torch.ones(n, device="cuda")
+    scale[[0, n - 1 - (window or 1), n - 1]] = 2.0 ** 40
+    kv, table, k, v = filled(kind, n, 16, 1, dim, scale)
+    attend(kv, table, n, n_q, 4, dim, k, v, window=window)
+    kv.close()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "i8"])
+@pytest.mark.parametrize("n_q", ROWS)
+def test_small_probabilities_where_the_large_ones_meet_zeros(kind, n_q):
+    # every second value of the heavy rows is zero: what the light ones give stands alone there, however small it is
+    n, dim, kv_heads = 200, 128, 2
+    g = torch.Generator(device="cuda").manual_seed(1)
+    kv = siso.PagedKV.allocate(1, -(-n // 16), 16, kv_heads, dim, ref.TYPES[kind])
+    k, v = (torch.randn((n, kv_heads, dim), device="cuda", generator=g) for _ in range(2))
+    k[::7] += 2.0
+    v[::7, :, ::2] = 0.0
+    slots = torch.arange(n, device="cuda")
+    kv.write(k, v, slots)
+    table = torch.arange(-(-n // 16), **I32)[None]
+    k, v = (x.to(torch.bfloat16).double() if kind == "bf16" else ref.values(*ref.quantised(x, kind)) for x in (k, v))
+    q = torch.full((n_q, 8, dim), 1.5, dtype=torch.bfloat16, device="cuda")        # heavy rows: scores higher by about 34
+    cu, lens = (torch.tensor(x, **I32) for x in ([0, n_q], [n]))
+    out, lse = kv.attention(q, cu, lens, table, n_q, want_lse=True)
+    check_attention(out, lse, ref.attention(q, k, v, n_q), dim)
+    kv.close()
