@@ -279,7 +279,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = cur.rt * MR + (wm * NT + t) * 8 + 2 * c + h;
-                pos[t][h] = row < cur.n_q * g.group ? cur.len - cur.n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))) : cur.s.last_pos;
+                pos[t][h] = row < cur.n_q * g.group ? position(cur.len, cur.n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(row)))) : cur.s.last_pos;
                 m[t][h] = -INFINITY;
                 l[t][h] = 0.f;
                 row_scale[t][h] = g.scale_log2 * __shfl_sync(0xFFFFFFFFu, back, (2 * c + h) * 4);

@@ -64,11 +64,14 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
     q0 = min(max(g.a.d_cu_q[b], 0), n);
     return max(0, min(g.a.d_cu_q[b + 1], n) - q0);
 }
+// Position of query i of a sequence.  Queries that stand before the sequence's start all count as standing at -1: they see the same there, and
+// differences of positions and windows, both up to 2^31 - 1, stay inside 32 bits
+__device__ __forceinline__ int position(int len, int n_q, int i) { return max(len - n_q + i, -1); }
 template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g, int len, int n_q, int rt) {
     Span s;
     const int rows = n_q * g.group;
-    s.first_pos = len - n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR)));
-    s.last_pos = len - n_q + static_cast<int>(g.by_group.div(static_cast<uint32_t>(min(rows, (rt + 1) * MR) - 1)));
+    s.first_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))));
+    s.last_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(min(rows, (rt + 1) * MR) - 1))));
     s.hi = (g.a.flags & SISO_ATTN_CAUSAL) ? max(0, min(len, s.last_pos + 1)) : len;
     s.lo = g.a.window > 0 ? max(0, s.first_pos - g.a.window + 1) : 0;
     s.tile0 = s.lo / TK;

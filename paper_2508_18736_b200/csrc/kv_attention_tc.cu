@@ -552,7 +552,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             out_token = real ? cur.q0 + i : -1;
             out_head = head;
             out_place = cur.tile == 0 && n == cur.s.tiles ? -1 : static_cast<int>(part_place(blockIdx.x, cur.tile > 0)) * TC_ROWS + in_tile;
-            const int pos = real ? cur.len - cur.n_q + i : cur.s.last_pos;
+            const int pos = real ? position(cur.len, cur.n_q, i) : cur.s.last_pos;
             m = -INFINITY;
             l = 0.f;
             const int k0 = split ? t : 0, k_step = split ? 2 : 1;
@@ -570,7 +570,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 tmem_ld_fence(rb);
                 if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
                     const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0 - half * 64;
-                    const int first = g.a.window > 0 ? pos - g.a.window + 1 - j0 - half * 64 : 0;
+                    const int first = g.a.window > 0 ? max(pos - g.a.window + 1, 0) - j0 - half * 64 : 0;
                     const uint32_t my_blocks = blocks >> (half * 8);
 #pragma unroll
                     for (int x = 0; x < 32; ++x) {

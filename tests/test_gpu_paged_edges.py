@@ -105,3 +105,14 @@ def test_small_probabilities_where_the_large_ones_meet_zeros(kind, n_q):
     out, lse = kv.attention(q, cu, lens, table, n_q, want_lse=True)
     check_attention(out, lse, ref.attention(q, k, v, n_q), dim)
     kv.close()
+
+
+# ---- windows ---------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["bf16", "i8"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 700, 1500, 1300, 1299])
+@pytest.mark.parametrize("n,n_q", [(1300, 1), (1300, 6), (1300, 150), (1300, 1300), (5, 8), (100, 260)])
+def test_windows_as_long_as_the_sequence_and_longer(kind, causal, window, n, n_q):
+    kv, table, k, v = filled(kind, n, 32, 2, 64)
+    attend(kv, table, n, n_q, 8, 64, k, v, causal=causal, window=window)
+    kv.close()
