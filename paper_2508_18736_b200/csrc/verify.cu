@@ -141,6 +141,8 @@ verify_kernel(Args g) {
     uint32_t rank;
     constexpr int split = SPLIT;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    // said here, waited for below: a CTA's shared memory may be written by others only once it is known to have started
+    if constexpr (SPLIT > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const long long b = blockIdx.x / split;
 
     // ---- which drafts stand: every warp finds it for itself
@@ -179,6 +181,7 @@ verify_kernel(Args g) {
         constexpr int U = W == 1 ? 16 : 4;       // (192 x 50257 bf16, entry by entry: 8 20.3 us, 16 15.1 us; 64 x 128256 fp32: 2 14.5 us, 4 13.5 us)
         unsigned long long sum = r.q ? chunk_sum<T, W, U, true>(r, lo, hi, lane) : chunk_sum<T, W, U, false>(r, lo, hi, lane);
         sum = warp_sum(sum);
+        if (SPLIT > 1 && pass == 0) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         if (lane < split) {
             const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[pass][me]));
             uint32_t there;

@@ -116,3 +116,18 @@ def test_windows_as_long_as_the_sequence_and_longer(kind, causal, window, n, n_q
     kv, table, k, v = filled(kind, n, 32, 2, 64)
     attend(kv, table, n, n_q, 8, 64, k, v, causal=causal, window=window)
     kv.close()
+
+
+# ---- verification ----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("seqs", [1, 3, 17, 70, 300, 600])          # clusters of 8, 8, 8, 4, 2 and 1 CTAs
+@pytest.mark.parametrize("n_max,vocab", [(0, 1), (0, 40), (1, 1), (2, 9)])
+def test_short_rows_are_shared_by_ctas_that_have_all_started(seqs, n_max, vocab):
+    # almost nothing stands between a CTA's start and what it writes to its neighbours; many calls, one close behind the other
+    g = torch.Generator(device="cuda").manual_seed(seqs + vocab)
+    target = torch.softmax(torch.randn((seqs, n_max + 1, vocab), device="cuda", generator=g), -1)
+    tokens = torch.randint(0, vocab, (seqs, n_max), device="cuda", generator=g, dtype=torch.int32)
+    u_accept, u_sample = torch.rand((seqs, n_max), device="cuda", generator=g), torch.rand(seqs, device="cuda", generator=g)
+    calls = [siso.verify_drafts(target, None, tokens, None, u_accept, u_sample) for _ in range(50)]
+    want, taken = ref.verify(target, None, tokens, None, u_accept, u_sample)
+    for out, n in calls:
+        assert torch.equal(out.cpu(), want) and torch.equal(n.cpu(), taken)
