@@ -491,9 +491,10 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  and 0 and -infinity where nothing is seen.  d_q, d_out bf16 [n_tokens, n_heads, head_dim] with strides in
  *                  elements (multiples of 8, bases 16-byte aligned); d_lse [n_tokens, n_heads] fp32 or NULL.  head_dim 64 or 128.
  *                  max_q: the most queries of one sequence (a hint that selects the kernel; any value gives the same result up
- *                  to rounding).  Places beyond kv_len may hold anything, NaN included; within it values must be
- *                  finite (a NaN there may reach rows that do not see it).  A page index outside the pool: SISO_ERR_INVALID_ARG in the
- *                  status word, its tokens are left out.  Sums and softmax statistics are fp32; probabilities (over 8-bit pages with few
+ *                  to rounding).  Places beyond kv_len and places before the windows of all of a sequence's queries may hold anything, NaN
+ *                  included, and pages that hold no others are not looked up; elsewhere values must be finite (a NaN may reach rows that
+ *                  do not see it).  A page index outside the pool: SISO_ERR_INVALID_ARG in the status word, its tokens are left out.
+ *                  Sums and softmax statistics are fp32; probabilities (over 8-bit pages with few
  *                  rows times a power of two that stands for the value's scale) are rounded to bf16 before they meet the values.
  *                  There a query's elements below 2^-31 of its row's largest lose bits, and below 2^-40 count as zero.
  * siso_kv_sync_status  Synchronises `stream`, returns the handle's device status word and clears it.

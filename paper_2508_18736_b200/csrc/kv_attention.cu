@@ -172,11 +172,12 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
                     tok[x] = j - at * g.kv.page_size;
                     page[x] = -1;
-                    if (j < cur.s.hi) {
+                    const bool wanted = holds_seen(g, cur.lo(g), cur.s.hi, j);
+                    if (wanted) {
                         page[x] = g.a.d_pages[cur.b * g.a.pages_stride + at];
                         if (page[x] < 0 || page[x] >= g.kv.n_pages) { page[x] = -1; set_status(g.status, SISO_ERR_INVALID_ARG); }
                     }
-                    first[x] = j < cur.s.hi && blk % box_blocks == 0;
+                    first[x] = wanted && blk % box_blocks == 0;
                 }
 #pragma unroll
                 for (int x = 0; x < HALVES; ++x) {
@@ -301,10 +302,13 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         const uint32_t blocks = ring.blocks[stage];
         const bool cut = j0 + TK > cur.s.hi || blocks != ALL || (causal && j0 + TK - 1 > cur.s.first_pos) ||
                          (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
-        if (j0 + TK > cur.s.hi) {    // values beyond the end may be anything: zeros, or 0 times NaN would reach the sums
+        const int lo = cut ? cur.lo(g) : 0;
+        if (cut && (j0 + TK > cur.s.hi || j0 < lo)) {    // values beyond the end or before every window may be anything: zeros, or 0 times NaN would reach the sums
             for (int x = wm * 32 + lane; x < NK * CH; x += 32 * WM) {
                 const int row = kg * NK + x / CH;
-                if (j0 + row >= cur.s.hi) *reinterpret_cast<uint4 *>(tile + TK * RB + chunk_at<RB, TK>(row, x % CH)) = make_uint4(0u, 0u, 0u, 0u);
+                if (j0 + row >= lo && j0 + row < cur.s.hi) continue;
+                *reinterpret_cast<uint4 *>(tile + TK * RB + chunk_at<RB, TK>(row, x % CH)) = make_uint4(0u, 0u, 0u, 0u);
+                if (EIGHT && x % CH == 0) meta[stage * S::META + TK + row] = 0;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if constexpr (WM == 1) __syncwarp();

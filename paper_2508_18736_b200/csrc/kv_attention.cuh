@@ -52,7 +52,7 @@ struct Args {
 #ifdef __CUDACC__
 // the row tile `rt` of a sequence: positions of its first and last row's token and the key tiles it has to see
 struct Span {
-    int first_pos, last_pos, lo, hi, tile0, tiles;
+    int first_pos, last_pos, hi, tile0, tiles;
 };
 __device__ __forceinline__ int seq_len(const Args &g, int b) {
     const long long cap = static_cast<long long>(g.a.max_pages) * g.kv.page_size;
@@ -67,17 +67,21 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
 // Position of query i of a sequence.  Queries that stand before the sequence's start all count as standing at -1: they see the same there, and
 // differences of positions and windows, both up to 2^31 - 1, stay inside 32 bits
 __device__ __forceinline__ int position(int len, int n_q, int i) { return max(len - n_q + i, -1); }
+__device__ __forceinline__ int first_seen(const Args &g, int first_pos) { return g.a.window > 0 ? max(0, first_pos - g.a.window + 1) : 0; }
 template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g, int len, int n_q, int rt) {
     Span s;
     const int rows = n_q * g.group;
     s.first_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))));
     s.last_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(min(rows, (rt + 1) * MR) - 1))));
     s.hi = (g.a.flags & SISO_ATTN_CAUSAL) ? max(0, min(len, s.last_pos + 1)) : len;
-    s.lo = g.a.window > 0 ? max(0, s.first_pos - g.a.window + 1) : 0;
-    s.tile0 = s.lo / TK;
+    const int lo = first_seen(g, s.first_pos);
+    s.tile0 = lo / TK;
     s.tiles = max(1, (s.hi + TK - 1) / TK - s.tile0);       // a row tile that sees nothing is one unit that writes zeros
     return s;
 }
+// Whether the TMA box of token j of a row tile's keys holds tokens that some row may see, and j is not beyond the last.  What lies wholly before
+// the window is not looked up: its pages may have been given back
+__device__ __forceinline__ bool holds_seen(const Args &g, int lo, int hi, int j) { return j < hi && (j | (g.box - 1)) >= lo; }
 // units of one key/value head of sequence b: a key tile counts W, and an item EXTRA more, for its beginning and end
 template <int MR, int TK, int EXTRA, int W> __device__ __forceinline__ int seq_units(const Args &g, int b) {
     int q0;
@@ -121,6 +125,8 @@ template <int MR, int TK, int EXTRA, int W> struct Cursor {
     }
     // key tiles of this item that belong to the run
     __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, (left + W - 1) / W); }
+    // the first key that a row of this item sees (worked out again where it is needed: kept, it costs registers)
+    __device__ __forceinline__ int lo(const Args &g) const { return g.a.window > 0 && tile == 0 ? first_seen(g, position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))))) : 0; }
     // n <= tiles_here() tiles further; false: the run is over
     __device__ __forceinline__ bool step(const Args &g, int n = 1) {
         tile += n;

@@ -12,7 +12,8 @@
 //   warp 16          issues the products: S_t = Q_t K^T (both from shared memory) and O_t += P_t V (P from TMEM, V as it lies, key by key:
 //                    an MN-major operand)
 //   warps 17, 18     fill the ring of K and V tiles by TMA, one box per run of tokens in one page
-//   warp 19          zeroes what lies beyond the end in the last values of an item (bf16 caches; the widening does it for the others)
+//   warp 19          zeroes what lies beyond the end in the last values of an item, and before the window in the first (bf16 caches; the
+//                    widening sees to it for the others)
 //   warps 20-27      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
 // TMEM: S_0, S_1 (128 columns each), O_0, O_1.
 // Measured, 32 query heads on 8 kv heads x 128, bf16: 2048 new tokens of 33333 870 to 900 us, 1.2 PFLOP/s (tensor pipe 69 %, exponentials
@@ -208,11 +209,17 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             int stage = 0, raw = 0;
             uint32_t phase = 0, raw_phase = 0;
             do {
-                const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;          // rows of the tile that are there
+                const int j0 = (cur.s.tile0 + cur.tile) * TK, left = cur.s.hi - j0, before = cur.lo(g) - j0;      // rows [before, left) of the tile are there
                 for (int is_v = 0; is_v < 2; ++is_v) {
                     wait_bar(&bars.raw_full[raw], raw_phase, gave_up);
                     wait_bar(&bars.kv_empty[stage], phase ^ 1u, gave_up);
                     const uint8_t *src = raws + raw * S::RAW, *exps = metas + raw * S::RAW_META + r0;
+                    if (is_v && (left < TK || before > 0)) {
+                        // anything may stand in the other rows: a scale of 2^-127 makes it finite, and their probabilities are zero
+                        const int r = (warp - 20) * MINE + lane;
+                        if (lane < MINE && (r >= left || r < before)) metas[raw * S::RAW_META + r] = 0;
+                        __syncwarp();
+                    }
                     uint8_t *dst = tiles + stage * S::TILE;
 #pragma unroll
                     for (int i = 0; i < MINE / PER; ++i) {
@@ -223,10 +230,6 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         uint32_t out[8];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) scale.widen(in[k], out[2 * k], out[2 * k + 1]);
-                        if (left < TK && r0 + i * PER >= left) {                    // anything may stand there
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) out[k] = 0u;
-                        }
                         const uint4 a = make_uint4(out[0], out[1], out[2], out[3]), b = make_uint4(out[4], out[5], out[6], out[7]);
                         *reinterpret_cast<uint4 *>(dst + (dst0 ^ x) + i * PER * 128) = flip ? b : a;
                         *reinterpret_cast<uint4 *>(dst + (dst1 ^ x) + i * PER * 128) = flip ? a : b;
@@ -243,18 +246,22 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
         if (warp == 19) {
             if constexpr (!EIGHT) {
-                // ---- what lies beyond the end in the last values of an item may be anything: zeros, or 0 times NaN would reach the sums
+                // ---- what lies beyond the end or before the window in an item's values may be anything: zeros, or 0 times NaN would reach the sums
                 int stage = 0;
                 uint32_t phases = 0;                          // bit i: the round that stage i's barrier is in
                 do {
                     if (++stage == STAGES) stage = 0;
-                    const int left = cur.s.hi - (cur.s.tile0 + cur.tile) * TK;
-                    if (left < TK) {
+                    const int j0 = (cur.s.tile0 + cur.tile) * TK, left = cur.s.hi - j0, before = cur.lo(g) - j0;
+                    if (left < TK || before > 0) {
                         wait_bar(&bars.landed[stage], (phases >> stage) & 1u, gave_up);
                         phases ^= 1u << stage;
                         uint8_t *dst = tiles + stage * S::TILE;
-                        for (int x = max(left, 0) * (RB / 16) + lane; x < TK * (RB / 16); x += 32)
-                            *reinterpret_cast<uint4 *>(dst + chunk_at<RB, TK>(x / (RB / 16), x % (RB / 16))) = make_uint4(0u, 0u, 0u, 0u);
+                        auto clear = [&](int from, int to) {
+                            for (int x = from * (RB / 16) + lane; x < to * (RB / 16); x += 32)
+                                *reinterpret_cast<uint4 *>(dst + chunk_at<RB, TK>(x / (RB / 16), x % (RB / 16))) = make_uint4(0u, 0u, 0u, 0u);
+                        };
+                        clear(0, before);
+                        clear(max(left, 0), TK);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&bars.kv_full[stage]);
@@ -269,22 +276,23 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             int stage = 0, unit = 0;
             uint32_t phase = 0;
             // this lane's run of 8 tokens of a unit; the page index is asked for one unit before it is needed
-            struct Place { int j0, hi, head, tok, page; } at;
+            struct Place { int head, tok, page; bool wanted, edge; } at;       // edge: part of the values is zeroed, by warp 19 for bf16 caches
             auto look_up = [&](Place &p) {
-                p.j0 = (cur.s.tile0 + cur.tile) * TK;
-                p.hi = cur.s.hi;
+                const int j0 = (cur.s.tile0 + cur.tile) * TK;
                 p.head = cur.head;
-                const int j = p.j0 + (lane & 15) * 8, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
+                p.edge = j0 + TK > cur.s.hi || j0 < cur.lo(g);
+                const int j = j0 + (lane & 15) * 8, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
                 p.tok = j - i * g.kv.page_size;
-                p.page = lane < 16 && j < p.hi ? g.a.d_pages[cur.b * g.a.pages_stride + i] : -1;
+                const bool wanted = lane < 16 && holds_seen(g, cur.lo(g), cur.s.hi, j);
+                p.page = wanted ? g.a.d_pages[cur.b * g.a.pages_stride + i] : -1;
+                p.wanted = wanted;
             };
             look_up(at);
             for (bool more = true; more; ++unit) {
                 Place ahead = at;
                 more = cur.step(g);
                 if (more) look_up(ahead);
-                const int j = at.j0 + (lane & 15) * 8;
-                const bool wanted = lane < 16 && j < at.hi, in_pool = wanted && at.page >= 0 && at.page < g.kv.n_pages;
+                const bool wanted = at.wanted, in_pool = wanted && at.page >= 0 && at.page < g.kv.n_pages;
                 if (wanted && !in_pool) set_status(g.status, SISO_ERR_INVALID_ARG);
                 const bool first = wanted && lane % box_blocks == 0;
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, in_pool);
@@ -294,8 +302,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                         uint64_t *full = EIGHT ? &bars.raw_full[stage] : &bars.kv_full[stage];
                         wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up);
                         uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
-                        // the last values of an item in a bf16 cache go through warp 19
-                        uint64_t *bar = !EIGHT && is_v && at.j0 + TK > at.hi ? &bars.landed[stage] : full;
+                        uint64_t *bar = !EIGHT && is_v && at.edge ? &bars.landed[stage] : full;
                         if (*gave_up == 0) {
                             if (lane == 0) {
                                 if (!is_v) bars.blocks[unit & 7] = there;

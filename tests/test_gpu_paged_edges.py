@@ -1,5 +1,7 @@
 """The paged key/value cache and what reads it at the edges of their arguments, against the 64-bit statements of paged_ref.  Tolerances are
 those of test_gpu_paged, derived there."""
+import math
+
 import pytest
 import torch
 
@@ -115,6 +117,22 @@ def test_small_probabilities_where_the_large_ones_meet_zeros(kind, n_q):
 def test_windows_as_long_as_the_sequence_and_longer(kind, causal, window, n, n_q):
     kv, table, k, v = filled(kind, n, 32, 2, 64)
     attend(kv, table, n, n_q, 8, 64, k, v, causal=causal, window=window)
+    kv.close()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "i8"])
+@pytest.mark.parametrize("page", [8, 48, 64, 128])
+@pytest.mark.parametrize("n_q,window", [(1, 100), (1, 1), (7, 300), (20, 77), (300, 50)])
+def test_pages_before_the_window_may_be_gone(kind, page, n_q, window):
+    # pages that end before the first query's window: every other one released, the others in other hands (all NaN); and NaN in the
+    # places of the window's first page that lie before it
+    n, dim = 1000, 128
+    kv, table, k, v = filled(kind, n, page, 2, dim, spare=2)
+    lo = n - n_q - window + 1
+    kv.write(torch.full((lo, 2, dim), math.nan, device="cuda"), torch.full((lo, 2, dim), math.nan, device="cuda"),
+             (table[0].long()[:, None] * page + torch.arange(page, device="cuda")).reshape(-1)[:lo])
+    table[0, :lo // page:2] = -1
+    attend(kv, table, n, n_q, 8, dim, k, v, window=window)
     kv.close()
 
 
