@@ -1,6 +1,9 @@
 """The language model's side of a cache miss: a paged key/value cache that is quantised as it is written, the attention of new
 tokens over it, and the verification of drafted tokens (a near hit's stored answer, or a drafting model's).  Argument
-marshalling only; names and rules follow include/siso.h."""
+marshalling only; names and rules follow include/siso.h.
+
+A call with `stream` runs on that stream as a whole, as under torch.cuda.stream: the copies of arguments that are not contiguous, the
+kernels, and the outputs, whose memory is that stream's.  The arguments have to be ready there and to live until it is done with them."""
 from __future__ import annotations
 
 import ctypes
@@ -17,6 +20,13 @@ _ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
 _raw_stream = torch._C._cuda_getCurrentRawStream        # the current stream's handle, without building a Stream object
+
+
+def _on(stream, index: int):
+    """The context of `stream`, which has to be one of device `index`."""
+    if stream.device_index != index:
+        raise ValueError(f"stream must be one of cuda:{index}")
+    return torch.cuda.stream(stream)
 
 
 class _KvConfig(ctypes.Structure):
@@ -130,6 +140,9 @@ class PagedKV:
 
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, layer: int = 0, stream=None) -> None:
         """Rows k, v [n, kv heads, head dim] (fp32 or bf16) into `slots` [n] = page * page size + token (-1: skipped)."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.write(k, v, slots, layer)
         slots = self._slots(slots)
         n = slots.shape[0]
         k, v = self._rows(k, n, "k"), self._rows(v, n, "v")
@@ -140,13 +153,16 @@ class PagedKV:
             k, v = k.contiguous(), v.contiguous()
             strides = k.stride()
         st = self._lib.siso_kv_write(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, strides[0], strides[1],
-                                     slots.data_ptr(), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+                                     slots.data_ptr(), _raw_stream(self._index))
         if st:
             self._check(st, "siso_kv_write")
 
     def read(self, slots: torch.Tensor, layer: int = 0, dtype: torch.dtype = torch.bfloat16, stream=None, out=None
              ) -> Tuple[torch.Tensor, torch.Tensor]:
         """The rows of `slots` as (k, v) [n, kv heads, head dim] of `dtype` (float32 or bfloat16); zeros for slots outside the pool."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.read(slots, layer, dtype, out=out)
         slots = self._slots(slots)
         n = slots.shape[0]
         if out is None:
@@ -160,7 +176,7 @@ class PagedKV:
                 raise ValueError("outputs must have contiguous rows, the same strides and the same type")
         strides = k.stride()
         st = self._lib.siso_kv_read(self._h, layer, k.data_ptr(), v.data_ptr(), _ROW_TYPES[k.dtype], n, strides[0], strides[1],
-                                    slots.data_ptr(), _raw_stream(self._index) if stream is None else stream.cuda_stream)
+                                    slots.data_ptr(), _raw_stream(self._index))
         if st:
             self._check(st, "siso_kv_read")
         return k, v
@@ -171,6 +187,9 @@ class PagedKV:
         """q [n, heads, head dim] bf16: the queries of all sequences one after the other, sequence b's from cu_q[b] on (int32
         [seqs + 1]); kv_len int32 [seqs]: tokens in all, the new ones included (already written); pages int32 [seqs, max pages].
         Returns out [n, heads, head dim], or (out, lse [n, heads] fp32) with want_lse."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.attention(q, cu_q, kv_len, pages, max_q, layer, scale, causal, window, want_lse, out=out)
         index, i32 = self._index, torch.int32
         shape = q.shape
         if q.dtype is not torch.bfloat16 or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
@@ -202,7 +221,7 @@ class PagedKV:
         _ATTENTION.pack_into(self._args, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, cu_q.data_ptr(), kv_len.data_ptr(),
                              pages.data_ptr(), sq[0], sq[1], so[0], so[1], pages.stride(0), n, seqs, max_q, table[1], heads, layer, window,
                              ATTN_CAUSAL if causal else 0, self._default_scale if scale is None else scale)
-        st = self._lib.siso_kv_attention(self._h, self._args, _raw_stream(index) if stream is None else stream.cuda_stream)
+        st = self._lib.siso_kv_attention(self._h, self._args, _raw_stream(index))
         if st:
             self._check(st, "siso_kv_attention")
         return (out, lse) if want_lse else out
@@ -222,6 +241,9 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: t
     """target [seqs, drafts + 1, vocab] and draft [seqs, drafts, vocab] (or None: certain drafts) probabilities, fp32 or bf16;
     tokens int32 [seqs, drafts]; n_drafts int32 [seqs] or None (all); u_accept [seqs, drafts], u_sample [seqs] fp32 in [0, 1).
     Returns (tokens out int32 [seqs, drafts + 1]: those that stand, one drawn, then -1; accepted int32 [seqs])."""
+    if stream is not None:
+        with _on(stream, target.get_device()):
+            return verify_drafts(target, draft, tokens, n_drafts, u_accept, u_sample, out=out)
     shape, i32, f32 = target.shape, torch.int32, torch.float32
     if target.dtype not in _ROW_TYPES or len(shape) != 3 or not target.is_cuda:
         raise ValueError("target must be a [seqs, drafts + 1, vocab] float32 or bfloat16 tensor on a GPU")
@@ -267,7 +289,7 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: t
         st = load_library().siso_verify_drafts(target.data_ptr(), 0 if draft is None else draft.data_ptr(), _ROW_TYPES[target.dtype], seqs, n_max, vocab,
                                                tokens.data_ptr(), 0 if n_drafts is None else n_drafts.data_ptr(), u_accept.data_ptr(),
                                                u_sample.data_ptr(), new.data_ptr(), accepted.data_ptr(),
-                                               _raw_stream(index) if stream is None else stream.cuda_stream)
+                                               _raw_stream(index))
     finally:
         if here != index:
             torch.cuda.set_device(here)

@@ -149,3 +149,74 @@ def test_short_rows_are_shared_by_ctas_that_have_all_started(seqs, n_max, vocab)
     want, taken = ref.verify(target, None, tokens, None, u_accept, u_sample)
     for out, n in calls:
         assert torch.equal(out.cpu(), want) and torch.equal(n.cpu(), taken)
+
+
+# ---- streams ---------------------------------------------------------------------------------------------------------------------
+def spread(t):
+    """The same values, not contiguous."""
+    wide = torch.zeros((*t.shape, 2), dtype=t.dtype, device=t.device)
+    wide[..., 0] = t
+    return wide[..., 0]
+
+
+@pytest.mark.parametrize("what", ["rows", "queries", "lengths", "drafts"])
+@pytest.mark.parametrize("busy", ["the current stream", "the given stream"])
+def test_arguments_that_are_copied_belong_to_the_given_stream(what, busy):
+    # the current stream busy: the copies must not wait there while the kernel runs; the given one busy: the copies must not be given back to
+    # the current stream, which writes over what it can get, before the kernel has run
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n, n_q, heads, dim, page = 400, 7, 8, 128, 16
+    kv, table, k, v = filled("bf16", n, page, 2, dim)
+    s = torch.cuda.Stream()
+    rows = [torch.randn((n, 2, dim), device="cuda", generator=g) for _ in range(2)]
+    i = torch.arange(n, device="cuda")
+    slots = table[0].long()[i // page] * page + i % page
+    q = torch.randn((n_q, heads, dim), device="cuda", generator=g).to(torch.bfloat16)
+    cu, lens = (torch.tensor(x, **I32) for x in ([0, 3, n_q], [n, n - 50]))
+    tables = table.repeat(2, 1)
+    target = torch.softmax(torch.randn((5, 4, 2000), device="cuda", generator=g), -1)
+    draft = torch.softmax(torch.randn((5, 3, 2000), device="cuda", generator=g), -1)
+    tokens = torch.randint(0, 2000, (5, 3), device="cuda", generator=g, dtype=torch.int32)
+    n_drafts, u, u_sample = torch.tensor([3, 2, 0, 3, 1], **I32), torch.rand((5, 3), device="cuda", generator=g), torch.rand(5, device="cuda", generator=g)
+
+    def call(f, stream):
+        if what == "rows":
+            kv.write(f(rows[0]), f(rows[1]), f(slots), stream=stream)
+            return kv.read(f(slots), stream=stream)
+        if what == "queries":
+            return kv.attention(f(q), cu, lens, tables, 4, want_lse=True, stream=stream)
+        if what == "lengths":
+            return kv.attention(q, f(cu), f(lens), f(tables), 4, want_lse=True, stream=stream)
+        return siso.verify_drafts(f(target), f(draft), f(tokens), f(n_drafts), f(u), f(u_sample), stream=stream)
+
+    want = [t.clone() for t in call(lambda t: t, None)]
+    for _ in range(3):
+        ready = {}                                    # the arguments are there, not contiguous, before the streams become busy
+        call(lambda t: ready.setdefault(id(t), spread(t)), None)
+        if what == "rows":
+            kv.write(torch.zeros_like(rows[0]), torch.zeros_like(rows[1]), slots)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.current_stream() if busy == "the current stream" else s):
+            torch.cuda._sleep(40_000_000)             # about 20 ms
+        got = call(lambda t: ready[id(t)], s)
+        if busy == "the given stream":                # what the call gave back is overwritten
+            over = [torch.full((m,), 0x7F, dtype=torch.uint8, device="cuda") for m in (1 << 9, 1 << 12, 1 << 14, 1 << 16, 200_000, 1 << 18, 1 << 20) for _ in range(6)]
+        s.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
+        over = None
+    kv.close()
+
+
+def test_a_stream_of_another_device_is_refused():
+    kv = siso.PagedKV.allocate(1, 4, 16, 2, 128)
+    other = torch.cuda.ExternalStream(torch.cuda.Stream().cuda_stream, device=torch.device("cuda", 0))
+    kv.read(torch.zeros(1, dtype=torch.int64, device="cuda"), stream=other)
+
+    class Elsewhere:
+        device_index, cuda_stream = 1, 0
+
+    with pytest.raises(ValueError):
+        kv.read(torch.zeros(1, dtype=torch.int64, device="cuda"), stream=Elsewhere())
+    kv.close()
