@@ -498,6 +498,8 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  rows times a power of two that stands for the value's scale) are rounded to bf16 before they meet the values.
  *                  There a query's elements below 2^-31 of its row's largest lose bits, and below 2^-40 count as zero.
  * siso_kv_sync_status  Synchronises `stream`, returns the handle's device status word and clears it.
+ * siso_kv_selftest_wait_timeout  Every wait inside the attention kernels is bounded (a second); one that runs out puts SISO_ERR_TIMEOUT into
+ *                  the status word and the kernel returns.  This call lets one run out, with the kernels' own wait and nothing in flight.
  * Calls on one handle must be issued on one stream or be ordered by the caller (they share the handle's scratch).
  *
  * siso_verify_drafts (no handle; current device)  d_target [n_seqs, n_max + 1, vocab] probabilities of the target (SISO_F32 or
@@ -542,6 +544,7 @@ siso_status_t siso_kv_read(siso_kv_t *kv, int32_t layer, void *d_k, void *d_v, i
                            int64_t stride_head, const int64_t *d_slots, void *stream);
 siso_status_t siso_kv_attention(siso_kv_t *kv, const siso_attention_t *args, void *stream);
 siso_status_t siso_kv_sync_status(siso_kv_t *kv, void *stream);
+siso_status_t siso_kv_selftest_wait_timeout(siso_kv_t *kv, void *stream);
 siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int32_t dtype, int64_t n_seqs, int32_t n_max, int32_t vocab,
                                  const int32_t *d_tokens, const int32_t *d_n_drafts, const float *d_u_accept, const float *d_u_sample,
                                  int32_t *d_out, int32_t *d_accepted, void *stream);

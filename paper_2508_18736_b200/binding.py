@@ -28,7 +28,8 @@ EXPORTS = ["siso_cache_create", "siso_cache_destroy", "siso_set_option", "siso_i
            "siso_measure_fp32_fma", "siso_pair_sweep_block", "siso_merge_resolve", "siso_merge_pack",
            "siso_merge_apply_shard", "siso_tier_build", "siso_tier_work_bytes", "siso_tier_lookup", "siso_free_slots",
            "siso_shard_plan", "siso_route_planned", "siso_select_evict_planned", "siso_norm_deviation", "siso_kv_create",
-           "siso_kv_destroy", "siso_kv_write", "siso_kv_read", "siso_kv_attention", "siso_kv_sync_status", "siso_verify_drafts"]
+           "siso_kv_destroy", "siso_kv_write", "siso_kv_read", "siso_kv_attention", "siso_kv_sync_status", "siso_verify_drafts",
+           "siso_kv_selftest_wait_timeout"]
 
 
 class SisoError(RuntimeError):
@@ -123,6 +124,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.siso_kv_read.argtypes = [vp, i32, vp, vp, i32, i64, i64, i64, vp, vp]
     L.siso_kv_attention.argtypes = [vp, vp, vp]
     L.siso_kv_sync_status.argtypes = [vp, vp]
+    L.siso_kv_selftest_wait_timeout.argtypes = [vp, vp]
     L.siso_verify_drafts.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     L.siso_launch_count.argtypes = [vp]
     L.siso_launch_count.restype = i64

@@ -52,6 +52,7 @@ inline KvView kv_view(const Kv *h, int layer) {
 }
 
 siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t s);
+namespace kva { siso_status_t launch_wait_timeout(Kv *h, cudaStream_t s); }
 
 #ifdef __CUDACC__
 // Launches a kernel that may be set up while the one before it in the stream still runs (programmatic dependent launch).  It calls

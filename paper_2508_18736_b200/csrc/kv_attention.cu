@@ -184,7 +184,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     there |= (__ballot_sync(0xFFFFFFFFu, page[x] >= 0) & 0xFFFFu) << (16 * x);
                     boxes += __popc(__ballot_sync(0xFFFFFFFFu, first[x]));
                 }
-                wait_bar(&ring.empty[stage], phase ^ 1u, gave_up);
+                wait_bar(&ring.empty[stage], phase ^ 1u, gave_up, g.status);
                 if (*gave_up) break;
                 uint64_t *bar = &ring.full[stage];
                 if (lane == 0) {
@@ -214,10 +214,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         } while (cur.step(g));
         if constexpr (EIGHT) asm volatile("cp.async.wait_all;" ::: "memory");
-        if (*gave_up) {
-            for (int i = 0; i < 64; ++i) __nanosleep(1000);      // copies in flight land before the shared memory is handed back
-            if (lane == 0) set_status(g.status, SISO_ERR_TIMEOUT);
-        }
+        let_copies_land(gave_up);
         return;
     }
 
@@ -293,7 +290,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     int stage = 0;
     uint32_t phase = 0;
     for (bool more = true; more;) {
-        wait_bar(&ring.full[stage], phase, gave_up);
+        wait_bar(&ring.full[stage], phase, gave_up, g.status);
         uint8_t *tile = smem + stage * S::STAGE;
         const int k_first = stage * S::STAGE + chunk_at<RB, TK>(key_of<RB>(r0), c);
         const uint32_t v_first = smem_u32(tile) + TK * RB + v_lane;
@@ -567,6 +564,21 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of<2>(run, done_left, done_b, done_head, done_rt, done_tiles, t_end - 1);
         if (more) begin_item();
     }
+    let_copies_land(gave_up);            // (the producers may have gone before the last wait gave up)
+}
+
+// Lets a wait of these kernels run out: a barrier that expects one arrival, and none comes
+__global__ void __launch_bounds__(64) wait_timeout_kernel(int *status) {
+    __shared__ uint64_t bar;
+    __shared__ int abandoned;
+    if (threadIdx.x == 0) {
+        abandoned = 0;
+        mbar_init(&bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    for (int i = 0; i < 3; ++i) wait_bar(&bar, 0, &abandoned, status);       // the first takes the time, the others find it given up
+    let_copies_land(&abandoned);
 }
 
 // ---- joining the parts ------------------------------------------------------------------------------------------------
@@ -658,6 +670,12 @@ siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
         case 32: return dim == 128 ? run_join<32, 128>(g, s) : run_join<32, 64>(g, s);
         default: return dim == 128 ? run_join<TC_ROWS, 128>(g, s) : run_join<TC_ROWS, 64>(g, s);
     }
+}
+
+siso_status_t launch_wait_timeout(Kv *h, cudaStream_t s) {
+    wait_timeout_kernel<<<1, 64, 0, s>>>(h->status);
+    SISO_CUDA(cudaGetLastError());
+    return SISO_OK;
 }
 
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s) {

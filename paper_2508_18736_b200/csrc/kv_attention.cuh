@@ -293,9 +293,9 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(d), "r"(head), "r"(token), "r"(page), "r"(layer), "r"(umma2::smem_u32(bar))
                  : "memory");
 }
-// A wait for this CTA's own copies or warps, bounded; once any has given up, none waits any more: the loops run to their ends on
-// whatever the ring holds, so every barrier of the CTA is still met.
-__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatile int *gave_up) {
+// A wait for this CTA's own copies or warps, bounded; one that gives up says so in the status word, whichever warp it belongs to.  Once any
+// has given up, none waits any more: the loops run to their ends on whatever the ring holds, so every barrier of the CTA is still met.
+__device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatile int *gave_up, int *status) {
     if (umma2::mbar_try_wait_cta(bar, parity)) return;
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
@@ -308,6 +308,11 @@ __device__ __forceinline__ void wait_bar(uint64_t *bar, uint32_t parity, volatil
         }
     }
     *gave_up = 1;
+    set_status(status, SISO_ERR_TIMEOUT);
+}
+// after a wait has given up: copies in flight land before the shared memory is handed back
+__device__ __forceinline__ void let_copies_land(const volatile int *gave_up) {
+    if (*gave_up) for (int i = 0; i < 64; ++i) __nanosleep(1000);
 }
 
 #endif  // __CUDACC__

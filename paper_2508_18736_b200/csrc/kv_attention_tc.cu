@@ -211,8 +211,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             do {
                 const int j0 = (cur.s.tile0 + cur.tile) * TK, left = cur.s.hi - j0, before = cur.lo(g) - j0;      // rows [before, left) of the tile are there
                 for (int is_v = 0; is_v < 2; ++is_v) {
-                    wait_bar(&bars.raw_full[raw], raw_phase, gave_up);
-                    wait_bar(&bars.kv_empty[stage], phase ^ 1u, gave_up);
+                    wait_bar(&bars.raw_full[raw], raw_phase, gave_up, g.status);
+                    wait_bar(&bars.kv_empty[stage], phase ^ 1u, gave_up, g.status);
                     const uint8_t *src = raws + raw * S::RAW, *exps = metas + raw * S::RAW_META + r0;
                     if (is_v && (left < TK || before > 0)) {
                         // anything may stand in the other rows: a scale of 2^-127 makes it finite, and their probabilities are zero
@@ -253,7 +253,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     if (++stage == STAGES) stage = 0;
                     const int j0 = (cur.s.tile0 + cur.tile) * TK, left = cur.s.hi - j0, before = cur.lo(g) - j0;
                     if (left < TK || before > 0) {
-                        wait_bar(&bars.landed[stage], (phases >> stage) & 1u, gave_up);
+                        wait_bar(&bars.landed[stage], (phases >> stage) & 1u, gave_up, g.status);
                         phases ^= 1u << stage;
                         uint8_t *dst = tiles + stage * S::TILE;
                         auto clear = [&](int from, int to) {
@@ -300,7 +300,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 for (int is_v = 0; is_v < 2; ++is_v) {
                     if (stage % PRODUCERS == warp - 17) {         // a stage is always filled by the same warp, so its rounds come in order
                         uint64_t *full = EIGHT ? &bars.raw_full[stage] : &bars.kv_full[stage];
-                        wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up);
+                        wait_bar(EIGHT ? &bars.raw_empty[stage] : &bars.kv_empty[stage], phase ^ 1u, gave_up, g.status);
                         uint8_t *dst = EIGHT ? raws + stage * S::RAW : tiles + stage * S::TILE;
                         uint64_t *bar = !EIGHT && is_v && at.edge ? &bars.landed[stage] : full;
                         if (*gave_up == 0) {
@@ -361,7 +361,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 const uint64_t b = v_desc + static_cast<uint64_t>(v_stage * (S::TILE >> 4));
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {               // the first 32 keys of both halves, the others: each as soon as its probabilities are there
-                    wait_bar(&bars.p_full[t][c], (p_phases >> t) & 1u, gave_up);
+                    wait_bar(&bars.p_full[t][c], (p_phases >> t) & 1u, gave_up, g.status);
                     tcgen05_fence_after();
                     if (elect_one()) {
 #pragma unroll
@@ -379,15 +379,15 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             int n;
             do {
                 n = __shfl_sync(0xFFFFFFFFu, cur.tiles_here(), 0);
-                wait_bar(&bars.q_full[0], q_phase, gave_up);
-                wait_bar(&bars.q_full[1], q_phase, gave_up);
+                wait_bar(&bars.q_full[0], q_phase, gave_up, g.status);
+                wait_bar(&bars.q_full[1], q_phase, gave_up, g.status);
                 q_phase ^= 1u;
                 // two tiles of rows, each with every tile of keys; or one twice, each with every other tile of keys.  (One loop for both:
                 // unrolled for each it spilled, six prompts 116 us and not 108)
                 const bool split = __any_sync(0xFFFFFFFFu, cur.n_q * g.group - cur.rt * TC_ROWS <= 128);
                 const int ahead = split ? 2 : 1, per_tile = split ? 1 : 2;
                 for (int j = -ahead; j < n; ++j) {
-                    if (j >= 0) wait_bar(&bars.kv_full[v_stage], v_phase, gave_up);
+                    if (j >= 0) wait_bar(&bars.kv_full[v_stage], v_phase, gave_up, g.status);
                     for (int i = 0; i < per_tile; ++i) {
                         const int t = split ? j & 1 : i;
                         if (j >= 0) values(t, j < ahead);
@@ -396,7 +396,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                             next(v_stage, v_phase);
                         }
                         if (j + ahead < n) {
-                            if (i == 0) wait_bar(&bars.kv_full[k_stage], k_phase, gave_up);
+                            if (i == 0) wait_bar(&bars.kv_full[k_stage], k_phase, gave_up, g.status);
                             tcgen05_fence_after();
                             scores(t);
                             if (i + 1 == per_tile) {
@@ -427,7 +427,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         auto everyone = [&]() { asm volatile("bar.sync 3, 512;" ::: "memory"); };
         auto store_item = [&](bool split_item) {
             const bool to_part = __any_sync(0xFFFFFFFFu, out_place >= 0), split = __any_sync(0xFFFFFFFFu, split_item);      // (uniform, visibly)
-            wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
+            wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up, g.status);
             tcgen05_fence_after();
             mine_out = l;
             together();
@@ -565,7 +565,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             const int k0 = split ? t : 0, k_step = split ? 2 : 1;
             for (int k = k0; k < n; k += k_step) {
                 const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
-                wait_bar(&bars.s_full[t], tile_phase, gave_up);
+                wait_bar(&bars.s_full[t], tile_phase, gave_up, g.status);
                 tcgen05_fence_after();
                 uint32_t ra[32], rb[32];
                 tmem_ld_32x32(s_at, ra);
@@ -609,7 +609,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                     m = m2;
                     l *= corr;
                     if (k > k0) {
-                        wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up);
+                        wait_bar(&bars.o_done[t], tile_phase ^ 1u, gave_up, g.status);
                         tcgen05_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < D / 2; c += 16) {         // 16 columns at a time: the scores stay in registers
@@ -664,10 +664,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
 
     // ---- teardown
     __syncwarp();
-    if (*gave_up) {
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);      // copies in flight land before the shared memory is handed back
-        if (threadIdx.x == 0) set_status(g.status, SISO_ERR_TIMEOUT);
-    }
+    let_copies_land(gave_up);
     tcgen05_fence_before();
     __syncthreads();
     if (warp == 16) {

@@ -396,6 +396,12 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *s
     return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
 }
 
+siso_status_t siso_kv_selftest_wait_timeout(siso_kv_t *h, void *stream) {
+    if (!h) return SISO_ERR_INVALID_ARG;
+    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    return kva::launch_wait_timeout(h, static_cast<cudaStream_t>(stream));
+}
+
 siso_status_t siso_kv_sync_status(siso_kv_t *h, void *stream) {
     if (!h) return SISO_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -230,6 +230,11 @@ class PagedKV:
         """Synchronise and return the handle's device status word (0 = clear); it is cleared by the call."""
         return int(self._lib.siso_kv_sync_status(self._h, _raw_stream(self._index) if stream is None else stream.cuda_stream))
 
+    def selftest_wait_timeout(self, stream=None) -> None:
+        """Lets one bounded wait of the attention kernels run out (see siso_kv_selftest_wait_timeout)."""
+        self._check(self._lib.siso_kv_selftest_wait_timeout(self._h, _raw_stream(self._index) if stream is None else stream.cuda_stream),
+                    "siso_kv_selftest_wait_timeout")
+
     def check_status(self, stream=None) -> None:
         st = self.sync_status(stream)
         if st != 0:

@@ -220,3 +220,13 @@ def test_a_stream_of_another_device_is_refused():
     with pytest.raises(ValueError):
         kv.read(torch.zeros(1, dtype=torch.int64, device="cuda"), stream=Elsewhere())
     kv.close()
+
+
+# ---- waits -----------------------------------------------------------------------------------------------------------------------
+def test_a_wait_that_runs_out_is_reported_and_the_handle_goes_on():
+    kv, table, k, v = filled("i8", 300, 16, 2, 128)
+    kv.selftest_wait_timeout()
+    assert kv.sync_status() == 6 and kv.sync_status() == 0          # SISO_ERR_TIMEOUT, once
+    attend(kv, table, 300, 2, 8, 128, k, v)
+    attend(kv, table, 300, 60, 8, 128, k, v)
+    kv.close()
