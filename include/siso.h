@@ -500,7 +500,8 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  * siso_kv_sync_status  Synchronises `stream`, returns the handle's device status word and clears it.
  * siso_kv_selftest_wait_timeout  Every wait inside the attention kernels is bounded (a second); one that runs out puts SISO_ERR_TIMEOUT into
  *                  the status word and the kernel returns.  This call lets one run out, with the kernels' own wait and nothing in flight.
- * Calls on one handle must be issued on one stream or be ordered by the caller (they share the handle's scratch).
+ * Calls on one handle must be issued on one stream or be ordered by the caller (they share the handle's scratch).  siso_kv_* calls
+ * leave the calling thread's current device as it was.
  *
  * siso_verify_drafts (no handle; current device)  d_target [n_seqs, n_max + 1, vocab] probabilities of the target (SISO_F32 or
  *                  SISO_BF16), row t the distribution of the token that draft t claims; d_draft [n_seqs, n_max, vocab] those the

@@ -31,6 +31,24 @@ struct Kv {
 
 inline int kv_elem_bytes(int dtype) { return dtype == SISO_BF16 ? 2 : 1; }
 
+// Makes a device the calling thread's for as long as this lives, then the one that was
+class OnDevice {
+    int before_ = 0, device_;
+    cudaError_t error_;
+
+public:
+    explicit OnDevice(int device) : device_(device) {
+        error_ = cudaGetDevice(&before_);
+        if (error_ == cudaSuccess && before_ != device_) error_ = cudaSetDevice(device_);
+    }
+    ~OnDevice() {
+        if (error_ == cudaSuccess && before_ != device_) cudaSetDevice(before_);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+    cudaError_t error() const { return error_; }
+};
+
 // the pages of one layer
 inline KvView kv_view(const Kv *h, int layer) {
     const siso_kv_config_t &g = h->cfg;

@@ -260,7 +260,8 @@ static siso_status_t rows_call(Kv *h, int layer, void *k, void *v, int dtype, lo
     if (!k || !v || !slots || stride_token < 0 || stride_head < 0) return SISO_ERR_INVALID_ARG;
     const int elems16 = dtype == SISO_F32 ? 4 : 8;
     if (!aligned16(k) || !aligned16(v) || stride_token % elems16 != 0 || stride_head % elems16 != 0) return SISO_ERR_UNSUPPORTED;
-    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    const OnDevice on(h->cfg.device);
+    SISO_CUDA(on.error());
     const Rows rows{k, v, n, stride_token, stride_head};
     const KvView kv = kv_view(h, layer);
     const long long *sl = reinterpret_cast<const long long *>(slots);
@@ -333,7 +334,8 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
     int n_dev = 0;
     SISO_CUDA(cudaGetDeviceCount(&n_dev));
     if (cfg->device < 0 || cfg->device >= n_dev) return SISO_ERR_INVALID_ARG;
-    SISO_CUDA(cudaSetDevice(cfg->device));
+    const OnDevice on(cfg->device);
+    SISO_CUDA(on.error());
     int major = 0, sms = 0;
     SISO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, cfg->device));
     SISO_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, cfg->device));
@@ -359,7 +361,7 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
 
 siso_status_t siso_kv_destroy(siso_kv_t *h) {
     if (!h) return SISO_ERR_INVALID_ARG;
-    cudaSetDevice(h->cfg.device);
+    const OnDevice on(h->cfg.device);
     cudaDeviceSynchronize();
     if (h->ws) h->cfg.allocator.free(h->ws, h->cfg.allocator.ctx);
     if (h->status) h->cfg.allocator.free(h->status, h->cfg.allocator.ctx);
@@ -392,20 +394,23 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *s
     if (!kvc::aligned16(a->d_q) || !kvc::aligned16(a->d_out)) return SISO_ERR_UNSUPPORTED;
     if (!kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
     if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
-    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    const OnDevice on(h->cfg.device);
+    SISO_CUDA(on.error());
     return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
 }
 
 siso_status_t siso_kv_selftest_wait_timeout(siso_kv_t *h, void *stream) {
     if (!h) return SISO_ERR_INVALID_ARG;
-    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    const OnDevice on(h->cfg.device);
+    SISO_CUDA(on.error());
     return kva::launch_wait_timeout(h, static_cast<cudaStream_t>(stream));
 }
 
 siso_status_t siso_kv_sync_status(siso_kv_t *h, void *stream) {
     if (!h) return SISO_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    SISO_CUDA(cudaSetDevice(h->cfg.device));
+    const OnDevice on(h->cfg.device);
+    SISO_CUDA(on.error());
     int st = 0;
     SISO_CUDA(cudaMemcpyAsync(&st, h->status, sizeof(int), cudaMemcpyDeviceToHost, s));
     SISO_CUDA(cudaMemsetAsync(h->status, 0, sizeof(int), s));

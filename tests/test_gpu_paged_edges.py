@@ -230,3 +230,16 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_goes_on():
     attend(kv, table, 300, 2, 8, 128, k, v)
     attend(kv, table, 300, 60, 8, 128, k, v)
     kv.close()
+
+
+# ---- devices ---------------------------------------------------------------------------------------------------------------------
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_calls_leave_the_current_device_as_it_was():
+    kv = siso.PagedKV.allocate(1, 4, 16, 2, 128, device=1)
+    here = dict(device="cuda:1")
+    slots, row = torch.zeros(1, dtype=torch.int64, **here), torch.randn((1, 2, 128), **here)
+    q, one = torch.zeros((1, 4, 128), dtype=torch.bfloat16, **here), torch.ones(1, dtype=torch.int32, **here)
+    for call in (lambda: kv.write(row, row, slots), lambda: kv.read(slots),
+                 lambda: kv.attention(q, torch.cat([one - 1, one]), one, (one - 1)[None], 1), lambda: kv.sync_status(), lambda: kv.close()):
+        call()
+        assert torch.cuda.current_device() == 0
