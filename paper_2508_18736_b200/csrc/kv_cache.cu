@@ -329,6 +329,10 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
         if (st < 0) return SISO_ERR_INVALID_ARG;
         if (st % 8 != 0 || st >= (1ll << 38)) return SISO_ERR_UNSUPPORTED;
     }
+    // entries that share their place: rows would be written over one another, and TMA takes no stride of 0
+    if ((cfg->n_layers > 1 && cfg->stride_layer == 0) || (cfg->n_pages > 1 && cfg->stride_page == 0) || cfg->stride_token == 0 ||
+        (cfg->n_kv_heads > 1 && cfg->stride_head == 0))
+        return SISO_ERR_UNSUPPORTED;
     if (!kvc::aligned16(cfg->d_k) || !kvc::aligned16(cfg->d_v) || !kvc::aligned16(cfg->d_k_exp) || !kvc::aligned16(cfg->d_v_exp))
         return SISO_ERR_UNSUPPORTED;
     int n_dev = 0;

@@ -243,3 +243,14 @@ def test_calls_leave_the_current_device_as_it_was():
                  lambda: kv.attention(q, torch.cat([one - 1, one]), one, (one - 1)[None], 1), lambda: kv.sync_status(), lambda: kv.close()):
         call()
         assert torch.cuda.current_device() == 0
+
+
+# ---- strides ---------------------------------------------------------------------------------------------------------------------
+def test_pages_whose_entries_share_a_place_are_refused():
+    one = torch.zeros((2, 4, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for dim in range(4):
+        shared = one.narrow(dim, 0, 1).expand(one.shape)
+        with pytest.raises(siso.SisoError) as e:
+            siso.PagedKV(shared, shared.clone().narrow(dim, 0, 1).expand(one.shape))
+        assert e.value.status == 2
+        siso.PagedKV(one.narrow(dim, 0, 1 if dim != 2 else 8), one.clone().narrow(dim, 0, 1 if dim != 2 else 8)).close()
