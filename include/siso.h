@@ -476,7 +476,7 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  the smallest that lets the row's largest magnitude fit (448 for e4m3, 127 for i8).  Byte 255 marks a row
  *                  that held a NaN or an infinity; it reads back as NaN.  page_size, head_dim multiples of 8 (head_dim at
  *                  most 256), base pointers 16-byte aligned, strides multiples of 8 elements (attention over 8-bit pages: of 16) and not 0
- *                  where there are several entries, else SISO_ERR_UNSUPPORTED.  The handle's scratch comes from the allocator on first use.  Synchronous.
+ *                  where there are several entries (strides of one entry count for nothing, here and below), else SISO_ERR_UNSUPPORTED.  The handle's scratch comes from the allocator on first use.  Synchronous.
  * siso_kv_write    Rows d_k, d_v [n_tokens, n_kv_heads, head_dim] (SISO_F32 or SISO_BF16, strides in elements, multiples of
  *                  16 bytes) into slots d_slots [n_tokens] = page * page_size + token; a slot outside the pool (-1) is skipped.
  *                  Slots of one call must differ.  Codes are rounded to nearest, ties to even.

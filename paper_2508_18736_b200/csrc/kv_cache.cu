@@ -257,6 +257,8 @@ static siso_status_t rows_call(Kv *h, int layer, void *k, void *v, int dtype, lo
     if (!h || layer < 0 || layer >= h->cfg.n_layers || n < 0) return SISO_ERR_INVALID_ARG;
     if (dtype != SISO_F32 && dtype != SISO_BF16) return SISO_ERR_INVALID_ARG;
     if (n == 0) return SISO_OK;
+    if (n == 1) stride_token = 0;                  // a dimension of one entry has no stride, whatever its tensor says
+    if (h->cfg.n_kv_heads == 1) stride_head = 0;
     if (!k || !v || !slots || stride_token < 0 || stride_head < 0) return SISO_ERR_INVALID_ARG;
     const int elems16 = dtype == SISO_F32 ? 4 : 8;
     if (!aligned16(k) || !aligned16(v) || stride_token % elems16 != 0 || stride_head % elems16 != 0) return SISO_ERR_UNSUPPORTED;
@@ -324,6 +326,12 @@ siso_status_t siso_kv_create(siso_kv_t **out, const siso_kv_config_t *cfg) {
     if ((cfg->allocator.alloc == nullptr) != (cfg->allocator.free == nullptr)) return SISO_ERR_INVALID_ARG;
     if (cfg->page_size % 8 != 0 || cfg->page_size > 65536 || cfg->head_dim % 8 != 0 || cfg->head_dim > kKvMaxDim || cfg->n_kv_heads > 4096)
         return SISO_ERR_UNSUPPORTED;
+    siso_kv_config_t own = *cfg;
+    cfg = &own;
+    // a dimension of one entry has no stride, whatever its tensor says
+    if (cfg->n_layers == 1) own.stride_layer = 0;
+    if (cfg->n_pages == 1) own.stride_page = 0;
+    if (cfg->n_kv_heads == 1) own.stride_head = 0;
     const long long strides[] = {cfg->stride_layer, cfg->stride_page, cfg->stride_token, cfg->stride_head};
     for (long long st : strides) {
         if (st < 0) return SISO_ERR_INVALID_ARG;
@@ -384,12 +392,17 @@ siso_status_t siso_kv_read(siso_kv_t *h, int32_t layer, void *d_k, void *d_v, in
     return kvc::rows_call<true>(h, layer, d_k, d_v, dtype, n_tokens, stride_token, stride_head, d_slots, static_cast<cudaStream_t>(stream));
 }
 
-siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *a, void *stream) {
+siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *args, void *stream) {
+    const siso_attention_t *a = args;
     if (!h || !a || a->n_tokens < 0 || a->n_seqs < 0 || a->layer < 0 || a->layer >= h->cfg.n_layers) return SISO_ERR_INVALID_ARG;
     if (a->n_heads < 1 || a->n_heads % h->cfg.n_kv_heads != 0 || a->window < 0 || a->max_q < 0 || a->max_pages < 0) return SISO_ERR_INVALID_ARG;
     if ((a->flags & ~SISO_ATTN_CAUSAL) != 0u || !(a->scale == a->scale)) return SISO_ERR_INVALID_ARG;
     if (a->n_tokens == 0 || a->n_seqs == 0) return SISO_OK;
     if (!a->d_q || !a->d_out || !a->d_cu_q || !a->d_kv_len || (a->max_pages > 0 && !a->d_pages) || a->pages_stride < 0) return SISO_ERR_INVALID_ARG;
+    siso_attention_t own = *args;
+    a = &own;
+    if (a->n_tokens == 1) own.q_stride_token = own.out_stride_token = 0;       // (one entry: no stride)
+    if (a->n_heads == 1) own.q_stride_head = own.out_stride_head = 0;
     const int64_t strides[] = {a->q_stride_token, a->q_stride_head, a->out_stride_token, a->out_stride_head};
     for (int64_t st : strides) {
         if (st < 0) return SISO_ERR_INVALID_ARG;

@@ -254,3 +254,37 @@ def test_pages_whose_entries_share_a_place_are_refused():
             siso.PagedKV(shared, shared.clone().narrow(dim, 0, 1).expand(one.shape))
         assert e.value.status == 2
         siso.PagedKV(one.narrow(dim, 0, 1 if dim != 2 else 8), one.clone().narrow(dim, 0, 1 if dim != 2 else 8)).close()
+
+
+def any_stride(t, dim, stride):
+    """t, whose dimension `dim` has one entry, with another stride there."""
+    assert t.shape[dim] == 1
+    s = list(t.stride())
+    s[dim] = stride
+    return t.as_strided(t.shape, s)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("stride", [0, 1, 83])
+def test_strides_of_one_entry_count_for_nothing(kind, stride):
+    # one layer, one kv head, one token: a row of a projection whose width is odd, pages turned out of another order
+    n, dim, page = 20, 64, 32
+    k, v, ke, ve = ref.make_pages(kind, 1, 1, page, 1, dim, fill="nan")
+    for d in (0, 1, 3):
+        k, v = any_stride(k, d, stride), any_stride(v, d, stride)
+    kv = siso.PagedKV(k, v, ke, ve)
+    rows = [torch.randn((n, 1, dim), device="cuda") for _ in range(2)]
+    slots = torch.arange(n, device="cuda")
+    kv.write(*(any_stride(r[:-1], 1, stride) for r in rows), slots[:-1])
+    kv.write(*(any_stride(any_stride(r[-1:], 1, stride), 0, stride) for r in rows), slots[-1:])
+    k, v = ([r.to(torch.bfloat16).double() if kind == "bf16" else ref.values(*ref.quantised(r, kind)) for r in rows])
+    got = torch.full((1, 1, dim), 7.0, device="cuda")
+    kv.read(slots[-1:], out=(any_stride(got, 0, stride), any_stride(torch.empty_like(got), 0, stride)))
+    assert torch.equal(got.double(), k[-1:])
+    for heads in (1, 4):
+        q = any_stride(torch.randn((1, heads, dim), device="cuda").to(torch.bfloat16), 0, stride)
+        q = any_stride(q, 1, stride) if heads == 1 else q
+        cu, lens, table = torch.tensor([0, 1], **I32), torch.tensor([n], **I32), torch.zeros((1, 1), **I32)
+        out, lse = kv.attention(q, cu, lens, table, 1, want_lse=True, out=any_stride(torch.empty((1, heads, dim), dtype=torch.bfloat16, device="cuda"), 0, stride))
+        check_attention(out, lse, ref.attention(q, k, v, 1), dim)
+    kv.close()
