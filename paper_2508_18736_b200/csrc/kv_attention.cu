@@ -129,7 +129,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     constexpr int LINE = RB < 128 ? RB : 128;                // bytes of a row that lie together
     constexpr int KT = SUB / 16, DT = D / 16;                // tiles of 16 keys, of 16 d
     extern __shared__ uint8_t smem_raw[];
-    __shared__ unsigned long long buf[S::THREADS / 32 + 2];
+    __shared__ unsigned long long buf[S::THREADS / 32 + 3];
     __shared__ Ring<STAGES> ring;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // (an offset: the loads stay shared loads)
     float *merge_o = reinterpret_cast<float *>(smem + STAGES * S::STAGE);

@@ -83,10 +83,10 @@ template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g,
 // the window is not looked up: its pages may have been given back
 __device__ __forceinline__ bool holds_seen(const Args &g, int lo, int hi, int j) { return j < hi && (j | (g.box - 1)) >= lo; }
 // units of one key/value head of sequence b: a key tile counts W, and an item EXTRA more, for its beginning and end
-template <int MR, int TK, int EXTRA, int W> __device__ __forceinline__ int seq_units(const Args &g, int b) {
+template <int MR, int TK, int EXTRA, int W> __device__ __forceinline__ long long seq_units(const Args &g, int b) {
     int q0;
     const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
-    int units = 0;
+    long long units = 0;
     for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
     return units;
 }
@@ -169,48 +169,53 @@ constexpr int FEW_TILES = 16;          // row tiles that one thread goes through
 
 // units of one head of the sequences b0 .. b0 + THREADS - 1 that the call has, one per thread
 template <int MR, int TK, int EXTRA, int W, int THREADS>
-__device__ __forceinline__ int chunk_units(const Args &g, int b0, unsigned long long *buf) {
+__device__ __forceinline__ long long chunk_units(const Args &g, int b0, unsigned long long *buf) {
     const int n = min(g.a.n_seqs - b0, THREADS);
     // a thread per sequence, unless there are a few long ones: then a thread per row tile (six prompts of 4 to 15 row tiles: 108 us and 111 us)
     if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA, W>(g, b0 + threadIdx.x) : 0;
-    int mine = 0;
+    long long mine = 0;
     for (int i = 0; i < n; ++i) {
         int q0;
         const int n_q = seq_queries(g, b0 + i, q0), len = seq_len(g, b0 + i), tiles = (n_q * g.group + MR - 1) / MR;
         unsigned long long x = 0ull, all;
         for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
         cta_scan<THREADS>(x, all, buf);
-        if (static_cast<int>(threadIdx.x) == i) mine = static_cast<int>(all);
+        if (static_cast<int>(threadIdx.x) == i) mine = static_cast<long long>(all);
     }
     return mine;
 }
 // This CTA's run and the cursor at its start; every thread of the CTA gets the same.  False: nothing to do.  The CTA's record
-// is cleared.  `buf`: THREADS / 32 + 2 words of shared memory.
+// is cleared.  `buf`: THREADS / 32 + 3 words of shared memory.  A run is counted in 32 bits: a call of 2^31 units a CTA (more than ten
+// minutes of work) is reported and not done.
 template <int MR, int TK, int EXTRA, int W, int THREADS>
 __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA, W> &cur, unsigned long long *buf) {
     constexpr int WARPS = THREADS / 32;
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) g.records[cta].valid = 0;
     unsigned long long mine = 0ull, upto = 0ull, all;          // units of this thread's sequence of the first chunk, and up to them
-    int per_head = 0;
+    long long per_head = 0;
     run.total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
-        const int ph = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
+        const long long ph = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
         const unsigned long long x = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads, s = cta_scan<THREADS>(x, all, buf);
         if (c0 == 0) { mine = x; upto = s; per_head = ph; }
         run.total += static_cast<long long>(all);
     }
     run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + W - 1) / W));      // (so that every run within an item has a tile)
     if (cta >= run.ctas) return false;
+    if (run.total / run.ctas >= 0x7FFFFFFFll - EXTRA) {
+        set_status(g.status, SISO_ERR_UNSUPPORTED);
+        return false;
+    }
     const unsigned long long want = static_cast<unsigned long long>(run.total * cta / run.ctas);
     run.end = run.total * (cta + 1) / run.ctas;
     cur.left = static_cast<int>(run.end - static_cast<long long>(want));
-    // buf[WARPS], buf[WARPS + 1]: what the one thread that finds it says
-    auto found = [&](bool here, unsigned long long a, unsigned long long b) {
+    // buf[WARPS] and the two after it: what the one thread that finds it says
+    auto found = [&](bool here, unsigned long long a, unsigned long long b, unsigned long long c) {
         __syncthreads();
         if (threadIdx.x == 0) buf[WARPS] = ~0ull;
         __syncthreads();
-        if (here) { buf[WARPS] = a; buf[WARPS + 1] = b; }
+        if (here) { buf[WARPS] = a; buf[WARPS + 1] = b; buf[WARPS + 2] = c; }
         __syncthreads();
         return buf[WARPS] != ~0ull;
     };
@@ -222,21 +227,21 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
             mine = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
             upto = base + cta_scan<THREADS>(mine, all, buf);
         }
-        if (found(want < upto && want >= upto - mine, (static_cast<unsigned long long>(c0 + threadIdx.x) << 32) | static_cast<uint32_t>(per_head), upto - mine)) break;
+        if (found(want < upto && want >= upto - mine, static_cast<unsigned long long>(c0 + threadIdx.x), upto - mine, static_cast<unsigned long long>(per_head))) break;
         __syncthreads();
         if (threadIdx.x == THREADS - 1) buf[0] = upto;
         __syncthreads();
         base = buf[0];
     }
-    cur.b = static_cast<int>(buf[WARPS] >> 32);
+    cur.b = static_cast<int>(buf[WARPS]);
     cur.load_seq(g);
-    const unsigned long long within = want - buf[WARPS + 1];
-    const int head_units = static_cast<int>(buf[WARPS] & 0xFFFFFFFFull), tiles = (cur.n_q * g.group + MR - 1) / MR;
+    const unsigned long long within = want - buf[WARPS + 1], head_units = buf[WARPS + 2];
+    const int tiles = (cur.n_q * g.group + MR - 1) / MR;
     cur.head = static_cast<int>(within / head_units);
-    int x = static_cast<int>(within - static_cast<unsigned long long>(cur.head) * head_units);
+    unsigned long long x = within - static_cast<unsigned long long>(cur.head) * head_units;
     cur.rt = 0;
     if (tiles <= FEW_TILES) {
-        for (cur.load_span(g); x >= W * cur.s.tiles + EXTRA; cur.load_span(g)) {
+        for (cur.load_span(g); x >= static_cast<unsigned long long>(W * cur.s.tiles + EXTRA); cur.load_span(g)) {
             x -= W * cur.s.tiles + EXTRA;
             ++cur.rt;
         }
@@ -246,14 +251,14 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
             const int rt = c0 + static_cast<int>(threadIdx.x);
             const unsigned long long n = rt < tiles ? W * span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
             const unsigned long long s = before + cta_scan<THREADS>(n, all, buf);
-            if (found(static_cast<unsigned long long>(x) < s && static_cast<unsigned long long>(x) >= s - n, static_cast<unsigned long long>(rt), s - n)) break;
+            if (found(x < s && x >= s - n, static_cast<unsigned long long>(rt), s - n, 0ull)) break;
             before += all;
         }
         cur.rt = static_cast<int>(buf[WARPS]);
-        x -= static_cast<int>(buf[WARPS + 1]);
+        x -= buf[WARPS + 1];
         cur.load_span(g);
     }
-    cur.enter(g, x);
+    cur.enter(g, static_cast<int>(x));
     return cur.left > 0;
 }
 // the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u

@@ -38,7 +38,7 @@ struct Bars {
     Run run;
     uint32_t tmem;
     int gave_up;
-    unsigned long long buf[30];
+    unsigned long long buf[31];
     float peer[2][2][128];     // a row's maximum, or sum, on its way to the other thread of the row
 };
 

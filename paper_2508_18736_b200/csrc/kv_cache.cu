@@ -410,7 +410,7 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *args, void
     }
     if (!kvc::aligned16(a->d_q) || !kvc::aligned16(a->d_out)) return SISO_ERR_UNSUPPORTED;
     if (!kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
-    if (a->n_tokens >= (1ll << 31) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
+    if (a->n_tokens >= ((1ll << 31) - 256) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     const OnDevice on(h->cfg.device);
     SISO_CUDA(on.error());
     return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));

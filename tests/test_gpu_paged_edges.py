@@ -288,3 +288,29 @@ def test_strides_of_one_entry_count_for_nothing(kind, stride):
         out, lse = kv.attention(q, cu, lens, table, 1, want_lse=True, out=any_stride(torch.empty((1, heads, dim), dtype=torch.bfloat16, device="cuda"), 0, stride))
         check_attention(out, lse, ref.attention(q, k, v, 1), dim)
     kv.close()
+
+
+# ---- size ------------------------------------------------------------------------------------------------------------------------
+def test_more_units_of_work_than_32_bits_count():
+    # 140,000 queries of 8 heads over 2 M tokens, sent to the kernel for few rows: 2.3 G units for the one kv head.  All queries are alike, so all
+    # outputs are
+    n, n_q, heads, dim, page = 1 << 21, 140_000, 8, 64, 4096
+    g = torch.Generator(device="cuda").manual_seed(2)
+    kv = siso.PagedKV.allocate(1, n // page, page, 1, dim, torch.int8)
+    for t in (kv.k, kv.v):
+        t.copy_(torch.randint(-127, 128, t.shape, device="cuda", generator=g, dtype=torch.int8))
+    kv.k_exp.fill_(127 - 9)
+    kv.v_exp.fill_(127 - 7)
+    table = torch.randperm(n // page, device="cuda", generator=g).to(torch.int32)[None]
+    q = torch.randn((1, heads, dim), device="cuda", generator=g).to(torch.bfloat16)
+    cu, lens = torch.tensor([0, n_q], **I32), torch.tensor([n], **I32)
+    out, lse = kv.attention(q.expand(n_q, heads, dim), cu, lens, table, 1, causal=False, want_lse=True)
+    assert kv.sync_status() == 0
+    k, v = kv.k.double().view(n, dim) * 2.0 ** -9, kv.v.double().view(n, dim) * 2.0 ** -7
+    x = q[0].double() @ k.T * dim ** -0.5
+    p = torch.softmax(x, -1)
+    want = ((p @ v)[None], torch.logsumexp(x, -1)[None], (p @ v.abs())[None], float((q[0].double().abs() @ k.abs().T).max()) * dim ** -0.5)
+    for i in range(0, n_q, 20_000):
+        m = min(20_000, n_q - i)
+        check_attention(out[i:i + m], lse[i:i + m], [w if isinstance(w, float) else w.expand(m, *w.shape[1:]) for w in want], dim)
+    kv.close()
