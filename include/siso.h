@@ -488,7 +488,8 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  tokens j < kv_len with j <= p (SISO_ATTN_CAUSAL) and j > p - window (window > 0).  Query head h reads
  *                  key/value head h / (n_heads / n_kv_heads).
  *                      out = sum_j softmax_j(scale q.k_j) v_j,   lse = ln sum_j exp(scale q.k_j)
- *                  and 0 and -infinity where nothing is seen.  d_q, d_out bf16 [n_tokens, n_heads, head_dim] with strides in
+ *                  and 0 and -infinity where nothing is seen; rows that no sequence covers are not written.  d_cu_q, d_kv_len and d_pages
+ *                  must not change while the call runs.  d_q, d_out bf16 [n_tokens, n_heads, head_dim] with strides in
  *                  elements (multiples of 8, bases 16-byte aligned); d_lse [n_tokens, n_heads] fp32 or NULL.  head_dim 64 or 128.
  *                  max_q: the most queries of one sequence (a hint that selects the kernel; any value gives the same result up
  *                  to rounding).  Places beyond kv_len and places before the windows of all of a sequence's queries may hold anything, NaN

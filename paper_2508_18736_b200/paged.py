@@ -186,7 +186,7 @@ class PagedKV:
                   out: Optional[torch.Tensor] = None):
         """q [n, heads, head dim] bf16: the queries of all sequences one after the other, sequence b's from cu_q[b] on (int32
         [seqs + 1]); kv_len int32 [seqs]: tokens in all, the new ones included (already written); pages int32 [seqs, max pages].
-        Returns out [n, heads, head dim], or (out, lse [n, heads] fp32) with want_lse."""
+        Rows of q that no sequence covers leave theirs of the outputs as they were (of new outputs: anything).  Returns out [n, heads, head dim], or (out, lse [n, heads] fp32) with want_lse."""
         if stream is not None:
             with _on(stream, self._index):
                 return self.attention(q, cu_q, kv_len, pages, max_q, layer, scale, causal, window, want_lse, out=out)

@@ -314,3 +314,20 @@ def test_more_units_of_work_than_32_bits_count():
         m = min(20_000, n_q - i)
         check_attention(out[i:i + m], lse[i:i + m], [w if isinstance(w, float) else w.expand(m, *w.shape[1:]) for w in want], dim)
     kv.close()
+
+
+# ---- rows that no sequence covers ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_q", [2, 90])
+def test_rows_that_no_sequence_covers_are_left_alone(n_q):
+    n, heads, dim = 200, 8, 128
+    kv, table, k, v = filled("bf16", n, 16, 2, dim)
+    q = torch.randn((n_q + 7, heads, dim), device="cuda").to(torch.bfloat16)
+    cu, lens = torch.tensor([3, 3 + n_q], **I32), torch.tensor([n], **I32)
+    out = torch.full_like(q, 7.0)
+    kv.attention(q, cu, lens, table, n_q, out=out)
+    assert (out[:3] == 7).all() and (out[3 + n_q:] == 7).all()
+    _, lse = kv.attention(q, cu, lens, table, n_q, want_lse=True)
+    check_attention(out[3:3 + n_q], lse[3:3 + n_q], ref.attention(q[3:3 + n_q], k, v, n_q), dim)
+    kv.attention(q, cu[:1], lens[:0], table[:0], n_q, out=out.fill_(7.0))         # no sequences at all
+    assert (out == 7).all()
+    kv.close()
