@@ -536,7 +536,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     if (whole) {
                         const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row)));
                         const int head = done_head * g.group + row - i * g.group;
-                        const float inv = l[t][h] > 0.f ? 1.f / l[t][h] : 0.f;
+                        const float inv = inverse_of(l[t][h]);
                         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(done_q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
 #pragma unroll
                         for (int d = 0; d < DT; ++d) {
@@ -548,7 +548,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                             }
                         }
                         if (g.a.d_lse && r0 == 0)
-                            g.a.d_lse[static_cast<long long>(done_q0 + i) * g.a.n_heads + head] = l[t][h] > 0.f ? (m[t][h] + log2f(l[t][h])) * 0.6931471805599453f : -INFINITY;
+                            g.a.d_lse[static_cast<long long>(done_q0 + i) * g.a.n_heads + head] = lse_of(m[t][h], l[t][h]);
                     } else {
                         const long long place = part_place(blockIdx.x, began_before) * MR + in_tile;
                         float *dst = g.part_o + place * D;
@@ -622,7 +622,7 @@ join_kernel(const __grid_constant__ Args g) {
                 }
 #pragma unroll
                 for (int f = 0; f < F; ++f) {
-                    if (ml[f].x == -INFINITY) continue;
+                    if (ml[f].y == 0.f) continue;                            // nothing seen there (a NaN is no zero)
                     const float m2 = fmaxf(m, ml[f].x), a = m == -INFINITY ? 0.f : ex2(m - m2), b = ex2(ml[f].x - m2);
                     l = l * a + ml[f].y * b;
                     m = m2;
@@ -641,7 +641,7 @@ join_kernel(const __grid_constant__ Args g) {
 #pragma unroll
             for (int w = 1; w < WPR; ++w) {
                 const float m1 = sml[warp + w][0], l1 = sml[warp + w][1];
-                if (m1 == -INFINITY) continue;
+                if (l1 == 0.f) continue;
                 const float m2 = fmaxf(m, m1), a = m == -INFINITY ? 0.f : ex2(m - m2), b = ex2(m1 - m2);
                 l = l * a + l1 * b;
                 m = m2;
@@ -651,12 +651,12 @@ join_kernel(const __grid_constant__ Args g) {
         }
         if (!real) return;
         const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = inverse_of(l);
         __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
 #pragma unroll
         for (int x = 0; x < N; ++x) dst[x * 32 + lane] = __float2bfloat16_rn(o[x] * inv);
         if (g.a.d_lse && lane == 0)
-            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m, l);
     }
 }
 

@@ -279,6 +279,10 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// From a row's maximum (in powers of two) and sum: a sum of zero means that nothing is seen; NaN stays NaN
+__device__ __forceinline__ float inverse_of(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
+
 constexpr unsigned long long WAIT_NS = 1000000000ull;       // a wait gives up after a second
 
 // byte offset of a 16-byte chunk in a tile of TK rows as TMA writes it: lines of 128 bytes with the chunk's place xor-ed with the

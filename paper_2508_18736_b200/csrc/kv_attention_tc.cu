@@ -451,8 +451,8 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 sum = sum * f0 + l1 * f1;
                 m = m2;
             }
-            const bool none = m == -INFINITY;                             // (the sum may hold remainders of 2^-126)
-            const float inv = none ? 0.f : 1.f / sum;
+            if (m == -INFINITY && sum == sum) sum = 0.f;                  // nothing seen (the sum may hold remainders of 2^-126)
+            const float inv = inverse_of(sum);
 #pragma unroll 1
             for (int c = 0; c < D / 64; ++c) {
                 uint32_t r[32];
@@ -505,7 +505,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             }
             if (out_token >= 0 && half == 0) {
                 if (out_place >= 0) *reinterpret_cast<float2 *>(g.part_ml + 2ll * out_place) = make_float2(m, sum);
-                else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_token) * g.a.n_heads + out_head] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+                else if (g.a.d_lse) g.a.d_lse[static_cast<long long>(out_token) * g.a.n_heads + out_head] = lse_of(m, sum);
             }
             tcgen05_fence_before();
             if (split) everyone();

@@ -331,3 +331,26 @@ def test_rows_that_no_sequence_covers_are_left_alone(n_q):
     kv.attention(q, cu[:1], lens[:0], table[:0], n_q, out=out.fill_(7.0))         # no sequences at all
     assert (out == 7).all()
     kv.close()
+
+
+# ---- queries that are not finite -------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,n_q", [(100, 1), (100, 4), (20_011, 1), (20_011, 7), (300, 12), (300, 150), (20_011, 20), (20_011, 100)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_that_is_not_finite_gives_nan_and_no_other_row_does(kind, dim, n, n_q, bad):
+    # in one part and in several, in every kernel: not a zero that looks like a row that sees nothing
+    kv, table, k, v = filled(kind, n, 64, 1, dim)
+    q = torch.randn((n_q, 4, dim), device="cuda").to(torch.bfloat16)
+    q[n_q // 2, 2, dim // 3] = bad
+    cu, lens = torch.tensor([0, n_q], **I32), torch.tensor([n], **I32)
+    out, lse = kv.attention(q, cu, lens, table, n_q, want_lse=True)
+    assert kv.sync_status() == 0
+    hurt = torch.zeros((n_q, 4), dtype=torch.bool, device="cuda")
+    hurt[n_q // 2, 2] = True
+    assert out[hurt].isnan().all() and lse[hurt].isnan().all()
+    want = ref.attention(q.masked_fill(hurt[:, :, None], 0), k, v, n_q)
+    check_attention(out.masked_fill(hurt[:, :, None], 0)[:, [0, 1, 3]], lse[:, [0, 1, 3]], [w if isinstance(w, float) else w[:, [0, 1, 3]] for w in want], dim)
+    rest = [i for i in range(n_q) if i != n_q // 2]
+    check_attention(out[rest], lse[rest], [w if isinstance(w, float) else w[rest] for w in want], dim)
+    kv.close()
