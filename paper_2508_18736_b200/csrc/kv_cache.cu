@@ -91,7 +91,7 @@ template <int KIND> __device__ __forceinline__ int exponent_of(float a) {
     int e = static_cast<int>(u >> 23) - static_cast<int>(top >> 23) + ((u & 0x7FFFFFu) > (top & 0x7FFFFFu) ? 1 : 0);
     return max(e, -127);          // zero and subnormal rows end here too
 }
-// 2^-e for e in [-127, 120]
+// 2^-e for e in [-127, 122] (e4m3 goes to 120)
 __device__ __forceinline__ float inverse_scale(int e) { return __uint_as_float(static_cast<uint32_t>(127 - e) << 23); }
 
 template <int KIND> __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inv) {
@@ -232,21 +232,21 @@ kv_rows_kernel(KvView kv, Rows rows, const long long *__restrict__ slots, int he
 }
 
 template <int KIND, typename T, bool READ>
-static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
+static siso_status_t run_rows(const KvView &kv, const Rows &rows, const long long *slots, int sm_count, cudaStream_t s) {
     const int g = kv.head_dim <= 64 ? 4 : kv.head_dim <= 128 ? 8 : 16;
     const long long blocks = (rows.n + THREADS / g - 1) / (THREADS / g);
     if (blocks > 0x7FFFFFFFll) return SISO_ERR_UNSUPPORTED;
     // a prompt's lanes go through all heads of their token; the few tokens of a step are spread over more CTAs, a head each
-    const int heads_each = blocks >= 148 ? kv.n_kv_heads : 1;
+    const int heads_each = blocks >= sm_count ? kv.n_kv_heads : 1;
     const dim3 grid(static_cast<unsigned>(blocks), 2, static_cast<unsigned>((kv.n_kv_heads + heads_each - 1) / heads_each));
     if (g == 4) return launch_early(kv_rows_kernel<KIND, T, 4, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
     if (g == 8) return launch_early(kv_rows_kernel<KIND, T, 8, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
     return launch_early(kv_rows_kernel<KIND, T, 16, READ>, grid, THREADS, 0, s, kv, rows, slots, heads_each);
 }
 template <typename T, bool READ>
-static siso_status_t run_kind(int kind, const KvView &kv, const Rows &rows, const long long *slots, cudaStream_t s) {
-    return kind == SISO_E4M3 ? run_rows<SISO_E4M3, T, READ>(kv, rows, slots, s)
-         : kind == SISO_I8 ? run_rows<SISO_I8, T, READ>(kv, rows, slots, s) : run_rows<SISO_BF16, T, READ>(kv, rows, slots, s);
+static siso_status_t run_kind(int kind, const KvView &kv, const Rows &rows, const long long *slots, int sm_count, cudaStream_t s) {
+    return kind == SISO_E4M3 ? run_rows<SISO_E4M3, T, READ>(kv, rows, slots, sm_count, s)
+         : kind == SISO_I8 ? run_rows<SISO_I8, T, READ>(kv, rows, slots, sm_count, s) : run_rows<SISO_BF16, T, READ>(kv, rows, slots, sm_count, s);
 }
 
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -267,8 +267,8 @@ static siso_status_t rows_call(Kv *h, int layer, void *k, void *v, int dtype, lo
     const Rows rows{k, v, n, stride_token, stride_head};
     const KvView kv = kv_view(h, layer);
     const long long *sl = reinterpret_cast<const long long *>(slots);
-    return dtype == SISO_F32 ? run_kind<float, READ>(h->cfg.dtype, kv, rows, sl, s)
-                             : run_kind<__nv_bfloat16, READ>(h->cfg.dtype, kv, rows, sl, s);
+    return dtype == SISO_F32 ? run_kind<float, READ>(h->cfg.dtype, kv, rows, sl, h->sm_count, s)
+                             : run_kind<__nv_bfloat16, READ>(h->cfg.dtype, kv, rows, sl, h->sm_count, s);
 }
 
 // Tensor maps of the pages for attention: boxes of `box` tokens of one page and head, 128 bytes wide (64 where a row has no more),
