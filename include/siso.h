@@ -474,13 +474,14 @@ siso_status_t siso_measure_fp32_fma(siso_cache_t *c, double *h_tflops, void *str
  *                  complement) with one exponent byte per row in d_k_exp / d_v_exp [n_layers, n_pages, n_kv_heads, page_size]
  *                  (NULL for SISO_BF16): a row of head_dim values is kept as codes c, value c * 2^(byte - 127), the byte being
  *                  the smallest that lets the row's largest magnitude fit (448 for e4m3, 127 for i8).  Byte 255 marks a row
- *                  that held a NaN or an infinity; it reads back as NaN.  page_size, head_dim multiples of 8 (head_dim at
+ *                  that held a NaN or an infinity; it reads back as NaN.  (siso_kv_write stores no NaN codes, 0x7F and 0xFF of e4m3; pages that were
+ *                  filled in another way must hold none where they are read.)  page_size, head_dim multiples of 8 (head_dim at
  *                  most 256), base pointers 16-byte aligned, strides multiples of 8 elements (attention over 8-bit pages: of 16) and not 0
  *                  where there are several entries (strides of one entry count for nothing, here and below), else SISO_ERR_UNSUPPORTED.  The handle's scratch comes from the allocator on first use.  Synchronous.
  * siso_kv_write    Rows d_k, d_v [n_tokens, n_kv_heads, head_dim] (SISO_F32 or SISO_BF16, strides in elements, multiples of
  *                  16 bytes) into slots d_slots [n_tokens] = page * page_size + token; a slot outside the pool (-1) is skipped.
  *                  Slots of one call must differ.  Codes are rounded to nearest, ties to even.
- * siso_kv_read     The reverse: rows of the slots as SISO_F32 or SISO_BF16 (8-bit values are exact in both); slots outside
+ * siso_kv_read     The reverse: rows of the slots as SISO_F32 or SISO_BF16 (8-bit values are exact in both, in bf16 down to its smallest, 2^-133); slots outside
  *                  the pool read as zeros.
  * siso_kv_attention  New tokens, already written to the cache, attend over it.  Sequence b has the queries
  *                  d_cu_q[b] .. d_cu_q[b + 1] - 1 and d_kv_len[b] tokens in all, in the pages d_pages[b * pages_stride + i] (max_pages

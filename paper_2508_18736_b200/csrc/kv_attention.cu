@@ -21,9 +21,10 @@
 // into fp16's range by a power of two per row (exact but for elements below 2^-31 of the row's largest).  Codes of values are turned into
 // bf16, exactly, and the value's scale goes to its probability, relative to the largest one so far: probabilities and scales of
 // neighbouring tokens may lie many powers of two apart, for which fp16 has no room (a probability of 2^-40 would be zero).  bf16 costs
-// nothing over i8; over e4m3 (no conversion to it) 0 to 6 %: 64 sequences of 201 to 8190 tokens 107 us either way, head size 64 72 and 76 us.
+// nothing over i8; over e4m3 (no conversion to it) 0 to 6 %: 64 sequences of 201 to 8190 tokens 109 us either way, head size 64 73 and 77 us.
 // Measured, 8 kv heads x 128, 4 query heads each, caches in HBM: 64 sequences of 4096 tokens bf16 164 us, 6.5 TB/s (8192 tokens: 6.8 TB/s);
-// e4m3 107 us, 5.1 TB/s, where the dependent steps of a consumer warp on a unit are the limit; one sequence of 1025 tokens 9.4 us, latency.
+// 201 to 8190 tokens e4m3 110 us, 5.0 TB/s, where the dependent steps of a consumer warp on a unit are the limit; one sequence of 1025 tokens
+// 10.1 us, latency.  (At head size 128 the shapes of 16 and 32 rows spill 24 to 68 bytes a thread.)
 #include <cuda_fp16.h>
 
 #include "kv_attention.cuh"

@@ -16,9 +16,9 @@
 //                    widening sees to it for the others)
 //   warps 20-27      8-bit caches only: turn codes into bf16 tiles, exactly (the row's scale is a power of two)
 // TMEM: S_0, S_1 (128 columns each), O_0, O_1.
-// Measured, 32 query heads on 8 kv heads x 128, bf16: 2048 new tokens of 33333 870 to 900 us, 1.2 PFLOP/s (tensor pipe 69 %, exponentials
-// 71 % of the time; the clock is at 1.5 GHz for power, and 1013 us in a run of seconds); six prompts of 129 to 903 tokens 110 us.  e4m3 in a
-// window of 4096, two chunks of 1000 tokens: 167 us, where widening the codes beside the softmax makes issue the limit.
+// Measured, 32 query heads on 8 kv heads x 128, bf16: 2048 new tokens of 33333 1000 to 1050 us in a run of seconds, 1.05 PFLOP/s; 880 us in one of
+// milliseconds (tensor pipe 67 %, exponentials 70 % of the time, the clock at 1.5 GHz for power); six prompts of 129 to 903 tokens 112 us.  e4m3 in a
+// window of 4096, two chunks of 1000 tokens: 166 us, where widening the codes beside the softmax makes issue the limit.
 #include "kv_attention.cuh"
 
 namespace siso {

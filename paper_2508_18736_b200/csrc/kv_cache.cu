@@ -11,7 +11,7 @@
 //
 // Both kernels move bytes: they are bound by HBM for prompts and by latency for a step's few tokens.  G lanes own the rows of one
 // token with 16 values each, so the maximum takes log2 G shuffles; they look the slot up once and go through heads, U rows in
-// flight.  16385 tokens x 8 x 128 bf16 into an 8-bit cache and back: 39.6 us together, 5 TB/s, issue at 60 % (one step's 48 tokens: 3.6 us).
+// flight.  16385 tokens x 8 x 128 bf16 into an 8-bit cache and back: 39.6 us together, 5 TB/s, issue at 60 % (one step's 48 tokens: 4 us).
 // (With 8 values a lane what a row costs beside its values made issue the limit: 23 us and 19 us for 16385 tokens x 8 x 128.)
 #include <cuda_fp8.h>
 

@@ -15,8 +15,8 @@
 // up to 8 CTAs shares a sequence: each warp sums the weights of one contiguous chunk, the chunk sums go to every CTA of the
 // cluster through distributed shared memory, and the CTA that owns the chunk with the crossing looks at it again (it comes
 // from L2) with a few consecutive entries per thread.  One launch, no scratch memory.
-// Measured with rows in HBM: 64 x 128256 fp32 (66 MB) 13.4 us, 4.9 TB/s; 192 x 50257 bf16 (39 MB, rows not aligned) 13.6 us, 2.8 TB/s; one
-// sequence of 32000 fp32 3.8 us, most of it the launch and three round trips to memory (which drafts stand, the row, the crossing).
+// Measured with rows in HBM: 64 x 128256 fp32 (66 MB) 14.4 us, 4.6 TB/s; 192 x 50257 bf16 (39 MB, rows not aligned) 16.5 us, 2.3 TB/s; one
+// sequence of 32000 fp32 4.4 us, most of it the launch and three round trips to memory (which drafts stand, the row, the crossing).
 #include "common.cuh"
 
 namespace siso {
@@ -253,7 +253,7 @@ template <typename T, int W, int THREADS, int SPLIT> static siso_status_t launch
 template <typename T, int W> static siso_status_t run(const Args &g, int64_t n_seqs, cudaStream_t s) {
     // A sequence is shared by as many CTAs as give each of the 148 SMs a few, small enough that all of them run at once (64 x 128256
     // fp32: 256 threads 13.4 us, 512 threads 17.3 us; 192 x 50257 bf16: four CTAs 13.6 us, two 15.1 us; 512 x 32000 fp32: two 32.8 us,
-    // one 34.8 us).  Few sequences with long rows get larger CTAs, fewer rounds of loads (4 x 128256 fp32: 512 threads 6.5 us, 256
+    // one 34.8 us; each with part of the rows in L2).  Few sequences with long rows get larger CTAs, fewer rounds of loads (4 x 128256 fp32: 512 threads 6.5 us, 256
     // threads 7.7 us; 1 x 32000: 4.2 us and 3.8 us)
     if (n_seqs <= 16 && g.vocab >= 65536) return launch<T, W, 512, 8>(g, n_seqs, s);
     if (n_seqs <= 64) return launch<T, W, 256, 8>(g, n_seqs, s);
