@@ -552,6 +552,75 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
                                  const int32_t *d_tokens, const int32_t *d_n_drafts, const float *d_u_accept, const float *d_u_sample,
                                  int32_t *d_out, int32_t *d_accepted, void *stream);
 
+/* ---- several near hits at once, and a cache that stays small ------------------------------------------------------------
+ * A lookup with k > 1 may find several entries just below the threshold.  Their stored answers, shared beginnings once, are a TREE of
+ * drafts: one pass of the model takes all of them, the verification walks down the tree, and the path that stands is moved to its
+ * place in the cache.  And a cache of long prompts is kept small by evicting tokens that attention gives little weight.
+ *
+ * The new tokens of sequence b are its nodes d_cu_q[b] .. d_cu_q[b + 1] - 1, numbered from 0; d_parents[node] is the number of an earlier node of
+ * the same sequence, anything else means none.  They lie in the cache's last places of the sequence, in order.
+ *
+ * siso_tree_mask   (no handle; current device)  d_mask [n_tokens, words]: bit j of a row (bit j % 32 of word j / 32) says that node j is the row's
+ *                  node or one of those above it; nodes beyond 32 * words have no bit.  d_depth [n_tokens] (may be NULL): how many nodes are above.
+ *                  Rows that no sequence covers are not written.
+ * siso_kv_tree_attention  siso_kv_attention in which new token i of a sequence sees the tokens before the new ones and, of the new ones,
+ *                  those of its row of d_mask [n_tokens, words], rows mask_stride words apart (any bits: ancestors of a tree as siso_tree_mask
+ *                  gives them, or whatever else; columns beyond `words` count as not set).  A window limits what is seen of the tokens before the new
+ *                  ones: a row that sees d new tokens stands at p = before + max(d - 1, 0), before = kv_len - (number of new tokens), and sees j > p -
+ *                  window; of the new ones the mask alone decides.  args->flags must be SISO_ATTN_CAUSAL.  What may stand in the cache's places and
+ *                  the rounding are siso_kv_attention's.
+ * siso_verify_tree (no handle; current device)  Verification of a tree.  Node 0 of a sequence is the last token that stands already, the others are
+ *                  drafts.  d_target [n_tokens, vocab]: row i the target's probabilities of the token after node i.  d_draft [n_tokens, vocab]: row i
+ *                  those that node i's children were drawn from, each by itself; NULL if the drafts were certain (stored answers).  From node 0 on, with r = p
+ *                  (the node's row of d_target), s = 1 and n = 0, the node's children are tried in order: child c with token x stands if
+ *                  u_accept[c] (s q(x)) < r(x) (q(x) = 1 without d_draft), and the walk goes on from it (n + 1).  Otherwise r becomes max(r - s q, 0)
+ *                  (r(x) = 0 without d_draft) and s the sum of floor(min(r, 1) 2^38), rounded to fp32, times 2^-38.  A token outside the vocabulary never stands.
+ *                  Where no child stands, or n = max_path, the next token is drawn from r (from p where r is empty) as siso_verify_drafts
+ *                  draws it; products and differences are rounded to fp32 one by one, so a tree that is a chain gives what siso_verify_drafts gives.
+ *                  d_accepted [n_seqs] = n, d_out [n_seqs, max_path + 1]: the n tokens that stand, the one drawn, -1 in the rest (all of it for a sequence
+ *                  without nodes); d_path [n_seqs, max_path] (may be NULL): their nodes, then -1.  vocab at most 2^18.
+ * siso_kv_keep_path  Moves the rows (all layers) of nodes d_path[b, t], t < d_accepted[b], to places before + 1 + t: the accepted path follows node 0.  A path
+ *                  ascends; an entry that does not, or is no node of the sequence, ends it (SISO_ERR_INVALID_ARG in the status word).  d_new_len [n_seqs] =
+ *                  before + 1 + t at its end (kv_len for a sequence without new tokens); it must not be d_kv_len itself.
+ * siso_kv_add_weights  Each query i of a sequence (as in siso_kv_attention; d_lse [n_tokens, n_heads] as that returns it) gives the tokens that it sees
+ *                  the weights exp(scale q.k_j - lse).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
+ *                  layer of the call, w_j = decay w_j + sum of the weights over the queries and query heads that read the kv head; tokens that are new
+ *                  in this call (the last ones, as many as the sequence has queries) start from 0, and with decay 0 all do, whatever stood there.  Sequences without
+ *                  queries are left alone.  A query whose lse is -infinity gives nothing.  Sums are fp32, in an order that does not change from call to call.
+ * siso_kv_evict    For each layer, sequence and kv head by itself: of kv_len tokens the last `recent` stay and, of the others, the budget - recent with the largest
+ *                  weights (ties: the earlier one; NaN counts as less than all else).  Their rows, exponents and weights are moved, in order, to places 0, 1, .. of the
+ *                  pages d_out_pages [n_seqs, out_max_pages] (d_pages itself: in place).  d_new_len [n_seqs] = min(kv_len, budget), the same for
+ *                  all layers and heads, must not be d_kv_len itself; d_kept [n_layers, n_seqs, n_kv_heads, budget] (NULL is refused): which places stayed, then -1.
+ *                  An entry of d_out_pages is the entry of d_pages at the same index, or a page that the call does not otherwise use; pages of different sequences
+ *                  differ.  A page index outside the pool: SISO_ERR_INVALID_ARG in the status word, its tokens count as NaN and are not moved.
+ *                  1 <= budget, 0 <= recent <= budget. */
+siso_status_t siso_tree_mask(const int32_t *d_parents, const int32_t *d_cu_q, int64_t n_tokens, int32_t n_seqs, int32_t words, uint32_t *d_mask,
+                             int32_t *d_depth, void *stream);
+siso_status_t siso_kv_tree_attention(siso_kv_t *kv, const siso_attention_t *args, const uint32_t *d_mask, int32_t words, int64_t mask_stride,
+                                     void *stream);
+siso_status_t siso_verify_tree(const void *d_target, const void *d_draft, int32_t dtype, int64_t n_tokens, int32_t n_seqs, int32_t vocab,
+                               const int32_t *d_tokens, const int32_t *d_parents, const int32_t *d_cu_q, int32_t max_path,
+                               const float *d_u_accept, const float *d_u_sample, int32_t *d_out, int32_t *d_accepted, int32_t *d_path, void *stream);
+siso_status_t siso_kv_keep_path(siso_kv_t *kv, const int32_t *d_path, const int32_t *d_accepted, int32_t max_path, const int32_t *d_cu_q,
+                                const int32_t *d_kv_len, const int32_t *d_pages, int64_t pages_stride, int32_t max_pages, int32_t n_seqs,
+                                int32_t *d_new_len, void *stream);
+
+typedef struct {
+    const void *d_q;
+    const float *d_lse;
+    float *d_weights;
+    const int32_t *d_cu_q, *d_kv_len, *d_pages;
+    int64_t q_stride_token, q_stride_head, pages_stride, n_tokens;
+    int32_t n_seqs, max_q, max_pages, n_heads, layer;
+    uint32_t flags;
+    float scale, decay;
+} siso_weights_t;
+
+siso_status_t siso_kv_add_weights(siso_kv_t *kv, const siso_weights_t *args, void *stream);
+siso_status_t siso_kv_evict(siso_kv_t *kv, float *d_weights, const int32_t *d_kv_len, const int32_t *d_pages, int64_t pages_stride, int32_t max_pages,
+                            const int32_t *d_out_pages, int64_t out_pages_stride, int32_t out_max_pages, int32_t n_seqs, int32_t budget,
+                            int32_t recent, int32_t *d_new_len, int32_t *d_kept, void *stream);
+
 /* Number of kernels this handle has launched so far (host-side count). */
 int64_t siso_launch_count(const siso_cache_t *c);
 const char *siso_status_string(siso_status_t s);

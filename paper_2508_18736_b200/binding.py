@@ -29,7 +29,8 @@ EXPORTS = ["siso_cache_create", "siso_cache_destroy", "siso_set_option", "siso_i
            "siso_merge_apply_shard", "siso_tier_build", "siso_tier_work_bytes", "siso_tier_lookup", "siso_free_slots",
            "siso_shard_plan", "siso_route_planned", "siso_select_evict_planned", "siso_norm_deviation", "siso_kv_create",
            "siso_kv_destroy", "siso_kv_write", "siso_kv_read", "siso_kv_attention", "siso_kv_sync_status", "siso_verify_drafts",
-           "siso_kv_selftest_wait_timeout"]
+           "siso_kv_selftest_wait_timeout", "siso_tree_mask", "siso_kv_tree_attention", "siso_verify_tree", "siso_kv_keep_path",
+           "siso_kv_add_weights", "siso_kv_evict"]
 
 
 class SisoError(RuntimeError):
@@ -126,6 +127,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.siso_kv_sync_status.argtypes = [vp, vp]
     L.siso_kv_selftest_wait_timeout.argtypes = [vp, vp]
     L.siso_verify_drafts.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.siso_tree_mask.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp]
+    L.siso_kv_tree_attention.argtypes = [vp, vp, vp, i32, i64, vp]
+    L.siso_verify_tree.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    L.siso_kv_keep_path.argtypes = [vp, vp, vp, i32, vp, vp, vp, i64, i32, i32, vp, vp]
+    L.siso_kv_add_weights.argtypes = [vp, vp, vp]
+    L.siso_kv_evict.argtypes = [vp, vp, vp, vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, vp]
     L.siso_launch_count.argtypes = [vp]
     L.siso_launch_count.restype = i64
     L.siso_status_string.argtypes = [i32]

@@ -69,7 +69,9 @@ inline KvView kv_view(const Kv *h, int layer) {
     return w;
 }
 
-siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t s);
+// mask: which new tokens each new token sees, rows of `words` words (NULL: by causality)
+siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, const uint32_t *mask, int words, int64_t mask_stride, cudaStream_t s);
+siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, cudaStream_t s);
 namespace kva { siso_status_t launch_wait_timeout(Kv *h, cudaStream_t s); }
 
 #ifdef __CUDACC__

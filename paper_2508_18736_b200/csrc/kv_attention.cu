@@ -119,7 +119,7 @@ template <int STAGES> struct Ring {
     int gave_up;
 };
 
-template <int KIND, int D, int WM, int NT>
+template <int KIND, int D, int WM, int NT, bool TREE>
 __global__ void __launch_bounds__(Shape<KIND, D, WM, NT>::THREADS, 1)
 attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using S = Shape<KIND, D, WM, NT>;
@@ -232,6 +232,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     uint32_t q[NT][D / 16][2];
     float o[NT][DT][4], m[NT][2], l[NT][2], row_scale[NT][2];
     int pos[NT][2], e_top = 0;
+    const uint32_t *mask[NT][2];         // TREE: the rows' bits
 
     // the queries of an item: 8 values of each of D / 32 pieces per lane.  bf16 cache: a lane's 16 bytes of a key hold 8 values;
     // 8-bit: 16 values, two pieces of 8
@@ -278,6 +279,10 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = cur.rt * MR + (wm * NT + t) * 8 + 2 * c + h;
+                if constexpr (TREE) {
+                    mask[t][h] = g.mask + static_cast<long long>(cur.q0 + (row < cur.n_q * g.group ? static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))) : 0)) * g.mask_stride;
+                    pos[t][h] = g.a.window > 0 && row < cur.n_q * g.group ? position(cur.len, cur.n_q, mask_depth(g, mask[t][h], cur.n_q)) : cur.len - 1;
+                } else
                 pos[t][h] = row < cur.n_q * g.group ? position(cur.len, cur.n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(row)))) : cur.s.last_pos;
                 m[t][h] = -INFINITY;
                 l[t][h] = 0.f;
@@ -298,8 +303,8 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         const uint8_t *mt = meta + stage * S::META;
         const int j0 = (cur.s.tile0 + cur.tile) * TK;
         const uint32_t blocks = ring.blocks[stage];
-        const bool cut = j0 + TK > cur.s.hi || blocks != ALL || (causal && j0 + TK - 1 > cur.s.first_pos) ||
-                         (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
+        const bool cut = j0 + TK > cur.s.hi || blocks != ALL || (causal && j0 + TK - 1 > cur.s.first_pos) || (TREE && j0 + TK > cur.len - cur.n_q) ||
+                         (g.a.window > 0 && j0 <= (TREE ? cur.len - 1 : cur.s.last_pos) - g.a.window);
         const int lo = cut ? cur.lo(g) : 0;
         if (cut && (j0 + TK > cur.s.hi || j0 < lo)) {    // values beyond the end or before every window may be anything: zeros, or 0 times NaN would reach the sums
             for (int x = wm * 32 + lane; x < NK * CH; x += 32 * WM) {
@@ -375,8 +380,14 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int h = 0; h < 2; ++h)
+                            for (int h = 0; h < 2; ++h) {
+                                if constexpr (TREE) {
+                                    const int node = j - (cur.len - cur.n_q);
+                                    const bool seen = node < 0 ? g.a.window == 0 || j > pos[t][h] - g.a.window : ((mask_word(g, mask[t][h], node >> 5) >> (node & 31)) & 1u) != 0u;
+                                    if (!in || !seen) s[i][t][2 * e + h] = -INFINITY;
+                                } else
                                 if (!in || (causal && j > pos[t][h]) || (g.a.window > 0 && j <= pos[t][h] - g.a.window)) s[i][t][2 * e + h] = -INFINITY;
+                            }
                     }
             }
             float shift[NT][2], corr[NT][2];
@@ -693,16 +704,19 @@ siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s) {
     return SISO_OK;
 }
 
-template <int KIND, int D, int WM, int NT> static siso_status_t run_few(Kv *h, Args &g, cudaStream_t s) {
+template <int KIND, int D, int WM, int NT, bool TREE> static siso_status_t run_few_as(Kv *h, Args &g, cudaStream_t s) {
     using S = Shape<KIND, D, WM, NT>;
-    constexpr uint32_t bit = 1u << (NT == 1 ? 0 : WM);        // a handle has one type and head_dim
+    constexpr uint32_t bit = 1u << ((NT == 1 ? 0 : WM) + (TREE ? 4 : 0));        // a handle has one type and head_dim
     if (!(h->attr_set & bit)) {
-        SISO_CUDA(cudaFuncSetAttribute(attention_few_rows_kernel<KIND, D, WM, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        SISO_CUDA(cudaFuncSetAttribute(attention_few_rows_kernel<KIND, D, WM, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    attention_few_rows_kernel<KIND, D, WM, NT><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
+    attention_few_rows_kernel<KIND, D, WM, NT, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
     SISO_CUDA(cudaGetLastError());
     return launch_join(g, S::MR, D, s);
+}
+template <int KIND, int D, int WM, int NT> static siso_status_t run_few(Kv *h, Args &g, cudaStream_t s) {
+    return g.mask ? run_few_as<KIND, D, WM, NT, true>(h, g, s) : run_few_as<KIND, D, WM, NT, false>(h, g, s);
 }
 template <int KIND, int D> static siso_status_t run_few_rows(Kv *h, Args &g, int mr, cudaStream_t s) {
     return mr == 8 ? run_few<KIND, D, 1, 1>(h, g, s) : mr == 16 ? run_few<KIND, D, 1, 2>(h, g, s) : run_few<KIND, D, 2, 2>(h, g, s);
@@ -713,11 +727,15 @@ template <int KIND> static siso_status_t run_few_dim(Kv *h, Args &g, int dim, in
 
 }  // namespace kva
 
-siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, cudaStream_t s) {
+siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, const uint32_t *mask, int words, int64_t mask_stride, cudaStream_t s) {
     using namespace kva;
     Args g;
+    g.mask = mask;
+    g.mask_words = words;
+    g.mask_stride = mask_stride;
     g.kv = kv_view(h, a->layer);
     g.a = *a;
+    if (mask) g.a.flags &= ~SISO_ATTN_CAUSAL;
     g.group = a->n_heads / h->cfg.n_kv_heads;
     g.by_page.set(static_cast<uint32_t>(h->cfg.page_size));
     g.by_group.set(static_cast<uint32_t>(g.group));

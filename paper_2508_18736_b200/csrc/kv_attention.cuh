@@ -47,6 +47,10 @@ struct Args {
     float *part_o, *part_ml;           // [2 grid][MR][D], [2 grid][MR][2]
     Record *records;                   // [grid]
     int *status;
+    // a tree: which new tokens each new token sees (a.flags without SISO_ATTN_CAUSAL), NULL otherwise
+    const uint32_t *mask;
+    long long mask_stride;
+    int mask_words;
 };
 
 #ifdef __CUDACC__
@@ -74,10 +78,24 @@ template <int MR, int TK> __device__ __forceinline__ Span span_of(const Args &g,
     s.first_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))));
     s.last_pos = position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(min(rows, (rt + 1) * MR) - 1))));
     s.hi = (g.a.flags & SISO_ATTN_CAUSAL) ? max(0, min(len, s.last_pos + 1)) : len;
+    if (g.mask) s.first_pos = position(len, n_q, 0);        // any node of a tree may stand right behind the tokens before it
     const int lo = first_seen(g, s.first_pos);
     s.tile0 = lo / TK;
     s.tiles = max(1, (s.hi + TK - 1) / TK - s.tile0);       // a row tile that sees nothing is one unit that writes zeros
     return s;
+}
+// A tree's row of bits: word w, and how many of the n_q new tokens stand above the row's (bits set, less its own)
+__device__ __forceinline__ uint32_t mask_word(const Args &g, const uint32_t *row, int w) { return w < g.mask_words ? row[w] : 0u; }
+__device__ __forceinline__ int mask_depth(const Args &g, const uint32_t *row, int n_q) {
+    int n = 0;
+    for (int w = 0; w < g.mask_words && 32 * w < n_q; ++w) n += __popc(n_q - 32 * w < 32 ? row[w] & ((1u << (n_q & 31)) - 1u) : row[w]);
+    return max(n - 1, 0);
+}
+// bits [at, at + 32) of a row, ones before it begins: tokens before the new ones are seen
+__device__ __forceinline__ uint32_t mask_bits(const Args &g, const uint32_t *row, int at) {
+    if (at <= -32) return 0xFFFFFFFFu;
+    if (at < 0) return (mask_word(g, row, 0) << -at) | ((1u << -at) - 1u);
+    return __funnelshift_r(mask_word(g, row, at >> 5), mask_word(g, row, (at >> 5) + 1), at & 31);
 }
 // Whether the TMA box of token j of a row tile's keys holds tokens that some row may see, and j is not beyond the last.  What lies wholly before
 // the window is not looked up: its pages may have been given back
@@ -126,7 +144,7 @@ template <int MR, int TK, int EXTRA, int W> struct Cursor {
     // key tiles of this item that belong to the run
     __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, (left + W - 1) / W); }
     // the first key that a row of this item sees (worked out again where it is needed: kept, it costs registers)
-    __device__ __forceinline__ int lo(const Args &g) const { return g.a.window > 0 && tile == 0 ? first_seen(g, position(len, n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))))) : 0; }
+    __device__ __forceinline__ int lo(const Args &g) const { return g.a.window > 0 && tile == 0 ? first_seen(g, position(len, n_q, g.mask ? 0 : static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))))) : 0; }
     // n <= tiles_here() tiles further; false: the run is over
     __device__ __forceinline__ bool step(const Args &g, int n = 1) {
         tile += n;

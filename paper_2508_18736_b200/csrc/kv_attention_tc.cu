@@ -158,7 +158,7 @@ __device__ __forceinline__ void turn4(uint4 (&w)[4], int lane) {
     swap_piece(w[1], w[3], 2, lane & 2);
 }
 
-template <int KIND, int D>
+template <int KIND, int D, bool TREE>
 __global__ void __launch_bounds__(Shape<KIND, D>::THREADS, 1)
 attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using S = Shape<KIND, D>;
@@ -559,7 +559,13 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             out_token = real ? cur.q0 + i : -1;
             out_head = head;
             out_place = cur.tile == 0 && n == cur.s.tiles ? -1 : static_cast<int>(part_place(blockIdx.x, cur.tile > 0)) * TC_ROWS + in_tile;
-            const int pos = real ? position(cur.len, cur.n_q, i) : cur.s.last_pos;
+            int pos = real ? position(cur.len, cur.n_q, i) : cur.s.last_pos;
+            const int before = cur.len - cur.n_q;                         // TREE: tokens before the new ones
+            const uint32_t *mask = nullptr;
+            if constexpr (TREE) {
+                mask = g.mask + static_cast<long long>(cur.q0 + (real ? i : 0)) * g.mask_stride;
+                if (real && g.a.window > 0) pos = position(cur.len, cur.n_q, mask_depth(g, mask, cur.n_q));
+            }
             m = -INFINITY;
             l = 0.f;
             const int k0 = split ? t : 0, k_step = split ? 2 : 1;
@@ -571,11 +577,22 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 tmem_ld_32x32(s_at, ra);
                 tmem_ld_32x32(s_at + 32, rb);
                 const uint32_t blocks = bars.blocks[(unit + k) & 7];
-                const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) ||
-                                 (g.a.window > 0 && j0 <= cur.s.last_pos - g.a.window);
+                const bool cut = j0 + TK > cur.s.hi || blocks != 0xFFFFu || (causal && j0 + TK - 1 > cur.s.first_pos) || (TREE && j0 + TK > before) ||
+                                 (g.a.window > 0 && j0 <= (TREE ? cur.len - 1 : cur.s.last_pos) - g.a.window);
                 tmem_ld_fence(ra);
                 tmem_ld_fence(rb);
-                if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
+                if constexpr (TREE) {
+                    if (cut) {   // as below, with the row's bits for the new tokens
+                        const int at = j0 + half * 64 - before, last = cur.s.hi - 1 - j0 - half * 64;
+                        const int first = g.a.window > 0 ? min(max(pos - g.a.window + 1, 0), max(before, 0)) - j0 - half * 64 : 0;
+                        const uint32_t see_a = mask_bits(g, mask, at), see_b = mask_bits(g, mask, at + 32), my_blocks = blocks >> (half * 8);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) {
+                            if (x > last || x < first || !((my_blocks >> (x / 8)) & 1u) || !((see_a >> x) & 1u)) ra[x] = 0xFF800000u;
+                            if (32 + x > last || 32 + x < first || !((my_blocks >> (4 + x / 8)) & 1u) || !((see_b >> x) & 1u)) rb[x] = 0xFF800000u;
+                        }
+                    }
+                } else if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
                     const int last = (causal ? min(pos, cur.s.hi - 1) : cur.s.hi - 1) - j0 - half * 64;
                     const int first = g.a.window > 0 ? max(pos - g.a.window + 1, 0) - j0 - half * 64 : 0;
                     const uint32_t my_blocks = blocks >> (half * 8);
@@ -673,16 +690,19 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     }
 }
 
-template <int KIND, int D> static siso_status_t run(Kv *h, Args &g, cudaStream_t s) {
+template <int KIND, int D, bool TREE> static siso_status_t run_as(Kv *h, Args &g, cudaStream_t s) {
     using S = Shape<KIND, D>;
-    constexpr uint32_t bit = 1u << 8;
+    constexpr uint32_t bit = 1u << (TREE ? 9 : 8);
     if (!(h->attr_set & bit)) {
-        SISO_CUDA(cudaFuncSetAttribute(attention_many_rows_kernel<KIND, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        SISO_CUDA(cudaFuncSetAttribute(attention_many_rows_kernel<KIND, D, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    attention_many_rows_kernel<KIND, D><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
+    attention_many_rows_kernel<KIND, D, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
     SISO_CUDA(cudaGetLastError());
     return launch_join(g, TC_ROWS, D, s);
+}
+template <int KIND, int D> static siso_status_t run(Kv *h, Args &g, cudaStream_t s) {
+    return g.mask ? run_as<KIND, D, true>(h, g, s) : run_as<KIND, D, false>(h, g, s);
 }
 
 }  // namespace tc

@@ -392,7 +392,7 @@ siso_status_t siso_kv_read(siso_kv_t *h, int32_t layer, void *d_k, void *d_v, in
     return kvc::rows_call<true>(h, layer, d_k, d_v, dtype, n_tokens, stride_token, stride_head, d_slots, static_cast<cudaStream_t>(stream));
 }
 
-siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *args, void *stream) {
+static siso_status_t attention_call(siso_kv_t *h, const siso_attention_t *args, const uint32_t *mask, int32_t words, int64_t mask_stride, void *stream) {
     const siso_attention_t *a = args;
     if (!h || !a || a->n_tokens < 0 || a->n_seqs < 0 || a->layer < 0 || a->layer >= h->cfg.n_layers) return SISO_ERR_INVALID_ARG;
     if (a->n_heads < 1 || a->n_heads % h->cfg.n_kv_heads != 0 || a->window < 0 || a->max_q < 0 || a->max_pages < 0) return SISO_ERR_INVALID_ARG;
@@ -413,7 +413,33 @@ siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *args, void
     if (a->n_tokens >= ((1ll << 31) - 256) / a->n_heads || static_cast<int64_t>(a->max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     const OnDevice on(h->cfg.device);
     SISO_CUDA(on.error());
-    return launch_kv_attention(h, a, static_cast<cudaStream_t>(stream));
+    return launch_kv_attention(h, a, mask, words, mask_stride, static_cast<cudaStream_t>(stream));
+}
+
+siso_status_t siso_kv_attention(siso_kv_t *h, const siso_attention_t *args, void *stream) { return attention_call(h, args, nullptr, 0, 0, stream); }
+
+siso_status_t siso_kv_tree_attention(siso_kv_t *h, const siso_attention_t *args, const uint32_t *d_mask, int32_t words, int64_t mask_stride,
+                                     void *stream) {
+    if (!args || args->flags != SISO_ATTN_CAUSAL || words < 1 || mask_stride < 0 || (args->n_tokens > 0 && args->n_seqs > 0 && !d_mask)) return SISO_ERR_INVALID_ARG;
+    return attention_call(h, args, d_mask, words, mask_stride, stream);
+}
+
+siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void *stream) {
+    if (!h || !args) return SISO_ERR_INVALID_ARG;
+    siso_weights_t a = *args;
+    if (a.n_tokens < 0 || a.n_seqs < 0 || a.layer < 0 || a.layer >= h->cfg.n_layers) return SISO_ERR_INVALID_ARG;
+    if (a.n_heads < 1 || a.n_heads % h->cfg.n_kv_heads != 0 || a.max_q < 0 || a.max_pages < 0) return SISO_ERR_INVALID_ARG;
+    if ((a.flags & ~SISO_ATTN_CAUSAL) != 0u || !(a.scale == a.scale) || !(a.decay >= 0.f) || a.decay > 3.4e38f) return SISO_ERR_INVALID_ARG;
+    if (a.n_tokens == 0 || a.n_seqs == 0) return SISO_OK;
+    if (!a.d_q || !a.d_lse || !a.d_weights || !a.d_cu_q || !a.d_kv_len || (a.max_pages > 0 && !a.d_pages) || a.pages_stride < 0) return SISO_ERR_INVALID_ARG;
+    if (a.n_tokens == 1) a.q_stride_token = 0;                    // (one entry: no stride)
+    if (a.n_heads == 1) a.q_stride_head = 0;
+    if (a.q_stride_token < 0 || a.q_stride_head < 0) return SISO_ERR_INVALID_ARG;
+    if (a.q_stride_token % 8 != 0 || a.q_stride_head % 8 != 0 || !kvc::aligned16(a.d_q) || !kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
+    if (a.n_tokens >= ((1ll << 31) - 256) / a.n_heads || static_cast<int64_t>(a.max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
+    const OnDevice on(h->cfg.device);
+    SISO_CUDA(on.error());
+    return launch_kv_weights(h, &a, static_cast<cudaStream_t>(stream));
 }
 
 siso_status_t siso_kv_selftest_wait_timeout(siso_kv_t *h, void *stream) {

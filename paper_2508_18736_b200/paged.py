@@ -39,6 +39,7 @@ class _KvConfig(ctypes.Structure):
 
 # siso_attention_t: 6 pointers, 6 int64, 6 int32, uint32, float.  Packed by hand: a call costs the host a few microseconds in all
 _ATTENTION = struct.Struct("@6P6q6iIf")
+_WEIGHTS = struct.Struct("@6P4q5iIff")          # siso_weights_t: 6 pointers, 4 int64, 5 int32, uint32, 2 floats
 
 
 class PagedKV:
@@ -190,6 +191,22 @@ class PagedKV:
         if stream is not None:
             with _on(stream, self._index):
                 return self.attention(q, cu_q, kv_len, pages, max_q, layer, scale, causal, window, want_lse, out=out)
+        return self._attend(None, q, cu_q, kv_len, pages, max_q, layer, scale, causal, window, want_lse, out)
+
+    def tree_attention(self, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, mask: torch.Tensor, max_q: int,
+                       layer: int = 0, scale: Optional[float] = None, window: int = 0, want_lse: bool = False, stream=None,
+                       out: Optional[torch.Tensor] = None):
+        """attention() of new tokens that are nodes of trees: each sees the tokens before the new ones and, of the new ones, those of its row of
+        mask int32 [n, words] (bit j % 32 of word j // 32: node j of its sequence; tree_mask() gives the ancestors).  A window counts from
+        a node's place below the tokens before the new ones, and limits only those; of the new ones the mask alone decides."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.tree_attention(q, cu_q, kv_len, pages, mask, max_q, layer, scale, window, want_lse, out=out)
+        if mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != q.shape[0] or mask.shape[1] < 1 or mask.get_device() != self._index:
+            raise ValueError(f"mask must be an int32 [n, words] tensor on {self._dev}")
+        return self._attend(mask if mask.stride(1) == 1 else mask.contiguous(), q, cu_q, kv_len, pages, max_q, layer, scale, True, window, want_lse, out)
+
+    def _attend(self, mask, q, cu_q, kv_len, pages, max_q, layer, scale, causal, window, want_lse, out):
         index, i32 = self._index, torch.int32
         shape = q.shape
         if q.dtype is not torch.bfloat16 or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
@@ -221,10 +238,117 @@ class PagedKV:
         _ATTENTION.pack_into(self._args, 0, q.data_ptr(), out.data_ptr(), lse.data_ptr() if want_lse else 0, cu_q.data_ptr(), kv_len.data_ptr(),
                              pages.data_ptr(), sq[0], sq[1], so[0], so[1], pages.stride(0), n, seqs, max_q, table[1], heads, layer, window,
                              ATTN_CAUSAL if causal else 0, self._default_scale if scale is None else scale)
-        st = self._lib.siso_kv_attention(self._h, self._args, _raw_stream(index))
-        if st:
-            self._check(st, "siso_kv_attention")
+        if mask is None:
+            st = self._lib.siso_kv_attention(self._h, self._args, _raw_stream(index))
+            if st:
+                self._check(st, "siso_kv_attention")
+        else:
+            st = self._lib.siso_kv_tree_attention(self._h, self._args, mask.data_ptr(), mask.shape[1], mask.stride(0), _raw_stream(index))
+            if st:
+                self._check(st, "siso_kv_tree_attention")
         return (out, lse) if want_lse else out
+
+    def _sequences(self, kv_len, pages, cu_q=None):
+        """(kv_len, pages, cu_q) as the library takes them: contiguous, rows of pages at any stride."""
+        i32, index = torch.int32, self._index
+        if kv_len.dtype is not i32 or pages.dtype is not i32 or kv_len.get_device() != index or pages.get_device() != index or \
+                (cu_q is not None and (cu_q.dtype is not i32 or cu_q.get_device() != index)):
+            raise ValueError(f"cu_q, kv_len and pages must be int32 tensors on {self._dev}")
+        if kv_len.dim() != 1 or pages.dim() != 2 or pages.shape[0] != kv_len.numel() or \
+                (cu_q is not None and (cu_q.dim() != 1 or cu_q.numel() != kv_len.numel() + 1)):
+            raise ValueError("cu_q must be [seqs + 1], kv_len [seqs], pages [seqs, max pages]")
+        if pages.stride(1) != 1:
+            pages = pages.contiguous()
+        if not kv_len.is_contiguous():
+            kv_len = kv_len.contiguous()
+        if cu_q is not None and not cu_q.is_contiguous():
+            cu_q = cu_q.contiguous()
+        return kv_len, pages, cu_q
+
+    def _weights(self, weights):
+        if weights.dtype is not torch.float32 or weights.get_device() != self._index or not weights.is_contiguous() or \
+                weights.shape != (self.n_layers, self.n_pages, self.n_kv_heads, self.page_size):
+            raise ValueError(f"weights must be a contiguous float32 [{self.n_layers}, {self.n_pages}, {self.n_kv_heads}, {self.page_size}] tensor "
+                             f"on {self._dev}")
+
+    def new_weights(self) -> torch.Tensor:
+        """A number for each cached row, zero: what add_weights() adds to and evict() goes by."""
+        return torch.zeros((self.n_layers, self.n_pages, self.n_kv_heads, self.page_size), dtype=torch.float32, device=self._dev)
+
+    def keep_path(self, path: torch.Tensor, accepted: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, stream=None
+                  ) -> torch.Tensor:
+        """Moves the rows (all layers) of the nodes path [seqs, longest], the first accepted [seqs] of each, behind node 0 of their sequence.
+        cu_q, kv_len, pages as tree_attention() had them.  Returns the tokens that the sequences have now, int32 [seqs]."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.keep_path(path, accepted, cu_q, kv_len, pages)
+        kv_len, pages, cu_q = self._sequences(kv_len, pages, cu_q)
+        seqs, i32, index = kv_len.numel(), torch.int32, self._index
+        if path.dtype is not i32 or path.dim() != 2 or path.shape[0] != seqs or path.get_device() != index or accepted.dtype is not i32 or \
+                accepted.shape != (seqs,) or accepted.get_device() != index:
+            raise ValueError(f"path must be [seqs, longest] and accepted [seqs], int32 on {self._dev}")
+        if not path.is_contiguous():
+            path = path.contiguous()
+        if not accepted.is_contiguous():
+            accepted = accepted.contiguous()
+        new_len = torch.empty_like(kv_len)
+        st = self._lib.siso_kv_keep_path(self._h, path.data_ptr(), accepted.data_ptr(), path.shape[1], cu_q.data_ptr(), kv_len.data_ptr(), pages.data_ptr(),
+                                         pages.stride(0), pages.shape[1], seqs, new_len.data_ptr(), _raw_stream(index))
+        if st:
+            self._check(st, "siso_kv_keep_path")
+        return new_len
+
+    def add_weights(self, weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor,
+                    max_q: int, layer: int = 0, scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, stream=None) -> None:
+        """Adds to weights (see new_weights()) what the queries q [n, heads, head dim] bf16 give each token that they see, summed over the
+        queries and the heads of a kv head: their probabilities, from lse [n, heads] as attention(want_lse=True) returned it.  What was there counts
+        `decay` times (0: not at all, whatever it is); the new tokens start from zero.  For the last queries of a longer chunk alone pass them with
+        their own cu_q."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.add_weights(weights, q, lse, cu_q, kv_len, pages, max_q, layer, scale, causal, decay)
+        index = self._index
+        shape = q.shape
+        if q.dtype is not torch.bfloat16 or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
+            raise ValueError(f"q must be a [n, heads, {self.head_dim}] bfloat16 tensor on {self._dev}")
+        if lse.dtype is not torch.float32 or lse.shape != shape[:2] or lse.get_device() != index:
+            raise ValueError(f"lse must be a [n, heads] float32 tensor on {self._dev}")
+        self._weights(weights)
+        kv_len, pages, cu_q = self._sequences(kv_len, pages, cu_q)
+        if q.stride(2) != 1:
+            q = q.contiguous()
+        if not lse.is_contiguous():
+            lse = lse.contiguous()
+        sq = q.stride()
+        _WEIGHTS.pack_into(self._args, 0, q.data_ptr(), lse.data_ptr(), weights.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), sq[0], sq[1],
+                           pages.stride(0), shape[0], kv_len.numel(), max_q, pages.shape[1], shape[1], layer, ATTN_CAUSAL if causal else 0,
+                           self._default_scale if scale is None else scale, decay)
+        st = self._lib.siso_kv_add_weights(self._h, self._args, _raw_stream(index))
+        if st:
+            self._check(st, "siso_kv_add_weights")
+
+    def evict(self, weights: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, budget: int, recent: int, out_pages: Optional[torch.Tensor] = None,
+              stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Cuts every sequence down to `budget` tokens, for each layer and kv head by itself: the last `recent` stay and the heaviest others (ties: the
+        earlier one), moved in order to the front of their pages, or of out_pages [seqs, max pages] (each the same as in pages at that index, or not otherwise in
+        use).  Returns (tokens now int32 [seqs], which places stayed int32 [layers, seqs, kv heads, budget], then -1)."""
+        if stream is not None:
+            with _on(stream, self._index):
+                return self.evict(weights, kv_len, pages, budget, recent, out_pages)
+        self._weights(weights)
+        kv_len, pages, _ = self._sequences(kv_len, pages)
+        out_pages = pages if out_pages is None else self._sequences(kv_len, out_pages)[1]
+        seqs = kv_len.numel()
+        if budget < 1 or not 0 <= recent <= budget:
+            raise ValueError("budget must be at least 1 and recent from 0 to budget")
+        new_len = torch.empty_like(kv_len)
+        kept = torch.empty((self.n_layers, seqs, self.n_kv_heads, budget), dtype=torch.int32, device=self._dev)
+        st = self._lib.siso_kv_evict(self._h, weights.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0), pages.shape[1], out_pages.data_ptr(),
+                                     out_pages.stride(0), out_pages.shape[1], seqs, budget, recent, new_len.data_ptr(), kept.data_ptr(),
+                                     _raw_stream(self._index))
+        if st:
+            self._check(st, "siso_kv_evict")
+        return new_len, kept
 
     def sync_status(self, stream=None) -> int:
         """Synchronise and return the handle's device status word (0 = clear); it is cleared by the call."""
@@ -301,3 +425,77 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: t
     if st:
         raise SisoError(st, "siso_verify_drafts", load_library().siso_last_cuda_error().decode() if st == 7 else "")
     return new, accepted
+
+
+def _call(index: int, where: str, *args) -> None:
+    """An entry point without a handle, on device `index` and its current stream."""
+    lib = load_library()
+    here = torch._C._cuda_getDevice()
+    if here != index:
+        torch.cuda.set_device(index)
+    try:
+        st = getattr(lib, where)(*args, _raw_stream(index))
+    finally:
+        if here != index:
+            torch.cuda.set_device(here)
+    if st:
+        raise SisoError(st, where, lib.siso_last_cuda_error().decode() if st == 7 else "")
+
+
+def tree_mask(parents: torch.Tensor, cu_q: torch.Tensor, max_nodes: int, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """parents int32 [n]: for each node of each sequence (from cu_q[b] on, int32 [seqs + 1]) the number of an earlier node of the sequence, anything
+    else: none.  Returns (mask int32 [n, words], depth int32 [n]): bit j of a row says that node j is the row's own or above it (max_nodes, the most of one
+    sequence, says how many words that takes), and how many are above.  Rows that no sequence covers hold anything."""
+    if stream is not None:
+        with _on(stream, parents.get_device()):
+            return tree_mask(parents, cu_q, max_nodes)
+    i32 = torch.int32
+    if parents.dtype is not i32 or parents.dim() != 1 or not parents.is_cuda:
+        raise ValueError("parents must be a one-dimensional int32 tensor on a GPU")
+    if cu_q.dtype is not i32 or cu_q.dim() != 1 or cu_q.numel() < 1 or cu_q.get_device() != parents.get_device():
+        raise ValueError(f"cu_q must be an int32 [seqs + 1] tensor on {parents.device}")
+    if not parents.is_contiguous():
+        parents = parents.contiguous()
+    if not cu_q.is_contiguous():
+        cu_q = cu_q.contiguous()
+    n, words = parents.numel(), max(1, -(-max_nodes // 32))
+    mask, depth = parents.new_empty((n, words)), torch.empty_like(parents)
+    _call(parents.get_device(), "siso_tree_mask", parents.data_ptr(), cu_q.data_ptr(), n, cu_q.numel() - 1, words, mask.data_ptr(), depth.data_ptr())
+    return mask, depth
+
+
+def verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: torch.Tensor, parents: torch.Tensor, cu_q: torch.Tensor, max_path: int,
+                u_accept: torch.Tensor, u_sample: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Verification of trees of drafts, nodes of all sequences one after the other (cu_q int32 [seqs + 1]), node 0 of each the last token that stands
+    already: target [n, vocab] probabilities of the token after each node, draft [n, vocab] those that a node's children were drawn from, each by itself (None:
+    the drafts were certain), fp32 or bf16; tokens, parents int32 [n]; u_accept [n], u_sample [seqs] fp32 in [0, 1).  Children are tried in order.
+    Returns (tokens out int32 [seqs, max_path + 1]: those that stand, one drawn, then -1; accepted int32 [seqs]; their nodes int32 [seqs, max_path], then -1)."""
+    if stream is not None:
+        with _on(stream, target.get_device()):
+            return verify_tree(target, draft, tokens, parents, cu_q, max_path, u_accept, u_sample)
+    shape, i32, f32 = target.shape, torch.int32, torch.float32
+    if target.dtype not in _ROW_TYPES or len(shape) != 2 or not target.is_cuda:
+        raise ValueError("target must be a [n, vocab] float32 or bfloat16 tensor on a GPU")
+    n, vocab = shape
+    index = target.get_device()
+    if draft is not None:
+        if draft.dtype is not target.dtype or draft.shape != shape or draft.get_device() != index:
+            raise ValueError("draft must be [n, vocab] of target's type and device")
+        if not draft.is_contiguous():
+            draft = draft.contiguous()
+    for t, kind, name in ((tokens, i32, "tokens"), (parents, i32, "parents"), (u_accept, f32, "u_accept")):
+        if t.dtype is not kind or t.shape != (n,) or t.get_device() != index:
+            raise ValueError(f"{name} must be a {str(kind)[6:]} [{n}] tensor on {target.device}")
+    seqs = u_sample.numel()
+    if u_sample.dtype is not f32 or u_sample.dim() != 1 or u_sample.get_device() != index:
+        raise ValueError(f"u_sample must be a float32 [seqs] tensor on {target.device}")
+    if cu_q.dtype is not i32 or cu_q.shape != (seqs + 1,) or cu_q.get_device() != index:
+        raise ValueError(f"cu_q must be an int32 [{seqs + 1}] tensor on {target.device}")
+    if max_path < 0:
+        raise ValueError("max_path must not be negative")
+    target, tokens, parents, cu_q, u_accept, u_sample = (t if t.is_contiguous() else t.contiguous()
+                                                         for t in (target, tokens, parents, cu_q, u_accept, u_sample))
+    out, accepted, path = tokens.new_empty((seqs, max_path + 1)), tokens.new_empty((seqs,)), tokens.new_empty((seqs, max_path))
+    _call(index, "siso_verify_tree", target.data_ptr(), 0 if draft is None else draft.data_ptr(), _ROW_TYPES[target.dtype], n, seqs, vocab, tokens.data_ptr(),
+          parents.data_ptr(), cu_q.data_ptr(), max_path, u_accept.data_ptr(), u_sample.data_ptr(), out.data_ptr(), accepted.data_ptr(), path.data_ptr())
+    return out, accepted, path
