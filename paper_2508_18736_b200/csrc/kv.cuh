@@ -26,6 +26,7 @@ struct Kv {
     int *status;                   // device status word (first error wins)
     CUtensorMap map_k, map_v;      // (d, head, token, page, layer), for attention: head_dim 64 or 128
     int box;                       // tokens of their boxes: the largest power of two that divides the page and 128
+    void *encode;                  // cuTensorMapEncodeTiled
     uint32_t attr_set;             // attention kernels that have been given their shared memory
 };
 

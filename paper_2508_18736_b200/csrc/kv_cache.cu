@@ -279,6 +279,7 @@ static siso_status_t encode_maps(Kv *h) {
     cudaDriverEntryPointQueryResult res;
     SISO_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &res));
     if (!fn || res != cudaDriverEntryPointSuccess) return check_cuda(cudaErrorNotSupported, "cuTensorMapEncodeTiled lookup");
+    h->encode = fn;
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     const cuuint64_t eb = kv_elem_bytes(g.dtype), row = g.head_dim * eb;
@@ -435,6 +436,9 @@ siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void
     if (a.n_tokens == 1) a.q_stride_token = 0;                    // (one entry: no stride)
     if (a.n_heads == 1) a.q_stride_head = 0;
     if (a.q_stride_token < 0 || a.q_stride_head < 0) return SISO_ERR_INVALID_ARG;
+    // queries come by TMA, which takes no stride of 0
+    if ((a.n_tokens > 1 && a.q_stride_token == 0) || (a.n_heads > 1 && a.q_stride_head == 0) || a.q_stride_token >= (1ll << 38) || a.q_stride_head >= (1ll << 38))
+        return SISO_ERR_UNSUPPORTED;
     if (a.q_stride_token % 8 != 0 || a.q_stride_head % 8 != 0 || !kvc::aligned16(a.d_q) || !kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
     if (a.n_tokens >= ((1ll << 31) - 256) / a.n_heads || static_cast<int64_t>(a.max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     const OnDevice on(h->cfg.device);

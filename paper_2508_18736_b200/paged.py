@@ -315,7 +315,7 @@ class PagedKV:
             raise ValueError(f"lse must be a [n, heads] float32 tensor on {self._dev}")
         self._weights(weights)
         kv_len, pages, cu_q = self._sequences(kv_len, pages, cu_q)
-        if q.stride(2) != 1:
+        if q.stride(2) != 1 or 0 in q.stride():
             q = q.contiguous()
         if not lse.is_contiguous():
             lse = lse.contiguous()
