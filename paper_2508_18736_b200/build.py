@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libsiso.so")
 SOURCES = ["api.cu", "lookup_simt.cu", "lookup_stream.cu", "lookup_tensor.cu", "lookup_tensor_pair.cu", "lookup_tensor_split.cu", "lookup_noalloc.cu", "sort.cu", "update.cu", "evict.cu",
            "merge.cu", "merge_tensor.cu", "cluster.cu", "swap.cu", "shard.cu", "tier.cu", "t2h.cu", "stream_maint.cu", "selftest.cu", "shard_merge.cu",
            "kv_cache.cu", "kv_attention.cu", "kv_attention_tc.cu", "verify.cu", "tree.cu",
-           "kv_evict.cu", "kv_weights.cu"]
+           "kv_evict.cu", "kv_weights.cu", "kv_weights_few.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--use_fast_math=false",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-O2"]
 

@@ -9,11 +9,11 @@
 // An item is (sequence, kv head, block of 256 keys = two tiles), a unit is an item with one tile of up to 128 query rows: whole tokens with all their heads of
 // the group (groups above 128: the largest part that divides them).  Units are dealt to one CTA per SM in equal runs, as in the attention; items that were cut are
 // joined by a second kernel in a fixed order.  With one row tile an item is one unit and nothing is cut (FEW).
-//   warps 0-7, 8-15  key tile 0, 1: a key belongs to two threads, which take every other 32 columns.  Scores from TMEM (two buffers), exponentials, sum
-//   warp 16          issues the products
-//   warp 17          fills the ring of key tiles by TMA, one box per run of tokens in one page
-//   warp 18          fills the ring of query tiles by TMA, and their -lse log2 e beside them
-//   warps 20-27      8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
+//   warps 0-3, 4-7   key tile 0, 1, a key per thread: scores from TMEM (two buffers), exponentials, sum
+//   warp 8           issues the products
+//   warp 9           fills the ring of key tiles by TMA, one box per run of tokens in one page
+//   warp 10          fills the ring of query tiles by TMA, and their -lse log2 e beside them
+//   warps 12-19      8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
 // Bounds: a step reads every key for a few rows: HBM.  A chunk's 256 x 128 scores take 1024 cycles of tcgen05.mma (d = 128) and 2048 of the SM's 16 exponentials a
 // cycle: the exponentials, of which some are taken on the FMA pipe.
 #include "kv_attention.cuh"
@@ -171,9 +171,16 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
     return true;
 }
 
+#ifndef MANY_PER_KEY
+#define MANY_PER_KEY 2
+#endif
+#ifndef POLY
+#define POLY (FEW ? 0 : 3)
+#endif
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
+constexpr int SHIFTS = 8;              // their ring: they are needed until the sums are done, the queries only until the products are
 struct Bars {
-    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], raw_full[8], raw_empty[8];
+    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8];
     uint32_t tmem;
     int gave_up;
     union {
@@ -183,16 +190,19 @@ struct Bars {
 };
 template <int KIND, int D, bool FEW> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
-    static constexpr int THREADS = EIGHT ? 896 : 640;
+    static constexpr int PER_KEY = FEW ? 1 : MANY_PER_KEY, SUM_WARPS = 8 * PER_KEY;    // threads of a key
+    static constexpr int THREADS = 32 * (SUM_WARPS + 4 + (EIGHT ? 8 : 0));
     static constexpr int TILE = TK * D * 2, Q_TILE = ROWS * D * 2, RAW = EIGHT ? TK * D : 0;
-    static constexpr int STAGES = D == 64 ? (EIGHT ? 4 : FEW ? 8 : 6) : (EIGHT ? (FEW ? 3 : 4) : FEW ? 5 : 4);
-    static constexpr int Q_STAGES = FEW || (EIGHT && D == 128) ? 2 : 3;
-    static constexpr int RAWS = !EIGHT ? 0 : FEW ? (D == 64 ? 8 : 4) : (D == 64 ? 4 : 2);
-    static constexpr int SMEM = STAGES * TILE + Q_STAGES * (Q_TILE + ROWS * 4) + RAWS * RAW + static_cast<int>(sizeof(Bars));
+    static constexpr int STAGES = D == 64 ? (EIGHT ? 4 : FEW ? 8 : 6) : (EIGHT ? 3 : 4);
+    static constexpr int Q_STAGES = 2;
+    static constexpr int RAWS = !EIGHT ? 0 : D == 64 ? 8 : 3;
+    static constexpr int SMEM = STAGES * TILE + Q_STAGES * Q_TILE + RAWS * RAW + SHIFTS * ROWS * 4 + static_cast<int>(sizeof(Bars));
     static_assert(SMEM <= 232448, "shared memory");
-    // registers: what the CTA has at launch (96 x 640 or 72 x 896), moved to the sums
-    static constexpr int SUM_REGS = EIGHT ? 96 : 104, OTHER_REGS = EIGHT ? 40 : 64, CONVERT_REGS = 40;
-    static_assert(4 * SUM_REGS + OTHER_REGS + (EIGHT ? 2 * CONVERT_REGS : 0) == (EIGHT ? 7 * 72 : 5 * 96), "register split");
+    // registers: what the CTA has at launch, moved to the sums
+    static constexpr int AT_LAUNCH = 65536 / THREADS / 8 * 8 > 168 ? 168 : 65536 / THREADS / 8 * 8;
+    static constexpr int SUM_REGS = PER_KEY == 1 ? (EIGHT ? 144 : 216) : (EIGHT ? 96 : 104);
+    static constexpr int OTHER_REGS = PER_KEY == 1 ? (EIGHT ? 64 : 72) : (EIGHT ? 40 : 64), CONVERT_REGS = PER_KEY == 1 ? 64 : 40;
+    static_assert(2 * PER_KEY * SUM_REGS + OTHER_REGS + (EIGHT ? 2 * CONVERT_REGS : 0) == THREADS / 128 * AT_LAUNCH, "register split");
 };
 __device__ __forceinline__ bool elect_one() {
     uint32_t one;
@@ -211,6 +221,24 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     asm("add.rn.f32x2 %0, %1, %2;"
         : "=l"(reinterpret_cast<unsigned long long &>(d)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
     return d;
+}
+// 2^x for x up to 127 on the FMA pipe, 0 below -127: x = n + f with n whole and f in [-1/2, 1/2], a polynomial of degree 5 for 2^f (largest relative
+// error on the interval minimised numerically: 1.5e-7), times 2^n, whose bits are n + 127 moved up
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.f));
+    const float big = 12583039.f;                     // 1.5 2^23 + 127: adding it leaves n + 127 in the low bits
+    const float2 t = add2(x, make_float2(big, big));
+    const float2 f = add2(x, fma2(t, make_float2(-1.f, -1.f), make_float2(big, big)));
+    float2 y = make_float2(0.0013276468962430954f, 0.0013276468962430954f);
+    y = fma2(y, f, make_float2(0.009675541892647743f, 0.009675541892647743f));
+    y = fma2(y, f, make_float2(0.05550713464617729f, 0.05550713464617729f));
+    y = fma2(y, f, make_float2(0.24022120237350464f, 0.24022120237350464f));
+    y = fma2(y, f, make_float2(0.6931469440460205f, 0.6931469440460205f));
+    y = fma2(y, f, make_float2(1.0000001192092896f, 1.0000001192092896f));
+    y.x *= __uint_as_float(__float_as_uint(t.x) << 23);
+    y.y *= __uint_as_float(__float_as_uint(t.y) << 23);
+    return y;
 }
 __device__ __forceinline__ void load_q_box(uint32_t dst, const CUtensorMap *map, int d, int head, int token, uint64_t *bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -240,24 +268,26 @@ __global__ void __launch_bounds__(Shape<KIND, D, FEW>::THREADS, 1)
 weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q) {
     using S = Shape<KIND, D, FEW>;
     constexpr bool EIGHT = S::EIGHT;
+    constexpr int SUM_WARPS = S::SUM_WARPS, PER_KEY = S::PER_KEY;
     constexpr int RB = D * (EIGHT ? 1 : 2), LINE = RB < 128 ? RB : 128;
     extern __shared__ __align__(1024) uint8_t smem[];           // all of it: nothing static, so that it begins on a boundary of the swizzle
     uint8_t *tiles = smem, *q_tiles = tiles + S::STAGES * S::TILE, *raws = q_tiles + S::Q_STAGES * S::Q_TILE;
     float *shifts = reinterpret_cast<float *>(raws + S::RAWS * S::RAW);              // -lse log2 e of a query tile's rows
-    Bars &bars = *reinterpret_cast<Bars *>(shifts + S::Q_STAGES * ROWS);
+    Bars &bars = *reinterpret_cast<Bars *>(shifts + SHIFTS * ROWS);
 
     if constexpr (!FEW) dependents_may_start();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 4; ++i) { mbar_init(&bars.s_full[0][0] + i, 1); mbar_init(&bars.s_empty[0][0] + i, 8); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&bars.s_full[0][0] + i, 1); mbar_init(&bars.s_empty[0][0] + i, SUM_WARPS / 2); }
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(&bars.k_full[i], EIGHT ? 8 : 1); mbar_init(&bars.k_empty[i], 1); }
-        for (int i = 0; i < S::Q_STAGES; ++i) { mbar_init(&bars.q_full[i], 2); mbar_init(&bars.q_empty[i], 1 + 16); }
+        for (int i = 0; i < S::Q_STAGES; ++i) { mbar_init(&bars.q_full[i], 1); mbar_init(&bars.q_empty[i], 1); }
+        for (int i = 0; i < SHIFTS; ++i) { mbar_init(&bars.sh_full[i], 1); mbar_init(&bars.sh_empty[i], SUM_WARPS); }
         for (int i = 0; i < S::RAWS; ++i) { mbar_init(&bars.raw_full[i], 1); mbar_init(&bars.raw_empty[i], 8); }
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int rows = g.hb * g.tb;                                // of a full row tile
-    const int n_cols = FEW ? (rows + 31) & ~31 : ROWS;
+    const int n_cols = FEW && rows <= 64 ? 64 : ROWS;
     // rows behind a full tile's: zeros, or what stands there would reach the scores as NaN
     for (int i = threadIdx.x; i < S::Q_STAGES * (D / 64) * (n_cols - rows) * 8; i += S::THREADS) {
         const int line = i / 8, part = line / (n_cols - rows), row = rows + line % (n_cols - rows);
@@ -269,7 +299,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     long long run_end, total;
     int ctas;
     if (!locate<FEW, S::THREADS>(g, cur, run_end, total, ctas, bars.find)) return;
-    if (warp == 16) {
+    if (warp == SUM_WARPS) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -279,13 +309,13 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     const uint32_t tmem = bars.tmem;
     volatile int *gave_up = &bars.gave_up;
 
-    if (warp >= 20) {
+    if (warp >= SUM_WARPS + 4) {
         if constexpr (EIGHT) {
             // ---- codes -> bf16 tiles.  8 (4) lanes share a row of 128 (64) bytes; each writes two chunks of 8 values, lanes of the upper half of a
             // row the second one first
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::CONVERT_REGS));
             constexpr int CH = RB / 16, PER = 32 / CH, MINE = TK / 8;     // chunks of a row, rows of a warp's step, rows of a warp
-            const int chunk = lane % CH, r0 = (warp - 20) * MINE + lane / CH, flip = CH == 8 ? chunk >> 2 : 0;
+            const int chunk = lane % CH, r0 = (warp - SUM_WARPS - 4) * MINE + lane / CH, flip = CH == 8 ? chunk >> 2 : 0;
             int stage = 0, raw = 0;
             uint32_t phase = 0, raw_phase = 0;
             do {
@@ -314,9 +344,9 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 }
             } while (cur.step(g));
         }
-    } else if (warp >= 16) {
+    } else if (warp >= SUM_WARPS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::OTHER_REGS));
-        if (warp == 17) {
+        if (warp == SUM_WARPS + 1) {
             // ---- keys: lanes 0-15 own the runs of 8 tokens of an item's first tile, lanes 16-31 of its second.  Pages are asked for one item ahead
             constexpr int RING = EIGHT ? S::RAWS : S::STAGES;
             const int box_blocks = g.box / 8;
@@ -356,10 +386,10 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 }
                 at = ahead;
             }
-        } else if (warp == 18) {
+        } else if (warp == SUM_WARPS + 2) {
             // ---- queries and their statistics, which are asked for one tile ahead
-            int stage = 0;
-            uint32_t phase = 0;
+            int stage = 0, sh = 0;
+            uint32_t phase = 0, sh_phase = 0;
             const uint32_t bytes = rows * (D * 2);
             struct Tile { int token, head, here; } at;         // first token (row of d_q), first head, tokens of the sequence from there on
             float shift[ROWS / 32];
@@ -392,13 +422,15 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                     place(ahead);
                     statistics(ahead, ahead_shift);
                 }
-                wait_bar(&bars.q_empty[stage], phase ^ 1u, gave_up, g.status);
+                wait_bar(&bars.sh_empty[sh], sh_phase ^ 1u, gave_up, g.status);
 #pragma unroll
                 for (int i = 0; i < ROWS / 32; ++i)             // nothing seen (-infinity), or no row: exponentials are zero
-                    shifts[stage * ROWS + i * 32 + lane] = shift[i] == -INFINITY ? -INFINITY : shift[i] * -1.4426950408889634f;
+                    shifts[sh * ROWS + i * 32 + lane] = shift[i] == -INFINITY ? -INFINITY : shift[i] * -1.4426950408889634f;
                 __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.sh_full[sh]);
+                if (++sh == SHIFTS) { sh = 0; sh_phase ^= 1u; }
+                wait_bar(&bars.q_empty[stage], phase ^ 1u, gave_up, g.status);
                 if (*gave_up == 0 && lane == 0) {
-                    mbar_arrive(&bars.q_full[stage]);
                     mbar_arrive_expect_tx(&bars.q_full[stage], bytes);
 #pragma unroll
                     for (int half = 0; half < D / 64; ++half)
@@ -410,7 +442,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
 #pragma unroll
                 for (int i = 0; i < ROWS / 32; ++i) shift[i] = ahead_shift[i];
             }
-        } else if (warp == 16) {
+        } else if (warp == SUM_WARPS) {
             // ---- products.  The whole warp goes through the loop; one lane issues
             const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
             const uint64_t k_desc = smem_desc_sw128(smem_u32(tiles)), q_desc = smem_desc_sw128(smem_u32(q_tiles));
@@ -456,14 +488,15 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
             } while (more);
         }
     } else {
-        // ---- sums: half of the columns of one key
+        // ---- sums: one or two threads per key, each with its part of the columns
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::SUM_REGS));
-        const int t = warp >> 3, half = (warp >> 2) & 1, key = threadIdx.x & 127;
-        const uint32_t s_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + t * 256;
+        const int t = warp / (4 * PER_KEY), half = (warp >> 2) % PER_KEY, key = threadIdx.x & 127;
+        const int mine_cols = n_cols / PER_KEY, col = half * mine_cols;
+        const uint32_t s_at = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + t * 256 + col;
         const bool causal = (g.a.flags & SISO_ATTN_CAUSAL) != 0u;
         float *held = g.a.d_weights + static_cast<long long>(g.a.layer) * g.kv.n_pages * g.kv.n_kv_heads * g.kv.page_size;
-        int q_stage = 0, buf = 0;
-        uint32_t q_phase = 0, s_phase = 0;
+        int sh = 0, buf = 0;
+        uint32_t sh_phase = 0, s_phase = 0;
         // what belongs to this thread's key of an item; asked for one item ahead
         struct Key { long long at; float old; uint32_t exp; } mine;
         auto look_up = [&](Key &x) {
@@ -497,23 +530,21 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 const int tile = tile_first + u, token0 = (g.chunks == 1 ? tile : tile / g.chunks) * g.tb;
                 // columns [first, last) are rows that see the key
                 const int last = min(rows, (n_q - token0) * g.hb);
-                const bool cut = last < rows || (causal && j0 + TK - 1 > before + token0);
+                const bool cut = __any_sync(0xFFFFFFFFu, last < rows || (causal && j0 + TK - 1 > before + token0));
                 const int first = causal && cut ? max(0, min(j - before - token0, ROWS)) * g.hb : 0;
-                wait_bar(&bars.q_full[q_stage], q_phase, gave_up, g.status);
-                wait_bar(&bars.s_full[t][buf], s_phase, gave_up, g.status);
-                tcgen05_fence_after();
-                const float4 *shift = reinterpret_cast<const float4 *>(shifts + q_stage * ROWS);
+                const float4 *shift = reinterpret_cast<const float4 *>(shifts + sh * ROWS);
+                uint64_t *const read = &bars.sh_empty[sh];
                 float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 auto weigh = [&](auto some, const uint32_t (&r)[32], int c0) __attribute__((always_inline)) {
 #pragma unroll
                     for (int x = 0; x < 32; x += 4) {
-                        const float4 sh = shift[(c0 + x) / 4];
-                        float2 y[2] = {fma2(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f), make_float2(sh.x, sh.y)),
-                                       fma2(make_float2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), make_float2(f, f), make_float2(sh.z, sh.w))};
+                        const float4 d = shift[(c0 + x) / 4];
+                        float2 y[2] = {fma2(make_float2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), make_float2(f, f), make_float2(d.x, d.y)),
+                                       fma2(make_float2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), make_float2(f, f), make_float2(d.z, d.w))};
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            y[i].x = kva::ex2(y[i].x);
-                            y[i].y = kva::ex2(y[i].y);
+                            if ((x / 2 + i) * POLY % 16 < POLY) y[i] = ex2_poly(y[i]);
+                            else { y[i].x = kva::ex2(y[i].x); y[i].y = kva::ex2(y[i].y); }
                             if constexpr (some.value) {
                                 const int c = c0 + x + 2 * i;
                                 if (c < first || c >= last) y[i].x = 0.f;
@@ -523,42 +554,47 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                         }
                     }
                 };
-                uint32_t ra[32], rb[32];
-                const int c0 = half * 32, c1 = 64 + half * 32;
-                const bool has0 = c0 < n_cols, has1 = c1 < n_cols;
-                if (has0) tmem_ld_32x32(s_at + buf * 128 + c0, ra);
-                if (has1) tmem_ld_32x32(s_at + buf * 128 + c1, rb);
-                if (has0) tmem_ld_fence(ra);
-                if (has1) tmem_ld_fence(rb);
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.s_empty[t][buf]);
-                if (__any_sync(0xFFFFFFFFu, cut)) {
-                    if (has0) weigh(Yes{}, ra, c0);
-                    if (has1) weigh(Yes{}, rb, c1);
-                } else {
-                    if (has0) weigh(No{}, ra, c0);
-                    if (has1) weigh(No{}, rb, c1);
+                wait_bar(&bars.sh_full[sh], sh_phase, gave_up, g.status);
+                wait_bar(&bars.s_full[t][buf], s_phase, gave_up, g.status);
+                tcgen05_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < mine_cols; c += 64) {
+                    uint32_t ra[32], rb[32];
+                    tmem_ld_32x32(s_at + buf * 128 + c, ra);
+                    tmem_ld_32x32(s_at + buf * 128 + c + 32, rb);
+                    tmem_ld_fence(ra);
+                    tmem_ld_fence(rb);
+                    if (c + 64 >= mine_cols) {
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bars.s_empty[t][buf]);
+                    }
+                    if (cut) {
+                        weigh(Yes{}, ra, col + c);
+                        weigh(Yes{}, rb, col + c + 32);
+                    } else {
+                        weigh(No{}, ra, col + c);
+                        weigh(No{}, rb, col + c + 32);
+                    }
                 }
+                if (++sh == SHIFTS) { sh = 0; sh_phase ^= 1u; }
+                if ((buf ^= 1) == 0) s_phase ^= 1u;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.q_empty[q_stage]);
+                if (lane == 0) mbar_arrive(read);
                 acc[0] = add2(acc[0], acc[1]);
                 sum += acc[0].x + acc[0].y;
-                if (++q_stage == S::Q_STAGES) { q_stage = 0; q_phase ^= 1u; }
-                if ((buf ^= 1) == 0) s_phase ^= 1u;
             }
-            if (n_cols > 32) {                            // (otherwise the first thread of the key has all columns)
+            if constexpr (PER_KEY == 2) {
                 if (half == 1) bars.peer[t][key] = sum;
                 asm volatile("bar.sync %0, 256;" ::"r"(1 + t) : "memory");
                 if (half == 0) sum += bars.peer[t][key];
                 asm volatile("bar.sync %0, 256;" ::"r"(1 + t) : "memory");
             }
-            if (half == 0) {
-                if (whole) {
-                    if (mine.at >= 0) held[mine.at] = g.a.decay * mine.old + sum;
-                } else {
-                    g.part[kva::part_place(blockIdx.x, began_before) * KB + t * TK + key] = sum;
-                }
+            if (half == 1) {
+            } else if (whole) {
+                if (mine.at >= 0) held[mine.at] = g.a.decay * mine.old + sum;
+            } else {
+                g.part[kva::part_place(blockIdx.x, began_before) * KB + t * TK + key] = sum;
             }
             mine = next;
         }
@@ -569,7 +605,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     kva::let_copies_land(gave_up);
     tcgen05_fence_before();
     __syncthreads();
-    if (warp == 16) {
+    if (warp == SUM_WARPS) {
         tcgen05_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
@@ -609,10 +645,15 @@ template <int KIND, int D> static siso_status_t run(Kv *h, const Args &g, bool f
     return few ? run_as<KIND, D, true>(h, g, map_q, s) : run_as<KIND, D, false>(h, g, map_q, s);
 }
 
+// up to 32 rows per kv head (kv_weights_few.cu)
+siso_status_t launch_few_rows(Kv *h, const siso_weights_t *a, int rows, cudaStream_t s);
+
 }  // namespace kvw
 
 siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, cudaStream_t s) {
     using namespace kvw;
+    const long long rows = static_cast<long long>(a->max_q) * (a->n_heads / h->cfg.n_kv_heads);
+    if (rows <= 32) return launch_few_rows(h, a, static_cast<int>(rows), s);
     Args g;
     g.kv = kv_view(h, a->layer);
     g.a = *a;
