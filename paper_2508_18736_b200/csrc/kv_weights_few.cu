@@ -2,8 +2,8 @@
 // The formulas are in kv_weights.cu.
 //
 // Every key meets few multiplications, so the call is bound by HBM and the point is to spend few instructions on a byte.  As in the attention over few rows four
-// producer warps fill a ring of units by TMA, one box per run of tokens in one page, and eight warps consume it; units are dealt to one CTA per SM in equal runs.  A
-// warp owns a sixteenth or an eighth of a unit's keys and shares nothing with the others: scores^T = K Q^T by mma.sync m16n8k16 (rows fill the 8 columns; tcgen05's
+// producer warps fill a ring of units by TMA, one box per run of tokens in one page, and groups of warps consume it in turn; units are dealt to one CTA per SM in equal
+// runs.  A warp owns 32 of a unit's keys and shares nothing with the others: scores^T = K Q^T by mma.sync m16n8k16 (rows fill the 8 columns; tcgen05's
 // 128 lanes or columns would be mostly empty, and 8-bit codes would have to go through shared memory once more), exponentials, the sum over a key's rows by
 // two shuffles.  What else belongs to a key (its exponent, its weight so far, where that lies) comes with the unit.  8-bit codes become fp16 in registers, exactly; queries
 // are brought to fp16 with a factor per row, exactly but for elements below 2^-31 of their row's largest.
@@ -22,7 +22,7 @@ using umma2::smem_u32;
 using kva::FastDiv;
 using kva::wait_bar;
 
-constexpr int PRODUCERS = 4, WARPS = 8, THREADS = 32 * (WARPS + PRODUCERS);
+constexpr int PRODUCERS = 4;             // warps that fill the ring; each has its own stages
 
 struct Args {
     KvView kv;
@@ -33,16 +33,21 @@ struct Args {
     int *status;
 };
 
-template <int KIND, int D> struct Shape {
+template <int KIND, int D, int NT> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
+    static constexpr int WARPS = NT > 1 ? 8 : EIGHT ? 16 : 12;      // consumers
+    static constexpr int THREADS = 32 * (WARPS + PRODUCERS);
     static constexpr int T = EIGHT ? 256 : 128;             // keys of a unit
+    static constexpr int NK = 32, GW = T / NK, GROUPS = WARPS / GW;      // keys of a warp, warps of a unit; groups of them take units in turn
     static constexpr int RB = D * (EIGHT ? 1 : 2), STAGE = T * RB;
     static constexpr int META = T * 4 + T / 8 * 8 + (EIGHT ? T : 0);      // weights so far, places of the blocks of 8, exponents
     static constexpr int FIT = (232448 - 1024 - 2048) / (STAGE + META);
-    static constexpr int STAGES = FIT > 12 ? 12 : FIT;
+    // a stage is always read by the same group: one that is ahead of the others must not ask for a round of a stage before the round before has come
+    static constexpr int STAGES = (FIT > 12 ? 12 : FIT) / GROUPS * GROUPS;
     static constexpr int SMEM = STAGES * (STAGE + META) + 1024;
-    static constexpr int PRODUCER_REGS = 40, CONSUMER_REGS = 232;
-    static_assert(WARPS * CONSUMER_REGS + PRODUCERS * PRODUCER_REGS == (WARPS + PRODUCERS) * 168, "168 registers a thread at launch");
+    static constexpr int AT_LAUNCH = WARPS == 8 ? 168 : WARPS == 12 ? 128 : 96, PRODUCER_REGS = WARPS == 8 ? 40 : WARPS == 12 ? 56 : 64,
+                         CONSUMER_REGS = WARPS == 8 ? 232 : WARPS == 12 ? 152 : 104;
+    static_assert(WARPS * CONSUMER_REGS + PRODUCERS * PRODUCER_REGS == (WARPS + PRODUCERS) * AT_LAUNCH, "registers at launch");
 };
 template <int STAGES> struct Ring {
     uint64_t full[STAGES], empty[STAGES];
@@ -80,7 +85,7 @@ template <int T> struct Cursor {
         return true;
     }
 };
-template <int T>
+template <int T, int THREADS>
 __device__ __forceinline__ bool locate(const Args &g, Cursor<T> &cur, unsigned long long *buf) {
     constexpr int W = THREADS / 32;
     unsigned long long mine = 0ull, upto = 0ull, all, total = 0ull;
@@ -148,13 +153,13 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t &
 }
 
 template <int KIND, int D, int NT>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(Shape<KIND, D, NT>::THREADS, 1)
 weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k) {
-    using S = Shape<KIND, D>;
+    using S = Shape<KIND, D, NT>;
     constexpr bool EIGHT = S::EIGHT;
-    constexpr int T = S::T, RB = S::RB, STAGES = S::STAGES, NK = T / WARPS, LINE = RB < 128 ? RB : 128, BLOCKS = T / 8, MR = 8 * NT;
+    constexpr int T = S::T, RB = S::RB, STAGES = S::STAGES, NK = S::NK, WARPS = S::WARPS, GW = S::GW, LINE = RB < 128 ? RB : 128, BLOCKS = T / 8, MR = 8 * NT;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ unsigned long long buf[THREADS / 32 + 3];
+    __shared__ unsigned long long buf[S::THREADS / 32 + 3];
     __shared__ Ring<STAGES> ring;
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // (an offset: the loads stay shared loads)
     long long *places = reinterpret_cast<long long *>(smem + STAGES * S::STAGE);      // [STAGES][BLOCKS]: of a block's first key among the weights, or -1
@@ -163,14 +168,14 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < STAGES; ++i) { mbar_init(&ring.full[i], 33); mbar_init(&ring.empty[i], WARPS); }      // 33: the bytes, and the lanes' small things
+        for (int i = 0; i < STAGES; ++i) { mbar_init(&ring.full[i], 33); mbar_init(&ring.empty[i], GW); }      // 33: the bytes, and the lanes' small things
         ring.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
     Cursor<T> cur;
-    if (!locate<T>(g, cur, buf)) return;
+    if (!locate<T, S::THREADS>(g, cur, buf)) return;
     volatile int *gave_up = &ring.gave_up;
     float *held = g.a.d_weights + static_cast<long long>(g.a.layer) * g.kv.n_pages * g.kv.n_kv_heads * g.kv.page_size;
 
@@ -288,41 +293,58 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
             }
         }
     };
-    fetch(cur, 0, next);
-    bool fresh = true;                                        // a kv head begins: its queries are in `next`
-    int stage = 0;
+    int stage = warp / GW;
     uint32_t phase = 0;
-    for (bool more = true; more;) {
+    auto onward = [&]() {                                     // to this group's next unit
+        for (int i = 0; i < S::GROUPS; ++i)
+            if (!cur.step(g)) return false;
+        stage += S::GROUPS;
+        if (stage >= STAGES) { stage -= STAGES; phase ^= 1u; }
+        return true;
+    };
+    static_assert(STAGES % S::GROUPS == 0 && STAGES > 0, "a stage is always read by the same group");
+    bool more = true;
+    for (int i = 0; i < warp / GW && more; ++i) more = cur.step(g);
+    int b_now = -1, head_now = -1, b_next = cur.b, head_next = cur.head;      // whose queries `now` and `next` are
+    if (more) fetch(cur, 0, next);
+    while (more) {
         const int row_tiles = (cur.n_q * g.group + MR - 1) / MR;      // (one, unless max_q says less than there is)
-        if (fresh) {
+        if (cur.b != b_now || cur.head != head_now) {
+            if (cur.b != b_next || cur.head != head_next) fetch(cur, 0, next);
             now = next;
             take(cur, 0);
+            b_now = cur.b;
+            head_now = cur.head;
             Cursor<T> after = cur;                            // the next kv head's queries are on their way meanwhile
             after.left -= cur.tiles - cur.tile;
             if (after.left > 0) {
                 after.next_head(g);
                 fetch(after, 0, next);
+                b_next = after.b;
+                head_next = after.head;
             }
         }
         wait_bar(&ring.full[stage], phase, gave_up, g.status);
-        const int j0 = cur.tile * T;
+        const int j0 = cur.tile * T, n0 = warp % GW * NK;
         const bool cut = causal && j0 + T - 1 > cur.len - cur.n_q;
-        const int k_first = stage * S::STAGE + kva::chunk_at<RB, T>(key_of<RB>(r0), c);
-#pragma unroll 1
-        for (int n0 = warp * NK; n0 < (warp + 1) * NK; n0 += 16) {
-            float sum[2] = {0.f, 0.f};
-            for (int rt = 0; rt < row_tiles; ++rt) {
-                if (row_tiles > 1) {
-                    fetch(cur, rt, now);
-                    take(cur, rt);
-                }
-                float s[NT][4];
+        const int k_first = stage * S::STAGE + kva::chunk_at<RB, T>(key_of<RB>(r0), c) + n0 * LINE;
+        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};           // of the keys r0 and r0 + 8 of two tiles of 16
+        for (int rt = 0; rt < row_tiles; ++rt) {
+            if (row_tiles > 1) {
+                fetch(cur, rt, now);
+                take(cur, rt);
+            }
+            float s[2][NT][4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) { s[t][0] = 0.f; s[t][1] = 0.f; s[t][2] = 0.f; s[t][3] = 0.f; }
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int a = 0; a < RB / 64; ++a) {
+                for (int t = 0; t < NT; ++t) { s[i][t][0] = 0.f; s[i][t][1] = 0.f; s[i][t][2] = 0.f; s[i][t][3] = 0.f; }
+#pragma unroll
+            for (int a = 0; a < RB / 64; ++a) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
                     // chunk 4 a + c of keys row and row + 8: tiles start at multiples of 1024, so a only flips bits
-                    const int at = ((k_first + n0 * LINE) ^ ((a & 1) << 6)) + (a >> 1) * (T * 128);
+                    const int at = ((k_first + 16 * i * LINE) ^ ((a & 1) << 6)) + (a >> 1) * (T * 128);
                     const uint4 w0 = *reinterpret_cast<const uint4 *>(smem + at), w1 = *reinterpret_cast<const uint4 *>(smem + at + 8 * LINE);
                     const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
                     if constexpr (!EIGHT) {
@@ -330,7 +352,7 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
                         for (int x = 0; x < 2; ++x) {
                             const uint32_t f[4] = {x0[2 * x], x1[2 * x], x0[2 * x + 1], x1[2 * x + 1]};
 #pragma unroll
-                            for (int t = 0; t < NT; ++t) mma<false>(s[t], f, now.q[t][2 * a + x]);
+                            for (int t = 0; t < NT; ++t) mma<false>(s[i][t], f, now.q[t][2 * a + x]);
                         }
                     } else {
 #pragma unroll
@@ -339,56 +361,58 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
                             widen<KIND>(x0[x], f[0], f[2]);
                             widen<KIND>(x1[x], f[1], f[3]);
 #pragma unroll
-                            for (int t = 0; t < NT; ++t) mma<true>(s[t], f, now.q[t][4 * a + x]);
+                            for (int t = 0; t < NT; ++t) mma<true>(s[i][t], f, now.q[t][4 * a + x]);
                         }
                     }
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int n = n0 + 8 * e + key_of<RB>(r0);
+                    const int n = n0 + 16 * i + 8 * e + key_of<RB>(r0);
                     // (byte 0: nothing above 2^-118, counts as zero; byte 255: infinity, then NaN)
                     const float f = EIGHT ? __uint_as_float(static_cast<uint32_t>(exps[stage * T + n]) << 23) : 1.f;
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float p = kva::ex2(fmaf(s[t][2 * e + h], EIGHT ? f * scale[t][h] : scale[t][h], shift[t][h]));
-                            sum[e] += cut && j0 + n > pos[t][h] ? 0.f : p;
+                            const float p = kva::ex2(fmaf(s[i][t][2 * e + h], EIGHT ? f * scale[t][h] : scale[t][h], shift[t][h]));
+                            sum[i][e] += cut && j0 + n > pos[t][h] ? 0.f : p;
                         }
                 }
-            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 1);
-                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 2);
+                sum[i][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[i][e], 1);
+                sum[i][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[i][e], 2);
             }
-            if (c < 2) {                                      // lane c = e writes key r0 + 8 e
-                const int n = n0 + 8 * c + key_of<RB>(r0), j = j0 + n;
-                const long long place = places[stage * BLOCKS + n / 8];
-                if (place >= 0 && j < cur.len) {
-                    const float old = g.a.decay != 0.f && j < cur.len - cur.n_q ? g.a.decay * olds[stage * T + n] : 0.f;
-                    held[place + (n & 7)] = old + (c ? sum[1] : sum[0]);
-                }
+        {                                                     // lane c of a key's four writes key r0 + 8 (c & 1) of tile c / 2
+            const int n = n0 + 8 * c + key_of<RB>(r0), j = j0 + n;
+            const long long place = places[stage * BLOCKS + n / 8];
+            const float given = c == 0 ? sum[0][0] : c == 1 ? sum[0][1] : c == 2 ? sum[1][0] : sum[1][1];
+            if (place >= 0 && j < cur.len) {
+                const float old = g.a.decay != 0.f && j < cur.len - cur.n_q ? g.a.decay * olds[stage * T + n] : 0.f;
+                held[place + (n & 7)] = old + given;
             }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&ring.empty[stage]);
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        const int b = cur.b, head = cur.head;
-        more = cur.step(g);
-        fresh = cur.b != b || cur.head != head;
+        more = onward();
     }
     kva::let_copies_land(gave_up);            // (the producers may have gone before the last wait gave up)
 }
 
 template <int KIND, int D, int NT> static siso_status_t run(Kv *h, const Args &g, cudaStream_t s) {
-    using S = Shape<KIND, D>;
+    using S = Shape<KIND, D, NT>;
     constexpr uint32_t bit = 1u << (NT == 1 ? 20 : NT == 2 ? 21 : 22);
     if (!(h->attr_set & bit)) {
         SISO_CUDA(cudaFuncSetAttribute(weights_few_rows_kernel<KIND, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    weights_few_rows_kernel<KIND, D, NT><<<h->sm_count, THREADS, S::SMEM, s>>>(g, h->map_k);
+    weights_few_rows_kernel<KIND, D, NT><<<h->sm_count, S::THREADS, S::SMEM, s>>>(g, h->map_k);
     SISO_CUDA(cudaGetLastError());
     return SISO_OK;
 }

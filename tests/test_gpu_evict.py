@@ -149,6 +149,14 @@ def test_many_row_tiles_for_few_keys_are_split_and_joined(kind):
     run_weights(kind, 128, 8, 1, 64, [20011, 3], [9, 3])
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "i8"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_len,heads", [(1, 8), (4, 32), (7, 32), (20, 32)])
+def test_many_units_for_each_sm(kind, dim, q_len, heads):
+    # 8 kv heads x 30,000 tokens: every ring goes round more than once
+    run_weights(kind, dim, heads, 8, 64, [29003, 1500], [q_len, q_len], decay=0.5)
+
+
 @pytest.mark.parametrize("n_q", [1, 20, 100])
 def test_pages_outside_the_pool_and_long_lengths(n_q):
     page, heads, dim = 16, 2, 128
