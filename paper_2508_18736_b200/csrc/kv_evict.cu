@@ -2,8 +2,7 @@
 //
 // Both move rows towards the front of their sequence, in order: the t-th row goes from place f(t) >= t (f ascending) to place t.  So the place that row t is
 // written to can be the source of rows up to t only, never of later ones: once the rows up to t have been read, row t may be written.
-#include "kv.cuh"
-#include "umma_pair.cuh"
+#include "kv_attention.cuh"
 
 namespace siso {
 namespace kve {
@@ -148,6 +147,7 @@ struct EvictArgs {
     const int32_t *kv_len, *pages, *out_pages;
     long long pages_stride, out_stride;
     int32_t *new_len, *kept;
+    kva::FastDiv by_page;
     int max_pages, out_max_pages, n_seqs, budget, recent, keys;
     int *status;
 };
@@ -163,12 +163,35 @@ template <typename T> __device__ __forceinline__ T remote(const T *p, uint32_t r
     return static_cast<T>(x);
 }
 
+// From the top digit down, where the wanted-th number lies: (digit, how many are in larger ones, how many in it).  For every warp by itself
+__device__ __forceinline__ uint3 find_digit(const uint32_t *counts, uint32_t wanted, int lane) {
+    uint32_t mine[8], total = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { mine[i] = counts[255 - (lane * 8 + i)]; total += mine[i]; }
+    uint32_t upto = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += y;
+    }
+    uint32_t before = upto - total, digit = 0u, larger = 0u, here = 0u;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (before < wanted && before + mine[i] >= wanted) { digit = 255u - (lane * 8 + i); larger = before; here = mine[i]; found = true; }
+        before += mine[i];
+    }
+    const int from = max(__ffs(__ballot_sync(0xFFFFFFFFu, found)) - 1, 0);
+    return make_uint3(__shfl_sync(0xFFFFFFFFu, digit, from), __shfl_sync(0xFFFFFFFFu, larger, from), __shfl_sync(0xFFFFFFFFu, here, from));
+}
+
 template <int PIECE>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 2)
 evict_kernel(const __grid_constant__ EvictArgs g) {
     using T = typename Bytes<PIECE>::T;
     extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[2][256], counts[2], warp_gt[WARPS], warp_eq[WARPS], chosen[2];
+    __shared__ uint32_t hist[4][256], sums[2][256], counts[2], warp_gt[WARPS], warp_eq[WARPS];
+    __shared__ int4 moves[THREADS];               // page and token that a row comes from, that it goes to; page -1: it is not moved
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t rank, n_ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -184,6 +207,10 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
     int32_t *kept = g.kept + static_cast<long long>(seg) * g.budget;
     auto in_pool = [&](int p) { return p >= 0 && p < g.p.n_pages; };
     auto small_at = [&](int p, int t) { return ((first_page + p) * g.p.n_kv_heads + head) * page_size + t; };       // of weights and exponents
+    auto together = [&]() {
+        if (n_ctas > 1) cluster_sync();
+        else __syncthreads();
+    };
 
     if (layer == 0 && head == 0 && rank == 0 && threadIdx.x == 0) g.new_len[b] = n_kept;
     const int step = static_cast<int>(n_ctas) * THREADS, me = static_cast<int>(rank) * THREADS + threadIdx.x;
@@ -196,61 +223,67 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
         const int each = ((cand + static_cast<int>(n_ctas) - 1) / static_cast<int>(n_ctas) + WARPS * 32 - 1) / (WARPS * 32) * (WARPS * 32);
         const int lo = static_cast<int>(min(static_cast<long long>(rank) * each, static_cast<long long>(cand))), hi = min(cand, lo + each);
         auto look_up = [&](int i) {
-            const int at = i / page_size, p = pages[at];
-            if (!in_pool(p)) { set_status(g.status, SISO_ERR_INVALID_ARG); return 0u; }
-            return order_of(g.weights[small_at(p, i - at * page_size)]);
+            const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(i))), p = pages[at];
+            return in_pool(p) ? order_of(g.weights[small_at(p, i - at * page_size)]) : 0u;
         };
         auto key = [&](int i) { return i - lo < g.keys ? keys[i - lo] : look_up(i); };
-        for (int i = threadIdx.x; i < 512; i += THREADS) (&hist[0][0])[i] = 0u;
+        for (int i = threadIdx.x; i < 4 * 256; i += THREADS) (&hist[0][0])[i] = 0u;
         __syncthreads();
         // the wanted-th largest: `least`, of which `ties` are wanted
         uint32_t least = 0u;
         int ties = wanted;
-        for (int pass = 0; pass < 4 && wanted > 0; ++pass) {
-            const int shift = 24 - 8 * pass;
-            uint32_t *h = hist[pass & 1];
-#pragma unroll 4
-            for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += THREADS) {
-                uint32_t x;
-                if (pass == 0) {
-                    x = look_up(i);
+        if (wanted > 0) {
+            constexpr int F = 4;                          // weights of a thread in flight: their pages, then they
+            for (int i0 = lo + static_cast<int>(threadIdx.x); i0 < hi; i0 += F * THREADS) {
+                int p[F], t[F];
+                float w[F];
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    const int i = min(i0 + f * THREADS, hi - 1), at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(i)));
+                    p[f] = pages[at];
+                    t[f] = i - at * page_size;
+                }
+#pragma unroll
+                for (int f = 0; f < F; ++f) w[f] = in_pool(p[f]) ? g.weights[small_at(p[f], t[f])] : __uint_as_float(0x7FC00000u);
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    const int i = i0 + f * THREADS;
+                    if (i >= hi) break;
+                    if (!in_pool(p[f])) set_status(g.status, SISO_ERR_INVALID_ARG);
+                    const uint32_t x = order_of(w[f]);
                     if (i - lo < g.keys) keys[i - lo] = x;
-                } else x = key(i);
-                if (pass == 0 || (x >> (shift + 8)) == least >> (shift + 8)) atomicAdd(&h[(x >> shift) & 255u], 1u);
-            }
-            cluster_sync();
-            if (warp < 8) {
-                uint32_t all = 0u;
-                for (uint32_t c = 0; c < n_ctas; ++c) all += remote(&h[threadIdx.x], c);
-                hist[(pass & 1) ^ 1][threadIdx.x] = all;      // (the other set is free: all have read it before this barrier; it is cleared below)
-            }
-            __syncthreads();
-            if (warp == 0) {              // from the top: the digit in which the wanted-th lies
-                const uint32_t *sum = hist[(pass & 1) ^ 1];
-                uint32_t mine[8], total = 0u;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { mine[i] = sum[255 - (lane * 8 + i)]; total += mine[i]; }
-                uint32_t upto = total;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-                    if (lane >= o) upto += y;
+                    atomicAdd(&hist[0][x >> 24], 1u);
                 }
-                uint32_t before = upto - total;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (before < static_cast<uint32_t>(ties) && before + mine[i] >= static_cast<uint32_t>(ties)) {
-                        chosen[0] = static_cast<uint32_t>(255 - (lane * 8 + i));
-                        chosen[1] = before;
+            }
+            for (int pass = 0;; ++pass) {
+                const int shift = 24 - 8 * pass;
+                together();
+                const uint32_t *h = hist[pass];
+                if (n_ctas > 1) {
+                    uint32_t *sum = sums[pass & 1];
+                    if (threadIdx.x < 256) {
+                        uint32_t all = 0u;
+                        for (uint32_t c = 0; c < n_ctas; ++c) all += remote(&hist[pass][threadIdx.x], c);
+                        sum[threadIdx.x] = all;
                     }
-                    before += mine[i];
+                    __syncthreads();
+                    h = sum;
+                }
+                const uint3 d = find_digit(h, static_cast<uint32_t>(ties), lane);
+                least |= d.x << shift;
+                ties -= static_cast<int>(d.y);
+                if (shift == 0) break;
+                if (static_cast<uint32_t>(ties) == d.z) {            // all of this digit stay: what is larger than the number before its first
+                    least -= 1u;
+                    ties = 0;
+                    break;
+                }
+                uint32_t *below = hist[pass + 1];
+                for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += THREADS) {
+                    const uint32_t x = key(i);
+                    if (x >> shift == least >> shift) atomicAdd(&below[(x >> (shift - 8)) & 255u], 1u);
                 }
             }
-            __syncthreads();
-            least |= chosen[0] << shift;
-            ties -= static_cast<int>(chosen[1]);
-            if (threadIdx.x < 256) hist[(pass & 1) ^ 1][threadIdx.x] = 0u;
-            __syncthreads();
         }
         // how many of each warp's places are heavier, and as heavy
         const int warp_each = each / WARPS, w_lo = min(hi, lo + warp * warp_each), w_hi = min(hi, w_lo + warp_each);
@@ -272,9 +305,11 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
             gt_before += warp_gt[w];
             eq_before += warp_eq[w];
         }
-        if (threadIdx.x == 0) { counts[0] = gt_before; counts[1] = eq_before; }
-        cluster_sync();
-        for (uint32_t c = 0; c < rank; ++c) { gt += remote(&counts[0], c); eq += remote(&counts[1], c); }
+        if (n_ctas > 1) {
+            if (threadIdx.x == 0) { counts[0] = gt_before; counts[1] = eq_before; }
+            cluster_sync();
+            for (uint32_t c = 0; c < rank; ++c) { gt += remote(&counts[0], c); eq += remote(&counts[1], c); }
+        }
         // their places in the list, in order
         if (wanted > 0)
             for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
@@ -289,64 +324,67 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
                 eq += __popc(is_eq);
             }
     }
+    // whether any row may be written to a place that another row is read from
+    bool same_page = false;
+    for (int i = threadIdx.x; i < g.out_max_pages && static_cast<long long>(i) * page_size < n_kept; i += THREADS)
+        same_page = same_page || (i < g.max_pages && out_pages[i] == pages[i]);
+    const bool in_place = __syncthreads_or(same_page) != 0;
     __threadfence();
-    cluster_sync();
+    together();
 
-    // ---- the rows move
+    // ---- the rows move, `wave` tokens at a time
     // tokens that the CTA takes side by side: no more than leave it a thread for the small things of each of U times as many
-    const int per_token = 2 * g.p.pieces, tokens_step = min(THREADS / per_token, THREADS / U);
+    const int per_token = 2 * g.p.pieces, tokens_step = min(THREADS / per_token, THREADS / U), cta_wave = tokens_step * U;
     const int off = static_cast<int>(threadIdx.x) / per_token, item = static_cast<int>(threadIdx.x) - off * per_token;
     const bool is_v = item >= g.p.pieces;
     char *base = (is_v ? g.p.v : g.p.k) + layer * g.p.stride_layer + head * g.p.stride_head + (is_v ? item - g.p.pieces : item) * PIECE;
-    // where place t of the list comes from and goes to: false where nothing is to be moved
-    auto places = [&](int t, int &p0, int &t0, int &p1, int &t1) {
-        const int j = kept[t];
-        if (j < t || j >= len) return false;                                      // (see above)
-        const int i0 = j / page_size, i1 = t / page_size;
-        t0 = j - i0 * page_size;
-        t1 = t - i1 * page_size;
-        p0 = pages[i0];
-        p1 = i1 < g.out_max_pages ? out_pages[i1] : -1;
-        if (!in_pool(p0) || !in_pool(p1)) { set_status(g.status, SISO_ERR_INVALID_ARG); return false; }
-        return p0 != p1 || t0 != t1;
-    };
-    const int wave = tokens_step * U * static_cast<int>(n_ctas);
-    for (int w0 = 0; w0 < n_kept; w0 += wave) {
-        T x[U];
-        long long to[U];
-        const int cta0 = w0 + static_cast<int>(rank) * tokens_step;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int t = cta0 + u * tokens_step * static_cast<int>(n_ctas) + off;
-            int p0, t0, p1, t1;
-            to[u] = -1;
-            if (off < tokens_step && t < n_kept && places(t, p0, t0, p1, t1)) {
-                x[u] = *reinterpret_cast<const T *>(base + p0 * g.p.stride_page + t0 * g.p.stride_token);
-                to[u] = p1 * g.p.stride_page + t1 * g.p.stride_token;
-            }
-        }
-        // the small things of the same tokens: weight and exponents
-        const int u_small = static_cast<int>(threadIdx.x) / tokens_step;
-        const int t_small = cta0 + u_small * tokens_step * static_cast<int>(n_ctas) + static_cast<int>(threadIdx.x) - u_small * tokens_step;
+    for (int w0 = 0; w0 < n_kept; w0 += cta_wave * static_cast<int>(n_ctas)) {
+        // thread i: where the i-th of the CTA's tokens comes from and goes to, and its weight and exponents
+        const int t_mine = w0 + static_cast<int>(rank) * cta_wave + static_cast<int>(threadIdx.x);
         long long small_to = -1;
         float weight = 0.f;
         uint8_t ke = 0, ve = 0;
-        int p0, t0, p1, t1;
-        if (u_small < U && t_small < n_kept && places(t_small, p0, t0, p1, t1)) {
-            const long long from = small_at(p0, t0);
-            small_to = small_at(p1, t1);
-            weight = g.weights[from];
-            if (g.p.k_exp) { ke = g.p.k_exp[from]; ve = g.p.v_exp[from]; }
+        if (static_cast<int>(threadIdx.x) < cta_wave) {
+            int4 m = make_int4(-1, 0, 0, 0);
+            if (t_mine < n_kept) {
+                const int j = kept[t_mine];
+                if (j >= t_mine && j < len) {                                     // (always, unless sequences share pages, see above)
+                    const int i0 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), i1 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(t_mine)));
+                    const int p0 = pages[i0], p1 = i1 < g.out_max_pages ? out_pages[i1] : -1;
+                    if (!in_pool(p0) || !in_pool(p1)) set_status(g.status, SISO_ERR_INVALID_ARG);
+                    else if (p0 != p1 || j - i0 * page_size != t_mine - i1 * page_size) m = make_int4(p0, j - i0 * page_size, p1, t_mine - i1 * page_size);
+                }
+            }
+            moves[threadIdx.x] = m;
+            if (m.x >= 0) {
+                const long long from = small_at(m.x, m.y);
+                small_to = small_at(m.z, m.w);
+                weight = g.weights[from];
+                if (g.p.k_exp) { ke = g.p.k_exp[from]; ve = g.p.v_exp[from]; }
+            }
         }
-        cluster_sync();
+        __syncthreads();
+        T x[U];
+        if (off < tokens_step)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (to[u] >= 0) *reinterpret_cast<T *>(base + to[u]) = x[u];
+            for (int u = 0; u < U; ++u) {
+                const int4 m = moves[u * tokens_step + off];
+                if (m.x >= 0) x[u] = *reinterpret_cast<const T *>(base + m.x * g.p.stride_page + m.y * g.p.stride_token);
+            }
+        if (in_place) together();
+        if (off < tokens_step)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int4 m = moves[u * tokens_step + off];
+                if (m.x >= 0) *reinterpret_cast<T *>(base + m.z * g.p.stride_page + m.w * g.p.stride_token) = x[u];
+            }
         if (small_to >= 0) {
             g.weights[small_to] = weight;
             if (g.p.k_exp) { g.p.k_exp[small_to] = ke; g.p.v_exp[small_to] = ve; }
         }
+        __syncthreads();                          // (`moves` is read until here)
     }
+    if (n_ctas > 1) cluster_sync();               // (no CTA leaves while another reads its shared memory)
 }
 
 template <int PIECE> static siso_status_t run_evict(Kv *h, const EvictArgs &g0, int max_cand, cudaStream_t s) {
@@ -446,6 +484,7 @@ extern "C" siso_status_t siso_kv_evict(siso_kv_t *h, float *d_weights, const int
     g.n_seqs = n_seqs;
     g.budget = budget;
     g.recent = recent;
+    g.by_page.set(static_cast<uint32_t>(h->cfg.page_size));
     g.status = h->status;
     const int max_cand = static_cast<int>(std::max<int64_t>(1, cap - recent));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
