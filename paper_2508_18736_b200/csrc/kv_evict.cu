@@ -139,7 +139,12 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
 // shared memory (as far as they fit), and the smallest weight that stays is found eight bits at a time from counts that the CTAs exchange.
 // The places that stay are listed in order (d_kept, an output anyway), then the rows are moved in waves: all CTAs read a wave's rows into
 // registers, meet, and write them, which is safe in place because of the order (see above).
-constexpr int THREADS = 512, WARPS = THREADS / 32, U = 8, KEYS = 40 * 1024;      // KEYS: weights that a CTA keeps in shared memory
+constexpr int THREADS = 512, WARPS = THREADS / 32, U = 8;        // U: pieces of a thread in flight
+constexpr int R = 16, KEYS = 40 * 1024;           // weights that a thread keeps in registers; that a CTA keeps in shared memory
+// Which places stay is found out by each CTA of the cluster from all weights (up to 8192), so that none waits for another's counts (24 sequences of up to 4200 tokens: 31 us
+// and 37 us); or the CTAs share the weights, in registers (16,385 tokens: 31 us and 35 us) or in shared memory
+enum Mode { ALONE, SHARED_REGS, SHARED };
+constexpr int SLOTS = 1024;                       // rows of a CTA whose places are worked out at a time
 
 struct EvictArgs {
     Pages p;
@@ -156,42 +161,49 @@ __device__ __forceinline__ uint32_t order_of(float w) {
     const uint32_t x = __float_as_uint(w + 0.f);
     return w != w ? 0u : (x & 0x80000000u) ? ~x : x | 0x80000000u;
 }
-template <typename T> __device__ __forceinline__ T remote(const T *p, uint32_t rank) {
-    uint32_t there, x;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(there) : "memory");
-    return static_cast<T>(x);
+// The same word of shared memory in CTA `rank` of the cluster: added to, written
+__device__ __forceinline__ uint32_t address_in(const uint32_t *p, uint32_t rank) {
+    return umma2::cluster_addr(static_cast<uint32_t>(__cvta_generic_to_shared(p)), rank);
 }
-
+__device__ __forceinline__ void add_in(uint32_t *p, uint32_t rank, uint32_t x) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(address_in(p, rank)), "r"(x) : "memory");
+}
+__device__ __forceinline__ void put_in(uint32_t *p, uint32_t rank, uint32_t x) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(address_in(p, rank)), "r"(x) : "memory");
+}
+// counts of a digit lie so that a lane's eight neighbouring digits are in its own bank
+__device__ __forceinline__ int place_of(uint32_t digit) { return static_cast<int>((digit & 7u) * 32u + (digit >> 3)); }
 // From the top digit down, where the wanted-th number lies: (digit, how many are in larger ones, how many in it).  For every warp by itself
 __device__ __forceinline__ uint3 find_digit(const uint32_t *counts, uint32_t wanted, int lane) {
     uint32_t mine[8], total = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { mine[i] = counts[255 - (lane * 8 + i)]; total += mine[i]; }
+    for (int i = 0; i < 8; ++i) { mine[i] = counts[(7 - i) * 32 + 31 - lane]; total += mine[i]; }
     uint32_t upto = total;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
         if (lane >= o) upto += y;
     }
+    const int from = max(__ffs(__ballot_sync(0xFFFFFFFFu, upto >= wanted)) - 1, 0);
     uint32_t before = upto - total, digit = 0u, larger = 0u, here = 0u;
-    bool found = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if (before < wanted && before + mine[i] >= wanted) { digit = 255u - (lane * 8 + i); larger = before; here = mine[i]; found = true; }
+        if (before < wanted) { digit = 255u - (lane * 8 + i); larger = before; here = mine[i]; }
         before += mine[i];
     }
-    const int from = max(__ffs(__ballot_sync(0xFFFFFFFFu, found)) - 1, 0);
     return make_uint3(__shfl_sync(0xFFFFFFFFu, digit, from), __shfl_sync(0xFFFFFFFFu, larger, from), __shfl_sync(0xFFFFFFFFu, here, from));
 }
 
-template <int PIECE>
+template <int PIECE, int MODE>
 __global__ void __launch_bounds__(THREADS, 2)
 evict_kernel(const __grid_constant__ EvictArgs g) {
     using T = typename Bytes<PIECE>::T;
+    constexpr bool BY_ITSELF = MODE == ALONE, REGS = MODE != SHARED;
     extern __shared__ uint32_t keys[];
-    __shared__ uint32_t hist[4][256], sums[2][256], counts[2], warp_gt[WARPS], warp_eq[WARPS];
-    __shared__ int4 moves[THREADS];               // page and token that a row comes from, that it goes to; page -1: it is not moved
+    uint16_t *list = reinterpret_cast<uint16_t *>(keys);          // BY_ITSELF: the places that stay
+    __shared__ uint32_t hist[4][256], sums[BY_ITSELF ? 1 : 4][256];   // counts of this CTA, of all
+    __shared__ uint32_t counts[2][8], warp_gt[WARPS], warp_eq[WARPS];
+    __shared__ int4 moves[SLOTS];                 // page and token that a row comes from, that it goes to; page -1: it is not moved
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t rank, n_ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -201,12 +213,12 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
     const int b = static_cast<int>(seg / g.p.n_kv_heads % g.n_seqs), layer = static_cast<int>(seg / g.p.n_kv_heads / g.n_seqs);
     const int page_size = g.p.page_size;
     const int32_t *pages = g.pages + b * g.pages_stride, *out_pages = g.out_pages + b * g.out_stride;
-    const long long first_page = static_cast<long long>(layer) * g.p.n_pages;
     const int len = static_cast<int>(min(static_cast<long long>(max(g.kv_len[b], 0)), static_cast<long long>(g.max_pages) * page_size));
     const int n_kept = min(len, g.budget);
     int32_t *kept = g.kept + static_cast<long long>(seg) * g.budget;
+    // of weights and exponents: row (page, token) of this layer and head
+    const long long small0 = (static_cast<long long>(layer) * g.p.n_pages * g.p.n_kv_heads + head) * page_size, small_page = static_cast<long long>(g.p.n_kv_heads) * page_size;
     auto in_pool = [&](int p) { return p >= 0 && p < g.p.n_pages; };
-    auto small_at = [&](int p, int t) { return ((first_page + p) * g.p.n_kv_heads + head) * page_size + t; };       // of weights and exponents
     auto together = [&]() {
         if (n_ctas > 1) cluster_sync();
         else __syncthreads();
@@ -215,191 +227,216 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
     if (layer == 0 && head == 0 && rank == 0 && threadIdx.x == 0) g.new_len[b] = n_kept;
     const int step = static_cast<int>(n_ctas) * THREADS, me = static_cast<int>(rank) * THREADS + threadIdx.x;
     for (int t = n_kept + me; t < g.budget; t += step) kept[t] = -1;
-    if (len <= g.budget) {
-        for (int t = me; t < n_kept; t += step) kept[t] = t;
-    } else {
-        const int cand = len - g.recent, wanted = g.budget - g.recent;         // (cand > wanted)
-        for (int i = me; i < g.recent; i += step) kept[wanted + i] = cand + i;
-        const int each = ((cand + static_cast<int>(n_ctas) - 1) / static_cast<int>(n_ctas) + WARPS * 32 - 1) / (WARPS * 32) * (WARPS * 32);
-        const int lo = static_cast<int>(min(static_cast<long long>(rank) * each, static_cast<long long>(cand))), hi = min(cand, lo + each);
+    const int cand = len - g.recent, wanted = g.budget - g.recent;
+    for (int t = (len <= g.budget ? 0 : wanted) + me; t < n_kept; t += step) kept[t] = len <= g.budget ? t : cand + t - wanted;
+    if constexpr (BY_ITSELF)
+        if (len > g.budget)
+            for (int t = wanted + static_cast<int>(threadIdx.x); t < n_kept; t += THREADS) list[t] = static_cast<uint16_t>(cand + t - wanted);
+    auto place_kept = [&](int t) { return BY_ITSELF ? (len <= g.budget ? t : static_cast<int>(list[t])) : kept[t]; };
+    if (len > g.budget && wanted > 0) {           // (cand > wanted)
+        // each CTA has a part of the places, each warp a part of it
+        const int parts = BY_ITSELF ? WARPS : static_cast<int>(n_ctas) * WARPS, warp_each = ((cand + parts - 1) / parts + 31) & ~31, each = warp_each * WARPS;
+        const int lo = BY_ITSELF ? 0 : static_cast<int>(min(static_cast<long long>(rank) * each, static_cast<long long>(cand))), hi = min(cand, lo + each);
+        const int w_lo = min(hi, lo + warp * warp_each), w_hi = min(hi, w_lo + warp_each);
+        uint32_t mine[REGS ? R : 1];
         auto look_up = [&](int i) {
             const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(i))), p = pages[at];
-            return in_pool(p) ? order_of(g.weights[small_at(p, i - at * page_size)]) : 0u;
+            if (!in_pool(p)) { set_status(g.status, SISO_ERR_INVALID_ARG); return 0u; }
+            return order_of(g.weights[small0 + p * small_page + i - at * page_size]);
         };
-        auto key = [&](int i) { return i - lo < g.keys ? keys[i - lo] : look_up(i); };
-        for (int i = threadIdx.x; i < 4 * 256; i += THREADS) (&hist[0][0])[i] = 0u;
-        __syncthreads();
+        // f(place, its number, whether there is one) for 32 neighbours at a time, in order
+        auto for_each = [&](auto f) __attribute__((always_inline)) {
+            if constexpr (REGS) {
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+                    if (w_lo + 32 * k < w_hi) f(w_lo + 32 * k + lane, mine[k], w_lo + 32 * k + lane < w_hi);
+            } else {
+                for (int i = w_lo + lane; i - lane < w_hi; i += 32)
+                    f(i, i >= w_hi ? 0u : i - lo < g.keys ? keys[i - lo] : look_up(i), i < w_hi);
+            }
+        };
+        for (int i = threadIdx.x; i < 4 * 256; i += THREADS) {
+            (&hist[0][0])[i] = 0u;
+            if constexpr (!BY_ITSELF) (&sums[0][0])[i] = 0u;
+        }
+        if constexpr (REGS) {                         // all of a thread's weights in flight: their pages, then they
+            // (no branches: a load that hangs on one waits for the one before it)
+            bool bad = false;
+            int p[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) p[k] = pages[g.by_page.div(static_cast<uint32_t>(min(w_lo + 32 * k + lane, cand - 1)))];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const int i = min(w_lo + 32 * k + lane, cand - 1), t = i - static_cast<int>(g.by_page.div(static_cast<uint32_t>(i))) * page_size;
+                mine[k] = __float_as_uint(g.weights[small0 + (in_pool(p[k]) ? p[k] : 0) * small_page + t]);
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                bad = bad || !in_pool(p[k]);
+                mine[k] = in_pool(p[k]) ? order_of(__uint_as_float(mine[k])) : 0u;
+            }
+            if (bad) set_status(g.status, SISO_ERR_INVALID_ARG);
+        } else {
+            for (int i = w_lo + lane; i < w_hi && i - lo < g.keys; i += 32) keys[i - lo] = look_up(i);
+        }
+        if constexpr (BY_ITSELF) __syncthreads();
+        else together();                              // (no CTA adds to another's counts before it has cleared them)
         // the wanted-th largest: `least`, of which `ties` are wanted
         uint32_t least = 0u;
         int ties = wanted;
-        if (wanted > 0) {
-            constexpr int F = 4;                          // weights of a thread in flight: their pages, then they
-            for (int i0 = lo + static_cast<int>(threadIdx.x); i0 < hi; i0 += F * THREADS) {
-                int p[F], t[F];
-                float w[F];
-#pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    const int i = min(i0 + f * THREADS, hi - 1), at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(i)));
-                    p[f] = pages[at];
-                    t[f] = i - at * page_size;
+        for (int pass = 0;; ++pass) {
+            const int shift = 24 - 8 * pass;
+            uint32_t *h = hist[pass];
+            for_each([&](int, uint32_t x, bool there) {
+                if (there && (pass == 0 || x >> (shift + 8) == least >> (shift + 8))) atomicAdd(&h[place_of((x >> shift) & 255u)], 1u);
+            });
+            // each CTA adds its counts to those of all: nothing is read from afar, the barrier sees to the rest
+            __syncthreads();
+            if (!BY_ITSELF && n_ctas > 1) {
+                if (threadIdx.x < 256) {
+                    const uint32_t n = h[threadIdx.x];
+                    if (n)
+                        for (uint32_t c = 0; c < n_ctas; ++c) add_in(&sums[BY_ITSELF ? 0 : pass][threadIdx.x], c, n);
                 }
-#pragma unroll
-                for (int f = 0; f < F; ++f) w[f] = in_pool(p[f]) ? g.weights[small_at(p[f], t[f])] : __uint_as_float(0x7FC00000u);
-#pragma unroll
-                for (int f = 0; f < F; ++f) {
-                    const int i = i0 + f * THREADS;
-                    if (i >= hi) break;
-                    if (!in_pool(p[f])) set_status(g.status, SISO_ERR_INVALID_ARG);
-                    const uint32_t x = order_of(w[f]);
-                    if (i - lo < g.keys) keys[i - lo] = x;
-                    atomicAdd(&hist[0][x >> 24], 1u);
-                }
+                cluster_sync();
+                h = sums[BY_ITSELF ? 0 : pass];
             }
-            for (int pass = 0;; ++pass) {
-                const int shift = 24 - 8 * pass;
-                together();
-                const uint32_t *h = hist[pass];
-                if (n_ctas > 1) {
-                    uint32_t *sum = sums[pass & 1];
-                    if (threadIdx.x < 256) {
-                        uint32_t all = 0u;
-                        for (uint32_t c = 0; c < n_ctas; ++c) all += remote(&hist[pass][threadIdx.x], c);
-                        sum[threadIdx.x] = all;
-                    }
-                    __syncthreads();
-                    h = sum;
-                }
-                const uint3 d = find_digit(h, static_cast<uint32_t>(ties), lane);
-                least |= d.x << shift;
-                ties -= static_cast<int>(d.y);
-                if (shift == 0) break;
-                if (static_cast<uint32_t>(ties) == d.z) {            // all of this digit stay: what is larger than the number before its first
-                    least -= 1u;
-                    ties = 0;
-                    break;
-                }
-                uint32_t *below = hist[pass + 1];
-                for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += THREADS) {
-                    const uint32_t x = key(i);
-                    if (x >> shift == least >> shift) atomicAdd(&below[(x >> (shift - 8)) & 255u], 1u);
-                }
+            const uint3 d = find_digit(h, static_cast<uint32_t>(ties), lane);
+            least |= d.x << shift;
+            ties -= static_cast<int>(d.y);
+            if (shift == 0) break;
+            if (static_cast<uint32_t>(ties) == d.z) {            // all of this digit stay: what is larger than the number before its first
+                least -= 1u;
+                ties = 0;
+                break;
             }
         }
-        // how many of each warp's places are heavier, and as heavy
-        const int warp_each = each / WARPS, w_lo = min(hi, lo + warp * warp_each), w_hi = min(hi, w_lo + warp_each);
+        // how many of each warp's places are heavier, and as heavy; how many before them
         uint32_t gt = 0u, eq = 0u;
-        if (wanted > 0) {
-            for (int i = w_lo + lane; i < w_hi; i += 32) {
-                const uint32_t x = key(i);
-                gt += x > least;
-                eq += x == least;
-            }
-            gt = __reduce_add_sync(0xFFFFFFFFu, gt);
-            eq = __reduce_add_sync(0xFFFFFFFFu, eq);
-        }
+        for_each([&](int, uint32_t x, bool there) {
+            gt += __popc(__ballot_sync(0xFFFFFFFFu, there && x > least));
+            eq += __popc(__ballot_sync(0xFFFFFFFFu, there && x == least));
+        });
         if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
         __syncthreads();
-        uint32_t gt_before = 0u, eq_before = 0u;
-        for (int w = 0; w < WARPS; ++w) {
-            if (w == warp) { gt = gt_before; eq = eq_before; }
-            gt_before += warp_gt[w];
-            eq_before += warp_eq[w];
-        }
-        if (n_ctas > 1) {
-            if (threadIdx.x == 0) { counts[0] = gt_before; counts[1] = eq_before; }
+        uint32_t w_gt = lane < WARPS ? warp_gt[lane] : 0u, w_eq = lane < WARPS ? warp_eq[lane] : 0u;
+        gt = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w_gt : 0u);
+        eq = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w_eq : 0u);
+        if (!BY_ITSELF && n_ctas > 1) {
+            w_gt = __reduce_add_sync(0xFFFFFFFFu, w_gt);
+            w_eq = __reduce_add_sync(0xFFFFFFFFu, w_eq);
+            if (threadIdx.x < n_ctas) { put_in(&counts[0][rank], threadIdx.x, w_gt); put_in(&counts[1][rank], threadIdx.x, w_eq); }
             cluster_sync();
-            for (uint32_t c = 0; c < rank; ++c) { gt += remote(&counts[0], c); eq += remote(&counts[1], c); }
+            for (uint32_t c = 0; c < rank; ++c) { gt += counts[0][c]; eq += counts[1][c]; }
         }
         // their places in the list, in order
-        if (wanted > 0)
-            for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
-                const uint32_t x = i0 + lane < w_hi ? key(i0 + lane) : 0u;
-                const bool there = i0 + lane < w_hi, more = there && x > least, same = there && x == least;
-                const uint32_t is_gt = __ballot_sync(0xFFFFFFFFu, more), is_eq = __ballot_sync(0xFFFFFFFFu, same), below = (1u << lane) - 1u;
-                const uint32_t my_gt = gt + __popc(is_gt & below), my_eq = eq + __popc(is_eq & below);
-                // (the bound holds unless weights change meanwhile, as where sequences share pages)
-                const uint32_t to = my_gt + min(my_eq, static_cast<uint32_t>(ties));
-                if ((more || (same && my_eq < static_cast<uint32_t>(ties))) && to < static_cast<uint32_t>(wanted)) kept[to] = i0 + lane;
-                gt += __popc(is_gt);
-                eq += __popc(is_eq);
+        for_each([&](int i, uint32_t x, bool there) {
+            const bool more = there && x > least, same = there && x == least;
+            const uint32_t is_gt = __ballot_sync(0xFFFFFFFFu, more), is_eq = __ballot_sync(0xFFFFFFFFu, same), below = (1u << lane) - 1u;
+            const uint32_t my_gt = gt + __popc(is_gt & below), my_eq = eq + __popc(is_eq & below);
+            // (the bound holds unless weights change meanwhile, as where sequences share pages)
+            const uint32_t to = my_gt + min(my_eq, static_cast<uint32_t>(ties));
+            if ((more || (same && my_eq < static_cast<uint32_t>(ties))) && to < static_cast<uint32_t>(wanted)) {
+                if constexpr (BY_ITSELF) list[to] = static_cast<uint16_t>(i);
+                else kept[to] = i;
             }
+            gt += __popc(is_gt);
+            eq += __popc(is_eq);
+        });
     }
     // whether any row may be written to a place that another row is read from
     bool same_page = false;
     for (int i = threadIdx.x; i < g.out_max_pages && static_cast<long long>(i) * page_size < n_kept; i += THREADS)
         same_page = same_page || (i < g.max_pages && out_pages[i] == pages[i]);
     const bool in_place = __syncthreads_or(same_page) != 0;
-    __threadfence();
-    together();
+    if constexpr (BY_ITSELF) {
+        if (len > g.budget)
+            for (int t = me; t < wanted; t += step) kept[t] = list[t];
+    } else {
+        __threadfence();
+        together();
+    }
 
-    // ---- the rows move, `wave` tokens at a time
-    // tokens that the CTA takes side by side: no more than leave it a thread for the small things of each of U times as many
-    const int per_token = 2 * g.p.pieces, tokens_step = min(THREADS / per_token, THREADS / U), cta_wave = tokens_step * U;
+    // ---- the rows move, in waves of cta_wave tokens of each CTA, the CTAs' one after the other
+    // tokens that the CTA takes side by side: no more than leave it a thread for the places of each of U times as many
+    const int per_token = 2 * g.p.pieces, tokens_step = min(THREADS / per_token, THREADS / U), cta_wave = tokens_step * U, wave = cta_wave * static_cast<int>(n_ctas);
+    const int waves = SLOTS / cta_wave;           // whose places are worked out at a time
     const int off = static_cast<int>(threadIdx.x) / per_token, item = static_cast<int>(threadIdx.x) - off * per_token;
     const bool is_v = item >= g.p.pieces;
     char *base = (is_v ? g.p.v : g.p.k) + layer * g.p.stride_layer + head * g.p.stride_head + (is_v ? item - g.p.pieces : item) * PIECE;
-    for (int w0 = 0; w0 < n_kept; w0 += cta_wave * static_cast<int>(n_ctas)) {
-        // thread i: where the i-th of the CTA's tokens comes from and goes to, and its weight and exponents
-        const int t_mine = w0 + static_cast<int>(rank) * cta_wave + static_cast<int>(threadIdx.x);
-        long long small_to = -1;
-        float weight = 0.f;
-        uint8_t ke = 0, ve = 0;
-        if (static_cast<int>(threadIdx.x) < cta_wave) {
+    for (int w0 = 0; w0 < n_kept; w0 += waves * wave) {
+        // where the CTA's tokens of these waves come from and go to; their weights and exponents, which are written once all CTAs have read theirs
+        long long small_to[SLOTS / THREADS];
+        float weight[SLOTS / THREADS];
+        uint32_t exps[SLOTS / THREADS];
+#pragma unroll
+        for (int x = 0; x < SLOTS / THREADS; ++x) {
+            const int slot = x * THREADS + static_cast<int>(threadIdx.x), nth = slot / cta_wave, t = w0 + nth * wave + static_cast<int>(rank) * cta_wave + slot - nth * cta_wave;
+            small_to[x] = -1;
             int4 m = make_int4(-1, 0, 0, 0);
-            if (t_mine < n_kept) {
-                const int j = kept[t_mine];
-                if (j >= t_mine && j < len) {                                     // (always, unless sequences share pages, see above)
-                    const int i0 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), i1 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(t_mine)));
+            if (nth < waves && t < n_kept) {
+                const int j = place_kept(t);
+                if (j >= t && j < len) {                                          // (always, unless sequences share pages, see above)
+                    const int i0 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j))), i1 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(t)));
                     const int p0 = pages[i0], p1 = i1 < g.out_max_pages ? out_pages[i1] : -1;
                     if (!in_pool(p0) || !in_pool(p1)) set_status(g.status, SISO_ERR_INVALID_ARG);
-                    else if (p0 != p1 || j - i0 * page_size != t_mine - i1 * page_size) m = make_int4(p0, j - i0 * page_size, p1, t_mine - i1 * page_size);
+                    else if (p0 != p1 || j - i0 * page_size != t - i1 * page_size) m = make_int4(p0, j - i0 * page_size, p1, t - i1 * page_size);
                 }
             }
-            moves[threadIdx.x] = m;
+            moves[slot] = m;
             if (m.x >= 0) {
-                const long long from = small_at(m.x, m.y);
-                small_to = small_at(m.z, m.w);
-                weight = g.weights[from];
-                if (g.p.k_exp) { ke = g.p.k_exp[from]; ve = g.p.v_exp[from]; }
+                const long long from = small0 + m.x * small_page + m.y;
+                small_to[x] = small0 + m.z * small_page + m.w;
+                weight[x] = g.weights[from];
+                if (g.p.k_exp) exps[x] = g.p.k_exp[from] | static_cast<uint32_t>(g.p.v_exp[from]) << 8;
             }
         }
         __syncthreads();
-        T x[U];
-        if (off < tokens_step)
+        for (int nth = 0; nth < waves && w0 + nth * wave < n_kept; ++nth) {
+            const int4 *here = moves + nth * cta_wave + off;
+            T x[U];
+            if (off < tokens_step)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int4 m = moves[u * tokens_step + off];
-                if (m.x >= 0) x[u] = *reinterpret_cast<const T *>(base + m.x * g.p.stride_page + m.y * g.p.stride_token);
-            }
-        if (in_place) together();
-        if (off < tokens_step)
+                for (int u = 0; u < U; ++u) {
+                    const int4 m = here[u * tokens_step];
+                    if (m.x >= 0) x[u] = *reinterpret_cast<const T *>(base + m.x * g.p.stride_page + m.y * g.p.stride_token);
+                }
+            if (in_place) together();
+            if (off < tokens_step)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int4 m = moves[u * tokens_step + off];
-                if (m.x >= 0) *reinterpret_cast<T *>(base + m.z * g.p.stride_page + m.w * g.p.stride_token) = x[u];
-            }
-        if (small_to >= 0) {
-            g.weights[small_to] = weight;
-            if (g.p.k_exp) { g.p.k_exp[small_to] = ke; g.p.v_exp[small_to] = ve; }
+                for (int u = 0; u < U; ++u) {
+                    const int4 m = here[u * tokens_step];
+                    if (m.x >= 0) *reinterpret_cast<T *>(base + m.z * g.p.stride_page + m.w * g.p.stride_token) = x[u];
+                }
+            if (nth == 0)
+#pragma unroll
+                for (int y = 0; y < SLOTS / THREADS; ++y)
+                    if (small_to[y] >= 0) {
+                        g.weights[small_to[y]] = weight[y];
+                        if (g.p.k_exp) { g.p.k_exp[small_to[y]] = static_cast<uint8_t>(exps[y]); g.p.v_exp[small_to[y]] = static_cast<uint8_t>(exps[y] >> 8); }
+                    }
         }
         __syncthreads();                          // (`moves` is read until here)
     }
-    if (n_ctas > 1) cluster_sync();               // (no CTA leaves while another reads its shared memory)
 }
 
 template <int PIECE> static siso_status_t run_evict(Kv *h, const EvictArgs &g0, int max_cand, cudaStream_t s) {
     EvictArgs g = g0;
     const long long segs = static_cast<long long>(g.p.n_layers) * g.n_seqs * g.p.n_kv_heads;
-    // as many CTAs for each as keep the SMs busy, and as the list and its rows give work for
+    const bool alone = max_cand <= THREADS * R && max_cand + g.recent <= 65536;      // (places in 2 bytes)
+    // as many CTAs for each as run at once (two per SM), or, where they share the weights, up to twice that
+    const long long room = 2ll * h->sm_count;
     int ctas = 1;
-    while (ctas < 8 && segs * ctas < 2ll * h->sm_count) ctas *= 2;
+    while (ctas < 8 && (segs * ctas * 2 <= (alone ? room : 2 * room) || (!alone && max_cand > ctas * THREADS * R))) ctas *= 2;
     if (segs * ctas >= (1ll << 31)) return SISO_ERR_UNSUPPORTED;
-    const int each = ((max_cand + ctas - 1) / ctas + THREADS - 1) / THREADS * THREADS;
+    const bool regs = max_cand <= ctas * THREADS * R;
+    const int each = ((max_cand + ctas * WARPS - 1) / (ctas * WARPS) + 31) / 32 * 32 * WARPS;
     g.keys = std::min(KEYS, each);
-    const size_t smem = static_cast<size_t>(g.keys) * 4;
-    constexpr uint32_t bit = 1u << 16;
-    if (!(h->attr_set & bit)) {
-        SISO_CUDA(cudaFuncSetAttribute(evict_kernel<PIECE>, cudaFuncAttributeMaxDynamicSharedMemorySize, KEYS * 4));
+    const size_t smem = alone ? (static_cast<size_t>(std::min(g.budget, max_cand + g.recent)) * 2 + 15) / 16 * 16 : regs ? 0 : static_cast<size_t>(g.keys) * 4;
+    auto *kernel = alone ? evict_kernel<PIECE, ALONE> : regs ? evict_kernel<PIECE, SHARED_REGS> : evict_kernel<PIECE, SHARED>;
+    const uint32_t bit = 1u << (alone ? 16 : 17);
+    if ((alone || !regs) && !(h->attr_set & bit)) {
+        SISO_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, alone ? 65536 * 2 : KEYS * 4));
         h->attr_set |= bit;
     }
     cudaLaunchConfig_t cfg = {};
@@ -413,7 +450,7 @@ template <int PIECE> static siso_status_t run_evict(Kv *h, const EvictArgs &g0, 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    SISO_CUDA(cudaLaunchKernelEx(&cfg, evict_kernel<PIECE>, g));
+    SISO_CUDA(cudaLaunchKernelEx(&cfg, kernel, g));
     return SISO_OK;
 }
 
