@@ -471,7 +471,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&ring.empty[stage]);
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-        if (__any_sync(0xFFFFFFFFu, cur.tiles_here() > 1)) {   // (uniform, visibly: the barriers further down cost no registers then)
+        if (__any_sync(0xFFFFFFFFu, cur.tiles_here(g) > 1)) {   // (uniform, visibly: the barriers further down cost no registers then)
             cur.step(g);
             continue;
         }
@@ -573,7 +573,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                     }
                 }
         }
-        if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of<2>(run, done_left, done_b, done_head, done_rt, done_tiles, t_end - 1);
+        if (!whole && !began_before && threadIdx.x == 0) g.records[blockIdx.x] = record_of(2, run, done_left, done_b, done_head, done_rt, done_tiles, t_end - 1);
         if (more) begin_item();
     }
     let_copies_land(gave_up);            // (the producers may have gone before the last wait gave up)
@@ -596,6 +596,7 @@ __global__ void __launch_bounds__(64) wait_timeout_kernel(int *status) {
 // ---- joining the parts ------------------------------------------------------------------------------------------------
 // CTA (x, y): the item that is recorded at CTA x, ROWS of its rows.  The parts lie at place 1 of CTA x and place 0 of the next
 // ones.  8 / ROWS warps share a row: 32 lanes over d, the warps over the parts; sums are taken in the same order every time.
+constexpr int JOIN_ROWS = 4;
 template <int MR, int D>
 __global__ void __launch_bounds__(256)
 join_kernel(const __grid_constant__ Args g) {
@@ -608,7 +609,59 @@ join_kernel(const __grid_constant__ Args g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int q0;
     const int n_q = seq_queries(g, rec.b, q0);
-    {
+    auto finish = [&](int row, float m, float l, const float (&o)[N]) {
+        const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
+        const float inv = inverse_of(l);
+        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
+#pragma unroll
+        for (int x = 0; x < N; ++x) dst[x * 32 + lane] = __float2bfloat16_rn(o[x] * inv);
+        if (g.a.d_lse && lane == 0)
+            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m, l);
+    };
+    if constexpr (WPR == 1) {                     // many rows: a warp has JOIN_ROWS of them at once (296 parts of up to 256 rows: one each 16 us, four XX us)
+        constexpr int F = 2;                      // parts in flight of each
+        const int in_tile0 = (static_cast<int>(blockIdx.y) * 8 + warp) * JOIN_ROWS, row0 = rec.row_tile * MR + in_tile0, rows = n_q * g.group;
+        if (row0 >= rows) return;
+        float m[JOIN_ROWS], l[JOIN_ROWS], o[JOIN_ROWS][N];
+#pragma unroll
+        for (int r = 0; r < JOIN_ROWS; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int x = 0; x < N; ++x) o[r][x] = 0.f;
+        }
+        for (int s = 0; s < rec.n_parts; s += F) {
+            float2 ml[F][JOIN_ROWS];
+            float y[F][JOIN_ROWS][N];
+#pragma unroll
+            for (int f = 0; f < F; ++f)
+#pragma unroll
+                for (int r = 0; r < JOIN_ROWS; ++r) {
+                    const int part = s + f;
+                    ml[f][r] = make_float2(-INFINITY, 0.f);
+                    if (part < rec.n_parts && row0 + r < rows) {
+                        const long long place = part_place(static_cast<int>(blockIdx.x) + part, part > 0) * MR + in_tile0 + r;
+                        ml[f][r] = *reinterpret_cast<const float2 *>(g.part_ml + place * 2);
+#pragma unroll
+                        for (int x = 0; x < N; ++x) y[f][r][x] = g.part_o[place * D + x * 32 + lane];
+                    }
+                }
+#pragma unroll
+            for (int r = 0; r < JOIN_ROWS; ++r)
+#pragma unroll
+                for (int f = 0; f < F; ++f) {
+                    if (ml[f][r].y == 0.f) continue;                     // nothing seen there (a NaN is no zero)
+                    const float m2 = fmaxf(m[r], ml[f][r].x), a = m[r] == -INFINITY ? 0.f : ex2(m[r] - m2), b = ex2(ml[f][r].x - m2);
+                    l[r] = l[r] * a + ml[f][r].y * b;
+                    m[r] = m2;
+#pragma unroll
+                    for (int x = 0; x < N; ++x) o[r][x] = o[r][x] * a + y[f][r][x] * b;
+                }
+        }
+#pragma unroll
+        for (int r = 0; r < JOIN_ROWS; ++r)
+            if (row0 + r < rows) finish(row0 + r, m[r], l[r], o[r]);
+    } else {
         const int base = blockIdx.y * ROWS;
         const int in_tile = base + warp / WPR, part0 = warp % WPR;
         const int row = rec.row_tile * MR + in_tile;
@@ -661,19 +714,12 @@ join_kernel(const __grid_constant__ Args g) {
                 for (int x = 0; x < N; ++x) o[x] = o[x] * a + so[warp + w][x * 32 + lane] * b;
             }
         }
-        if (!real) return;
-        const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
-        const float inv = inverse_of(l);
-        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
-#pragma unroll
-        for (int x = 0; x < N; ++x) dst[x * 32 + lane] = __float2bfloat16_rn(o[x] * inv);
-        if (g.a.d_lse && lane == 0)
-            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m, l);
+        if (real) finish(row, m, l, o);
     }
 }
 
 template <int MR, int D> static siso_status_t run_join(const Args &g, cudaStream_t s) {
-    return launch_early(join_kernel<MR, D>, dim3(static_cast<unsigned>(g.grid), MR >= 64 ? MR / 8 : 8), 256, 0, s, g);
+    return launch_early(join_kernel<MR, D>, dim3(static_cast<unsigned>(g.grid), MR >= 64 ? MR / (8 * JOIN_ROWS) : 8), 256, 0, s, g);
 }
 siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s) {
     switch (mr) {
@@ -745,7 +791,11 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, const uint32
     g.grid = h->sm_count;
     const int dim = h->cfg.head_dim;
     const long long rows = static_cast<long long>(a->max_q) * g.group;      // rows per key/value head of the longest chunk
-    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : TC_ROWS;
+    // A tree of 33 to 64 rows over little cache (by what the page table can hold: no more than 16 units of 128 keys a CTA if each is read twice) goes through the few-rows kernel in two row
+    // tiles: its beginning and end cost less (one sequence of 1025 tokens, 36 rows: 22 us and 35 us with its mask; 24 sequences of 517 to 6211 tokens, 64 rows: 170 us and 90 us)
+    const long long twice = 2ll * a->n_seqs * h->cfg.n_kv_heads * ((static_cast<long long>(a->max_pages) * h->cfg.page_size + 127) / 128);
+    const bool little = mask && rows <= 64 && twice <= 16ll * h->sm_count;
+    const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 || little ? 32 : TC_ROWS;
     const size_t records = pad256(sizeof(Record) * g.grid), ml = pad256(sizeof(float) * 2 * g.grid * mr * 2);
     // sized for the widest kernel, so that a handle that has served one call serves every other without a new block
     const size_t most = records + pad256(sizeof(float) * 2 * g.grid * TC_ROWS * 2) + sizeof(float) * 2 * g.grid * TC_ROWS * static_cast<size_t>(dim);

@@ -100,17 +100,20 @@ __device__ __forceinline__ uint32_t mask_bits(const Args &g, const uint32_t *row
 // Whether the TMA box of token j of a row tile's keys holds tokens that some row may see, and j is not beyond the last.  What lies wholly before
 // the window is not looked up: its pages may have been given back
 __device__ __forceinline__ bool holds_seen(const Args &g, int lo, int hi, int j) { return j < hi && (j | (g.box - 1)) >= lo; }
-// units of one key/value head of sequence b: a key tile counts W, and an item EXTRA more, for its beginning and end
-template <int MR, int TK, int EXTRA, int W> __device__ __forceinline__ long long seq_units(const Args &g, int b) {
+// What a key tile of a row tile counts that has `rows` rows from its first on: W; with HALF half of that where the rows fill no more than half of the tile (the tcgen05 kernel
+// then takes two key tiles at once)
+template <int MR, int W, bool HALF> __device__ __forceinline__ int tile_cost(int rows) { return HALF && rows <= MR / 2 ? W / 2 : W; }
+// units of one key/value head of sequence b: its key tiles, and an item EXTRA more, for its beginning and end
+template <int MR, int TK, int EXTRA, int W, bool HALF> __device__ __forceinline__ long long seq_units(const Args &g, int b) {
     int q0;
     const int n_q = seq_queries(g, b, q0), len = seq_len(g, b);
     long long units = 0;
-    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
+    for (int rt = 0; rt * MR < n_q * g.group; ++rt) units += tile_cost<MR, W, HALF>(n_q * g.group - rt * MR) * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
     return units;
 }
 
 // A place in this CTA's run of units: an item and a key tile of it.
-template <int MR, int TK, int EXTRA, int W> struct Cursor {
+template <int MR, int TK, int EXTRA, int W, bool HALF = false> struct Cursor {
     int b, head, rt, q0, n_q, len, tile;
     int left;                                                  // units from this tile's first to the run's end
     Span s;
@@ -118,6 +121,7 @@ template <int MR, int TK, int EXTRA, int W> struct Cursor {
         n_q = seq_queries(g, b, q0);
         len = seq_len(g, b);
     }
+    __device__ __forceinline__ int cost(const Args &g) const { return tile_cost<MR, W, HALF>(n_q * g.group - rt * MR); }
     __device__ __forceinline__ void load_span(const Args &g) { s = span_of<MR, TK>(g, len, n_q, rt); }
     __device__ __forceinline__ void next_item(const Args &g) {
         tile = 0;
@@ -134,21 +138,25 @@ template <int MR, int TK, int EXTRA, int W> struct Cursor {
     // from the item `rt` of its head, `x` units into it, to the first tile that begins there or later: a tile belongs to the run that
     // its first unit lies in
     __device__ __forceinline__ void enter(const Args &g, int x) {
-        tile = max(x - EXTRA + W - 1, 0) / W;
-        left -= EXTRA + W * tile - x;
+        const int w = cost(g);
+        tile = max(x - EXTRA + w - 1, 0) / w;
+        left -= EXTRA + w * tile - x;
         if (left > 0 && tile == s.tiles) {
             left -= EXTRA;
             if (left > 0) next_item(g);
         }
     }
     // key tiles of this item that belong to the run
-    __device__ __forceinline__ int tiles_here() const { return min(s.tiles - tile, (left + W - 1) / W); }
+    __device__ __forceinline__ int tiles_here(const Args &g) const {
+        const int w = cost(g);
+        return min(s.tiles - tile, (left + w - 1) / w);
+    }
     // the first key that a row of this item sees (worked out again where it is needed: kept, it costs registers)
     __device__ __forceinline__ int lo(const Args &g) const { return g.a.window > 0 && tile == 0 ? first_seen(g, position(len, n_q, g.mask ? 0 : static_cast<int>(g.by_group.div(static_cast<uint32_t>(rt * MR))))) : 0; }
     // n <= tiles_here() tiles further; false: the run is over
     __device__ __forceinline__ bool step(const Args &g, int n = 1) {
+        left -= cost(g) * n;
         tile += n;
-        left -= W * n;
         if (left > 0 && tile == s.tiles) {
             left -= EXTRA;
             if (left > 0) next_item(g);
@@ -186,17 +194,17 @@ struct Run {
 constexpr int FEW_TILES = 16;          // row tiles that one thread goes through alone; the CTA takes more of them together
 
 // units of one head of the sequences b0 .. b0 + THREADS - 1 that the call has, one per thread
-template <int MR, int TK, int EXTRA, int W, int THREADS>
+template <int MR, int TK, int EXTRA, int W, bool HALF, int THREADS>
 __device__ __forceinline__ long long chunk_units(const Args &g, int b0, unsigned long long *buf) {
     const int n = min(g.a.n_seqs - b0, THREADS);
     // a thread per sequence, unless there are a few long ones: then a thread per row tile (six prompts of 4 to 15 row tiles: 108 us and 111 us)
-    if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA, W>(g, b0 + threadIdx.x) : 0;
+    if (MR < TC_ROWS || n > 16 || static_cast<long long>(g.a.max_q) * g.group <= 32 * MR) return static_cast<int>(threadIdx.x) < n ? seq_units<MR, TK, EXTRA, W, HALF>(g, b0 + threadIdx.x) : 0;
     long long mine = 0;
     for (int i = 0; i < n; ++i) {
         int q0;
         const int n_q = seq_queries(g, b0 + i, q0), len = seq_len(g, b0 + i), tiles = (n_q * g.group + MR - 1) / MR;
         unsigned long long x = 0ull, all;
-        for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += W * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
+        for (int rt = threadIdx.x; rt < tiles; rt += THREADS) x += tile_cost<MR, W, HALF>(n_q * g.group - rt * MR) * span_of<MR, TK>(g, len, n_q, rt).tiles + EXTRA;
         cta_scan<THREADS>(x, all, buf);
         if (static_cast<int>(threadIdx.x) == i) mine = static_cast<long long>(all);
     }
@@ -205,8 +213,8 @@ __device__ __forceinline__ long long chunk_units(const Args &g, int b0, unsigned
 // This CTA's run and the cursor at its start; every thread of the CTA gets the same.  False: nothing to do.  The CTA's record
 // is cleared.  `buf`: THREADS / 32 + 3 words of shared memory.  A run is counted in 32 bits: a call of 2^31 units a CTA (more than ten
 // minutes of work) is reported and not done.
-template <int MR, int TK, int EXTRA, int W, int THREADS>
-__device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA, W> &cur, unsigned long long *buf) {
+template <int MR, int TK, int EXTRA, int W, int THREADS, bool HALF = false>
+__device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, EXTRA, W, HALF> &cur, unsigned long long *buf) {
     constexpr int WARPS = THREADS / 32;
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) g.records[cta].valid = 0;
@@ -214,12 +222,22 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     long long per_head = 0;
     run.total = 0;
     for (int c0 = 0; c0 < g.a.n_seqs; c0 += THREADS) {
-        const long long ph = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
+        const long long ph = chunk_units<MR, TK, EXTRA, W, HALF, THREADS>(g, c0, buf);
         const unsigned long long x = static_cast<unsigned long long>(ph) * g.kv.n_kv_heads, s = cta_scan<THREADS>(x, all, buf);
         if (c0 == 0) { mine = x; upto = s; per_head = ph; }
         run.total += static_cast<long long>(all);
     }
-    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + W - 1) / W));      // (so that every run within an item has a tile)
+    // (so that every run within an item has a tile)
+    int most = W;
+    if constexpr (HALF) {
+        bool full = false;
+        for (int b = threadIdx.x; b < g.a.n_seqs; b += THREADS) {
+            int q0;
+            full = full || seq_queries(g, b, q0) * g.group > MR / 2;
+        }
+        most = __any_sync(0xFFFFFFFFu, __syncthreads_or(full) != 0) ? W : W / 2;       // (uniform, visibly)
+    }
+    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + most - 1) / most));
     if (cta >= run.ctas) return false;
     if (run.total / run.ctas >= 0x7FFFFFFFll - EXTRA) {
         set_status(g.status, SISO_ERR_UNSUPPORTED);
@@ -241,7 +259,7 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
-            per_head = chunk_units<MR, TK, EXTRA, W, THREADS>(g, c0, buf);
+            per_head = chunk_units<MR, TK, EXTRA, W, HALF, THREADS>(g, c0, buf);
             mine = static_cast<unsigned long long>(per_head) * g.kv.n_kv_heads;
             upto = base + cta_scan<THREADS>(mine, all, buf);
         }
@@ -259,15 +277,15 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     unsigned long long x = within - static_cast<unsigned long long>(cur.head) * head_units;
     cur.rt = 0;
     if (tiles <= FEW_TILES) {
-        for (cur.load_span(g); x >= static_cast<unsigned long long>(W * cur.s.tiles + EXTRA); cur.load_span(g)) {
-            x -= W * cur.s.tiles + EXTRA;
+        for (cur.load_span(g); x >= static_cast<unsigned long long>(cur.cost(g) * cur.s.tiles + EXTRA); cur.load_span(g)) {
+            x -= cur.cost(g) * cur.s.tiles + EXTRA;
             ++cur.rt;
         }
     } else {
         unsigned long long before = 0ull;
         for (int c0 = 0;; c0 += THREADS) {
             const int rt = c0 + static_cast<int>(threadIdx.x);
-            const unsigned long long n = rt < tiles ? W * span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
+            const unsigned long long n = rt < tiles ? tile_cost<MR, W, HALF>(cur.n_q * g.group - rt * MR) * span_of<MR, TK>(g, cur.len, cur.n_q, rt).tiles + EXTRA : 0;
             const unsigned long long s = before + cta_scan<THREADS>(n, all, buf);
             if (found(x < s && x >= s - n, static_cast<unsigned long long>(rt), s - n, 0ull)) break;
             before += all;
@@ -283,10 +301,9 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
     return static_cast<int>(((u + 1) * ctas - 1) / total);
 }
-// what is noted of an item whose first part ends this CTA's run; tile `tile` of it begins `left` units before the run's end
-template <int W>
-__device__ __forceinline__ Record record_of(const Run &run, int left, int b, int head, int row_tile, int tiles, int tile) {
-    return Record{1, b, head, row_tile, cta_of(run.end - left + W * (tiles - 1 - tile), run.total, run.ctas) - static_cast<int>(blockIdx.x) + 1};
+// what is noted of an item whose first part ends this CTA's run; tile `tile` of it, of `cost` each, begins `left` units before the run's end
+__device__ __forceinline__ Record record_of(int cost, const Run &run, int left, int b, int head, int row_tile, int tiles, int tile) {
+    return Record{1, b, head, row_tile, cta_of(run.end - left + cost * (tiles - 1 - tile), run.total, run.ctas) - static_cast<int>(blockIdx.x) + 1};
 }
 // Where a part goes: a CTA's run has at most one item that began before it (place 0) and one that goes on after it (place 1).
 __device__ __forceinline__ long long part_place(int cta, bool began_before) { return 2ll * cta + (began_before ? 0 : 1); }

@@ -513,7 +513,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         };
         look_up(mine);
         for (bool more = true; more;) {
-            const int n = cur.units_here(), tile_first = cur.tile, j0 = cur.kb * KB + t * TK, j = j0 + key;
+            const int n = __shfl_sync(0xFFFFFFFFu, cur.units_here(), 0), tile_first = cur.tile, j0 = cur.kb * KB + t * TK, j = j0 + key;
             const int n_q = cur.s.n_q, before = cur.s.len - n_q;
             const bool whole = FEW || cur.whole(n), began_before = cur.tile > cur.tile0;
             if (!FEW && !whole && !began_before && threadIdx.x == 0) {
@@ -521,7 +521,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 const long long last = run_end - cur.left + (cur.s.tiles - cur.tile0);
                 g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.kb, kva::cta_of(last, total, ctas) - static_cast<int>(blockIdx.x) + 1};
             }
-            more = cur.step(g);
+            more = __any_sync(0xFFFFFFFFu, cur.step(g));         // (uniform, visibly: barriers and TMEM loads in the loop cost no registers then)
             Key next = mine;
             if (more) look_up(next);
             const float f = EIGHT ? g.scale_log2 * kv_scale(mine.exp) : g.scale_log2;
