@@ -13,6 +13,7 @@
 //   warp 8           issues the products
 //   warp 9           fills the ring of key tiles by TMA, one box per run of tokens in one page
 //   warp 10          fills the ring of query tiles by TMA, and their -lse log2 e beside them
+//   warp 11          brings what else belongs to the keys: their weights so far and where they lie, exponents
 //   warps 12-19      8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
 // Bounds: a step reads every key for a few rows: HBM.  A chunk's 256 x 128 scores take 1024 cycles of tcgen05.mma (d = 128) and 2048 of the SM's 16 exponentials a
 // cycle: the exponentials, of which some are taken on the FMA pipe.
@@ -179,14 +180,21 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
 #endif
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 constexpr int SHIFTS = 8;              // their ring: they are needed until the sums are done, the queries only until the products are
+constexpr int METAS = 4;               // items whose keys' small things are there or on their way
 struct Bars {
-    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8];
+    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8], meta_full[METAS], meta_empty[METAS];
     uint32_t tmem;
     int gave_up;
     union {
         Find find;
         float peer[2][TK];             // a key's sum on its way to the other thread of the key
     };
+};
+// What belongs to an item's keys: where their weights lie (of blocks of 8, -1: nowhere), the weights so far, the exponents
+struct Meta {
+    long long place[KB / 8];
+    float old[KB];
+    uint8_t exp[KB];
 };
 template <int KIND, int D, bool FEW> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
@@ -196,7 +204,7 @@ template <int KIND, int D, bool FEW> struct Shape {
     static constexpr int STAGES = D == 64 ? (EIGHT ? 4 : FEW ? 8 : 6) : (EIGHT ? 3 : 4);
     static constexpr int Q_STAGES = 2;
     static constexpr int RAWS = !EIGHT ? 0 : D == 64 ? 8 : 3;
-    static constexpr int SMEM = STAGES * TILE + Q_STAGES * Q_TILE + RAWS * RAW + SHIFTS * ROWS * 4 + static_cast<int>(sizeof(Bars));
+    static constexpr int SMEM = STAGES * TILE + Q_STAGES * Q_TILE + RAWS * RAW + SHIFTS * ROWS * 4 + METAS * static_cast<int>(sizeof(Meta)) + static_cast<int>(sizeof(Bars));
     static_assert(SMEM <= 232448, "shared memory");
     // registers: what the CTA has at launch, moved to the sums
     static constexpr int AT_LAUNCH = 65536 / THREADS / 8 * 8 > 168 ? 168 : 65536 / THREADS / 8 * 8;
@@ -273,7 +281,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     extern __shared__ __align__(1024) uint8_t smem[];           // all of it: nothing static, so that it begins on a boundary of the swizzle
     uint8_t *tiles = smem, *q_tiles = tiles + S::STAGES * S::TILE, *raws = q_tiles + S::Q_STAGES * S::Q_TILE;
     float *shifts = reinterpret_cast<float *>(raws + S::RAWS * S::RAW);              // -lse log2 e of a query tile's rows
-    Bars &bars = *reinterpret_cast<Bars *>(shifts + SHIFTS * ROWS);
+    Meta *metas = reinterpret_cast<Meta *>(shifts + SHIFTS * ROWS);
+    Bars &bars = *reinterpret_cast<Bars *>(metas + METAS);
 
     if constexpr (!FEW) dependents_may_start();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
@@ -283,6 +292,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         for (int i = 0; i < S::Q_STAGES; ++i) { mbar_init(&bars.q_full[i], 1); mbar_init(&bars.q_empty[i], 1); }
         for (int i = 0; i < SHIFTS; ++i) { mbar_init(&bars.sh_full[i], 1); mbar_init(&bars.sh_empty[i], SUM_WARPS); }
         for (int i = 0; i < S::RAWS; ++i) { mbar_init(&bars.raw_full[i], 1); mbar_init(&bars.raw_empty[i], 8); }
+        for (int i = 0; i < METAS; ++i) { mbar_init(&bars.meta_full[i], 33); mbar_init(&bars.meta_empty[i], SUM_WARPS); }      // 33: the copies, and the places
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -442,6 +452,41 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
 #pragma unroll
                 for (int i = 0; i < ROWS / 32; ++i) shift[i] = ahead_shift[i];
             }
+        } else if (warp == SUM_WARPS + 3) {
+            // ---- the keys' small things: a lane has a block of 8 keys.  Pages are asked for one item ahead
+            const bool old = g.a.decay != 0.f;
+            const float *held = g.a.d_weights + static_cast<long long>(g.a.layer) * g.kv.n_pages * g.kv.n_kv_heads * g.kv.page_size;
+            int slot = 0;
+            uint32_t phase = 0;
+            struct Place { int head, tok, page; } at;
+            auto look_up = [&](Place &p) {
+                const int j = cur.kb * KB + lane * 8, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
+                p.head = cur.head;
+                p.tok = j - i * g.kv.page_size;
+                p.page = j < cur.s.len ? g.a.d_pages[cur.b * g.a.pages_stride + i] : -1;
+            };
+            look_up(at);
+            for (bool more = true; more;) {
+                Place ahead = at;
+                more = cur.step(g);
+                if (more) look_up(ahead);
+                const bool there = at.page >= 0 && at.page < g.kv.n_pages;             // (the warp that loads the keys reports pages outside the pool)
+                const long long place = there ? (static_cast<long long>(at.page) * g.kv.n_kv_heads + at.head) * g.kv.page_size + at.tok : -1;
+                wait_bar(&bars.meta_empty[slot], phase ^ 1u, gave_up, g.status);
+                Meta &m = metas[slot];
+                m.place[lane] = place;
+                if (there && old) {
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(m.old + lane * 8)), "l"(held + place) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(m.old + lane * 8 + 4)), "l"(held + place + 4) : "memory");
+                }
+                if (EIGHT && there) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(m.exp + lane * 8)), "l"(g.kv.k_exp + place) : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(&bars.meta_full[slot])) : "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.meta_full[slot]);
+                if (++slot == METAS) { slot = 0; phase ^= 1u; }
+                at = ahead;
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         } else if (warp == SUM_WARPS) {
             // ---- products.  The whole warp goes through the loop; one lane issues
             const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
@@ -497,21 +542,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         float *held = g.a.d_weights + static_cast<long long>(g.a.layer) * g.kv.n_pages * g.kv.n_kv_heads * g.kv.page_size;
         int sh = 0, buf = 0;
         uint32_t sh_phase = 0, s_phase = 0;
-        // what belongs to this thread's key of an item; asked for one item ahead
-        struct Key { long long at; float old; uint32_t exp; } mine;
-        auto look_up = [&](Key &x) {
-            const int j = cur.kb * KB + t * TK + key, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
-            x.at = -1;
-            x.old = 0.f;
-            x.exp = 127u;
-            if (j >= cur.s.len) return;
-            const int page = g.a.d_pages[cur.b * g.a.pages_stride + i];
-            if (page < 0 || page >= g.kv.n_pages) return;                      // (reported by the warp that loads the keys)
-            x.at = (static_cast<long long>(page) * g.kv.n_kv_heads + cur.head) * g.kv.page_size + j - i * g.kv.page_size;
-            if (EIGHT) x.exp = g.kv.k_exp[x.at];
-            if (half == 0 && j < cur.s.len - cur.s.n_q && g.a.decay != 0.f) x.old = held[x.at];
-        };
-        look_up(mine);
+        int slot = 0;
+        uint32_t meta_phase = 0;
         for (bool more = true; more;) {
             const int n = __shfl_sync(0xFFFFFFFFu, cur.units_here(), 0), tile_first = cur.tile, j0 = cur.kb * KB + t * TK, j = j0 + key;
             const int n_q = cur.s.n_q, before = cur.s.len - n_q;
@@ -521,10 +553,11 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 const long long last = run_end - cur.left + (cur.s.tiles - cur.tile0);
                 g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.kb, kva::cta_of(last, total, ctas) - static_cast<int>(blockIdx.x) + 1};
             }
+            const bool is_old = j < before && g.a.decay != 0.f;
             more = __any_sync(0xFFFFFFFFu, cur.step(g));         // (uniform, visibly: barriers and TMEM loads in the loop cost no registers then)
-            Key next = mine;
-            if (more) look_up(next);
-            const float f = EIGHT ? g.scale_log2 * kv_scale(mine.exp) : g.scale_log2;
+            wait_bar(&bars.meta_full[slot], meta_phase, gave_up, g.status);
+            const Meta &meta = metas[slot];
+            const float f = EIGHT ? g.scale_log2 * kv_scale(meta.exp[t * TK + key]) : g.scale_log2;
             float sum = 0.f;
             for (int u = 0; u < n; ++u) {
                 const int tile = tile_first + u, token0 = (g.chunks == 1 ? tile : tile / g.chunks) * g.tb;
@@ -592,11 +625,14 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
             }
             if (half == 1) {
             } else if (whole) {
-                if (mine.at >= 0) held[mine.at] = g.a.decay * mine.old + sum;
+                const long long place = meta.place[t * (TK / 8) + key / 8];
+                if (place >= 0 && j < before + n_q) held[place + (key & 7)] = (is_old ? g.a.decay * meta.old[t * TK + key] : 0.f) + sum;
             } else {
                 g.part[kva::part_place(blockIdx.x, began_before) * KB + t * TK + key] = sum;
             }
-            mine = next;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.meta_empty[slot]);
+            if (++slot == METAS) { slot = 0; meta_phase ^= 1u; }
         }
     }
 

@@ -68,6 +68,20 @@ template <typename T> __device__ __forceinline__ float value(const T *p) {
 }
 // 38-bit weight; NaN and negative values weigh nothing
 __device__ __forceinline__ unsigned long long weight(float r) { return __float2ull_rz(__saturatef(r) * 274877906944.f); }
+// Sum of such weights of a few entries without 64-bit conversions: an entry times 2^22 is split at its binary point by an addition that rounds down (the whole number
+// then stands in the low bits), what is left times 2^16 is rounded down the same way.  Up to 256 entries
+struct Weights {
+    uint32_t high = 0u, low = 0u, n = 0u;
+    __device__ __forceinline__ void add(float r) {
+        const float y = __saturatef(r) * 4194304.f, t = __fadd_rd(y, 8388608.f), u = __fadd_rd((y - (t - 8388608.f)) * 65536.f, 8388608.f);
+        high += __float_as_uint(t);
+        low += __float_as_uint(u);
+        ++n;
+    }
+    __device__ __forceinline__ unsigned long long sum() const {
+        return (static_cast<unsigned long long>(high - n * 0x4B000000u) << 16) + (low - n * 0x4B000000u);
+    }
+};
 __device__ __forceinline__ float left_of(float r, float s, float q) { return fmaxf(__fsub_rn(r, __fmul_rn(s, q)), 0.f); }
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long x) {
 #pragma unroll
@@ -101,7 +115,7 @@ template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *
 }
 
 template <typename T, bool WIDE>
-__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(THREADS)
+__global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(THREADS, 2)
 verify_tree_kernel(Args g) {
     extern __shared__ __align__(16) float r[];                       // this CTA's part of r, [WARPS * chunk]
     __shared__ unsigned long long sums[2][CHUNKS], scan[WARPS];
@@ -146,28 +160,39 @@ verify_tree_kernel(Args g) {
     // at sums[(passes - 1) & 1] and returns their sum
     auto pass = [&](int at, bool again, bool less, float s, int without) {
         const T *p = target + static_cast<long long>(at) * g.vocab, *q = draft + static_cast<long long>(at) * g.vocab;
-        unsigned long long sum = 0ull;
-        for (int v = lo_v + lane * 8; v < hi_v; v += 256) {
-            float x[8], y[8];
-            const int there = hi_v - v;
-            if (again) {
+        Weights weights;
+        constexpr int F = sizeof(T) == 2 ? 2 : 1;                          // eights of a lane in flight: with the rows in DRAM a trip takes a microsecond
+        for (int v0 = lo_v + lane * 8; v0 < hi_v; v0 += F * 256) {
+            float x[F][8], y[F][8];
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(x + i) = *reinterpret_cast<const float4 *>(mine + v + i);
-            } else load8<T, WIDE>(p + v, there, x);
-            if (less) {
-                load8<T, WIDE>(q + v, there, y);
+            for (int f = 0; f < F; ++f) {
+                const int v = v0 + f * 256, there = hi_v - v;
+                if (there <= 0) continue;
+                if (again) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = left_of(x[i], s, y[i]);
-            }
-            if (without >= v && without < v + 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) if (v + i == without) x[i] = 0.f;
+                    for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(x[f] + i) = *reinterpret_cast<const float4 *>(mine + v + i);
+                } else load8<T, WIDE>(p + v, there, x[f]);
+                if (less) load8<T, WIDE>(q + v, there, y[f]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += weight(x[i]);
+            for (int f = 0; f < F; ++f) {
+                const int v = v0 + f * 256;
+                if (v >= hi_v) continue;
+                if (less) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(mine + v + i) = *reinterpret_cast<const float4 *>(x + i);
+                    for (int i = 0; i < 8; ++i) x[f][i] = left_of(x[f][i], s, y[f][i]);
+                }
+                if (without >= v && without < v + 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (v + i == without) x[f][i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) weights.add(x[f][i]);
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(mine + v + i) = *reinterpret_cast<const float4 *>(x[f] + i);
+            }
         }
+        unsigned long long sum = weights.sum();
         sum = warp_sum(sum);
         if (!started) {
             asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
