@@ -73,7 +73,7 @@ __device__ __forceinline__ unsigned long long weight(float r) { return __float2u
 struct Weights {
     uint32_t high = 0u, low = 0u, n = 0u;
     __device__ __forceinline__ void add(float r) {
-        const float y = __saturatef(r) * 4194304.f, t = __fadd_rd(y, 8388608.f), u = __fadd_rd((y - (t - 8388608.f)) * 65536.f, 8388608.f);
+        const float y = __saturatef(r), t = __fmaf_rd(y, 4194304.f, 8388608.f), u = __fmaf_rd(fmaf(y, 4194304.f, 8388608.f - t), 65536.f, 8388608.f);
         high += __float_as_uint(t);
         low += __float_as_uint(u);
         ++n;
@@ -83,6 +83,13 @@ struct Weights {
     }
 };
 __device__ __forceinline__ float left_of(float r, float s, float q) { return fmaxf(__fsub_rn(r, __fmul_rn(s, q)), 0.f); }
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// The same word of shared memory in CTA `rank` of the cluster is written
+__device__ __forceinline__ void put_in(const float *p, uint32_t rank, float x) {
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(p))), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(x) : "memory");
+}
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long x) {
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
@@ -96,23 +103,27 @@ __device__ __forceinline__ unsigned long long warp_scan(unsigned long long x, in
     }
     return x;
 }
-// 8 consecutive entries as fp32; WIDE: from a 16-byte boundary, all of them there
-template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *p, int there, float (&x)[8]) {
-    if constexpr (WIDE) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+// 8 consecutive entries as they lie in memory; WIDE: from a 16-byte boundary, all of them there
+template <typename T, bool WIDE> struct Eight {
+    static constexpr int N = WIDE && sizeof(T) == 2 ? 4 : 8;
+    uint32_t w[N];
+    __device__ __forceinline__ void load(const T *p, int there) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const uint4 r = reinterpret_cast<const uint4 *>(p)[i / 4];
+                w[i] = r.x; w[i + 1] = r.y; w[i + 2] = r.z; w[i + 3] = r.w;
+            }
         } else {
-            const uint4 r = *reinterpret_cast<const uint4 *>(p);
-            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+            for (int i = 0; i < 8; ++i) w[i] = i < there ? __float_as_uint(value(p + i)) : 0u;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < there ? value(p + i) : 0.f;
     }
-}
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (N == 8) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+};
 
 template <typename T, bool WIDE>
 __global__ void __cluster_dims__(SPLIT, 1, 1) __launch_bounds__(THREADS, 2)
@@ -126,7 +137,6 @@ verify_tree_kernel(Args g) {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     // said here, waited for below: a CTA's shared memory may be written by others only once it is known to have started
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    bool started = false;
     const int b = blockIdx.x / SPLIT;
     const int lo = min(max(g.cu_q[b], 0), g.n_tokens), n_nodes = max(0, min(g.cu_q[b + 1], g.n_tokens) - lo);
     const T *target = static_cast<const T *>(g.target) + static_cast<long long>(lo) * g.vocab;
@@ -136,20 +146,27 @@ verify_tree_kernel(Args g) {
     auto token_of = [&](int i) { return i < NODES ? token[i] : g.tokens[lo + i]; };
     auto in_vocab = [&](int x) { return x >= 0 && x < g.vocab; };
     for (int i = threadIdx.x; i < min(n_nodes, NODES); i += THREADS) {
-        const int up = g.parents[lo + i], x = g.tokens[lo + i];
-        parent[i] = up;
-        token[i] = x;
+        parent[i] = g.parents[lo + i];
+        token[i] = g.tokens[lo + i];
         u_at[i] = g.u_accept[lo + i];
+    }
+    // each CTA fetches p and q of every eighth node and gives them to all: rows are far apart, and what their addresses cost to translate is paid once (32 trees of
+    // 9 to 25 nodes: 31 us and 33 us with every CTA fetching all)
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    for (int i = static_cast<int>(rank) + SPLIT * static_cast<int>(threadIdx.x); i < min(n_nodes, NODES); i += SPLIT * THREADS) {
+        const int up = g.parents[lo + i], x = g.tokens[lo + i];
         float p = 0.f, q = 1.f;
         if (up >= 0 && up < i && in_vocab(x)) {
             const long long at = static_cast<long long>(up) * g.vocab + x;
             p = value(target + at);
             if (draft) q = value(draft + at);
         }
-        p_at[i] = p;
-        q_at[i] = q;
+        for (uint32_t c = 0; c < SPLIT; ++c) {
+            put_in(p_at + i, c, p);
+            put_in(q_at + i, c, q);
+        }
     }
-    __syncthreads();
+    cluster_sync();
 
     const int first = (static_cast<int>(rank) * WARPS + warp) * g.chunk;                 // this warp's chunk
     const int lo_v = min(g.vocab, first), hi_v = min(g.vocab, first + g.chunk);
@@ -161,43 +178,41 @@ verify_tree_kernel(Args g) {
     auto pass = [&](int at, bool again, bool less, float s, int without) {
         const T *p = target + static_cast<long long>(at) * g.vocab, *q = draft + static_cast<long long>(at) * g.vocab;
         Weights weights;
-        constexpr int F = sizeof(T) == 2 ? 2 : 1;                          // eights of a lane in flight: with the rows in DRAM a trip takes a microsecond
+        constexpr int F = WIDE && sizeof(T) == 2 ? 4 : 2;      // eights of a lane in flight: with the rows in DRAM a trip takes over a microsecond
         for (int v0 = lo_v + lane * 8; v0 < hi_v; v0 += F * 256) {
-            float x[F][8], y[F][8];
+            Eight<T, WIDE> x[F], y[F];
 #pragma unroll
             for (int f = 0; f < F; ++f) {
-                const int v = v0 + f * 256, there = hi_v - v;
-                if (there <= 0) continue;
-                if (again) {
-#pragma unroll
-                    for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(x[f] + i) = *reinterpret_cast<const float4 *>(mine + v + i);
-                } else load8<T, WIDE>(p + v, there, x[f]);
-                if (less) load8<T, WIDE>(q + v, there, y[f]);
+                const int v = v0 + f * 256;
+                if (!again && v < hi_v) x[f].load(p + v, hi_v - v);
+                if (less && v < hi_v) y[f].load(q + v, hi_v - v);
             }
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const int v = v0 + f * 256;
                 if (v >= hi_v) continue;
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    if (again) *reinterpret_cast<float4 *>(z + i) = *reinterpret_cast<const float4 *>(mine + v + i);
+                    else { z[i] = x[f].get(i); z[i + 1] = x[f].get(i + 1); z[i + 2] = x[f].get(i + 2); z[i + 3] = x[f].get(i + 3); }
+                }
                 if (less) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[f][i] = left_of(x[f][i], s, y[f][i]);
+                    for (int i = 0; i < 8; ++i) z[i] = left_of(z[i], s, y[f].get(i));
                 }
                 if (without >= v && without < v + 8) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) if (v + i == without) x[f][i] = 0.f;
+                    for (int i = 0; i < 8; ++i) if (v + i == without) z[i] = 0.f;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) weights.add(x[f][i]);
+                for (int i = 0; i < 8; ++i) weights.add(z[i]);
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(mine + v + i) = *reinterpret_cast<const float4 *>(x[f] + i);
+                for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(mine + v + i) = *reinterpret_cast<const float4 *>(z + i);
             }
         }
         unsigned long long sum = weights.sum();
         sum = warp_sum(sum);
-        if (!started) {
-            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-            started = true;
-        }
         unsigned long long *to = sums[passes & 1];
         if (lane < SPLIT) {
             const uint32_t here = static_cast<uint32_t>(__cvta_generic_to_shared(&to[static_cast<int>(rank) * WARPS + warp]));
@@ -206,7 +221,7 @@ verify_tree_kernel(Args g) {
             asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there), "l"(sum) : "memory");
         }
         // (two sets of sums: a CTA writes a set again only after a barrier that all reach once they have read it)
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        cluster_sync();
         unsigned long long all = 0ull;
         for (int c = lane; c < CHUNKS; c += 32) all += to[c];
         ++passes;
@@ -242,7 +257,7 @@ verify_tree_kernel(Args g) {
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(x / (WARPS * g.chunk)));
                 asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(rx) : "r"(there) : "memory");
                 // nobody writes r again before all have read
-                asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+                cluster_sync();
             }
         }
         if (real && __fmul_rn(u, __fmul_rn(s, qx)) < rx) {
@@ -267,8 +282,7 @@ verify_tree_kernel(Args g) {
             if (rx > 0.f) total -= weight(rx);
             if (x >= cta_lo && x < cta_lo + WARPS * g.chunk && threadIdx.x == 0) r[x - cta_lo] = 0.f;
             stale = true;
-            // the entry may be asked for by another CTA, and a CTA's later writes to it by none
-            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (n_nodes > NODES) cluster_sync();       // (another CTA may ask for the entry)
         }
         s = __fmul_rn(__ull2float_rn(total), 3.637978807091713e-12f);          // 2^-38
         __syncthreads();
@@ -278,8 +292,6 @@ verify_tree_kernel(Args g) {
     if (n_nodes > 0) {
         if (!have || stale) total = pass(at, have, false, 0.f, -1);
         if (total == 0ull) total = pass(at, false, false, 0.f, -1);
-    } else if (!started) {
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
     if (rank == 0) {
         int32_t *out = g.out + static_cast<long long>(b) * (g.max_path + 1);

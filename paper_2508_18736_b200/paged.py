@@ -483,18 +483,22 @@ def verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: tor
             raise ValueError("draft must be [n, vocab] of target's type and device")
         if not draft.is_contiguous():
             draft = draft.contiguous()
-    for t, kind, name in ((tokens, i32, "tokens"), (parents, i32, "parents"), (u_accept, f32, "u_accept")):
-        if t.dtype is not kind or t.shape != (n,) or t.get_device() != index:
-            raise ValueError(f"{name} must be a {str(kind)[6:]} [{n}] tensor on {target.device}")
-    seqs = u_sample.numel()
+    if tokens.dtype is not i32 or parents.dtype is not i32 or tokens.dim() != 1 or parents.dim() != 1 or tokens.numel() != n or parents.numel() != n or \
+            tokens.get_device() != index or parents.get_device() != index:
+        raise ValueError(f"tokens and parents must be int32 [{n}] tensors on {target.device}")
+    if u_accept.dtype is not f32 or u_accept.dim() != 1 or u_accept.numel() != n or u_accept.get_device() != index:
+        raise ValueError(f"u_accept must be a float32 [{n}] tensor on {target.device}")
     if u_sample.dtype is not f32 or u_sample.dim() != 1 or u_sample.get_device() != index:
         raise ValueError(f"u_sample must be a float32 [seqs] tensor on {target.device}")
-    if cu_q.dtype is not i32 or cu_q.shape != (seqs + 1,) or cu_q.get_device() != index:
+    seqs = u_sample.numel()
+    if cu_q.dtype is not i32 or cu_q.dim() != 1 or cu_q.numel() != seqs + 1 or cu_q.get_device() != index:
         raise ValueError(f"cu_q must be an int32 [{seqs + 1}] tensor on {target.device}")
     if max_path < 0:
         raise ValueError("max_path must not be negative")
-    target, tokens, parents, cu_q, u_accept, u_sample = (t if t.is_contiguous() else t.contiguous()
-                                                         for t in (target, tokens, parents, cu_q, u_accept, u_sample))
+    if not target.is_contiguous():
+        target = target.contiguous()
+    if not (tokens.is_contiguous() and parents.is_contiguous() and cu_q.is_contiguous() and u_accept.is_contiguous() and u_sample.is_contiguous()):
+        tokens, parents, cu_q, u_accept, u_sample = (t.contiguous() for t in (tokens, parents, cu_q, u_accept, u_sample))
     out, accepted, path = tokens.new_empty((seqs, max_path + 1)), tokens.new_empty((seqs,)), tokens.new_empty((seqs, max_path))
     _call(index, "siso_verify_tree", target.data_ptr(), 0 if draft is None else draft.data_ptr(), _ROW_TYPES[target.dtype], n, seqs, vocab, tokens.data_ptr(),
           parents.data_ptr(), cu_q.data_ptr(), max_path, u_accept.data_ptr(), u_sample.data_ptr(), out.data_ptr(), accepted.data_ptr(), path.data_ptr())
