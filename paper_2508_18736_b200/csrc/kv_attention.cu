@@ -370,6 +370,14 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
                         for (int h = 0; h < 2; ++h) s[i][t][2 * e + h] *= EIGHT ? f * row_scale[t][h] : row_scale[t][h];
                 }
             if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
+                uint32_t see[NT][2];                     // TREE: the rows' bits for these keys
+                if constexpr (TREE) {
+                    const int at = j0 + n0 - (cur.len - cur.n_q);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) see[t][h] = mask_bits(g, mask[t][h], at);
+                }
 #pragma unroll
                 for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -382,9 +390,9 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 if constexpr (TREE) {
-                                    const int node = j - (cur.len - cur.n_q);
-                                    const bool seen = node < 0 ? g.a.window == 0 || j > pos[t][h] - g.a.window : ((mask_word(g, mask[t][h], node >> 5) >> (node & 31)) & 1u) != 0u;
-                                    if (!in || !seen) s[i][t][2 * e + h] = -INFINITY;
+                                    const bool seen = ((see[t][h] >> (16 * i + 8 * e + key_of<RB>(r0))) & 1u) != 0u;
+                                    const bool gone = g.a.window > 0 && j <= pos[t][h] - g.a.window && j < cur.len - cur.n_q;       // (before the window)
+                                    if (!in || !seen || gone) s[i][t][2 * e + h] = -INFINITY;
                                 } else
                                 if (!in || (causal && j > pos[t][h]) || (g.a.window > 0 && j <= pos[t][h] - g.a.window)) s[i][t][2 * e + h] = -INFINITY;
                             }

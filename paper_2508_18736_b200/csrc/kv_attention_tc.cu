@@ -144,6 +144,12 @@ __device__ __forceinline__ float2 ex2_poly(float2 x) {
     y.y = __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23));
     return y;
 }
+// bits first .. last of 32, as far as there are such; every bit of the lowest four as eight
+__device__ __forceinline__ uint32_t bits_between(int first, int last) {
+    const uint32_t from = first <= 0 ? 0xFFFFFFFFu : first > 31 ? 0u : 0xFFFFFFFFu << first;
+    return from & (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : 0xFFFFFFFFu >> (31 - last));
+}
+__device__ __forceinline__ uint32_t bits_of_blocks(uint32_t b) { return ((b & 1u) | (b & 2u) << 7 | (b & 4u) << 14 | (b & 8u) << 21) * 0xFFu; }
 // Lane i of every four has pieces 0 to 3 of row i: afterwards it has piece i of rows 0 to 3
 __device__ __forceinline__ void swap_piece(uint4 &keep, uint4 &give, int mask, bool upper) {      // lanes with `upper` give `keep`'s place away
     const uint4 x = upper ? keep : give;
@@ -575,8 +581,19 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
             m = -INFINITY;
             l = 0.f;
             const int k0 = split ? t : 0, k_step = split ? 2 : 1;
+            uint32_t next_a = 0xFFFFFFFFu, next_b = 0xFFFFFFFFu;         // TREE: the row's bits for its 64 keys of a tile, asked for one tile ahead
+            auto look_at_mask = [&](int k) {
+                const int at = (cur.s.tile0 + cur.tile + k) * TK - before;
+                if (at + TK > 0 && k < n) {
+                    next_a = mask_bits(g, mask, at + half * 64);
+                    next_b = mask_bits(g, mask, at + half * 64 + 32);
+                }
+            };
+            if constexpr (TREE) look_at_mask(k0);
             for (int k = k0; k < n; k += k_step) {
                 const int j0 = (cur.s.tile0 + cur.tile + k) * TK;
+                const uint32_t see_a = next_a, see_b = next_b;
+                if constexpr (TREE) look_at_mask(k + k_step);
                 wait_bar(&bars.s_full[t], tile_phase, gave_up, g.status);
                 tcgen05_fence_after();
                 uint32_t ra[32], rb[32];
@@ -588,14 +605,15 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
                 tmem_ld_fence(ra);
                 tmem_ld_fence(rb);
                 if constexpr (TREE) {
-                    if (cut) {   // as below, with the row's bits for the new tokens
-                        const int at = j0 + half * 64 - before, last = cur.s.hi - 1 - j0 - half * 64;
+                    if (cut) {   // as below, with the row's bits for the new tokens, as one bit a key
+                        const int last = cur.s.hi - 1 - j0 - half * 64;
                         const int first = g.a.window > 0 ? min(max(pos - g.a.window + 1, 0), max(before, 0)) - j0 - half * 64 : 0;
-                        const uint32_t see_a = mask_bits(g, mask, at), see_b = mask_bits(g, mask, at + 32), my_blocks = blocks >> (half * 8);
+                        const uint32_t there = blocks >> (half * 8);
+                        const uint32_t in_a = see_a & bits_between(first, last) & bits_of_blocks(there), in_b = see_b & bits_between(first - 32, last - 32) & bits_of_blocks(there >> 4);
 #pragma unroll
                         for (int x = 0; x < 32; ++x) {
-                            if (x > last || x < first || !((my_blocks >> (x / 8)) & 1u) || !((see_a >> x) & 1u)) ra[x] = 0xFF800000u;
-                            if (32 + x > last || 32 + x < first || !((my_blocks >> (4 + x / 8)) & 1u) || !((see_b >> x) & 1u)) rb[x] = 0xFF800000u;
+                            if (!((in_a >> x) & 1u)) ra[x] = 0xFF800000u;
+                            if (!((in_b >> x) & 1u)) rb[x] = 0xFF800000u;
                         }
                     }
                 } else if (cut) {       // keys that are not seen, or not there, are left out by selection: they may hold anything
