@@ -137,6 +137,7 @@ attention_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant_
     float *merge_ml = merge_o + S::MERGE_O;
     uint8_t *meta = reinterpret_cast<uint8_t *>(merge_ml + WARPS / 2 * 16 * NT);
 
+    if constexpr (TREE) wait_for_earlier();                     // (launched early: its mask is often the kernel before it)
     dependents_may_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
@@ -765,7 +766,8 @@ template <int KIND, int D, int WM, int NT, bool TREE> static siso_status_t run_f
         SISO_CUDA(cudaFuncSetAttribute(attention_few_rows_kernel<KIND, D, WM, NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    attention_few_rows_kernel<KIND, D, WM, NT, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
+    if constexpr (TREE) SISO_TRY(launch_early(attention_few_rows_kernel<KIND, D, WM, NT, TREE>, dim3(static_cast<unsigned>(g.grid)), S::THREADS, S::SMEM, s, g, h->map_k, h->map_v));
+    else attention_few_rows_kernel<KIND, D, WM, NT, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
     SISO_CUDA(cudaGetLastError());
     return launch_join(g, S::MR, D, s);
 }

@@ -176,6 +176,7 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
     Bars &bars = *reinterpret_cast<Bars *>(metas + RAWS * S::RAW_META);
     unsigned long long *buf = bars.buf;
 
+    if constexpr (TREE) wait_for_earlier();                     // (launched early: its mask is often the kernel before it)
     dependents_may_start();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
@@ -721,7 +722,8 @@ template <int KIND, int D, bool TREE> static siso_status_t run_as(Kv *h, Args &g
         SISO_CUDA(cudaFuncSetAttribute(attention_many_rows_kernel<KIND, D, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    attention_many_rows_kernel<KIND, D, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
+    if constexpr (TREE) SISO_TRY(launch_early(attention_many_rows_kernel<KIND, D, TREE>, dim3(static_cast<unsigned>(g.grid)), S::THREADS, S::SMEM, s, g, h->map_k, h->map_v));
+    else attention_many_rows_kernel<KIND, D, TREE><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, h->map_v);
     SISO_CUDA(cudaGetLastError());
     return launch_join(g, TC_ROWS, D, s);
 }

@@ -60,6 +60,8 @@ __global__ void __launch_bounds__(KEEP_THREADS)
 keep_path_kernel(const __grid_constant__ KeepArgs g) {
     using T = typename Bytes<PIECE>::T;
     __shared__ int32_t page[2][KEEP], tok[2][KEEP];           // where a row comes from and goes to; page -1: it stays
+    wait_for_earlier();
+    dependents_may_start();
     const int b = blockIdx.x, layer = blockIdx.y;
     const long long cap = static_cast<long long>(g.max_pages) * g.p.page_size;
     const int len = static_cast<int>(min(static_cast<long long>(max(g.kv_len[b], 0)), cap));
@@ -208,6 +210,8 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
     uint32_t rank, n_ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ctas));
+    wait_for_earlier();
+    dependents_may_start();
     const unsigned seg = blockIdx.x / n_ctas;
     const int head = static_cast<int>(seg % g.p.n_kv_heads);
     const int b = static_cast<int>(seg / g.p.n_kv_heads % g.n_seqs), layer = static_cast<int>(seg / g.p.n_kv_heads / g.n_seqs);
@@ -444,12 +448,14 @@ template <int PIECE> static siso_status_t run_evict(Kv *h, const EvictArgs &g0, 
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = static_cast<unsigned>(ctas);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // (as launch_early)
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     SISO_CUDA(cudaLaunchKernelEx(&cfg, kernel, g));
     return SISO_OK;
 }
@@ -486,10 +492,7 @@ extern "C" siso_status_t siso_kv_keep_path(siso_kv_t *h, const int32_t *d_path, 
     const int z = std::min(64, (g.items + kve::KEEP_THREADS - 1) / kve::KEEP_THREADS);
     const dim3 grid(static_cast<unsigned>(n_seqs), static_cast<unsigned>(g.p.n_layers), static_cast<unsigned>(z));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (piece == 16) kve::keep_path_kernel<16><<<grid, kve::KEEP_THREADS, 0, s>>>(g);
-    else kve::keep_path_kernel<8><<<grid, kve::KEEP_THREADS, 0, s>>>(g);
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    return launch_early(piece == 16 ? kve::keep_path_kernel<16> : kve::keep_path_kernel<8>, grid, kve::KEEP_THREADS, 0, s, g);
 }
 
 extern "C" siso_status_t siso_kv_evict(siso_kv_t *h, float *d_weights, const int32_t *d_kv_len, const int32_t *d_pages, int64_t pages_stride,

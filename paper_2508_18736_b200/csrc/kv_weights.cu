@@ -248,6 +248,11 @@ __device__ __forceinline__ float2 ex2_poly(float2 x) {
     y.y *= __uint_as_float(__float_as_uint(t.y) << 23);
     return y;
 }
+// bits first .. last of 32, as far as there are such
+__device__ __forceinline__ uint32_t bits_between(int first, int last) {
+    const uint32_t from = first <= 0 ? 0xFFFFFFFFu : first > 31 ? 0u : 0xFFFFFFFFu << first;
+    return from & (last >= 31 ? 0xFFFFFFFFu : last < 0 ? 0u : 0xFFFFFFFFu >> (31 - last));
+}
 __device__ __forceinline__ void load_q_box(uint32_t dst, const CUtensorMap *map, int d, int head, int token, uint64_t *bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(d), "r"(head), "r"(token), "r"(smem_u32(bar)) : "memory");
@@ -284,7 +289,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     Meta *metas = reinterpret_cast<Meta *>(shifts + SHIFTS * ROWS);
     Bars &bars = *reinterpret_cast<Bars *>(metas + METAS);
 
-    if constexpr (!FEW) dependents_may_start();
+    wait_for_earlier();
+    dependents_may_start();
     const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);      // (uniform)
     if (threadIdx.x == 0) {
         for (int i = 0; i < 4; ++i) { mbar_init(&bars.s_full[0][0] + i, 1); mbar_init(&bars.s_empty[0][0] + i, SUM_WARPS / 2); }
@@ -569,6 +575,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 uint64_t *const read = &bars.sh_empty[sh];
                 float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 auto weigh = [&](auto some, const uint32_t (&r)[32], int c0) __attribute__((always_inline)) {
+                    const uint32_t in = some.value ? bits_between(first - c0, last - 1 - c0) : 0u;
 #pragma unroll
                     for (int x = 0; x < 32; x += 4) {
                         const float4 d = shift[(c0 + x) / 4];
@@ -579,9 +586,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                             if ((x / 2 + i) * POLY % 16 < POLY) y[i] = ex2_poly(y[i]);
                             else { y[i].x = kva::ex2(y[i].x); y[i].y = kva::ex2(y[i].y); }
                             if constexpr (some.value) {
-                                const int c = c0 + x + 2 * i;
-                                if (c < first || c >= last) y[i].x = 0.f;
-                                if (c + 1 < first || c + 1 >= last) y[i].y = 0.f;
+                                if (!((in >> (x + 2 * i)) & 1u)) y[i].x = 0.f;
+                                if (!((in >> (x + 2 * i + 1)) & 1u)) y[i].y = 0.f;
                             }
                             acc[i] = add2(acc[i], y[i]);
                         }
@@ -673,8 +679,7 @@ template <int KIND, int D, bool FEW> static siso_status_t run_as(Kv *h, const Ar
         SISO_CUDA(cudaFuncSetAttribute(weights_kernel<KIND, D, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    weights_kernel<KIND, D, FEW><<<g.grid, S::THREADS, S::SMEM, s>>>(g, h->map_k, map_q);
-    SISO_CUDA(cudaGetLastError());
+    SISO_TRY(launch_early(weights_kernel<KIND, D, FEW>, dim3(static_cast<unsigned>(g.grid)), S::THREADS, S::SMEM, s, g, h->map_k, map_q));
     return FEW ? SISO_OK : launch_early(weights_join_kernel, dim3(static_cast<unsigned>(g.grid)), KB, 0, s, g);
 }
 template <int KIND, int D> static siso_status_t run(Kv *h, const Args &g, bool few, const CUtensorMap &map_q, cudaStream_t s) {

@@ -166,6 +166,8 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
     float *olds = reinterpret_cast<float *>(places + STAGES * BLOCKS);                // [STAGES][T]
     uint8_t *exps = reinterpret_cast<uint8_t *>(olds + STAGES * T);                   // [STAGES][T]
 
+    wait_for_earlier();
+    dependents_may_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) { mbar_init(&ring.full[i], 33); mbar_init(&ring.empty[i], GW); }      // 33: the bytes, and the lanes' small things
@@ -412,9 +414,7 @@ template <int KIND, int D, int NT> static siso_status_t run(Kv *h, const Args &g
         SISO_CUDA(cudaFuncSetAttribute(weights_few_rows_kernel<KIND, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         h->attr_set |= bit;
     }
-    weights_few_rows_kernel<KIND, D, NT><<<h->sm_count, S::THREADS, S::SMEM, s>>>(g, h->map_k);
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    return launch_early(weights_few_rows_kernel<KIND, D, NT>, dim3(static_cast<unsigned>(h->sm_count)), S::THREADS, S::SMEM, s, g, h->map_k);
 }
 template <int KIND> static siso_status_t run_rows(Kv *h, const Args &g, int rows, cudaStream_t s) {
     if (h->cfg.head_dim == 128) return rows <= 8 ? run<KIND, 128, 1>(h, g, s) : rows <= 16 ? run<KIND, 128, 2>(h, g, s) : run<KIND, 128, 4>(h, g, s);

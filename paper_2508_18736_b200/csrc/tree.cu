@@ -12,7 +12,7 @@
 // A row has to be read only at nodes where a child falls or the walk ends; until then the walk needs p and q at the children's tokens alone,
 // which all CTAs fetch for all nodes at the start.  A cluster of CTAs shares a sequence: each warp owns one contiguous chunk of the vocabulary,
 // r stays in shared memory (fp32) from the first fall at a node on, and the chunk sums go to every CTA through distributed shared memory.
-#include "common.cuh"
+#include "kv.cuh"
 
 namespace siso {
 namespace tree {
@@ -25,6 +25,8 @@ __global__ void __launch_bounds__(MASK_THREADS)
 tree_mask_kernel(const int32_t *__restrict__ parents, const int32_t *__restrict__ cu_q, int n_tokens, int words, uint32_t *__restrict__ mask,
                  int32_t *__restrict__ depth) {
     __shared__ int32_t near[MASK_NODES];
+    wait_for_earlier();
+    dependents_may_start();
     const int lo = min(max(cu_q[blockIdx.x], 0), n_tokens), n = max(0, min(cu_q[blockIdx.x + 1], n_tokens) - lo);
     for (int i = threadIdx.x; i < min(n, MASK_NODES); i += MASK_THREADS) near[i] = parents[lo + i];
     __syncthreads();
@@ -135,6 +137,8 @@ verify_tree_kernel(Args g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t rank;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    wait_for_earlier();
+    dependents_may_start();
     // said here, waited for below: a CTA's shared memory may be written by others only once it is known to have started
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const int b = blockIdx.x / SPLIT;
@@ -346,9 +350,7 @@ template <typename T, bool WIDE> static siso_status_t run(const Args &g, int n_s
     const int smem = WARPS * g.chunk * static_cast<int>(sizeof(float));
     // (asked for at every call: which device the function has it on is not known here)
     if (smem > 24 * 1024) SISO_CUDA(cudaFuncSetAttribute(verify_tree_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    verify_tree_kernel<T, WIDE><<<static_cast<unsigned>(n_seqs) * SPLIT, THREADS, smem, s>>>(g);
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    return launch_early(verify_tree_kernel<T, WIDE>, dim3(static_cast<unsigned>(n_seqs) * SPLIT), THREADS, static_cast<size_t>(smem), s, g);
 }
 
 }  // namespace tree
@@ -362,10 +364,8 @@ extern "C" siso_status_t siso_tree_mask(const int32_t *d_parents, const int32_t 
     if (n_tokens == 0 || n_seqs == 0) return SISO_OK;
     if (!d_parents || !d_cu_q || !d_mask) return SISO_ERR_INVALID_ARG;
     if (n_tokens >= (1ll << 31)) return SISO_ERR_UNSUPPORTED;
-    tree::tree_mask_kernel<<<static_cast<unsigned>(n_seqs), tree::MASK_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
-        d_parents, d_cu_q, static_cast<int>(n_tokens), words, d_mask, d_depth);
-    SISO_CUDA(cudaGetLastError());
-    return SISO_OK;
+    return launch_early(tree::tree_mask_kernel, dim3(static_cast<unsigned>(n_seqs)), tree::MASK_THREADS, 0, static_cast<cudaStream_t>(stream), d_parents, d_cu_q,
+                        static_cast<int>(n_tokens), words, d_mask, d_depth);
 }
 
 extern "C" siso_status_t siso_verify_tree(const void *d_target, const void *d_draft, int32_t dtype, int64_t n_tokens, int32_t n_seqs, int32_t vocab,
