@@ -606,6 +606,9 @@ __global__ void __launch_bounds__(64) wait_timeout_kernel(int *status) {
 // CTA (x, y): the item that is recorded at CTA x, ROWS of its rows.  The parts lie at place 1 of CTA x and place 0 of the next
 // ones.  8 / ROWS warps share a row: 32 lanes over d, the warps over the parts; sums are taken in the same order every time.
 constexpr int JOIN_ROWS = 4;
+template <int N> struct Vec;
+template <> struct Vec<4> { using T = float4; };
+template <> struct Vec<2> { using T = float2; };
 template <int MR, int D>
 __global__ void __launch_bounds__(256)
 join_kernel(const __grid_constant__ Args g) {
@@ -618,16 +621,9 @@ join_kernel(const __grid_constant__ Args g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int q0;
     const int n_q = seq_queries(g, rec.b, q0);
-    auto finish = [&](int row, float m, float l, const float (&o)[N]) {
-        const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
-        const float inv = inverse_of(l);
-        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
-#pragma unroll
-        for (int x = 0; x < N; ++x) dst[x * 32 + lane] = __float2bfloat16_rn(o[x] * inv);
-        if (g.a.d_lse && lane == 0)
-            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m, l);
-    };
-    if constexpr (WPR == 1) {                     // many rows: a warp has JOIN_ROWS of them at once (296 parts of up to 256 rows: one each 16 us, four XX us)
+    if constexpr (WPR == 1) {                     // many rows: a warp has JOIN_ROWS of them at once, a lane N neighbouring values (296 parts of up to 256 rows, caches cold: one row a
+                                                  // warp 16 us, so 14.5 us)
+        using V = typename Vec<N>::T;
         constexpr int F = 2;                      // parts in flight of each
         const int in_tile0 = (static_cast<int>(blockIdx.y) * 8 + warp) * JOIN_ROWS, row0 = rec.row_tile * MR + in_tile0, rows = n_q * g.group;
         if (row0 >= rows) return;
@@ -641,19 +637,18 @@ join_kernel(const __grid_constant__ Args g) {
         }
         for (int s = 0; s < rec.n_parts; s += F) {
             float2 ml[F][JOIN_ROWS];
-            float y[F][JOIN_ROWS][N];
+            V y[F][JOIN_ROWS];
 #pragma unroll
             for (int f = 0; f < F; ++f)
 #pragma unroll
                 for (int r = 0; r < JOIN_ROWS; ++r) {
-                    const int part = s + f;
-                    ml[f][r] = make_float2(-INFINITY, 0.f);
-                    if (part < rec.n_parts && row0 + r < rows) {
-                        const long long place = part_place(static_cast<int>(blockIdx.x) + part, part > 0) * MR + in_tile0 + r;
-                        ml[f][r] = *reinterpret_cast<const float2 *>(g.part_ml + place * 2);
-#pragma unroll
-                        for (int x = 0; x < N; ++x) y[f][r][x] = g.part_o[place * D + x * 32 + lane];
-                    }
+                    // (beyond the last part or row: the first again, counted as nothing)
+                    const bool there = s + f < rec.n_parts && row0 + r < rows;
+                    const int part = there ? s + f : 0;
+                    const long long place = part_place(static_cast<int>(blockIdx.x) + part, part > 0) * MR + in_tile0 + (there ? r : 0);
+                    ml[f][r] = *reinterpret_cast<const float2 *>(g.part_ml + place * 2);
+                    y[f][r] = *reinterpret_cast<const V *>(g.part_o + place * D + lane * N);
+                    if (!there) ml[f][r] = make_float2(-INFINITY, 0.f);
                 }
 #pragma unroll
             for (int r = 0; r < JOIN_ROWS; ++r)
@@ -664,12 +659,19 @@ join_kernel(const __grid_constant__ Args g) {
                     l[r] = l[r] * a + ml[f][r].y * b;
                     m[r] = m2;
 #pragma unroll
-                    for (int x = 0; x < N; ++x) o[r][x] = o[r][x] * a + y[f][r][x] * b;
+                    for (int x = 0; x < N; ++x) o[r][x] = o[r][x] * a + reinterpret_cast<const float *>(&y[f][r])[x] * b;
                 }
         }
 #pragma unroll
-        for (int r = 0; r < JOIN_ROWS; ++r)
-            if (row0 + r < rows) finish(row0 + r, m[r], l[r], o[r]);
+        for (int r = 0; r < JOIN_ROWS; ++r) {
+            if (row0 + r >= rows) continue;
+            const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row0 + r))), head = rec.head * g.group + row0 + r - i * g.group;
+            const float inv = inverse_of(l[r]);
+            uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head + lane * N);
+            if constexpr (N == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(pack(o[r][0] * inv, o[r][1] * inv, false), pack(o[r][2] * inv, o[r][3] * inv, false));
+            else *dst = pack(o[r][0] * inv, o[r][1] * inv, false);
+            if (g.a.d_lse && lane == 0) g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m[r], l[r]);
+        }
     } else {
         const int base = blockIdx.y * ROWS;
         const int in_tile = base + warp / WPR, part0 = warp % WPR;
@@ -723,7 +725,14 @@ join_kernel(const __grid_constant__ Args g) {
                 for (int x = 0; x < N; ++x) o[x] = o[x] * a + so[warp + w][x * 32 + lane] * b;
             }
         }
-        if (real) finish(row, m, l, o);
+        if (!real) return;
+        const int i = static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))), head = rec.head * g.group + row - i * g.group;
+        const float inv = inverse_of(l);
+        __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(g.a.d_out) + static_cast<long long>(q0 + i) * g.a.out_stride_token + head * g.a.out_stride_head;
+#pragma unroll
+        for (int x = 0; x < N; ++x) dst[x * 32 + lane] = __float2bfloat16_rn(o[x] * inv);
+        if (g.a.d_lse && lane == 0)
+            g.a.d_lse[static_cast<long long>(q0 + i) * g.a.n_heads + head] = lse_of(m, l);
     }
 }
 

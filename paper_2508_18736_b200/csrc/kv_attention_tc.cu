@@ -188,14 +188,14 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    // a tree's row tiles are often half empty: they count half (24 trees of 119 to 441 rows: 88 us and 100 us; not over 8 bits, where widening a key tile costs as much
-    // for few rows as for many: four trees of 516 to 1020 rows 540 us and 400 us)
+    // a tree's row tiles are often half empty: they count half (24 trees of 119 to 441 rows: 89 us and 100 us; not over 8 bits, where widening a key tile costs as much
+    // for few rows as for many), and an item's beginning and end three tiles (24 trees of 256 rows: two 117 us, three 113 us, six 117 us)
     constexpr bool HALF = TREE && !EIGHT;
-    constexpr int W = HALF ? 2 : 1;
-    Cursor<TC_ROWS, TK, W * EXTRA, W, HALF> cur;
+    constexpr int W = HALF ? 2 : 1, MORE = HALF ? 3 * W : EXTRA;
+    Cursor<TC_ROWS, TK, MORE, W, HALF> cur;
     {
         Run run;
-        if (!locate<TC_ROWS, TK, W * EXTRA, W, S::THREADS, HALF>(g, run, cur, buf)) return;
+        if (!locate<TC_ROWS, TK, MORE, W, S::THREADS, HALF>(g, run, cur, buf)) return;
         if (threadIdx.x == 0) bars.run = run;
     }
     if (warp == 16) {
