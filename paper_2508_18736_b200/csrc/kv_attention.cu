@@ -816,9 +816,7 @@ siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, const uint32
     const bool little = mask && rows <= 64 && twice <= 16ll * h->sm_count;
     const int mr = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 || little ? 32 : TC_ROWS;
     const size_t records = pad256(sizeof(Record) * g.grid), ml = pad256(sizeof(float) * 2 * g.grid * mr * 2);
-    // sized for the widest kernel, so that a handle that has served one call serves every other without a new block
-    const size_t most = records + pad256(sizeof(float) * 2 * g.grid * TC_ROWS * 2) + sizeof(float) * 2 * g.grid * TC_ROWS * static_cast<size_t>(dim);
-    SISO_TRY(kv_scratch(h, most, s));
+    SISO_TRY(kv_scratch(h, attention_scratch(h), s));
     char *ws = static_cast<char *>(h->ws);
     g.records = reinterpret_cast<Record *>(ws);
     g.part_ml = reinterpret_cast<float *>(ws + records);

@@ -366,6 +366,11 @@ siso_status_t launch_join(const Args &g, int mr, int dim, cudaStream_t s);
 // many rows per key/value head (tcgen05)
 siso_status_t launch_many_rows(Kv *h, Args &g, cudaStream_t s);
 siso_status_t kv_scratch(Kv *h, size_t bytes, cudaStream_t s);
+// what the widest kernel takes, so that a handle that has served one call serves every other without a new block
+inline size_t attention_scratch(const Kv *h) {
+    const size_t grid = static_cast<size_t>(h->sm_count);
+    return pad256(sizeof(Record) * grid) + pad256(sizeof(float) * 2 * grid * TC_ROWS * 2) + sizeof(float) * 2 * grid * TC_ROWS * static_cast<size_t>(h->cfg.head_dim);
+}
 
 }  // namespace kva
 }  // namespace siso

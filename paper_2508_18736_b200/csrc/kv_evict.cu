@@ -51,6 +51,7 @@ struct KeepArgs {
     const int32_t *path, *accepted, *cu_q, *kv_len, *pages;
     long long pages_stride;
     int32_t *new_len;
+    kva::FastDiv by_page, by_pieces;
     int max_path, max_pages, items;              // items: pieces and exponents of one layer and token
     int *status;
 };
@@ -63,10 +64,19 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
     wait_for_earlier();
     dependents_may_start();
     const int b = blockIdx.x, layer = blockIdx.y;
+    const int32_t *path = g.path + static_cast<long long>(b) * g.max_path;
+    // the entries of a block of the path, asked for before it is known how many count
+    int node = 0, earlier = 0;
+    auto look_up = [&](int t) {
+        if (threadIdx.x < KEEP && t < g.max_path) {
+            node = path[t];
+            earlier = t > 0 ? path[t - 1] : 0;
+        }
+    };
+    look_up(threadIdx.x);
     const long long cap = static_cast<long long>(g.max_pages) * g.p.page_size;
     const int len = static_cast<int>(min(static_cast<long long>(max(g.kv_len[b], 0)), cap));
     const int n_q = max(0, g.cu_q[b + 1] - g.cu_q[b]), before = len - n_q;
-    const int32_t *path = g.path + static_cast<long long>(b) * g.max_path;
     const bool first = layer == 0 && blockIdx.z == 0;
     const int wanted = before < 0 ? 0 : min(max(g.accepted[b], 0), g.max_path);
     bool bad = before < 0 && n_q > 0;
@@ -76,12 +86,11 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
         const int t = t0 + threadIdx.x;
         bool fine = true;
         if (threadIdx.x < KEEP && t < wanted) {
-            const int node = path[t], earlier = t > 0 ? path[t - 1] : 0;
-            fine = node > earlier && node < n_q;
+            fine = node > max(earlier, 0) && node < n_q;
             page[0][threadIdx.x] = page[1][threadIdx.x] = -1;
             if (fine && node != t + 1) {
                 const int from = before + node, to = before + 1 + t;
-                const int i0 = from / g.p.page_size, i1 = to / g.p.page_size;
+                const int i0 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(from))), i1 = static_cast<int>(g.by_page.div(static_cast<uint32_t>(to)));
                 const int p0 = g.pages[b * g.pages_stride + i0], p1 = g.pages[b * g.pages_stride + i1];
                 if (p0 >= 0 && p0 < g.p.n_pages && p1 >= 0 && p1 < g.p.n_pages) {
                     page[0][threadIdx.x] = p0;
@@ -104,7 +113,7 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
         for (int item = blockIdx.z * KEEP_THREADS + threadIdx.x; item < g.items; item += gridDim.z * KEEP_THREADS) {
             const int rows = 2 * g.p.n_kv_heads, n_pieces = rows * g.p.pieces;
             if (item < n_pieces) {
-                const int row = item / g.p.pieces, head = row >> 1;
+                const int row = static_cast<int>(g.by_pieces.div(static_cast<uint32_t>(item))), head = row >> 1;
                 char *base = ((row & 1) ? g.p.v : g.p.k) + layer * g.p.stride_layer + head * g.p.stride_head + (item - row * g.p.pieces) * PIECE;
                 for (int t1 = 0; t1 < n; t1 += KEEP_U) {
                     T x[KEEP_U];
@@ -128,6 +137,7 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
             }
         }
         done += n;
+        look_up(t + KEEP);
         __syncthreads();
     }
     if (first && threadIdx.x == 0) {
@@ -240,8 +250,9 @@ evict_kernel(const __grid_constant__ EvictArgs g) {
     if (len > g.budget && wanted > 0) {           // (cand > wanted)
         // each CTA has a part of the places, each warp a part of it
         const int parts = BY_ITSELF ? WARPS : static_cast<int>(n_ctas) * WARPS, warp_each = ((cand + parts - 1) / parts + 31) & ~31, each = warp_each * WARPS;
-        const int lo = BY_ITSELF ? 0 : static_cast<int>(min(static_cast<long long>(rank) * each, static_cast<long long>(cand))), hi = min(cand, lo + each);
-        const int w_lo = min(hi, lo + warp * warp_each), w_hi = min(hi, w_lo + warp_each);
+        const int lo = BY_ITSELF ? 0 : static_cast<int>(min(static_cast<long long>(rank) * each, static_cast<long long>(cand))), hi = static_cast<int>(min(static_cast<long long>(lo) + each, static_cast<long long>(cand)));
+        const int w_lo = static_cast<int>(min(static_cast<long long>(lo) + warp * warp_each, static_cast<long long>(hi))),
+                  w_hi = static_cast<int>(min(static_cast<long long>(w_lo) + warp_each, static_cast<long long>(hi)));
         uint32_t mine[REGS ? R : 1];
         auto look_up = [&](int i) {
             const int at = static_cast<int>(g.by_page.div(static_cast<uint32_t>(i))), p = pages[at];
@@ -487,6 +498,8 @@ extern "C" siso_status_t siso_kv_keep_path(siso_kv_t *h, const int32_t *d_path, 
     g.new_len = d_new_len;
     g.max_path = max_path;
     g.max_pages = max_pages;
+    g.by_page.set(static_cast<uint32_t>(h->cfg.page_size));
+    g.by_pieces.set(static_cast<uint32_t>(g.p.pieces));
     g.items = 2 * g.p.n_kv_heads * (g.p.pieces + (g.p.k_exp ? 1 : 0));
     g.status = h->status;
     const int z = std::min(64, (g.items + kve::KEEP_THREADS - 1) / kve::KEEP_THREADS);

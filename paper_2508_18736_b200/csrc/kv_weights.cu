@@ -172,12 +172,6 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
     return true;
 }
 
-#ifndef MANY_PER_KEY
-#define MANY_PER_KEY 2
-#endif
-#ifndef POLY
-#define POLY (FEW ? 0 : 3)
-#endif
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------
 constexpr int SHIFTS = 8;              // their ring: they are needed until the sums are done, the queries only until the products are
 constexpr int METAS = 4;               // items whose keys' small things are there or on their way
@@ -198,8 +192,10 @@ struct Meta {
 };
 template <int KIND, int D, bool FEW> struct Shape {
     static constexpr bool EIGHT = KIND != SISO_BF16;
-    static constexpr int PER_KEY = FEW ? 1 : MANY_PER_KEY, SUM_WARPS = 8 * PER_KEY;    // threads of a key
+    static constexpr int PER_KEY = FEW ? 1 : 2, SUM_WARPS = 8 * PER_KEY;    // threads of a key
     static constexpr int THREADS = 32 * (SUM_WARPS + 4 + (EIGHT ? 8 : 0));
+    // of 16 pairs of exponentials so many are taken on the FMA pipe (chunk of 4096 queries over 8193 tokens: none 282 us, two 280 us, three 274 us, five 287 us, before other steps)
+    static constexpr int POLY = FEW ? 0 : 3;
     static constexpr int TILE = TK * D * 2, Q_TILE = ROWS * D * 2, RAW = EIGHT ? TK * D : 0;
     static constexpr int STAGES = D == 64 ? (EIGHT ? 4 : FEW ? 8 : 6) : (EIGHT ? 3 : 4);
     static constexpr int Q_STAGES = 2;
@@ -583,7 +579,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                                        fma2(make_float2(__uint_as_float(r[x + 2]), __uint_as_float(r[x + 3])), make_float2(f, f), make_float2(d.z, d.w))};
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            if ((x / 2 + i) * POLY % 16 < POLY) y[i] = ex2_poly(y[i]);
+                            if ((x / 2 + i) * S::POLY % 16 < S::POLY) y[i] = ex2_poly(y[i]);
                             else { y[i].x = kva::ex2(y[i].x); y[i].y = kva::ex2(y[i].y); }
                             if constexpr (some.value) {
                                 if (!((in >> (x + 2 * i)) & 1u)) y[i].x = 0.f;
@@ -721,7 +717,9 @@ siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, cudaStream_t s) 
                                             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return check_cuda(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     const size_t records = pad256(sizeof(Record) * g.grid);
-    SISO_TRY(kva::kv_scratch(h, records + sizeof(float) * 2 * g.grid * KB, s));
+    // (the attention's, which is larger: a block that a captured call uses is never replaced by a later call's)
+    static_assert(sizeof(Record) <= sizeof(kva::Record) && KB <= kva::TC_ROWS, "fits the attention's scratch");
+    SISO_TRY(kva::kv_scratch(h, kva::attention_scratch(h), s));
     g.records = static_cast<Record *>(h->ws);
     g.part = reinterpret_cast<float *>(static_cast<char *>(h->ws) + records);
     const bool wide = dim == 128;

@@ -387,6 +387,28 @@ def test_streams_and_graphs():
     kv.close()
 
 
+def test_a_captured_call_keeps_its_scratch_when_later_calls_need_theirs():
+    k, v, _, _ = ref.make_pages("bf16", 1, 64, 16, 2, 128)
+    kv = siso.PagedKV(k, v)
+    q = torch.randn((300, 8, 128), device="cuda").to(torch.bfloat16)
+    cu, lens, table = i32([0, 300]), i32([1000]), torch.arange(64, **I32)[None]
+    lse = torch.full((300, 8), 5.0, device="cuda")
+    w = kv.new_weights()
+    kv.add_weights(w, q, lse, cu, lens, table, 300, decay=0.0)
+    want, blocks = w.clone(), dict(kv._blocks)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kv.add_weights(w, q, lse, cu, lens, table, 300, decay=0.0)
+    for n in (1, 300):
+        kv.attention(q[:n], i32([0, n]), lens, table, n)
+    assert dict(kv._blocks).keys() == blocks.keys()
+    w.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(w, want)
+    kv.close()
+
+
 def test_empty_calls_and_refusals():
     kv = siso.PagedKV.allocate(1, 4, 16, 2, 128)
     w = kv.new_weights()

@@ -199,6 +199,22 @@ def test_pages_before_the_window_are_not_looked_up_and_bad_ones_are_reported(n):
     kv.close()
 
 
+@pytest.mark.parametrize("n", [4, 20, 90])
+def test_rows_that_no_sequence_covers_and_strided_outputs(n):
+    kv, table, k, v = filled("e4m3", 300, 16, 2, 64)
+    q = torch.randn((n + 5, 8, 64), device="cuda").to(torch.bfloat16)
+    q[:2], q[n + 2:] = math.nan, math.nan
+    cu = i32([2, n + 2])
+    mask, _ = siso.tree_mask(i32([9, 9] + some_tree(n, 1) + [9] * 3), cu, n)
+    wide = torch.full((8, n + 5, 72), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = wide.transpose(0, 1)[:, :, :64]
+    got = kv.tree_attention(q, cu, i32([300]), table, mask, n, out=out)
+    assert got is out and (wide[:, :2] == 7).all() and (wide[:, n + 2:] == 7).all() and (wide[:, :, 64:] == 7).all()
+    o, _, mass, _ = tree.attention(q[2:n + 2], k, v, tree.seen_of(tree.ancestors(some_tree(n, 1))[0], 300, 0))
+    assert ((got[2:n + 2].double() - o).abs() <= 2.0 ** -8 * o.abs() + 1.02 * mass * 2.0 ** -8 + 1e-4 * mass).all()
+    kv.close()
+
+
 # ---- verification ----------------------------------------------------------------------------------------------------------
 def drafted(sizes, vocab, dtype, probs, seed, kinds=("random", "chain", "star")):
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -341,7 +357,7 @@ def test_paths_that_do_not_ascend_end_and_are_reported():
     kv = siso.PagedKV(k, v)
     table, cu, lens = torch.arange(8, **I32).view(2, 4), i32([0, 20, 40]), i32([40, 50])
     for path, accepted, want in (([[3, 2, 5], [1, 2, 3]], [3, 3], [22, 34]), ([[3, 20, 5], [1, 1, 3]], [3, 2], [22, 32]), ([[0, 2, 5], [-1, 2, 3]], [3, 1], [21, 31]),
-                                 ([[3, 5, 0], [4, 2 ** 31 - 1, 3]], [3, 2], [23, 32])):
+                                 ([[3, 5, 0], [4, 2 ** 31 - 1, 3]], [3, 2], [23, 32]), ([[-2 ** 31, -2 ** 31 + 1, -5], [-9, -8, 1]], [3, 3], [21, 31])):
         assert kv.keep_path(i32(path), i32(accepted), cu, lens, table).tolist() == want and kv.sync_status() == 1
     assert kv.keep_path(i32([[2, 3, 4], [1, 2, 3]]), i32([-4, 99]), cu, lens, table).tolist() == [21, 34] and kv.sync_status() == 0
     bad = table.clone()
