@@ -186,6 +186,11 @@ __device__ __forceinline__ unsigned long long cta_scan(unsigned long long x, uns
     return before + x;
 }
 
+// a / b.  64-bit divisions take hundreds of cycles, of which a short call's CTAs notice every one
+__device__ __forceinline__ unsigned long long quotient(unsigned long long a, unsigned long long b) {
+    return ((a | b) >> 32) == 0ull ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
+}
+
 // The run of this CTA among the call's units: it ends before unit `end` of `total`, which `ctas` CTAs share.
 struct Run {
     long long end, total;
@@ -239,12 +244,12 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     }
     run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + most - 1) / most));
     if (cta >= run.ctas) return false;
-    if (run.total / run.ctas >= 0x7FFFFFFFll - EXTRA) {
+    if (run.total >= (0x7FFFFFFFll - EXTRA) * run.ctas) {
         set_status(g.status, SISO_ERR_UNSUPPORTED);
         return false;
     }
-    const unsigned long long want = static_cast<unsigned long long>(run.total * cta / run.ctas);
-    run.end = run.total * (cta + 1) / run.ctas;
+    const unsigned long long want = quotient(static_cast<unsigned long long>(run.total) * cta, run.ctas);
+    run.end = static_cast<long long>(quotient(static_cast<unsigned long long>(run.total) * (cta + 1), run.ctas));
     cur.left = static_cast<int>(run.end - static_cast<long long>(want));
     // buf[WARPS] and the two after it: what the one thread that finds it says
     auto found = [&](bool here, unsigned long long a, unsigned long long b, unsigned long long c) {
@@ -273,7 +278,7 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
     cur.load_seq(g);
     const unsigned long long within = want - buf[WARPS + 1], head_units = buf[WARPS + 2];
     const int tiles = (cur.n_q * g.group + MR - 1) / MR;
-    cur.head = static_cast<int>(within / head_units);
+    cur.head = static_cast<int>(quotient(within, head_units));
     unsigned long long x = within - static_cast<unsigned long long>(cur.head) * head_units;
     cur.rt = 0;
     if (tiles <= FEW_TILES) {
@@ -299,7 +304,7 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
 }
 // the CTA that unit u is dealt to: the last c with floor(total c / ctas) <= u
 __device__ __forceinline__ int cta_of(long long u, long long total, int ctas) {
-    return static_cast<int>(((u + 1) * ctas - 1) / total);
+    return static_cast<int>(quotient(static_cast<unsigned long long>((u + 1) * ctas - 1), static_cast<unsigned long long>(total)));
 }
 // what is noted of an item whose first part ends this CTA's run; tile `tile` of it, of `cost` each, begins `left` units before the run's end
 __device__ __forceinline__ Record record_of(int cost, const Run &run, int left, int b, int head, int row_tile, int tiles, int tile) {

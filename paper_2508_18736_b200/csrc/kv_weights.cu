@@ -130,8 +130,8 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
     }
     ctas = static_cast<int>(min(static_cast<long long>(g.grid), (total + 1) / 2));
     if (static_cast<int>(blockIdx.x) >= ctas) return false;
-    const unsigned long long want = static_cast<unsigned long long>(total / ctas * blockIdx.x + total % ctas * blockIdx.x / ctas);
-    end = total / ctas * (blockIdx.x + 1) + total % ctas * (blockIdx.x + 1) / ctas;
+    const unsigned long long want = kva::quotient(static_cast<unsigned long long>(total) * blockIdx.x, ctas);
+    end = static_cast<long long>(kva::quotient(static_cast<unsigned long long>(total) * (blockIdx.x + 1), ctas));
     unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
         if (c0 > 0) {
@@ -153,10 +153,10 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
     cur.b = static_cast<int>(f.found[0]);
     cur.s.load(g, cur.b);
     const unsigned long long within = want - f.found[1];
-    cur.head = static_cast<int>(within / f.found[2]);
+    cur.head = static_cast<int>(kva::quotient(within, f.found[2]));
     long long x = static_cast<long long>(within - static_cast<unsigned long long>(cur.head) * f.found[2]);
     const int full_cost = cur.s.tiles + 1;
-    cur.kb = static_cast<int>(min(x / full_cost, static_cast<long long>(cur.s.full)));
+    cur.kb = static_cast<int>(min(static_cast<long long>(kva::quotient(static_cast<unsigned long long>(x), full_cost)), static_cast<long long>(cur.s.full)));
     x -= static_cast<long long>(cur.kb) * full_cost;
     while (cur.kb >= cur.s.full && x >= cur.s.cost(g, cur.kb)) x -= cur.s.cost(g, cur.kb++);
     cur.tile0 = cur.s.first_tile(g, cur.kb);
@@ -310,10 +310,13 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
     Cursor<FEW> cur;
     long long run_end, total;
     int ctas;
-    if (!locate<FEW, S::THREADS>(g, cur, run_end, total, ctas, bars.find)) return;
-    if (warp == SUM_WARPS) {
+    if (warp == SUM_WARPS) {                       // (while the others look for their run)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (!locate<FEW, S::THREADS>(g, cur, run_end, total, ctas, bars.find)) {
+        if (warp == SUM_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*const_cast<volatile uint32_t *>(&bars.tmem)), "r"(512u) : "memory");
+        return;
     }
     tcgen05_fence_before();
     __syncthreads();

@@ -100,8 +100,8 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<T> &cur, unsigned l
         if (c0 == 0) { mine = x; upto = to; }
         total += all;
     }
-    const unsigned long long n = gridDim.x, want = total / n * blockIdx.x + total % n * blockIdx.x / n;
-    cur.left = static_cast<long long>(total / n * (blockIdx.x + 1) + total % n * (blockIdx.x + 1) / n - want);
+    const unsigned long long n = gridDim.x, want = kva::quotient(total * blockIdx.x, n);
+    cur.left = static_cast<long long>(kva::quotient(total * (blockIdx.x + 1), n) - want);
     if (cur.left <= 0) return false;
     unsigned long long base = 0ull;
     for (int c0 = 0;; c0 += THREADS) {
@@ -123,8 +123,8 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<T> &cur, unsigned l
     cur.b = static_cast<int>(buf[W]);
     cur.load(g);
     const unsigned long long within = want - buf[W + 1];
-    cur.head = static_cast<int>(within / cur.tiles);
-    cur.tile = static_cast<int>(within % cur.tiles);
+    cur.head = static_cast<int>(kva::quotient(within, static_cast<unsigned long long>(cur.tiles)));
+    cur.tile = static_cast<int>(within - static_cast<unsigned long long>(cur.head) * cur.tiles);
     return true;
 }
 
