@@ -100,9 +100,9 @@ __device__ __forceinline__ uint32_t mask_bits(const Args &g, const uint32_t *row
 // Whether the TMA box of token j of a row tile's keys holds tokens that some row may see, and j is not beyond the last.  What lies wholly before
 // the window is not looked up: its pages may have been given back
 __device__ __forceinline__ bool holds_seen(const Args &g, int lo, int hi, int j) { return j < hi && (j | (g.box - 1)) >= lo; }
-// What a key tile of a row tile counts that has `rows` rows from its first on: W; with HALF half of that where the rows fill no more than half of the tile (the tcgen05 kernel
-// then takes two key tiles at once)
-template <int MR, int W, bool HALF> __device__ __forceinline__ int tile_cost(int rows) { return HALF && rows <= MR / 2 ? W / 2 : W; }
+// What a key tile of a row tile counts that has `rows` rows from its first on: W; with HALF a sixth less where the rows fill no more than half of the tile (the tcgen05 kernel
+// then takes two key tiles at once, and waits for memory: 2165 cycles a tile, 2610 a full one)
+template <int MR, int W, bool HALF> __device__ __forceinline__ int tile_cost(int rows) { return HALF && rows <= MR / 2 ? W - W / 6 : W; }
 // units of one key/value head of sequence b: its key tiles, and an item EXTRA more, for its beginning and end
 template <int MR, int TK, int EXTRA, int W, bool HALF> __device__ __forceinline__ long long seq_units(const Args &g, int b) {
     int q0;
@@ -232,17 +232,18 @@ __device__ __forceinline__ bool locate(const Args &g, Run &run, Cursor<MR, TK, E
         if (c0 == 0) { mine = x; upto = s; per_head = ph; }
         run.total += static_cast<long long>(all);
     }
-    // (so that every run within an item has a tile)
-    int most = W;
-    if constexpr (HALF) {
+    // so that every run within an item has a tile
+    if constexpr (HALF) {                        // (no run is shorter than the largest tile of the call)
         bool full = false;
         for (int b = threadIdx.x; b < g.a.n_seqs; b += THREADS) {
             int q0;
             full = full || seq_queries(g, b, q0) * g.group > MR / 2;
         }
-        most = __any_sync(0xFFFFFFFFu, __syncthreads_or(full) != 0) ? W : W / 2;       // (uniform, visibly)
+        const int most = __any_sync(0xFFFFFFFFu, __syncthreads_or(full) != 0) ? W : W - W / 6;       // (uniform, visibly)
+        run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), run.total == 0 ? 0ll : max(run.total / most, 1ll)));
+    } else {                                     // (tiles of 1 or 2: of runs of 2 only the first may be shorter)
+        run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + W - 1) / W));
     }
-    run.ctas = static_cast<int>(min(static_cast<long long>(g.grid), (run.total + most - 1) / most));
     if (cta >= run.ctas) return false;
     if (run.total >= (0x7FFFFFFFll - EXTRA) * run.ctas) {
         set_status(g.status, SISO_ERR_UNSUPPORTED);

@@ -188,10 +188,10 @@ attention_many_rows_kernel(const __grid_constant__ Args g, const __grid_constant
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncthreads();
-    // a tree's row tiles are often half empty: they count half (24 trees of 119 to 441 rows: 89 us and 100 us; not over 8 bits, where widening a key tile costs as much
-    // for few rows as for many), and an item's beginning and end three tiles (24 trees of 256 rows: two 117 us, three 113 us, six 117 us)
+    // a tree's row tiles are often half empty: they count a sixth less, and an item's beginning and end three tiles and a third, as measured over 24 trees of 119 to 441 rows (cycles
+    // of a CTA = 8514 items + 2610 full tiles + 2165 half tiles).  Not over 8 bits, where widening a key tile costs as much for few rows as for many
     constexpr bool HALF = TREE && !EIGHT;
-    constexpr int W = HALF ? 2 : 1, MORE = HALF ? 3 * W : EXTRA;
+    constexpr int W = HALF ? 6 : 1, MORE = HALF ? 20 : EXTRA;
     Cursor<TC_ROWS, TK, MORE, W, HALF> cur;
     {
         Run run;

@@ -83,3 +83,32 @@ def test_the_c_entry_points_refuse_bad_arguments_before_any_launch():
     assert lib.siso_kv_keep_path(None, big, big, 1, big, big, big, 1, 1, 1, big, None) == 1
     assert lib.siso_kv_add_weights(None, None, None) == 1
     assert lib.siso_kv_evict(None, big, big, big, 1, 1, big, 1, 1, 1, 4, 1, big, big, None) == 1
+
+
+def test_no_run_within_an_item_is_without_a_unit():
+    # how units are dealt to CTAs, as a model: an item cut at runs' borders has a part in every run from its first unit's to its last one's, which is what the kernels that join parts
+    # count on.  Trees over bf16: tiles of 6 (5 where no sequence has more), 20 more for an item; weights: a unit each and one more for an item
+    import bisect
+    import random
+    rng = random.Random(1)
+
+    def holds(starts, total, ctas):
+        borders = [total * c // ctas for c in range(ctas + 1)]
+        return all(set(range(o[0], o[-1] + 1)) == set(o) for o in ([bisect.bisect_right(borders, s) - 1 for s in item] for item in starts))
+
+    for _ in range(4000):
+        grid = rng.choice([3, 17, 148])
+        only_half = rng.random() < 0.3
+        at, starts, most = 0, [], 5
+        for _ in range(rng.randint(1, 12)):
+            cost, tiles = (5 if only_half or rng.random() < 0.5 else 6), rng.randint(1, rng.choice([3, 20, 60]))
+            most = max(most, cost)
+            starts.append([at + 20 + cost * k for k in range(tiles)])
+            at += 20 + cost * tiles
+        assert holds(starts, at, min(grid, max(at // most, 1)))
+        at, starts = 0, []
+        for _ in range(rng.randint(1, 12)):
+            n = rng.randint(1, rng.choice([2, 9, 200]))
+            starts.append([at] + [at + k + 1 for k in range(1, n)])
+            at += n + 1
+        assert holds(starts, at, min(grid, (at + 1) // 2))
