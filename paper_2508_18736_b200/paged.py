@@ -1,6 +1,6 @@
 """The language model's side of a cache miss: a paged key/value cache that is quantised as it is written, the attention of new
-tokens over it, and the verification of drafted tokens (a near hit's stored answer, or a drafting model's).  Argument
-marshalling only; names and rules follow include/siso.h.
+tokens over it, the verification of drafted tokens (a near hit's stored answer, or a drafting model's), the same for trees of drafts (several near
+hits), and eviction from the cache by the weight that attention gives.  Argument marshalling only; names and rules follow include/siso.h.
 
 A call with `stream` runs on that stream as a whole, as under torch.cuda.stream: the copies of arguments that are not contiguous, the
 kernels, and the outputs, whose memory is that stream's.  The arguments have to be ready there and to live until it is done with them."""
