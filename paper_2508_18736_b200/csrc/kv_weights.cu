@@ -9,14 +9,16 @@
 // An item is (sequence, kv head, block of 256 keys = two tiles), a unit is an item with one tile of up to 128 query rows: whole tokens with all their heads of
 // the group (groups above 128: the largest part that divides them).  Units are dealt to one CTA per SM in equal runs, as in the attention; items that were cut are
 // joined by a second kernel in a fixed order.  With one row tile an item is one unit and nothing is cut (FEW).
-//   warps 0-3, 4-7   key tile 0, 1, a key per thread: scores from TMEM (two buffers), exponentials, sum
-//   warp 8           issues the products
-//   warp 9           fills the ring of key tiles by TMA, one box per run of tokens in one page
-//   warp 10          fills the ring of query tiles by TMA, and their -lse log2 e beside them
-//   warp 11          brings what else belongs to the keys: their weights so far and where they lie, exponents
-//   warps 12-19      8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
-// Bounds: a step reads every key for a few rows: HBM.  A chunk's 256 x 128 scores take 1024 cycles of tcgen05.mma (d = 128) and 2048 of the SM's 16 exponentials a
+//   the first warps (FEW: 8, a thread per key; else 16, two threads per key, which share the columns): scores from TMEM (two buffers), exponentials, sum
+//   one warp         issues the products
+//   one warp         fills the ring of key tiles by TMA, one box per run of tokens in one page
+//   one warp         fills the ring of query tiles by TMA, and their -lse log2 e beside them
+//   one warp         brings what else belongs to the keys: their weights so far and where they lie, exponents
+//   8 warps          8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
+// Bounds: few rows read every key once: HBM.  A chunk's 256 x 128 scores take 1024 cycles of tcgen05.mma (d = 128) and 2048 of the SM's 16 exponentials a
 // cycle: the exponentials, of which some are taken on the FMA pipe.
+// Measured (8 kv heads x 128 with 4 query heads each, bf16, the kernel and its join): 4096 queries over 8193 tokens 235 us, the exponentials' pipe 72 % busy; 32 query tokens
+// (128 rows a kv head) of each of 64 sequences over 4096 tokens 125 us.
 #include "kv_attention.cuh"
 
 namespace siso {
