@@ -586,7 +586,7 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
  *                  the weights exp(scale q.k_j - lse).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
  *                  layer of the call, w_j = decay w_j + sum of the weights over the queries and query heads that read the kv head; tokens that are new
  *                  in this call (the last ones, as many as the sequence has queries) start from 0, and with decay 0 all do, whatever stood there.  Sequences without
- *                  queries are left alone.  A query whose lse is -infinity gives nothing.  d_q as in siso_kv_attention, but with no stride of 0 where there are several entries.  Sums are fp32, in an order that does not change from call to call.
+ *                  queries are left alone.  A query whose lse is -infinity gives nothing.  d_q as in siso_kv_attention, but with no stride of 0 where there are several entries; d_weights 16-byte aligned.  Sums are fp32, in an order that does not change from call to call.
  * siso_kv_evict    For each layer, sequence and kv head by itself: of kv_len tokens the last `recent` stay and, of the others, the budget - recent with the largest
  *                  weights (ties: the earlier one; NaN counts as less than all else).  Their rows, exponents and weights are moved, in order, to places 0, 1, .. of the
  *                  pages d_out_pages [n_seqs, out_max_pages] (d_pages itself: in place).  d_new_len [n_seqs] = min(kv_len, budget), the same for

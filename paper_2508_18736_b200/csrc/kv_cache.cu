@@ -439,7 +439,9 @@ siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void
     // queries come by TMA, which takes no stride of 0
     if ((a.n_tokens > 1 && a.q_stride_token == 0) || (a.n_heads > 1 && a.q_stride_head == 0) || a.q_stride_token >= (1ll << 38) || a.q_stride_head >= (1ll << 38))
         return SISO_ERR_UNSUPPORTED;
-    if (a.q_stride_token % 8 != 0 || a.q_stride_head % 8 != 0 || !kvc::aligned16(a.d_q) || !kvc::attends(h->cfg)) return SISO_ERR_UNSUPPORTED;
+    // weights so far come 16 bytes at a time (a page's are a multiple of 32 bytes)
+    if (a.q_stride_token % 8 != 0 || a.q_stride_head % 8 != 0 || !kvc::aligned16(a.d_q) || !kvc::aligned16(a.d_weights) || !kvc::attends(h->cfg))
+        return SISO_ERR_UNSUPPORTED;
     if (a.n_tokens >= ((1ll << 31) - 256) / a.n_heads || static_cast<int64_t>(a.max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     const OnDevice on(h->cfg.device);
     SISO_CUDA(on.error());

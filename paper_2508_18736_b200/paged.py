@@ -272,7 +272,7 @@ class PagedKV:
                              f"on {self._dev}")
 
     def new_weights(self) -> torch.Tensor:
-        """A number for each cached row, zero: what add_weights() adds to and evict() goes by."""
+        """A number for each cached row, zero: what add_weights() adds to (it wants them to begin on a 16-byte boundary, as these do) and evict() goes by."""
         return torch.zeros((self.n_layers, self.n_pages, self.n_kv_heads, self.page_size), dtype=torch.float32, device=self._dev)
 
     def keep_path(self, path: torch.Tensor, accepted: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, stream=None
