@@ -178,7 +178,7 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
 constexpr int SHIFTS = 8;              // their ring: they are needed until the sums are done, the queries only until the products are
 constexpr int METAS = 4;               // items whose keys' small things are there or on their way
 struct Bars {
-    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8], meta_full[METAS], meta_empty[METAS];
+    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8], meta_full[METAS], meta_empty[METAS], q_landed;
     uint32_t tmem;
     int gave_up;
     union {
@@ -297,6 +297,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         for (int i = 0; i < SHIFTS; ++i) { mbar_init(&bars.sh_full[i], 1); mbar_init(&bars.sh_empty[i], SUM_WARPS); }
         for (int i = 0; i < S::RAWS; ++i) { mbar_init(&bars.raw_full[i], 1); mbar_init(&bars.raw_empty[i], 8); }
         for (int i = 0; i < METAS; ++i) { mbar_init(&bars.meta_full[i], 33); mbar_init(&bars.meta_empty[i], SUM_WARPS); }      // 33: the copies, and the places
+        mbar_init(&bars.q_landed, 1);
         bars.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -406,7 +407,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         } else if (warp == SUM_WARPS + 2) {
             // ---- queries and their statistics, which are asked for one tile ahead
             int stage = 0, sh = 0;
-            uint32_t phase = 0, sh_phase = 0;
+            uint32_t phase = 0, sh_phase = 0, landed_phase = 0;
             const uint32_t bytes = rows * (D * 2);
             struct Tile { int token, head, here; } at;         // first token (row of d_q), first head, tokens of the sequence from there on
             float shift[ROWS / 32];
@@ -446,12 +447,33 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.sh_full[sh]);
                 if (++sh == SHIFTS) { sh = 0; sh_phase ^= 1u; }
+                // rows whose lse is -infinity may hold anything, and a NaN times zero is one: they are written over with zeros once they have come
+                uint32_t dead[ROWS / 32], some = 0u;
+#pragma unroll
+                for (int i = 0; i < ROWS / 32; ++i) {
+                    dead[i] = __ballot_sync(0xFFFFFFFFu, shift[i] == -INFINITY);
+                    some |= dead[i];
+                }
                 wait_bar(&bars.q_empty[stage], phase ^ 1u, gave_up, g.status);
-                if (*gave_up == 0 && lane == 0) {
-                    mbar_arrive_expect_tx(&bars.q_full[stage], bytes);
+                uint64_t *const landed = some ? &bars.q_landed : &bars.q_full[stage];
+                const bool go = *gave_up == 0;
+                if (go && lane == 0) {
+                    mbar_arrive_expect_tx(landed, bytes);
 #pragma unroll
                     for (int half = 0; half < D / 64; ++half)
-                        load_q_box(smem_u32(q_tiles + stage * S::Q_TILE) + half * (ROWS * 128), &map_q, half * 64, at.head, at.token, &bars.q_full[stage]);
+                        load_q_box(smem_u32(q_tiles + stage * S::Q_TILE) + half * (ROWS * 128), &map_q, half * 64, at.head, at.token, landed);
+                }
+                if (some && __any_sync(0xFFFFFFFFu, go)) {
+                    wait_bar(landed, landed_phase, gave_up, g.status);
+                    landed_phase ^= 1u;
+#pragma unroll
+                    for (int i = 0; i < ROWS / 32; ++i)
+                        for (uint32_t left = dead[i]; left; left &= left - 1u)
+                            if (lane < D / 8)
+                                *reinterpret_cast<uint4 *>(q_tiles + stage * S::Q_TILE + (lane >> 3) * (ROWS * 128) + (i * 32 + __ffs(left) - 1) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.q_full[stage]);
                 }
                 __syncwarp();
                 if (++stage == S::Q_STAGES) { stage = 0; phase ^= 1u; }

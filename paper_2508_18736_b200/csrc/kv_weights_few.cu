@@ -243,7 +243,7 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
         float lse[NT][2];
     } now, next;
     float scale[NT][2], shift[NT][2];
-    int pos[NT][2];
+    int pos[NT][2];                     // the last key that a row gives anything; -1: none (its lse is -infinity, and its scores may be anything)
     // rows rt * MR .. of a kv head: 8 values of each of D / 32 pieces per lane (bf16 cache: a lane's 16 bytes of a key hold 8 values; 8-bit: 16 values, two pieces)
     auto fetch = [&](const Cursor<T> &at, int rt, Queries &x) {
 #pragma unroll
@@ -291,7 +291,7 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = rt * MR + t * 8 + 2 * c + h;
-                pos[t][h] = kva::position(at.len, at.n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(row))));
+                pos[t][h] = now.lse[t][h] == -INFINITY ? -1 : causal ? kva::position(at.len, at.n_q, static_cast<int>(g.by_group.div(static_cast<uint32_t>(row)))) : 0x7FFFFFFF;
                 shift[t][h] = now.lse[t][h] == -INFINITY ? -INFINITY : now.lse[t][h] * -1.4426950408889634f;      // nothing seen, or no row: exponentials are zero
                 scale[t][h] = g.scale_log2 * __shfl_sync(0xFFFFFFFFu, back, (2 * c + h) * 4);
             }
@@ -330,7 +330,6 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
         }
         wait_bar(&ring.full[stage], phase, gave_up, g.status);
         const int j0 = cur.tile * T, n0 = warp % GW * NK;
-        const bool cut = causal && j0 + T - 1 > cur.len - cur.n_q;
         const int k_first = stage * S::STAGE + kva::chunk_at<RB, T>(key_of<RB>(r0), c) + n0 * LINE;
         float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};           // of the keys r0 and r0 + 8 of two tiles of 16
         for (int rt = 0; rt < row_tiles; ++rt) {
@@ -382,7 +381,7 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const float p = kva::ex2(fmaf(s[i][t][2 * e + h], EIGHT ? f * scale[t][h] : scale[t][h], shift[t][h]));
-                            sum[i][e] += cut && j0 + n > pos[t][h] ? 0.f : p;
+                            sum[i][e] += j0 + n > pos[t][h] ? 0.f : p;
                         }
                 }
         }
