@@ -581,15 +581,19 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
  *                  without nodes); d_path [n_seqs, max_path] (may be NULL): their nodes, then -1.  vocab at most 2^18.
  * siso_kv_keep_path  Moves the rows (all layers) of nodes d_path[b, t], t < d_accepted[b], to places before + 1 + t: the accepted path follows node 0.  A path
  *                  ascends; an entry that does not, or is no node of the sequence, ends it (SISO_ERR_INVALID_ARG in the status word).  d_new_len [n_seqs] =
- *                  before + 1 + t at its end (kv_len for a sequence without new tokens); it must not be d_kv_len itself.
+ *                  before + 1 + t at its end (kv_len for a sequence without new tokens); it must not be d_kv_len itself.  Weights (below) stay where they
+ *                  are: node 0 and the rows of the path are new tokens to them.  Their queries and lse, gathered in the path's order, are those of a causal chunk.
  * siso_kv_add_weights  Each query i of a sequence (as in siso_kv_attention; d_lse [n_tokens, n_heads] as that returns it) gives the tokens that it sees
  *                  the weights exp(scale q.k_j - lse).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
  *                  layer of the call, w_j = decay w_j + sum of the weights over the queries and query heads that read the kv head; tokens that are new
- *                  in this call (the last ones, as many as the sequence has queries) start from 0, and with decay 0 all do, whatever stood there.  Sequences without
+ *                  in this call (the last ones, as many as the sequence has queries) start from 0, and with decay 0 all do, whatever stood there (in the places of tokens
+ *                  that were evicted, of drafts, of a page's last owner there may be anything).  Where other tokens than the call's queries are new too (a chunk
+ *                  of which only the last queries are given, a path of drafts that the next query follows), siso_kv_add_weights_new is told how many: the last
+ *                  d_new[b] tokens of sequence b start from 0 (d_new [n_seqs]; below 0 counts as 0, above kv_len as kv_len; NULL: as many as it has queries).  Sequences without
  *                  queries are left alone.  A query whose lse is -infinity gives nothing.  d_q as in siso_kv_attention, but with no stride of 0 where there are several entries; d_weights 16-byte aligned.  Sums are fp32, in an order that does not change from call to call.
  * siso_kv_evict    For each layer, sequence and kv head by itself: of kv_len tokens the last `recent` stay and, of the others, the budget - recent with the largest
  *                  weights (ties: the earlier one; NaN counts as less than all else).  Their rows, exponents and weights are moved, in order, to places 0, 1, .. of the
- *                  pages d_out_pages [n_seqs, out_max_pages] (d_pages itself: in place).  d_new_len [n_seqs] = min(kv_len, budget), the same for
+ *                  pages d_out_pages [n_seqs, out_max_pages] (d_pages itself: in place).  Places that nothing is moved to keep what they held, weights among it.  d_new_len [n_seqs] = min(kv_len, budget), the same for
  *                  all layers and heads, must not be d_kv_len itself; d_kept [n_layers, n_seqs, n_kv_heads, budget] (NULL is refused): which places stayed, then -1.
  *                  An entry of d_out_pages is the entry of d_pages at the same index, or a page that the call does not otherwise use; pages of different sequences
  *                  differ.  A page index outside the pool: SISO_ERR_INVALID_ARG in the status word, its tokens count as NaN and are not moved.
@@ -617,6 +621,7 @@ typedef struct {
 } siso_weights_t;
 
 siso_status_t siso_kv_add_weights(siso_kv_t *kv, const siso_weights_t *args, void *stream);
+siso_status_t siso_kv_add_weights_new(siso_kv_t *kv, const siso_weights_t *args, const int32_t *d_new, void *stream);
 siso_status_t siso_kv_evict(siso_kv_t *kv, float *d_weights, const int32_t *d_kv_len, const int32_t *d_pages, int64_t pages_stride, int32_t max_pages,
                             const int32_t *d_out_pages, int64_t out_pages_stride, int32_t out_max_pages, int32_t n_seqs, int32_t budget,
                             int32_t recent, int32_t *d_new_len, int32_t *d_kept, void *stream);

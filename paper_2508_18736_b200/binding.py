@@ -30,7 +30,7 @@ EXPORTS = ["siso_cache_create", "siso_cache_destroy", "siso_set_option", "siso_i
            "siso_shard_plan", "siso_route_planned", "siso_select_evict_planned", "siso_norm_deviation", "siso_kv_create",
            "siso_kv_destroy", "siso_kv_write", "siso_kv_read", "siso_kv_attention", "siso_kv_sync_status", "siso_verify_drafts",
            "siso_kv_selftest_wait_timeout", "siso_tree_mask", "siso_kv_tree_attention", "siso_verify_tree", "siso_kv_keep_path",
-           "siso_kv_add_weights", "siso_kv_evict"]
+           "siso_kv_add_weights", "siso_kv_add_weights_new", "siso_kv_evict"]
 
 
 class SisoError(RuntimeError):
@@ -132,6 +132,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     L.siso_verify_tree.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     L.siso_kv_keep_path.argtypes = [vp, vp, vp, i32, vp, vp, vp, i64, i32, i32, vp, vp]
     L.siso_kv_add_weights.argtypes = [vp, vp, vp]
+    L.siso_kv_add_weights_new.argtypes = [vp, vp, vp, vp]
     L.siso_kv_evict.argtypes = [vp, vp, vp, vp, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, vp]
     L.siso_launch_count.argtypes = [vp]
     L.siso_launch_count.restype = i64

@@ -72,7 +72,8 @@ inline KvView kv_view(const Kv *h, int layer) {
 
 // mask: which new tokens each new token sees, rows of `words` words (NULL: by causality)
 siso_status_t launch_kv_attention(Kv *h, const siso_attention_t *a, const uint32_t *mask, int words, int64_t mask_stride, cudaStream_t s);
-siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, cudaStream_t s);
+// fresh: how many of each sequence's tokens are weighed for the first time (NULL: as many as it has queries)
+siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, const int32_t *fresh, cudaStream_t s);
 namespace kva { siso_status_t launch_wait_timeout(Kv *h, cudaStream_t s); }
 
 #ifdef __CUDACC__

@@ -425,7 +425,7 @@ siso_status_t siso_kv_tree_attention(siso_kv_t *h, const siso_attention_t *args,
     return attention_call(h, args, d_mask, words, mask_stride, stream);
 }
 
-siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void *stream) {
+siso_status_t siso_kv_add_weights_new(siso_kv_t *h, const siso_weights_t *args, const int32_t *d_new, void *stream) {
     if (!h || !args) return SISO_ERR_INVALID_ARG;
     siso_weights_t a = *args;
     if (a.n_tokens < 0 || a.n_seqs < 0 || a.layer < 0 || a.layer >= h->cfg.n_layers) return SISO_ERR_INVALID_ARG;
@@ -445,8 +445,10 @@ siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void
     if (a.n_tokens >= ((1ll << 31) - 256) / a.n_heads || static_cast<int64_t>(a.max_pages) * h->cfg.page_size >= (1ll << 31) - 65536) return SISO_ERR_UNSUPPORTED;
     const OnDevice on(h->cfg.device);
     SISO_CUDA(on.error());
-    return launch_kv_weights(h, &a, static_cast<cudaStream_t>(stream));
+    return launch_kv_weights(h, &a, d_new, static_cast<cudaStream_t>(stream));
 }
+
+siso_status_t siso_kv_add_weights(siso_kv_t *h, const siso_weights_t *args, void *stream) { return siso_kv_add_weights_new(h, args, nullptr, stream); }
 
 siso_status_t siso_kv_selftest_wait_timeout(siso_kv_t *h, void *stream) {
     if (!h) return SISO_ERR_INVALID_ARG;

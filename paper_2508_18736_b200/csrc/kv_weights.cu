@@ -1,7 +1,7 @@
 // The weight that attention gives to each cached token, accumulated: for the eviction by it.
 //
 // Query i of a sequence (head g of the kv head's group) gives token j, if it sees it, exp(scale q.k_j - lse): its probability.  For each token and
-// kv head the call takes w_j <- decay w_j + sum over queries and heads.  The statistics (lse) are the attention's, so one pass over the keys is all.
+// kv head the call takes w_j <- decay w_j + sum over queries and heads (from 0 where the token has no weight yet).  The statistics (lse) are the attention's, so one pass over the keys is all.
 //
 // Scores are taken transposed, S^T = K Q^T by tcgen05: keys are the 128 lanes of TMEM and query rows its columns.  A thread then owns a key: the sum over
 // queries stays in one register, a scale of an 8-bit row is one factor, causality is one first column, and keys that are not there spoil their own thread only.
@@ -36,6 +36,7 @@ struct Record {                        // an item that several CTAs share, kept 
 struct Args {
     KvView kv;
     siso_weights_t a;
+    const int32_t *fresh;
     FastDiv by_page;
     int group, hb, tb, chunks;         // a row tile: hb heads of tb tokens; chunks = group / hb
     int box, grid;
@@ -57,10 +58,11 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
 }
 // What the items of a sequence cost: `tiles` row tiles and one more, for the beginning and end, as long as all of them see the block (`full` blocks), fewer tiles then
 struct Seq {
-    int q0, n_q, len, tiles, blocks, full;
+    int q0, n_q, len, n_old, tiles, blocks, full;        // n_old: tokens that have a weight already
     __device__ __forceinline__ void load(const Args &g, int b) {
         n_q = seq_queries(g, b, q0);
         len = n_q > 0 ? seq_len(g, b) : 0;
+        n_old = len - (g.fresh ? min(max(g.fresh[b], 0), len) : n_q);
         tiles = (n_q + g.tb - 1) / g.tb * g.chunks;
         blocks = (len + KB - 1) / KB;
         full = !(g.a.flags & SISO_ATTN_CAUSAL) ? blocks : len >= n_q ? min(blocks, (len - n_q) / KB + 1) : 0;
@@ -582,7 +584,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 const long long last = run_end - cur.left + (cur.s.tiles - cur.tile0);
                 g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.kb, kva::cta_of(last, total, ctas) - static_cast<int>(blockIdx.x) + 1};
             }
-            const bool is_old = j < before && g.a.decay != 0.f;
+            const bool is_old = j < cur.s.n_old && g.a.decay != 0.f;
             more = __any_sync(0xFFFFFFFFu, cur.step(g));         // (uniform, visibly: barriers and TMEM loads in the loop cost no registers then)
             wait_bar(&bars.meta_full[slot], meta_phase, gave_up, g.status);
             const Meta &meta = metas[slot];
@@ -691,7 +693,7 @@ weights_join_kernel(const __grid_constant__ Args g) {
     float sum = 0.f;
     for (int p = 0; p < rec.n_parts; ++p) sum += g.part[kva::part_place(static_cast<int>(blockIdx.x) + p, p > 0) * KB + threadIdx.x];
     float *w = g.a.d_weights + ((static_cast<long long>(g.a.layer) * g.kv.n_pages + page) * g.kv.n_kv_heads + rec.head) * g.kv.page_size + j - i * g.kv.page_size;
-    *w = (j < s.len - s.n_q && g.a.decay != 0.f ? g.a.decay * *w : 0.f) + sum;
+    *w = (j < s.n_old && g.a.decay != 0.f ? g.a.decay * *w : 0.f) + sum;
 }
 #endif
 
@@ -710,15 +712,16 @@ template <int KIND, int D> static siso_status_t run(Kv *h, const Args &g, bool f
 }
 
 // up to 32 rows per kv head (kv_weights_few.cu)
-siso_status_t launch_few_rows(Kv *h, const siso_weights_t *a, int rows, cudaStream_t s);
+siso_status_t launch_few_rows(Kv *h, const siso_weights_t *a, const int32_t *fresh, int rows, cudaStream_t s);
 
 }  // namespace kvw
 
-siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, cudaStream_t s) {
+siso_status_t launch_kv_weights(Kv *h, const siso_weights_t *a, const int32_t *fresh, cudaStream_t s) {
     using namespace kvw;
     const long long rows = static_cast<long long>(a->max_q) * (a->n_heads / h->cfg.n_kv_heads);
-    if (rows <= 32) return launch_few_rows(h, a, static_cast<int>(rows), s);
+    if (rows <= 32) return launch_few_rows(h, a, fresh, static_cast<int>(rows), s);
     Args g;
+    g.fresh = fresh;
     g.kv = kv_view(h, a->layer);
     g.a = *a;
     g.group = a->n_heads / h->cfg.n_kv_heads;

@@ -29,6 +29,7 @@ constexpr int PRODUCERS = 4;             // warps that fill the ring; each has i
 struct Args {
     KvView kv;
     siso_weights_t a;
+    const int32_t *fresh;
     FastDiv by_page, by_group;
     int group, box;
     float scale_log2;
@@ -66,11 +67,12 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
 }
 // A unit of this CTA's run: tile of a kv head of a sequence
 template <int T> struct Cursor {
-    int b, head, tile, tiles, len, q0, n_q;
+    int b, head, tile, tiles, len, q0, n_q, n_old;              // n_old: tokens that have a weight already
     long long left;
     __device__ __forceinline__ void load(const Args &g) {
         n_q = seq_queries(g, b, q0);
         len = n_q > 0 ? seq_len(g, b) : 0;
+        n_old = len - (g.fresh ? min(max(g.fresh[b], 0), len) : n_q);
         tiles = (len + T - 1) / T;
     }
     // to the first tile of the next kv head that has any; only called while units are left
@@ -397,7 +399,7 @@ weights_few_rows_kernel(const __grid_constant__ Args g, const __grid_constant__ 
             const long long place = places[stage * BLOCKS + n / 8];
             const float given = c == 0 ? sum[0][0] : c == 1 ? sum[0][1] : c == 2 ? sum[1][0] : sum[1][1];
             if (place >= 0 && j < cur.len) {
-                const float old = g.a.decay != 0.f && j < cur.len - cur.n_q ? g.a.decay * olds[stage * T + n] : 0.f;
+                const float old = g.a.decay != 0.f && j < cur.n_old ? g.a.decay * olds[stage * T + n] : 0.f;
                 held[place + (n & 7)] = old + given;
             }
         }
@@ -424,8 +426,9 @@ template <int KIND> static siso_status_t run_rows(Kv *h, const Args &g, int rows
 
 }  // namespace few
 
-siso_status_t launch_few_rows(Kv *h, const siso_weights_t *a, int rows, cudaStream_t s) {
+siso_status_t launch_few_rows(Kv *h, const siso_weights_t *a, const int32_t *fresh, int rows, cudaStream_t s) {
     few::Args g;
+    g.fresh = fresh;
     g.kv = kv_view(h, a->layer);
     g.a = *a;
     g.group = a->n_heads / h->cfg.n_kv_heads;

@@ -277,7 +277,8 @@ class PagedKV:
 
     def keep_path(self, path: torch.Tensor, accepted: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, stream=None
                   ) -> torch.Tensor:
-        """Moves the rows (all layers) of the nodes path [seqs, longest], the first accepted [seqs] of each, behind node 0 of their sequence.
+        """Moves the rows (all layers) of the nodes path [seqs, longest], the first accepted [seqs] of each, behind node 0 of their sequence (rows, not weights:
+        node 0 and the path's are new tokens to add_weights(); their queries and lse, gathered in the path's order, are those of a causal chunk).
         cu_q, kv_len, pages as tree_attention() had them.  Returns the tokens that the sequences have now, int32 [seqs]."""
         if stream is not None:
             with _on(stream, self._index):
@@ -299,14 +300,17 @@ class PagedKV:
         return new_len
 
     def add_weights(self, weights: torch.Tensor, q: torch.Tensor, lse: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor,
-                    max_q: int, layer: int = 0, scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, stream=None) -> None:
+                    max_q: int, layer: int = 0, scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, stream=None,
+                    n_new: Optional[torch.Tensor] = None) -> None:
         """Adds to weights (see new_weights()) what the queries q [n, heads, head dim] bf16 give each token that they see, summed over the
         queries and the heads of a kv head: their probabilities, from lse [n, heads] as attention(want_lse=True) returned it.  What was there counts
-        `decay` times (0: not at all, whatever it is); the new tokens start from zero.  For the last queries of a longer chunk alone pass them with
-        their own cu_q."""
+        `decay` times (0: not at all, whatever it is); the new tokens start from zero: a sequence's last ones, as many as it has queries, or n_new int32 [seqs] of
+        them.  For the last queries of a longer chunk alone pass them with their own cu_q and the chunk's length as n_new, for the first query behind a
+        path that keep_path() kept the path's tokens and the query's: until a call has counted a token as new, its place may hold an evicted token's weight, a
+        draft's, or that of a page's last owner."""
         if stream is not None:
             with _on(stream, self._index):
-                return self.add_weights(weights, q, lse, cu_q, kv_len, pages, max_q, layer, scale, causal, decay)
+                return self.add_weights(weights, q, lse, cu_q, kv_len, pages, max_q, layer, scale, causal, decay, n_new=n_new)
         index = self._index
         shape = q.shape
         if q.dtype is not torch.bfloat16 or len(shape) != 3 or shape[2] != self.head_dim or q.get_device() != index:
@@ -319,11 +323,19 @@ class PagedKV:
             q = q.contiguous()
         if not lse.is_contiguous():
             lse = lse.contiguous()
+        if n_new is not None:
+            if n_new.dtype is not torch.int32 or n_new.shape != kv_len.shape or n_new.get_device() != index:
+                raise ValueError(f"n_new must be an int32 [{kv_len.numel()}] tensor on {self._dev}")
+            if not n_new.is_contiguous():
+                n_new = n_new.contiguous()
         sq = q.stride()
         _WEIGHTS.pack_into(self._args, 0, q.data_ptr(), lse.data_ptr(), weights.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), sq[0], sq[1],
                            pages.stride(0), shape[0], kv_len.numel(), max_q, pages.shape[1], shape[1], layer, ATTN_CAUSAL if causal else 0,
                            self._default_scale if scale is None else scale, decay)
-        st = self._lib.siso_kv_add_weights(self._h, self._args, _raw_stream(index))
+        if n_new is None:
+            st = self._lib.siso_kv_add_weights(self._h, self._args, _raw_stream(index))
+        else:
+            st = self._lib.siso_kv_add_weights_new(self._h, self._args, n_new.data_ptr(), _raw_stream(index))
         if st:
             self._check(st, "siso_kv_add_weights")
 
@@ -331,7 +343,7 @@ class PagedKV:
               stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Cuts every sequence down to `budget` tokens, for each layer and kv head by itself: the last `recent` stay and the heaviest others (ties: the
         earlier one), moved in order to the front of their pages, or of out_pages [seqs, max pages] (each the same as in pages at that index, or not otherwise in
-        use).  Returns (tokens now int32 [seqs], which places stayed int32 [layers, seqs, kv heads, budget], then -1)."""
+        use).  Places that nothing is moved to keep what they held, weights among it: tokens written there are new ones to add_weights().  Returns (tokens now int32 [seqs], which places stayed int32 [layers, seqs, kv heads, budget], then -1)."""
         if stream is not None:
             with _on(stream, self._index):
                 return self.evict(weights, kv_len, pages, budget, recent, out_pages)
