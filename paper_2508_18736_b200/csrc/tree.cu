@@ -349,9 +349,12 @@ verify_tree_kernel(Args g) {
 }
 
 template <typename T, bool WIDE> static siso_status_t run(const Args &g, int n_seqs, cudaStream_t s) {
+    constexpr int MOST = MAX_VOCAB / SPLIT * static_cast<int>(sizeof(float));
+    static_assert(MAX_VOCAB % (CHUNKS * 8) == 0, "a CTA's part of the largest vocabulary is no larger than its share");
     const int smem = WARPS * g.chunk * static_cast<int>(sizeof(float));
-    // (asked for at every call: which device the function has it on is not known here)
-    if (smem > 24 * 1024) SISO_CUDA(cudaFuncSetAttribute(verify_tree_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // asked for at every call, as which device the function has it on is not known here; always the most that any call takes, or one thread's call would
+    // take it from another's between its asking and its launch
+    if (smem > 24 * 1024) SISO_CUDA(cudaFuncSetAttribute(verify_tree_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST));
     return launch_early(verify_tree_kernel<T, WIDE>, dim3(static_cast<unsigned>(n_seqs) * SPLIT), THREADS, static_cast<size_t>(smem), s, g);
 }
 
