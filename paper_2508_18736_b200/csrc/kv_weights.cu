@@ -56,13 +56,14 @@ __device__ __forceinline__ int seq_queries(const Args &g, int b, int &q0) {
     q0 = min(max(g.a.d_cu_q[b], 0), n);
     return max(0, min(g.a.d_cu_q[b + 1], n) - q0);
 }
+// tokens of a sequence that have a weight already
+__device__ __forceinline__ int old_tokens(const Args &g, int b, int len, int n_q) { return len - (g.fresh ? min(max(g.fresh[b], 0), len) : n_q); }
 // What the items of a sequence cost: `tiles` row tiles and one more, for the beginning and end, as long as all of them see the block (`full` blocks), fewer tiles then
 struct Seq {
-    int q0, n_q, len, n_old, tiles, blocks, full;        // n_old: tokens that have a weight already
+    int q0, n_q, len, tiles, blocks, full;
     __device__ __forceinline__ void load(const Args &g, int b) {
         n_q = seq_queries(g, b, q0);
         len = n_q > 0 ? seq_len(g, b) : 0;
-        n_old = len - (g.fresh ? min(max(g.fresh[b], 0), len) : n_q);
         tiles = (n_q + g.tb - 1) / g.tb * g.chunks;
         blocks = (len + KB - 1) / KB;
         full = !(g.a.flags & SISO_ATTN_CAUSAL) ? blocks : len >= n_q ? min(blocks, (len - n_q) / KB + 1) : 0;
@@ -180,17 +181,19 @@ __device__ __forceinline__ bool locate(const Args &g, Cursor<FEW> &cur, long lon
 constexpr int SHIFTS = 8;              // their ring: they are needed until the sums are done, the queries only until the products are
 constexpr int METAS = 4;               // items whose keys' small things are there or on their way
 struct Bars {
-    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8], meta_full[METAS], meta_empty[METAS], q_landed;
+    uint64_t s_full[2][2], s_empty[2][2], k_full[8], k_empty[8], q_full[3], q_empty[3], sh_full[SHIFTS], sh_empty[SHIFTS], raw_full[8], raw_empty[8], meta_full[METAS], meta_empty[METAS];
     uint32_t tmem;
     int gave_up;
+    int dead[3];                       // of a query tile that has rows whose lse is -infinity: where its statistics lie among the SHIFTS, and 1; else 0
     union {
         Find find;
         float peer[2][TK];             // a key's sum on its way to the other thread of the key
     };
 };
-// What belongs to an item's keys: where their weights lie (of blocks of 8, -1: nowhere), the weights so far, the exponents
+// What belongs to an item's keys: where their weights lie (of blocks of 8, -1: nowhere), the weights so far, the exponents; how many of the sequence's tokens have weights
 struct Meta {
     long long place[KB / 8];
+    int n_old, pad[3];
     float old[KB];
     uint8_t exp[KB];
 };
@@ -276,6 +279,15 @@ template <int KIND> __device__ __forceinline__ void widen(uint32_t w, uint32_t &
     b = __byte_perm(even, odd, 0x7632);
 }
 
+// Rows of a query tile that has come whose lse is -infinity (their `shift` too) may hold anything, and a NaN less infinity is one: zeros, for the products.  Not inlined,
+// and by the warp that issues the products: in the sums it cost a chunk of 4096 queries 1 to 2 %, inlined with the queries' loads 64 rows over 8 bits 8 %
+template <int D> __device__ __noinline__ void clear_rows(uint8_t *tile, const float *shift, int rows, int lane) {
+    for (int r = 0; r < rows; ++r)
+        if (lane < D / 8 && shift[r] == -INFINITY) *reinterpret_cast<uint4 *>(tile + (lane >> 3) * (ROWS * 128) + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
 template <int KIND, int D, bool FEW>
 __global__ void __launch_bounds__(Shape<KIND, D, FEW>::THREADS, 1)
 weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q) {
@@ -299,8 +311,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         for (int i = 0; i < SHIFTS; ++i) { mbar_init(&bars.sh_full[i], 1); mbar_init(&bars.sh_empty[i], SUM_WARPS); }
         for (int i = 0; i < S::RAWS; ++i) { mbar_init(&bars.raw_full[i], 1); mbar_init(&bars.raw_empty[i], 8); }
         for (int i = 0; i < METAS; ++i) { mbar_init(&bars.meta_full[i], 33); mbar_init(&bars.meta_empty[i], SUM_WARPS); }      // 33: the copies, and the places
-        mbar_init(&bars.q_landed, 1);
         bars.gave_up = 0;
+        for (int i = 0; i < S::Q_STAGES; ++i) bars.dead[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     const int rows = g.hb * g.tb;                                // of a full row tile
@@ -409,7 +421,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
         } else if (warp == SUM_WARPS + 2) {
             // ---- queries and their statistics, which are asked for one tile ahead
             int stage = 0, sh = 0;
-            uint32_t phase = 0, sh_phase = 0, landed_phase = 0;
+            uint32_t phase = 0, sh_phase = 0;
             const uint32_t bytes = rows * (D * 2);
             struct Tile { int token, head, here; } at;         // first token (row of d_q), first head, tokens of the sequence from there on
             float shift[ROWS / 32];
@@ -442,6 +454,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                     place(ahead);
                     statistics(ahead, ahead_shift);
                 }
+                const int mine = sh;
                 wait_bar(&bars.sh_empty[sh], sh_phase ^ 1u, gave_up, g.status);
 #pragma unroll
                 for (int i = 0; i < ROWS / 32; ++i)             // nothing seen (-infinity), or no row: exponentials are zero
@@ -449,33 +462,17 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.sh_full[sh]);
                 if (++sh == SHIFTS) { sh = 0; sh_phase ^= 1u; }
-                // rows whose lse is -infinity may hold anything, and a NaN times zero is one: they are written over with zeros once they have come
-                uint32_t dead[ROWS / 32], some = 0u;
+                bool dead = false;
 #pragma unroll
-                for (int i = 0; i < ROWS / 32; ++i) {
-                    dead[i] = __ballot_sync(0xFFFFFFFFu, shift[i] == -INFINITY);
-                    some |= dead[i];
-                }
+                for (int i = 0; i < ROWS / 32; ++i) dead = dead || shift[i] == -INFINITY;
+                const int some = __any_sync(0xFFFFFFFFu, dead) ? mine + 1 : 0;
                 wait_bar(&bars.q_empty[stage], phase ^ 1u, gave_up, g.status);
-                uint64_t *const landed = some ? &bars.q_landed : &bars.q_full[stage];
-                const bool go = *gave_up == 0;
-                if (go && lane == 0) {
-                    mbar_arrive_expect_tx(landed, bytes);
+                if (*gave_up == 0 && lane == 0) {
+                    bars.dead[stage] = some;
+                    mbar_arrive_expect_tx(&bars.q_full[stage], bytes);
 #pragma unroll
                     for (int half = 0; half < D / 64; ++half)
-                        load_q_box(smem_u32(q_tiles + stage * S::Q_TILE) + half * (ROWS * 128), &map_q, half * 64, at.head, at.token, landed);
-                }
-                if (some && __any_sync(0xFFFFFFFFu, go)) {
-                    wait_bar(landed, landed_phase, gave_up, g.status);
-                    landed_phase ^= 1u;
-#pragma unroll
-                    for (int i = 0; i < ROWS / 32; ++i)
-                        for (uint32_t left = dead[i]; left; left &= left - 1u)
-                            if (lane < D / 8)
-                                *reinterpret_cast<uint4 *>(q_tiles + stage * S::Q_TILE + (lane >> 3) * (ROWS * 128) + (i * 32 + __ffs(left) - 1) * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bars.q_full[stage]);
+                        load_q_box(smem_u32(q_tiles + stage * S::Q_TILE) + half * (ROWS * 128), &map_q, half * 64, at.head, at.token, &bars.q_full[stage]);
                 }
                 __syncwarp();
                 if (++stage == S::Q_STAGES) { stage = 0; phase ^= 1u; }
@@ -489,10 +486,11 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
             const float *held = g.a.d_weights + static_cast<long long>(g.a.layer) * g.kv.n_pages * g.kv.n_kv_heads * g.kv.page_size;
             int slot = 0;
             uint32_t phase = 0;
-            struct Place { int head, tok, page; } at;
+            struct Place { int head, tok, page, n_old; } at;
             auto look_up = [&](Place &p) {
                 const int j = cur.kb * KB + lane * 8, i = static_cast<int>(g.by_page.div(static_cast<uint32_t>(j)));
                 p.head = cur.head;
+                p.n_old = old_tokens(g, cur.b, cur.s.len, cur.s.n_q);
                 p.tok = j - i * g.kv.page_size;
                 p.page = j < cur.s.len ? g.a.d_pages[cur.b * g.a.pages_stride + i] : -1;
             };
@@ -506,6 +504,7 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 wait_bar(&bars.meta_empty[slot], phase ^ 1u, gave_up, g.status);
                 Meta &m = metas[slot];
                 m.place[lane] = place;
+                if (lane == 0) m.n_old = at.n_old;
                 if (there && old) {
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(m.old + lane * 8)), "l"(held + place) : "memory");
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(m.old + lane * 8 + 4)), "l"(held + place + 4) : "memory");
@@ -538,6 +537,8 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 }
                 for (int u = 0; u < n; ++u) {
                     wait_bar(&bars.q_full[q_stage], q_phase, gave_up, g.status);
+                    const int dead = bars.dead[q_stage];
+                    if (__any_sync(0xFFFFFFFFu, dead != 0)) clear_rows<D>(q_tiles + q_stage * S::Q_TILE, shifts + (dead - 1) * ROWS, rows, lane);
                     const uint64_t b = q_desc + static_cast<uint64_t>(q_stage * (S::Q_TILE >> 4));
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
@@ -584,10 +585,10 @@ weights_kernel(const __grid_constant__ Args g, const __grid_constant__ CUtensorM
                 const long long last = run_end - cur.left + (cur.s.tiles - cur.tile0);
                 g.records[blockIdx.x] = Record{1, cur.b, cur.head, cur.kb, kva::cta_of(last, total, ctas) - static_cast<int>(blockIdx.x) + 1};
             }
-            const bool is_old = j < cur.s.n_old && g.a.decay != 0.f;
             more = __any_sync(0xFFFFFFFFu, cur.step(g));         // (uniform, visibly: barriers and TMEM loads in the loop cost no registers then)
             wait_bar(&bars.meta_full[slot], meta_phase, gave_up, g.status);
             const Meta &meta = metas[slot];
+            const bool is_old = j < meta.n_old && g.a.decay != 0.f;
             const float f = EIGHT ? g.scale_log2 * kv_scale(meta.exp[t * TK + key]) : g.scale_log2;
             float sum = 0.f;
             for (int u = 0; u < n; ++u) {
@@ -693,7 +694,7 @@ weights_join_kernel(const __grid_constant__ Args g) {
     float sum = 0.f;
     for (int p = 0; p < rec.n_parts; ++p) sum += g.part[kva::part_place(static_cast<int>(blockIdx.x) + p, p > 0) * KB + threadIdx.x];
     float *w = g.a.d_weights + ((static_cast<long long>(g.a.layer) * g.kv.n_pages + page) * g.kv.n_kv_heads + rec.head) * g.kv.page_size + j - i * g.kv.page_size;
-    *w = (j < s.n_old && g.a.decay != 0.f ? g.a.decay * *w : 0.f) + sum;
+    *w = (j < old_tokens(g, rec.b, s.len, s.n_q) && g.a.decay != 0.f ? g.a.decay * *w : 0.f) + sum;
 }
 #endif
 
