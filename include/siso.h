@@ -583,6 +583,7 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
  *                  ascends; an entry that does not, or is no node of the sequence, ends it (SISO_ERR_INVALID_ARG in the status word).  d_new_len [n_seqs] =
  *                  before + 1 + t at its end (kv_len for a sequence without new tokens); it must not be d_kv_len itself.  Weights (below) stay where they
  *                  are: node 0 and the rows of the path are new tokens to them.  Their queries and lse, gathered in the path's order, are those of a causal chunk.
+ *                  Sequences that move rows share no page that they move them in.
  * siso_kv_add_weights  Each query i of a sequence (as in siso_kv_attention; d_lse [n_tokens, n_heads] as that returns it) gives the tokens that it sees
  *                  the weights exp(scale q.k_j - lse).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
  *                  layer of the call, w_j = decay w_j + sum of the weights over the queries and query heads that read the kv head; tokens that are new
@@ -590,7 +591,9 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
  *                  that were evicted, of drafts, of a page's last owner there may be anything).  Where other tokens than the call's queries are new too (a chunk
  *                  of which only the last queries are given, a path of drafts that the next query follows), siso_kv_add_weights_new is told how many: the last
  *                  d_new[b] tokens of sequence b start from 0 (d_new [n_seqs]; below 0 counts as 0, above kv_len as kv_len; NULL: as many as it has queries).  Sequences without
- *                  queries are left alone.  A query whose lse is -infinity gives nothing.  d_q as in siso_kv_attention, but with no stride of 0 where there are several entries; d_weights 16-byte aligned.  Sums are fp32, in an order that does not change from call to call.
+ *                  queries are left alone.  A query whose lse is -infinity gives nothing.  Entries of d_pages (of sequences with queries, as far as
+ *                  kv_len reaches) name different pages: of two that share one (a common prefix, say, which attention reads without harm) each would write its weights without the
+ *                  other's, in any order.  (siso_kv_evict and siso_kv_keep_path move the rows of such pages, and ask the same.)  d_q as in siso_kv_attention, but with no stride of 0 where there are several entries; d_weights 16-byte aligned.  Sums are fp32, in an order that does not change from call to call.
  * siso_kv_evict    For each layer, sequence and kv head by itself: of kv_len tokens the last `recent` stay and, of the others, the budget - recent with the largest
  *                  weights (ties: the earlier one; NaN counts as less than all else).  Their rows, exponents and weights are moved, in order, to places 0, 1, .. of the
  *                  pages d_out_pages [n_seqs, out_max_pages] (d_pages itself: in place).  Places that nothing is moved to keep what they held, weights among it.  d_new_len [n_seqs] = min(kv_len, budget), the same for

@@ -307,7 +307,8 @@ class PagedKV:
         `decay` times (0: not at all, whatever it is); the new tokens start from zero: a sequence's last ones, as many as it has queries, or n_new int32 [seqs] of
         them.  For the last queries of a longer chunk alone pass them with their own cu_q and the chunk's length as n_new, for the first query behind a
         path that keep_path() kept the path's tokens and the query's: until a call has counted a token as new, its place may hold an evicted token's weight, a
-        draft's, or that of a page's last owner."""
+        draft's, or that of a page's last owner.  Sequences of one call that have queries must not share pages, though attention() lets them: each would write the
+        shared tokens' weights without the other's."""
         if stream is not None:
             with _on(stream, self._index):
                 return self.add_weights(weights, q, lse, cu_q, kv_len, pages, max_q, layer, scale, causal, decay, n_new=n_new)
