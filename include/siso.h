@@ -585,7 +585,8 @@ siso_status_t siso_verify_drafts(const void *d_target, const void *d_draft, int3
  *                  are: node 0 and the rows of the path are new tokens to them.  Their queries and lse, gathered in the path's order, are those of a causal chunk.
  *                  Sequences that move rows share no page that they move them in.
  * siso_kv_add_weights  Each query i of a sequence (as in siso_kv_attention; d_lse [n_tokens, n_heads] as that returns it) gives the tokens that it sees
- *                  the weights exp(scale q.k_j - lse).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
+ *                  the weights exp(scale q.k_j - lse).  There is no window here and no tree: with the lse of a call that had a window, tokens before it would be weighed
+ *                  too, by numbers that may be above 1, and with that of siso_kv_tree_attention a node's sisters (but see siso_kv_keep_path).  d_weights [n_layers, n_pages, n_kv_heads, page_size] keeps one fp32 number for each cached row: for the
  *                  layer of the call, w_j = decay w_j + sum of the weights over the queries and query heads that read the kv head; tokens that are new
  *                  in this call (the last ones, as many as the sequence has queries) start from 0, and with decay 0 all do, whatever stood there (in the places of tokens
  *                  that were evicted, of drafts, of a page's last owner there may be anything).  Where other tokens than the call's queries are new too (a chunk

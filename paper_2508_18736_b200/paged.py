@@ -303,7 +303,9 @@ class PagedKV:
                     max_q: int, layer: int = 0, scale: Optional[float] = None, causal: bool = True, decay: float = 1.0, stream=None,
                     n_new: Optional[torch.Tensor] = None) -> None:
         """Adds to weights (see new_weights()) what the queries q [n, heads, head dim] bf16 give each token that they see, summed over the
-        queries and the heads of a kv head: their probabilities, from lse [n, heads] as attention(want_lse=True) returned it.  What was there counts
+        queries and the heads of a kv head: their probabilities, from lse [n, heads] as attention(want_lse=True) returned it for the same queries and
+        `causal`, without a window (tokens before it would be weighed too, by numbers that may be above 1); a tree's queries are weighed once their path is kept (see
+        keep_path()), as before that each would weigh its sisters.  What was there counts
         `decay` times (0: not at all, whatever it is); the new tokens start from zero: a sequence's last ones, as many as it has queries, or n_new int32 [seqs] of
         them.  For the last queries of a longer chunk alone pass them with their own cu_q and the chunk's length as n_new, for the first query behind a
         path that keep_path() kept the path's tokens and the query's: until a call has counted a token as new, its place may hold an evicted token's weight, a
