@@ -148,16 +148,16 @@ keep_path_kernel(const __grid_constant__ KeepArgs g) {
 }
 
 // ---- eviction ---------------------------------------------------------------------------------------------------------------
-// A cluster of CTAs per (layer, sequence, kv head).  Weights become whole numbers of the same order, each CTA keeps those of its part of the places in
-// shared memory (as far as they fit), and the smallest weight that stays is found eight bits at a time from counts that the CTAs exchange.
-// The places that stay are listed in order (d_kept, an output anyway), then the rows are moved in waves: all CTAs read a wave's rows into
+// A cluster of CTAs per (layer, sequence, kv head).  Weights become whole numbers of the same order, and the smallest weight that stays is found eight bits at a time
+// from counts of the numbers' digits.  The places that stay are listed in order, then the rows are moved in waves: all CTAs read a wave's rows into
 // registers, meet, and write them, which is safe in place because of the order (see above).
 constexpr int THREADS = 512, WARPS = THREADS / 32, U = 8;        // U: pieces of a thread in flight
 constexpr int R = 16, KEYS = 40 * 1024;           // weights that a thread keeps in registers; that a CTA keeps in shared memory
 // Which places stay is found out by each CTA of the cluster from all weights (up to 8192), so that none waits for another's counts (24 sequences of up to 4200 tokens: 31 us
-// and 37 us); or the CTAs share the weights, in registers (16,385 tokens: 31 us and 35 us) or in shared memory
-// (above 65,536).  Bound by latency up to the rows: weights, digits, list and places are trips and barriers one after another; the rows then go at bandwidth.  Now measured: 16,385 to 2048
-// tokens, four layers x 8 heads x 128 bf16, 33 us, about 10 of them for the rows; 24 sequences of 1100 to 4200 tokens to 1000, two layers x 4 heads x 64 e4m3, 31 us.
+// and 37 us); or each has a part of the weights, in registers (16,385 tokens: 31 us and 35 us) or, above 65,536, in shared memory as far as they fit, and the counts are exchanged.
+// Bound by latency up to the rows: weights, digits, list and places are trips and barriers one after another; the rows then go at bandwidth.  Now measured: 16,385 to 2048
+// tokens, four layers x 8 heads x 128 bf16, 35 us, about 10 of them for the rows; 24 sequences of 1100 to 4200 tokens to 1000, two layers x 4 heads x 64 e4m3, 28 us; in place
+// 42 and 29 us, as all CTAs of a cluster meet between reading and writing a wave (inputs not in L2).
 enum Mode { ALONE, SHARED_REGS, SHARED };
 constexpr int SLOTS = 1024;                       // rows of a CTA whose places are worked out at a time
 

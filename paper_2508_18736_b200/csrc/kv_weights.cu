@@ -17,8 +17,8 @@
 //   8 warps          8-bit caches only: turn codes into bf16 tiles (without the scale, exactly)
 // Bounds: few rows read every key once: HBM.  A chunk's 256 x 128 scores take 1024 cycles of tcgen05.mma (d = 128) and 2048 of the SM's 16 exponentials a
 // cycle: the exponentials, of which some are taken on the FMA pipe.
-// Measured (8 kv heads x 128 with 4 query heads each, bf16, the kernel and its join): 4096 queries over 8193 tokens 235 us, the exponentials' pipe 72 % busy; 32 query tokens
-// (128 rows a kv head) of each of 64 sequences over 4096 tokens 125 us.
+// Measured (8 kv heads x 128 with 4 query heads each, bf16, the kernel and its join): 4096 queries over 8193 tokens 250 to 254 us in runs of seconds (222 us in short ones), the
+// exponentials' pipe 72 % busy; 32 query tokens (128 rows a kv head) of each of 64 sequences over 4096 tokens 119 us, 16 of them 97 us.
 #include "kv_attention.cuh"
 
 namespace siso {

@@ -7,8 +7,8 @@
 // 128 lanes or columns would be mostly empty, and 8-bit codes would have to go through shared memory once more), exponentials, the sum over a key's rows by
 // two shuffles.  What else belongs to a key (its exponent, its weight so far, where that lies) comes with the unit.  8-bit codes become fp16 in registers, exactly; queries
 // are brought to fp16 with a factor per row, exactly but for elements below 2^-31 of their row's largest.
-// Measured (8 kv heads x 128, 4 rows each): one token of each of 64 sequences over 201 to 8190 tokens, e4m3, 65 us (4.4 TB/s; consumers' instructions, most of them for
-// the codes, and HBM are both a little over half busy); 64 x 4096 tokens of bf16 92 us (6.0 TB/s).
+// Measured (8 kv heads x 128, 4 rows each): one token of each of 64 sequences over 201 to 8190 tokens, e4m3, 64 us (4.5 TB/s; consumers' instructions, most of them for
+// the codes, and HBM are both a little over half busy); 64 x 4096 tokens of bf16 90 us (6.2 TB/s).
 #include <cuda_fp16.h>
 
 #include "kv_attention.cuh"

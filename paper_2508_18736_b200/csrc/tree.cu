@@ -58,7 +58,7 @@ tree_mask_kernel(const int32_t *__restrict__ parents, const int32_t *__restrict_
 // ---- verification --------------------------------------------------------------------------------------------------------
 constexpr int THREADS = 512, WARPS = THREADS / 32, SPLIT = 8, CHUNKS = SPLIT * WARPS;
 constexpr int NODES = 512;                        // nodes whose numbers are kept in shared memory
-constexpr int MAX_VOCAB = 1 << 18;                // so that a CTA's part of r fits its shared memory
+constexpr int MAX_VOCAB = 1 << 18;                // a CTA's part of r is 128 KB of its shared memory then; eight CTAs could hold over 400,000 entries, but nothing has asked for more
 
 struct Args {
     const void *target, *draft;                   // [n_tokens, vocab]
